@@ -65,6 +65,7 @@ extern "C" {
 #define SP_MAX_LM_LAYERS 96       /* decoder layers of the LM */
 #define SP_MAX_KMAX 1024          /* per-episode cap on retained tokens */
 #define SP_MAX_NVIS 16384         /* visual tokens of one image */
+#define SP_MAX_BEAMS 16           /* beams of one element */
 
 typedef enum {
   SP_OK = 0,
@@ -530,6 +531,170 @@ typedef struct {
 SP_API size_t sp_decode_workspace(const sp_model* m, int B);
 SP_API sp_status sp_decode(const sp_model* m, const sp_decode_io* io, void* workspace, size_t workspace_bytes,
                            sp_stream stream);
+
+/* ------------------------------------------------------------------------ */
+/* Several sequences over one pruned prefix: a paged cache and beams.         */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * Questions about one image, samples and beams continue the same prefix.  In a
+ * paged cache they share its keys and values: a pool of pages of page_size
+ * positions, and per sequence a table of its pages.  Position p of a sequence
+ * is row p % page_size of page table[p / page_size].  One layer's pool is
+ *   kv  DEVICE [2][n_pages][page_size][n_kv_heads * head_dim] bf16 (K, then V).
+ * Table entries behind a sequence's pages are not read (-1, say).  A page
+ * outside 0..n_pages-1 where one is needed sets SP_DEVERR_INDEX; nothing is
+ * written for it, and read it counts as keys and values of zero.
+ */
+typedef struct {
+  void* kv;                 /* DEVICE pool of one layer, 16-byte aligned */
+  int n_pages;              /* n_pages * page_size <= 2^30 */
+  int page_size;            /* a power of two, 16..1024 */
+  const int* table;         /* DEVICE [B, max_pages] int32 */
+  int max_pages;
+  const int* lens;          /* DEVICE [B] int32 positions per sequence (each call says which) */
+} sp_paged_kv;
+
+/*
+ * Appends rows to the cache, rotated on the way: row j of sequence b goes to
+ * position cache.lens[b] + j (lens: the positions cached before; NULL: 0).
+ *   rope  DEVICE [max_pos, head_dim / 2, 2] fp32 (cos, sin) of each rotary
+ *         position and pair; pair i of a head is its elements i and
+ *         i + head_dim / 2 (as in sp_prefill).  NULL: rows are already rotated.
+ *   pos   DEVICE [T_cap] rotary position of each row; or
+ *   pos3  DEVICE [T_cap, 4] (t, h, w, unused) with mrope_section as in
+ *         sp_model_cfg (sp_mrope_positions writes it).
+ * Queries and keys are rotated in fp32 and rounded once; values are copied.
+ * q_out may be qkv itself (with ld_q = ld): the queries are then rotated in
+ * place.  lens is not changed.  Rows outside cu_rows[0] .. cu_rows[B] - 1 are
+ * not read.  A position outside its table or a rotary position outside
+ * 0..max_pos-1 sets SP_DEVERR_INDEX and the row's keys and values (for a rotary
+ * position its queries too) are skipped.
+ */
+typedef struct {
+  int B;                    /* sequences, 1..SP_MAX_BATCH */
+  int T_cap;                /* rows of qkv, at most 2^31 - 1; B without cu_rows */
+  const int* cu_rows;       /* DEVICE [B + 1] ascending: sequence b's rows; NULL: row b is sequence b's */
+  const void* qkv;          /* DEVICE [T_cap, ld] bf16: q | k | v of every row */
+  long long ld;             /* elements between rows, a multiple of 8 */
+  void* q_out;              /* DEVICE [T_cap, ld_q] bf16, or NULL: keys and values only */
+  long long ld_q;
+  int n_heads, n_kv_heads, head_dim;  /* head_dim 64 or 128 */
+  const float* rope;
+  int max_pos;
+  const int* pos;
+  const int* pos3;
+  int mrope_section[3];
+  sp_paged_kv cache;
+  int* err;                 /* DEVICE error word or NULL */
+} sp_paged_append_io;
+
+SP_API sp_status sp_paged_append(const sp_paged_append_io* io, sp_stream stream);
+
+/*
+ * Attention of rows whose sequences share prefixes.  The sequences
+ * group_cu[g] .. group_cu[g+1] - 1 share prefix g: prefix_lens[g] positions of
+ * the same pool, in the pages of prefix_table.  Row j of sequence b (of its
+ * n_b rows) sees its group's whole prefix and, of the sequence's own
+ * cache.lens[b] positions (these rows' own keys, appended before, among them),
+ * those up to lens[b] - n_b + j.  Sequences outside every group have no prefix.
+ *   out = softmax(scale <q, k>) v over the visible keys, lse = log sum exp of
+ *   the scaled scores; a row that sees no key gets zeros and lse -infinity.
+ * A prefix is read once for all rows that share it.  Scores, statistics and
+ * sums are fp32; the weights are rounded to bf16 for the product with V.
+ * Lengths are read on the device (they may change between replays of a graph);
+ * the workspace depends on the arguments of its query alone and keeps nothing.
+ * Rows outside cu_rows[0] .. cu_rows[B] - 1 are left as they were.  The result
+ * does not depend on timing (no atomics); it is summed in an order that depends
+ * on the lengths of the whole batch.
+ */
+typedef struct {
+  int B;                    /* sequences, 1..SP_MAX_BATCH */
+  int T_cap;                /* rows of q; B without cu_rows; T_cap * n_heads <= 2^28 */
+  const int* cu_rows;       /* DEVICE [B + 1] ascending, or NULL: one row per sequence */
+  const void* q;            /* DEVICE [T_cap, ld_q] bf16 rotated queries */
+  long long ld_q;           /* elements between rows, a multiple of 8 */
+  void* out;                /* DEVICE [T_cap, ld_out] bf16 (must not overlap q) */
+  long long ld_out;
+  float* lse;               /* DEVICE [T_cap, n_heads] fp32 or NULL */
+  int n_heads, n_kv_heads, head_dim;
+  float scale;              /* 0: 1 / sqrt(head_dim) */
+  sp_paged_kv cache;        /* lens: own positions, the rows of this call included */
+  int n_groups;             /* 0..SP_MAX_BATCH; 0: no prefixes (the group arguments are ignored) */
+  const int* group_cu;      /* DEVICE [n_groups + 1] ascending */
+  const int* prefix_table;  /* DEVICE [n_groups, prefix_max_pages] int32 */
+  int prefix_max_pages;
+  const int* prefix_lens;   /* DEVICE [n_groups] */
+  int* err;                 /* DEVICE error word or NULL */
+} sp_prefix_attention_io;
+
+SP_API size_t sp_prefix_attention_workspace(int T_cap, int B, int n_groups, int n_heads, int n_kv_heads,
+                                            int head_dim);
+SP_API sp_status sp_prefix_attention(const sp_prefix_attention_io* io, void* workspace, size_t workspace_bytes,
+                                     sp_stream stream);
+
+/*
+ * Beam search's selection: of the W beams of each of B elements and the V
+ * tokens, the n_out continuations with the largest
+ *   cum[w] + log softmax(logits[w])[v],
+ * best first.  Scores are compared in 64 bits; equal ones go to the lower beam,
+ * then the lower token (within a beam the order is that of the logits).
+ *   - A beam with cum -infinity (or NaN) is not alive: it proposes nothing.
+ *   - A finished beam (done != 0) proposes only itself: token eos, score cum;
+ *     its logits are not read.
+ *   - NaN and -infinity logits have no weight and are never chosen; a row with
+ *     +infinity spreads its weight over them (the softmax's limit).
+ * Places for which no continuation is left get score -infinity, parent and
+ * token -1.
+ */
+typedef struct {
+  int B, W, V;              /* 1..SP_MAX_BATCH, 1..SP_MAX_BEAMS, 1..2^24 */
+  const void* logits;       /* DEVICE [B * W, ld] fp32 or bf16, aligned to its type */
+  int logits_f32;           /* 1: fp32, 0: bf16 */
+  long long ld;             /* elements between rows, at least V */
+  const float* cum;         /* DEVICE [B, W] */
+  const unsigned char* done;/* DEVICE [B, W] or NULL */
+  int eos;
+  int n_out;                /* 1..2 SP_MAX_BEAMS */
+  float* score;             /* DEVICE [B, n_out] */
+  int* parent;              /* DEVICE [B, n_out] beam of the element */
+  int* token;               /* DEVICE [B, n_out] */
+} sp_beam_select_io;
+
+SP_API size_t sp_beam_select_workspace(int B, int W, int V, int n_out);
+SP_API sp_status sp_beam_select(const sp_beam_select_io* io, void* workspace, size_t workspace_bytes,
+                                sp_stream stream);
+
+/*
+ * Puts the cache of every element's beams into a new order: beam w becomes a
+ * continuation of beam parent[w] (of the same element; -1: of itself).  Row
+ * e * W + w of table and own_table belongs to beam w of element e; lens are the
+ * positions cached, equal for the beams of an element.
+ * own_table names pages of each beam's own for every place of its table, in
+ * which no other row of own_table has a page; it does not change.  table starts
+ * as a copy of it.  A beam appends to table[len / page_size], which is then its
+ * own page: after this call table holds the parent's entries for full pages
+ * (never written again, so shared) and the beam's own behind them, and the rows
+ * of the partly filled page are copied from the parent's own page, all layers.
+ * Unequal lengths, a length outside the table or a parent outside -1..W-1 set
+ * SP_DEVERR_INDEX: such an element stays as it was (such a parent: -1).
+ */
+typedef struct {
+  int B, W;                 /* elements, beams */
+  int n_layers;             /* pools, one after the other */
+  void* kv;                 /* DEVICE [n_layers][2][n_pages][page_size][row_elems] bf16 */
+  int n_pages, page_size;   /* as in sp_paged_kv */
+  int row_elems;            /* n_kv_heads * head_dim, a multiple of 8 */
+  int* table;               /* DEVICE [B * W, max_pages], updated */
+  const int* own_table;     /* DEVICE [B * W, max_pages] */
+  int max_pages;
+  const int* lens;          /* DEVICE [B * W] */
+  const int* parent;        /* DEVICE [B, ld_parent] (sp_beam_select's) */
+  int ld_parent;
+  int* err;                 /* DEVICE error word or NULL */
+} sp_beam_reorder_io;
+
+SP_API sp_status sp_beam_reorder(const sp_beam_reorder_io* io, sp_stream stream);
 
 /* ------------------------------------------------------------------------ */
 /* The whole path: select -> compact -> project -> prefill.                  */

@@ -21,6 +21,7 @@ SP_MAX_ENC_LAYERS = 4
 SP_MAX_LM_LAYERS = 96
 SP_MAX_KMAX = 1024
 SP_MAX_NVIS = 16384
+SP_MAX_BEAMS = 16
 
 STATUS = {0: "SP_OK", 1: "SP_ERR_INVALID_ARG", 2: "SP_ERR_SHAPE", 3: "SP_ERR_ALIGN", 4: "SP_ERR_WORKSPACE",
           5: "SP_ERR_CUDA", 6: "SP_ERR_TIMEOUT", 7: "SP_ERR_UNSUPPORTED", 8: "SP_ERR_DEVICE"}
@@ -35,6 +36,8 @@ EXPORTS = [
     "sp_profile_begin", "sp_profile_end", "sp_select_noalloc",
     "sp_decode_workspace", "sp_decode", "sp_select_train", "sp_soft_topk", "sp_vp_gate",
     "sp_mrope_positions", "sp_wait_probe",
+    "sp_paged_append", "sp_prefix_attention_workspace", "sp_prefix_attention", "sp_beam_select_workspace",
+    "sp_beam_select", "sp_beam_reorder",
 ]
 SP_SELECT_NOALLOC_SCRATCH_BYTES = 64 << 20
 
@@ -119,6 +122,37 @@ class sp_decode_io(C.Structure):
                 ("hidden", P), ("err", P), ("rope_pos", P)]
 
 
+class sp_paged_kv(C.Structure):
+    _fields_ = [("kv", P), ("n_pages", C.c_int), ("page_size", C.c_int), ("table", P), ("max_pages", C.c_int),
+                ("lens", P)]
+
+
+class sp_paged_append_io(C.Structure):
+    _fields_ = [("B", C.c_int), ("T_cap", C.c_int), ("cu_rows", P), ("qkv", P), ("ld", C.c_longlong), ("q_out", P),
+                ("ld_q", C.c_longlong), ("n_heads", C.c_int), ("n_kv_heads", C.c_int), ("head_dim", C.c_int),
+                ("rope", P), ("max_pos", C.c_int), ("pos", P), ("pos3", P), ("mrope_section", C.c_int * 3),
+                ("cache", sp_paged_kv), ("err", P)]
+
+
+class sp_prefix_attention_io(C.Structure):
+    _fields_ = [("B", C.c_int), ("T_cap", C.c_int), ("cu_rows", P), ("q", P), ("ld_q", C.c_longlong), ("out", P),
+                ("ld_out", C.c_longlong), ("lse", P), ("n_heads", C.c_int), ("n_kv_heads", C.c_int),
+                ("head_dim", C.c_int), ("scale", C.c_float), ("cache", sp_paged_kv), ("n_groups", C.c_int),
+                ("group_cu", P), ("prefix_table", P), ("prefix_max_pages", C.c_int), ("prefix_lens", P), ("err", P)]
+
+
+class sp_beam_select_io(C.Structure):
+    _fields_ = [("B", C.c_int), ("W", C.c_int), ("V", C.c_int), ("logits", P), ("logits_f32", C.c_int),
+                ("ld", C.c_longlong), ("cum", P), ("done", P), ("eos", C.c_int), ("n_out", C.c_int), ("score", P),
+                ("parent", P), ("token", P)]
+
+
+class sp_beam_reorder_io(C.Structure):
+    _fields_ = [("B", C.c_int), ("W", C.c_int), ("n_layers", C.c_int), ("kv", P), ("n_pages", C.c_int),
+                ("page_size", C.c_int), ("row_elems", C.c_int), ("table", P), ("own_table", P),
+                ("max_pages", C.c_int), ("lens", P), ("parent", P), ("ld_parent", C.c_int), ("err", P)]
+
+
 class sp_pipeline_io(C.Structure):
     _fields_ = [("sel", sp_select_in), ("k_cap", C.c_int), ("idx", P), ("count", P), ("cu_seqlens", P),
                 ("hidden", P), ("err", P)]
@@ -169,6 +203,12 @@ def lib():
         "sp_soft_topk": (C.c_int, [C.c_int, IP, C.c_int, P, P, C.c_float, P, P, P]),
         "sp_vp_gate": (C.c_int, [C.c_int, C.c_int, P, P, P, P, P]),
         "sp_mrope_positions": (C.c_int, [C.c_int, IP, IP, IP, P, C.c_int, P, P, C.c_int, P, P]),
+        "sp_paged_append": (C.c_int, [C.POINTER(sp_paged_append_io), P]),
+        "sp_prefix_attention_workspace": (C.c_size_t, [C.c_int] * 6),
+        "sp_prefix_attention": (C.c_int, [C.POINTER(sp_prefix_attention_io), P, C.c_size_t, P]),
+        "sp_beam_select_workspace": (C.c_size_t, [C.c_int] * 4),
+        "sp_beam_select": (C.c_int, [C.POINTER(sp_beam_select_io), P, C.c_size_t, P]),
+        "sp_beam_reorder": (C.c_int, [C.POINTER(sp_beam_reorder_io), P]),
         "sp_wait_probe": (C.c_int, [P, C.c_uint, C.c_int, P, P, P]),
         "sp_profile_begin": (C.c_int, [C.c_int]),
         "sp_profile_end": (C.c_int, [C.POINTER(C.c_double), C.POINTER(C.c_longlong), C.POINTER(C.c_double),
@@ -566,6 +606,213 @@ def sp_mrope_positions(n_vis, n_txt, grid_w, *, idx, count, k_cap, T_cap, stream
                                     ptr(count), ptr(pos3), int(T_cap), ptr(err), _stream(stream)),
            "sp_mrope_positions")
     return {"pos3": pos3, "err": err}
+
+
+# ----------------------------------------------------------------------------- paged cache, shared prefixes, beams
+
+class _On:
+    """The device that a call's tensors lie on, current for the call; checks the tensors handed to it."""
+
+    def __init__(self, who: str, first):
+        torch = _torch()
+        if not first.is_cuda:
+            raise ValueError(f"{who}: tensors must be on a CUDA device")
+        self.who, self.dev = who, first.device
+        self._guard = torch.cuda.device(self.dev) if torch.cuda.current_device() != self.dev.index else None
+
+    def __enter__(self):
+        if self._guard is not None:
+            self._guard.__enter__()
+        return self
+
+    def __exit__(self, *a):
+        if self._guard is not None:
+            self._guard.__exit__(*a)
+
+    def ptr(self, name, t, dtype, shape, optional=False):
+        """Address of a contiguous tensor of this type and shape (None in a shape: any size)."""
+        if t is None:
+            if optional:
+                return None
+            raise ValueError(f"{self.who}: {name} is required")
+        if (t.dtype is not dtype or t.device != self.dev or t.dim() != len(shape) or not t.is_contiguous()
+                or any(n is not None and n != m for n, m in zip(shape, t.shape))):
+            raise ValueError(f"{self.who}: {name} must be contiguous {dtype} {tuple('?' if n is None else n for n in shape)} "
+                             f"on {self.dev}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        return t.data_ptr()
+
+    def rows(self, name, t, width):
+        """(address, row stride) of bf16 rows of `width` elements, which may lie apart."""
+        torch = _torch()
+        if t is None or t.dtype is not torch.bfloat16 or t.device != self.dev or t.dim() != 2 or t.shape[1] != width or t.stride(1) != 1:
+            raise ValueError(f"{self.who}: {name} must be bf16 rows of {width} elements on {self.dev}")
+        return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else max(t.stride(0), width))
+
+
+def rope_table(max_pos: int, head_dim: int, theta: float = 10000.0, device="cuda"):
+    """(cos, sin) of every rotary position and pair, [max_pos, head_dim / 2, 2] fp32 (angles in 64 bits)."""
+    torch = _torch()
+    inv = float(theta) ** (-torch.arange(0, head_dim, 2, dtype=torch.float64, device=device) / head_dim)
+    a = torch.arange(max_pos, dtype=torch.float64, device=device)[:, None] * inv
+    return torch.stack((a.cos(), a.sin()), dim=-1).to(torch.float32)
+
+
+def paged_pool(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, n_layers: int = 1, device="cuda"):
+    """Zeroed page pools [n_layers, 2, n_pages, page_size, n_kv_heads * head_dim] bf16; pool[l] is one layer's."""
+    torch = _torch()
+    return torch.zeros((n_layers, 2, n_pages, page_size, n_kv_heads * head_dim), dtype=torch.bfloat16, device=device)
+
+
+def _cache(on: _On, kv, table, lens, B, width, lens_optional=False):
+    torch = _torch()
+    k = on.ptr("kv", kv, torch.bfloat16, (2, None, None, width))
+    t = on.ptr("table", table, torch.int32, (B, None))
+    return sp_paged_kv(k, kv.shape[1], kv.shape[2], t, table.shape[1],
+                       on.ptr("lens", lens, torch.int32, (B,), optional=lens_optional))
+
+
+def sp_paged_append(*, qkv, kv, table, n_heads, n_kv_heads, head_dim, lens=None, cu_rows=None, rope=None, pos=None,
+                    pos3=None, mrope_section=None, q_out=None, keys_only=False, err=None, stream=None) -> Dict:
+    """Rows q | k | v [T, (n_heads + 2 n_kv_heads) head_dim] into the pages of kv (one layer's pool): row j of
+    sequence b at position lens[b] + j (lens None: 0); cu_rows [B + 1] int32 are the sequences' rows (None: row b
+    is sequence b's).  rope (rope_table) rotates queries and keys at pos [T] or pos3 [T, 4] (mrope_section); None
+    leaves them as they are.  The queries go to q_out (new when None; a view of qkv's first columns rotates in
+    place; keys_only: nowhere).  Returns q and err."""
+    torch = _torch()
+    with _On("sp_paged_append", qkv) as on:
+        B = int(table.shape[0])
+        x, ld = on.rows("qkv", qkv, (n_heads + 2 * n_kv_heads) * head_dim)
+        T = int(qkv.shape[0])
+        if q_out is None and not keys_only:
+            q_out = torch.empty((T, n_heads * head_dim), dtype=torch.bfloat16, device=on.dev)
+        q, ld_q = on.rows("q_out", q_out, n_heads * head_dim) if not keys_only else (None, 0)
+        if q_out is not None and not keys_only and q_out.shape[0] != T:
+            raise ValueError("sp_paged_append: q_out must have qkv's rows")
+        if err is None:
+            err = torch.zeros(1, dtype=torch.int32, device=on.dev)
+        sec = (C.c_int * 3)(*(mrope_section or (0, 0, 0)))
+        io = sp_paged_append_io(B, T, on.ptr("cu_rows", cu_rows, torch.int32, (B + 1,), optional=True), x, ld, q, ld_q,
+                                n_heads, n_kv_heads, head_dim,
+                                on.ptr("rope", rope, torch.float32, (None, head_dim // 2, 2), optional=True),
+                                int(rope.shape[0]) if rope is not None else 0,
+                                on.ptr("pos", pos, torch.int32, (T,), optional=True),
+                                on.ptr("pos3", pos3, torch.int32, (T, 4), optional=True), sec,
+                                _cache(on, kv, table, lens, B, n_kv_heads * head_dim, lens_optional=True),
+                                on.ptr("err", err, torch.int32, (1,)))
+        _check(lib().sp_paged_append(C.byref(io), _stream(stream)), "sp_paged_append")
+    return {"q": q_out, "err": err}
+
+
+def prefix_attention_workspace(*, T_cap, B, n_heads, n_kv_heads, head_dim, n_groups=0, device="cuda"):
+    """A workspace for sp_prefix_attention calls of up to these sizes."""
+    with _torch().cuda.device(device):
+        n = lib().sp_prefix_attention_workspace(int(T_cap), int(B), int(n_groups), int(n_heads), int(n_kv_heads),
+                                                int(head_dim))
+    if n == 0:
+        raise SPError("sp_prefix_attention_workspace: " + lib().sp_last_error().decode(errors="replace"))
+    return workspace(n, device)
+
+
+def sp_prefix_attention(*, q, kv, table, lens, n_heads, n_kv_heads, head_dim, prefix_table=None, prefix_lens=None,
+                        group_cu=None, cu_rows=None, scale=0.0, out=None, lse=None, ws=None, err=None,
+                        stream=None) -> Dict:
+    """Rotated rows q [T, n_heads head_dim] over their group's prefix pages (sequences group_cu[g] ..
+    group_cu[g+1] - 1 share prefix_table[g], prefix_lens[g] positions) and, causally, over their sequence's own
+    pages (table, lens: positions with these rows' own).  Returns out [T, n_heads head_dim] bf16, lse (the given
+    [T, n_heads] fp32 tensor or None) and err."""
+    torch = _torch()
+    with _On("sp_prefix_attention", q) as on:
+        B, T = int(table.shape[0]), int(q.shape[0])
+        x, ld_q = on.rows("q", q, n_heads * head_dim)
+        if out is None:
+            out = torch.empty((T, n_heads * head_dim), dtype=torch.bfloat16, device=on.dev)
+        o, ld_out = on.rows("out", out, n_heads * head_dim)
+        if out.shape[0] != T:
+            raise ValueError("sp_prefix_attention: out must have q's rows")
+        if err is None:
+            err = torch.zeros(1, dtype=torch.int32, device=on.dev)
+        groups = int(prefix_table.shape[0]) if prefix_table is not None else 0
+        if ws is None:
+            ws = prefix_attention_workspace(T_cap=T, B=B, n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim,
+                                            n_groups=groups, device=on.dev)
+        some = groups > 0
+        io = sp_prefix_attention_io(
+            B, T, on.ptr("cu_rows", cu_rows, torch.int32, (B + 1,), optional=True), x, ld_q, o, ld_out,
+            on.ptr("lse", lse, torch.float32, (T, n_heads), optional=True), n_heads, n_kv_heads, head_dim, float(scale),
+            _cache(on, kv, table, lens, B, n_kv_heads * head_dim), groups,
+            on.ptr("group_cu", group_cu, torch.int32, (groups + 1,)) if some else None,
+            on.ptr("prefix_table", prefix_table, torch.int32, (groups, None)) if some else None,
+            int(prefix_table.shape[1]) if some else 0,
+            on.ptr("prefix_lens", prefix_lens, torch.int32, (groups,)) if some else None,
+            on.ptr("err", err, torch.int32, (1,)))
+        _check(lib().sp_prefix_attention(C.byref(io), on.ptr("ws", ws, torch.uint8, (None,)), ws.numel(),
+                                         _stream(stream)), "sp_prefix_attention")
+    return {"out": out, "lse": lse, "err": err, "_ws": ws}
+
+
+def beam_select_workspace(*, B, W, V, n_out, device="cuda"):
+    """A workspace for sp_beam_select calls of these sizes."""
+    with _torch().cuda.device(device):
+        n = lib().sp_beam_select_workspace(int(B), int(W), int(V), int(n_out))
+    if n == 0:
+        raise SPError("sp_beam_select_workspace: " + lib().sp_last_error().decode(errors="replace"))
+    return workspace(n, device)
+
+
+def sp_beam_select(*, logits, cum, n_out, done=None, eos=0, score=None, parent=None, token=None, ws=None,
+                   stream=None) -> Dict:
+    """The n_out best continuations of every element's beams: logits [B, W, V] fp32 or bf16 (rows may lie apart),
+    cum [B, W] fp32, done [B, W] bool or None (a finished beam proposes itself with token eos).  Returns score,
+    parent (beam) and token [B, n_out], best first; places without a continuation hold -infinity, -1, -1."""
+    torch = _torch()
+    with _On("sp_beam_select", logits) as on:
+        if logits.dim() != 3 or logits.dtype not in (torch.float32, torch.bfloat16) or (logits.shape[2] > 1 and logits.stride(2) != 1):
+            raise ValueError("sp_beam_select: logits must be [B, W, V] fp32 or bf16, tokens next to each other")
+        B, W, V = (int(n) for n in logits.shape)
+        ld = logits.stride(1) if W > 1 else logits.stride(0) if B > 1 else V
+        if B > 1 and W > 1 and logits.stride(0) != W * ld:
+            raise ValueError("sp_beam_select: the rows of logits must lie evenly apart")
+        if score is None:
+            score = torch.empty((B, n_out), dtype=torch.float32, device=on.dev)
+        if parent is None:
+            parent = torch.empty((B, n_out), dtype=torch.int32, device=on.dev)
+        if token is None:
+            token = torch.empty((B, n_out), dtype=torch.int32, device=on.dev)
+        if ws is None:
+            ws = beam_select_workspace(B=B, W=W, V=V, n_out=n_out, device=on.dev)
+        io = sp_beam_select_io(B, W, V, logits.data_ptr(), 1 if logits.dtype is torch.float32 else 0, ld,
+                               on.ptr("cum", cum, torch.float32, (B, W)),
+                               on.ptr("done", done, torch.bool, (B, W), optional=True), int(eos), int(n_out),
+                               on.ptr("score", score, torch.float32, (B, n_out)),
+                               on.ptr("parent", parent, torch.int32, (B, n_out)),
+                               on.ptr("token", token, torch.int32, (B, n_out)))
+        _check(lib().sp_beam_select(C.byref(io), on.ptr("ws", ws, torch.uint8, (None,)), ws.numel(), _stream(stream)),
+               "sp_beam_select")
+    return {"score": score, "parent": parent, "token": token, "_ws": ws}
+
+
+def sp_beam_reorder(*, kv, table, own_table, lens, parent, err=None, stream=None):
+    """Puts the cache into the beams' new order: table rows and the rows of the partly filled pages of all layers
+    (kv [n_layers, 2, n_pages, page_size, width]) follow parent [B, W or more] (its first W columns); table is
+    updated in place.  Returns err."""
+    torch = _torch()
+    with _On("sp_beam_reorder", kv) as on:
+        if parent.dim() != 2 or parent.shape[0] < 1 or table.dim() != 2 or table.shape[0] % parent.shape[0] != 0:
+            raise ValueError("sp_beam_reorder: table must have the beams of parent's elements")
+        B, R = int(parent.shape[0]), int(table.shape[0])
+        if parent.dtype is not torch.int32 or parent.device != on.dev or parent.shape[1] < R // B or parent.stride(1) != 1:
+            raise ValueError(f"sp_beam_reorder: parent must be int32 [{B}, at least {R // B}]")
+        if err is None:
+            err = torch.zeros(1, dtype=torch.int32, device=on.dev)
+        k = on.ptr("kv", kv, torch.bfloat16, (None, 2, None, None, None))
+        io = sp_beam_reorder_io(B, R // B, kv.shape[0], k, kv.shape[2], kv.shape[3], kv.shape[4],
+                                on.ptr("table", table, torch.int32, (R, None)),
+                                on.ptr("own_table", own_table, torch.int32, (R, table.shape[1])), table.shape[1],
+                                on.ptr("lens", lens, torch.int32, (R,)), parent.data_ptr(),
+                                parent.stride(0) if B > 1 else max(parent.stride(0), R // B),
+                                on.ptr("err", err, torch.int32, (1,)))
+        _check(lib().sp_beam_reorder(C.byref(io), _stream(stream)), "sp_beam_reorder")
+    return err
 
 
 class Pipeline:

@@ -302,6 +302,35 @@ cudaError_t vp_gate_launch(const void* X, const void* noise, const float* alpha,
 cudaError_t restore_launch(const BatchDesc& bd, const int* order, const int* ep_count, int k_max,
                            int* idx, int k_cap, int* count, int* err, cudaStream_t st);
 
+// ------------------------------------------------------------- paged cache, beams (paged.cu, beam.cu)
+struct PagedAppendArgs {
+  const __nv_bfloat16* qkv;
+  long long ld;
+  __nv_bfloat16* q_out;  // NULL: queries are not wanted
+  long long ld_q;
+  __nv_bfloat16* kv;     // [2][n_pages][page][Hkv dh]
+  int n_pages, page_shift;
+  const int* table;
+  int max_pages;
+  const int* lens;       // NULL: 0
+  const int* cu_rows;    // NULL: row b is sequence b's
+  int B, T_cap, Hq, Hkv, dh;
+  const float2* rope;    // [max_pos, dh / 2] (cos, sin), NULL: no rotation
+  int max_pos;
+  const int* pos;
+  const int* pos3;       // [T_cap, 4]
+  int sec1, sec2;        // pos3: pairs below sec1 take its first component, below sec2 its second
+  int* err;
+};
+cudaError_t paged_append_launch(const PagedAppendArgs& a, cudaStream_t st);
+size_t beam_select_bytes(int rows, int V, int n_out);
+cudaError_t beam_select_launch(const void* logits, bool f32, long long ld, int B, int W, int V, const float* cum,
+                               const unsigned char* done, int eos, int n_out, void* ws, float* score, int* parent,
+                               int* token, cudaStream_t st);
+cudaError_t beam_reorder_launch(void* kv, int n_layers, int n_pages, int page_shift, int row_bytes, int* table,
+                                const int* own, int max_pages, const int* lens, const int* parent, int ld_parent,
+                                int B, int W, int* err, cudaStream_t st);
+
 // ------------------------------------------------------------- entry-point helpers (api.cu)
 // Records a thread-local error message (sp_last_error) and returns `s`.
 sp_status report(sp_status s, const char* fmt, ...);

@@ -1,0 +1,401 @@
+// Attention of rows that share a prefix, over a paged cache: every row of a sequence reads its group's
+// prefix and, causally, its sequence's own keys; grouped-query heads map query head i to kv head
+// i / (Hq / Hkv).  prefix_plan.cuh says how the work is cut; here are the kernel for few query vectors
+// per entry and the kernel that joins the segments.
+//
+// Score s_k = scale <q, K_k>, m = max s_k, l = sum exp(s_k - m), o = sum exp(s_k - m) V_k / l, one pass over
+// the keys with the running m, l and o in fp32; exponentials in base 2 with scale log2(e) folded into the
+// scores.  P is rounded to bf16 for the second product (relative 2^-9 of each weight, the operand's type),
+// the sum l takes the unrounded weights.  A row without a visible key has l = 0: zeros out, lse -infinity.
+#include <algorithm>
+
+#include "internal.h"
+#include "prefix_plan.cuh"
+
+namespace sp {
+
+namespace {
+
+SP_DEVINL float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+SP_DEVINL void cp_async16(uint32_t dst, const void* src, int bytes) {  // bytes 16, or 0: zeros
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+SP_DEVINL void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+SP_DEVINL void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+SP_DEVINL void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+SP_DEVINL void ldsm4_t(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+// c += a b, 16 x 8 x 16, bf16 in, fp32 sums
+SP_DEVINL void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+      "{%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// --------------------------------------------------------------- few query vectors per entry
+// A worker is one warp with its own ring of key tiles in shared memory: 16 query vectors against 16 keys at
+// a time (a tile never crosses a page, whose size is a multiple of 16), no barrier between warps.  Bound by
+// the cache's bytes: the products are padded to 16 rows, which the memory's pace leaves room for.
+constexpr int WK_WARPS = 8, WK_NT = WK_WARPS * 32, WK_KEYS = 16, WK_ROWS = 16;
+
+template <int DH>
+struct WkCfg {
+  static constexpr int ROW = DH * 2;                     // bytes of a key's row
+  static constexpr int STAGE = 2 * WK_KEYS * ROW;        // K tile, V tile
+  static constexpr int NS = DH == 128 ? 3 : 6;           // tiles in flight per warp: 24 KB
+  static constexpr size_t SMEM = (size_t)WK_WARPS * NS * STAGE;
+};
+
+template <int DH>
+__global__ void __launch_bounds__(WK_NT, 1) prefix_warp_kernel(const PrefixArgs a, const PlanArgs p) {
+  using C = WkCfg<DH>;
+  constexpr int CPR = DH / 8;  // 16-byte chunks of a row
+  extern __shared__ __align__(128) uint8_t ring_all[];
+  __shared__ PlanShared plan;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int E = a.n_groups + a.B, G = a.Hq / a.Hkv;
+  pdl_wait();
+  pdl_trigger();
+  build_plan<WK_NT>(a, p, plan, blockIdx.x == 0);
+  const long long N = plan.tile0[E];
+  if (N == 0) return;
+  const int P = plan_workers(N, p.workers, p.min_tiles);
+  const int w = blockIdx.x + warp * gridDim.x;  // (a short list goes to different SMs first)
+  if (w >= P) return;
+  const long long t0 = part_begin(N, P, w), t1 = part_begin(N, P, w + 1);
+  if (t0 >= t1) return;
+
+  const uint32_t ring = smem_u32(ring_all) + warp * C::NS * C::STAGE;
+  const size_t W = (size_t)a.Hkv * DH;
+  const size_t plane = ((size_t)a.n_pages << a.page_shift) * W;
+
+  TileCursor put, get;
+  put.seek(plan, p, E, a.Hkv, t0);
+  get = put;
+
+  // one tile into ring slot `slot`: lane = 16-byte chunk of a row, rows in turn; rows past the keys are zeros
+  auto load_tile = [&](int slot) {
+    const bool pre = put.e < a.n_groups;
+    const int k0 = put.j * WK_KEYS;
+    const int n = min(WK_KEYS, plan.keys[put.e] - k0);
+    const int* tb = pre ? a.ptable + (size_t)put.e * a.pmax_pages : a.table + (size_t)(put.e - a.n_groups) * a.max_pages;
+    int page = __ldg(tb + (k0 >> a.page_shift));
+    bool ok = page >= 0 && page < a.n_pages;
+    if (!ok) {
+      if (lane == 0) set_error(a.err, SP_DEVERR_INDEX);
+      page = 0;
+    }
+    const __nv_bfloat16* src =
+        a.kv + (((size_t)page << a.page_shift) + (k0 & ((1 << a.page_shift) - 1))) * W + put.kvh * DH;
+    const uint32_t dst = ring + slot * C::STAGE;
+    const int c = lane % CPR;
+#pragma unroll
+    for (int r0 = 0; r0 < WK_KEYS; r0 += 32 / CPR) {
+      const int r = r0 + lane / CPR;
+      const bool in = ok && r < n;
+      const __nv_bfloat16* s = src + (in ? r : 0) * W + c * 8;
+      const uint32_t d = dst + r * C::ROW + ((c ^ (r & 7)) << 4);
+      cp_async16(d, s, in ? 16 : 0);
+      cp_async16(d + WK_KEYS * C::ROW, s + plane, in ? 16 : 0);
+    }
+  };
+
+  long long t_put = t0;
+#pragma unroll
+  for (int s = 0; s < C::NS - 1; ++s) {
+    if (t_put < t1) {
+      load_tile(s);
+      if (++t_put < t1) put.next(plan, p, a.Hkv);
+    }
+    cp_async_commit();
+  }
+
+  uint32_t qf[DH / 16][4];
+  float o[DH / 8][4];
+  float m[2], l[2];
+  int lim[2];
+  bool fresh = true;
+  int slot = 0, slot_put = C::NS - 1;
+  const int row_a = lane >> 2, col = (lane & 3) * 2;
+
+  for (long long t = t0; t < t1; ++t) {
+    if (fresh) {  // a new segment: its query vectors, empty statistics
+      const int M = plan.rows[get.e] * G;
+      const int keys = plan.keys[get.e], R = plan.rows[get.e];
+      const bool pre = get.e < a.n_groups;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int mv = get.rt * WK_ROWS + row_a + 8 * h;
+        const int r = mv / G, g = mv - r * G;
+        const bool have = mv < M;
+        lim[h] = have ? (pre ? keys : min(max(keys - R + r + 1, 0), keys)) : 0;
+        const __nv_bfloat16* qr = a.q + (have ? (plan.row0[get.e] + r) * a.ld_q + (get.kvh * G + g) * DH : 0) + col;
+#pragma unroll
+        for (int kk = 0; kk < DH / 16; ++kk) {
+          qf[kk][h] = have ? __ldg(reinterpret_cast<const unsigned int*>(qr + kk * 16)) : 0u;
+          qf[kk][h + 2] = have ? __ldg(reinterpret_cast<const unsigned int*>(qr + kk * 16 + 8)) : 0u;
+        }
+        m[h] = -INFINITY;
+        l[h] = 0.f;
+      }
+#pragma unroll
+      for (int n = 0; n < DH / 8; ++n)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[n][c] = 0.f;
+      fresh = false;
+    }
+    if (t_put < t1) {
+      load_tile(slot_put);
+      if (++t_put < t1) put.next(plan, p, a.Hkv);
+    }
+    cp_async_commit();
+    if (++slot_put == C::NS) slot_put = 0;
+    cp_async_wait<C::NS - 1>();
+    __syncwarp();  // every lane's copies of this tile have landed and are visible to the warp
+
+    const uint32_t kt = ring + slot * C::STAGE, vt = kt + WK_KEYS * C::ROW;
+    float s[2][4];
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) s[n][c] = 0.f;
+    {
+      const int r = (lane >> 4) * 8 + (lane & 7), cb = (lane >> 3) & 1;
+#pragma unroll
+      for (int kk = 0; kk < DH / 16; ++kk) {
+        uint32_t b[4];
+        ldsm4(kt + r * C::ROW + (((2 * kk + cb) ^ (r & 7)) << 4), b);
+        mma16816(s[0], qf[kk], b[0], b[1]);
+        mma16816(s[1], qf[kk], b[2], b[3]);
+      }
+    }
+    const int k0 = get.j * WK_KEYS;
+    uint32_t pf[4];
+    float corr[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float x[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int key = k0 + (c >> 1) * 8 + col + (c & 1);
+        x[c] = key < lim[h] ? s[c >> 1][2 * h + (c & 1)] * a.scale_log2 : -INFINITY;
+      }
+      float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+      const float mn = fmaxf(m[h], mx);
+      const float mz = mn == -INFINITY ? 0.f : mn;
+      corr[h] = ex2(m[h] - mz);  // (0 while m is -infinity)
+      m[h] = mn;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) x[c] = ex2(x[c] - mz);
+      l[h] = l[h] * corr[h] + ((x[0] + x[1]) + (x[2] + x[3]));
+      pf[h] = pack_bf16x2(x[0], x[1]);
+      pf[h + 2] = pack_bf16x2(x[2], x[3]);
+    }
+    if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
+#pragma unroll
+      for (int n = 0; n < DH / 8; ++n) {
+        o[n][0] *= corr[0];
+        o[n][1] *= corr[0];
+        o[n][2] *= corr[1];
+        o[n][3] *= corr[1];
+      }
+    }
+    {
+      const int r = ((lane >> 3) & 1) * 8 + (lane & 7), cb = lane >> 4;
+#pragma unroll
+      for (int nn = 0; nn < DH / 16; ++nn) {
+        uint32_t b[4];
+        ldsm4_t(vt + r * C::ROW + (((2 * nn + cb) ^ (r & 7)) << 4), b);
+        mma16816(o[2 * nn], pf, b[0], b[1]);
+        mma16816(o[2 * nn + 1], pf, b[2], b[3]);
+      }
+    }
+    __syncwarp();  // the tile is read before a lane's next copies overwrite it
+    if (++slot == C::NS) slot = 0;
+
+    if (t + 1 == t1 || get.j + 1 == get.kt) {  // the segment ends
+      const int M = plan.rows[get.e] * G;
+      const size_t base = ((size_t)get.item + w) * p.slot_rows;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float sum = l[h];
+        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+        const int mr = row_a + 8 * h;
+        if (get.rt * WK_ROWS + mr < M) {
+          float* po = p.part_o + (base + mr) * DH + col;
+#pragma unroll
+          for (int n = 0; n < DH / 8; ++n)
+            *reinterpret_cast<float2*>(po + n * 8) = make_float2(o[n][2 * h], o[n][2 * h + 1]);
+          if ((lane & 3) == 0) p.part_ml[base + mr] = make_float2(m[h], sum);
+        }
+      }
+      fresh = true;
+    }
+    if (t + 1 < t1) get.next(plan, p, a.Hkv);
+  }
+  cp_async_wait<0>();
+}
+
+// --------------------------------------------------------------- joining the segments
+// One warp per (row, query head): the segments of its prefix item and of its own item, in key order.
+template <int DH>
+__global__ void __launch_bounds__(256) prefix_merge_kernel(const PrefixArgs a, const PlanArgs pp, const PlanArgs po) {
+  pdl_wait();
+  pdl_trigger();
+  const int lane = threadIdx.x & 31;
+  const int E = a.n_groups + a.B, G = a.Hq / a.Hkv;
+  const long long rows = row_begin(a, a.B);
+  const long long first = row_begin(a, 0);
+  for (long long i = blockIdx.x * 8ll + (threadIdx.x >> 5); i < (rows - first) * a.Hq; i += gridDim.x * 8ll) {
+    const int row = (int)(first + i / a.Hq), h = (int)(i % a.Hq);
+    int lo = 0, hi = a.B - 1;
+    while (lo < hi) {  // the row's sequence
+      const int mid = (lo + hi + 1) >> 1;
+      if (row_begin(a, mid) <= row) lo = mid; else hi = mid - 1;
+    }
+    const int b = lo;
+    int g = -1;
+    if (a.n_groups > 0) {  // its group, if it is in one
+      lo = 0;
+      hi = a.n_groups - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (__ldg(a.group_cu + mid) <= b) lo = mid; else hi = mid - 1;
+      }
+      if (__ldg(a.group_cu + lo) <= b && b < __ldg(a.group_cu + lo + 1)) g = lo;
+    }
+    constexpr int V = DH / 32;
+    float acc[V], mm = -INFINITY, ll = 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) acc[v] = 0.f;
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+      const PlanArgs& p = side == 0 ? pp : po;
+      const int e = side == 0 ? g : a.n_groups + b;
+      if (e < 0) continue;
+      const long long N = __ldcg(p.tile0 + E), e0 = __ldcg(p.tile0 + e), e1 = __ldcg(p.tile0 + e + 1);
+      const int i0 = __ldcg(p.item0 + e), n_items = __ldcg(p.item0 + e + 1) - i0;
+      if (e1 <= e0) continue;
+      const long long kt = (e1 - e0) / n_items;
+      const int r0 = side == 0 ? row_begin(a, __ldg(a.group_cu + g)) : row_begin(a, b);
+      const int mv = (row - r0) * G + h % G;
+      const int rt = mv / p.tile_rows, mr = mv - rt * p.tile_rows;
+      const int in = rt * a.Hkv + h / G;
+      if (in < 0 || in >= n_items) continue;  // (row offsets that do not ascend)
+      const long long t0 = e0 + in * kt;
+      const int P = plan_workers(N, p.workers, p.min_tiles);
+      const int w0 = part_of(N, P, t0), w1 = part_of(N, P, t0 + kt - 1);
+      for (int w = w0; w <= w1; ++w) {
+        const size_t at = ((size_t)(i0 + in) + w) * p.slot_rows + mr;
+        const float2 ml = __ldcg(p.part_ml + at);
+        if (ml.x == -INFINITY) continue;
+        const float mn = fmaxf(mm, ml.x);
+        const float ca = ex2(mm - mn), cb = ex2(ml.x - mn);
+        const float* x = p.part_o + at * DH + lane * V;
+        float y[V];
+        if (V == 4) *reinterpret_cast<float4*>(y) = __ldcg(reinterpret_cast<const float4*>(x));
+        else *reinterpret_cast<float2*>(y) = __ldcg(reinterpret_cast<const float2*>(x));
+#pragma unroll
+        for (int v = 0; v < V; ++v) acc[v] = acc[v] * ca + y[v] * cb;
+        ll = ll * ca + ml.y * cb;
+        mm = mn;
+      }
+    }
+    const float inv = ll > 0.f ? 1.f / ll : 0.f;
+    __nv_bfloat16* d = a.out + row * a.ld_out + (long long)h * DH + lane * V;
+    if (V == 4)
+      *reinterpret_cast<uint2*>(d) = make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv),
+                                                pack_bf16x2(acc[V - 2] * inv, acc[V - 1] * inv));
+    else
+      *reinterpret_cast<uint32_t*>(d) = pack_bf16x2(acc[0] * inv, acc[1] * inv);
+    if (a.lse && lane == 0)
+      a.lse[(size_t)row * a.Hq + h] = ll > 0.f ? (mm + log2f(ll)) * 0.69314718055994531f : -INFINITY;
+  }
+}
+
+}  // namespace
+
+// Rows of an item's slot and slots of one launch at most, from what the host knows.
+static size_t plan_slots(const PlanArgs& p, int T_cap, int B, int n_groups, int G, int Hkv) {
+  size_t items = 0;
+  const size_t full = ((size_t)T_cap * G) / p.tile_rows;
+  if (p.prefix) items += (full + n_groups) * Hkv;
+  if (p.own) items += (full + B) * Hkv;
+  return items + p.workers;
+}
+
+PrefixLayout prefix_layout(int T_cap, int B, int n_groups, int Hq, int Hkv, int dh) {
+  PrefixLayout L;
+  const int G = Hq / Hkv;
+  const int sms = device_sm_count();
+  PlanArgs& p = L.warp;
+  p = PlanArgs();
+  p.tile_rows = WK_ROWS;
+  p.key_shift = 4;
+  p.min_tiles = 2;
+  p.workers = sms * WK_WARPS;
+  p.prefix = n_groups > 0;
+  p.own = true;
+  p.slot_rows = (int)std::min<size_t>(WK_ROWS, (size_t)T_cap * G);
+  L.slots = plan_slots(p, T_cap, B, n_groups, G, Hkv);
+  const size_t E = (size_t)n_groups + B + 1;
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off = (off + bytes + 255) & ~size_t(255);
+    return at;
+  };
+  L.off_tile0 = take(E * 8);
+  L.off_item0 = take(E * 4);
+  L.off_ml = take(L.slots * p.slot_rows * 8);
+  L.off_o = take(L.slots * p.slot_rows * dh * 4);
+  L.bytes = off;
+  return L;
+}
+
+cudaError_t prefix_attention_launch(const PrefixArgs& a, int dh, void* ws, cudaStream_t st) {
+  if (a.T_cap == 0) return cudaSuccess;
+  PrefixLayout L = prefix_layout(a.T_cap, a.B, a.n_groups, a.Hq, a.Hkv, dh);
+  char* base = static_cast<char*>(ws);
+  PlanArgs p = L.warp;
+  p.tile0 = reinterpret_cast<long long*>(base + L.off_tile0);
+  p.item0 = reinterpret_cast<int*>(base + L.off_item0);
+  p.part_ml = reinterpret_cast<float2*>(base + L.off_ml);
+  p.part_o = reinterpret_cast<float*>(base + L.off_o);
+  const int sms = device_sm_count();
+  const size_t smem = dh == 128 ? WkCfg<128>::SMEM : WkCfg<64>::SMEM;
+  auto* kern = dh == 128 ? prefix_warp_kernel<128> : prefix_warp_kernel<64>;
+  cudaError_t r = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (r != cudaSuccess) return r;
+  prof_begin_launch(st);
+  r = launch_pdl(kern, dim3(sms), dim3(WK_NT), smem, st, a, p);
+  prof_end_launch(st, SP_K_ATTN, 0.0, 0.0);
+  if (r != cudaSuccess) return r;
+  const long long warps = (long long)a.T_cap * a.Hq;
+  const int grid = (int)std::min<long long>((warps + 7) / 8, (long long)sms * 8);
+  prof_begin_launch(st);
+  r = launch_pdl(dh == 128 ? prefix_merge_kernel<128> : prefix_merge_kernel<64>, dim3(grid), dim3(256), 0, st, a, p, p);
+  prof_end_launch(st, SP_K_ATTN, 0.0, 0.0);
+  return r;
+}
+
+}  // namespace sp

@@ -1,0 +1,213 @@
+// How the attention over shared prefixes (prefix_attn.cu, prefix_attn_tc.cu) is cut into work.
+//
+// The keys a call reads form entries: entry g < n_groups is group g's prefix, read by all rows of the
+// group's sequences; entry n_groups + b is sequence b's own keys, read by its rows.  For one key / value
+// head the G = Hq / Hkv query heads of a row read the same keys, so an entry with R rows is a product of
+// M = R G query vectors (vector m: row m / G, head m % G of the kv head's G) with the entry's keys.  The M
+// vectors are cut into row tiles, the keys into key tiles; an item is (entry, row tile, kv head) and the
+// items' key tiles, one after the other, are one list of N tiles.  P workers (warps, or the two pipelines
+// of a CTA) take equal consecutive parts of it, whatever the entries' lengths: worker w the tiles
+// [w N / P, (w + 1) N / P).  The part of an item that one worker takes is a segment; a segment writes its
+// running max, sum and weighted values in 32 bits to slot (item index + worker index), which is its own:
+// going along the list, each next segment has the next item or the next worker.  prefix_merge_kernel joins
+// every row's segments.  All lengths are read on the device; every CTA builds the same plan from them.
+#pragma once
+#include "common.cuh"
+
+namespace sp {
+
+constexpr int kPlanEntries = 2 * SP_MAX_BATCH;
+
+struct PrefixArgs {
+  const __nv_bfloat16* q;
+  long long ld_q;
+  __nv_bfloat16* out;
+  long long ld_out;
+  float* lse;              // [T_cap, Hq] or NULL
+  const __nv_bfloat16* kv; // [2][n_pages][page][Hkv DH]
+  int n_pages, page_shift;
+  const int* table;
+  int max_pages;
+  const int* lens;
+  const int* ptable;
+  int pmax_pages;
+  const int* plens;
+  const int* group_cu;
+  int n_groups;
+  const int* cu_rows;      // NULL: row b is sequence b's
+  int B, T_cap, Hq, Hkv;
+  float scale_log2;        // scale * log2(e): scores are exponentiated in base 2
+  int* err;
+};
+
+// One launch's share of the entries, and where its segments go.
+struct PlanArgs {
+  int tile_rows;           // query vectors of a row tile
+  int key_shift;           // log2 of the keys of a key tile
+  int min_tiles;           // key tiles a worker takes at least (while there are enough)
+  int workers;
+  bool prefix, own;        // which entries this launch covers
+  long long* tile0;        // [n_groups + B + 1] first tile of each entry, then N      (written for the merge)
+  int* item0;              // [n_groups + B + 1] first item of each entry, then the item count
+  float* part_o;           // [slots][slot_rows][DH]
+  float2* part_ml;         // [slots][slot_rows] (max in log2 units, sum)
+  int slot_rows;
+};
+
+// Rows of sequence b begin here (b in 0..B), clamped to the rows there are.
+SP_DEVINL int row_begin(const PrefixArgs& a, int b) {
+  return min(max(a.cu_rows ? __ldg(a.cu_rows + b) : b, 0), a.T_cap);
+}
+
+struct PlanShared {
+  long long tile0[kPlanEntries + 1];
+  int item0[kPlanEntries + 1];
+  int row0[kPlanEntries], rows[kPlanEntries], keys[kPlanEntries];
+  long long wsum_t[32];
+  int wsum_i[32];
+};
+
+SP_DEVINL int plan_workers(long long N, int workers, int min_tiles) {
+  const long long most = (N + min_tiles - 1) / min_tiles;
+  return (int)(most < workers ? (most < 1 ? 1 : most) : workers);
+}
+// First tile of worker w's part.
+SP_DEVINL long long part_begin(long long N, int P, int w) { return (long long)w * N / P; }
+// The worker whose part holds tile t: the largest w with floor(w N / P) <= t.
+SP_DEVINL int part_of(long long N, int P, long long t) { return (int)(((t + 1) * P - 1) / N); }
+
+// Called by all NT threads of the CTA (a multiple of 32, at most 1,024).
+template <int NT>
+SP_DEVINL void build_plan(const PrefixArgs& a, const PlanArgs& p, PlanShared& s, bool write) {
+  const int E = a.n_groups + a.B, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int G = a.Hq / a.Hkv;
+  constexpr int PER = (kPlanEntries + NT - 1) / NT;
+  long long t_sum = 0;
+  int i_sum = 0;
+  long long tl[PER];
+  int il[PER];
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const int e = tid * PER + k;
+    int items = 0;
+    long long tiles = 0;
+    if (e < E) {
+      const bool pre = e < a.n_groups;
+      const int b = e - a.n_groups;
+      const int b0 = pre ? min(max(__ldg(a.group_cu + e), 0), a.B) : b;
+      const int b1 = pre ? min(max(__ldg(a.group_cu + e + 1), 0), a.B) : b + 1;
+      const int r0 = row_begin(a, b0), r = max(row_begin(a, b1) - r0, 0);
+      const int L = pre ? __ldg(a.plens + e) : __ldg(a.lens + b);
+      const int cap = (pre ? a.pmax_pages : a.max_pages) << a.page_shift;
+      if ((L < 0 || L > cap) && write) set_error(a.err, SP_DEVERR_INDEX);
+      const int keys = min(max(L, 0), cap);
+      s.row0[e] = r0;
+      s.rows[e] = r;
+      s.keys[e] = keys;
+      if (pre ? p.prefix : p.own) {
+        items = (r * G + p.tile_rows - 1) / p.tile_rows * a.Hkv;
+        tiles = (long long)items * ((keys + (1 << p.key_shift) - 1) >> p.key_shift);
+      }
+    }
+    il[k] = items;
+    tl[k] = tiles;
+    i_sum += items;
+    t_sum += tiles;
+  }
+  int ix = i_sum;
+  long long tx = t_sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int iu = __shfl_up_sync(0xffffffffu, ix, o);
+    const long long tu = __shfl_up_sync(0xffffffffu, tx, o);
+    if (lane >= o) {
+      ix += iu;
+      tx += tu;
+    }
+  }
+  if (lane == 31) {
+    s.wsum_i[warp] = ix;
+    s.wsum_t[warp] = tx;
+  }
+  __syncthreads();
+  ix -= i_sum;
+  tx -= t_sum;
+  for (int w = 0; w < warp; ++w) {
+    ix += s.wsum_i[w];
+    tx += s.wsum_t[w];
+  }
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const int e = tid * PER + k;
+    if (e <= E) {
+      s.item0[e] = ix;
+      s.tile0[e] = tx;
+      if (write) {
+        p.item0[e] = ix;
+        p.tile0[e] = tx;
+      }
+    }
+    ix += il[k];
+    tx += tl[k];
+  }
+  if (tid == NT - 1 && E == NT * PER) {  // (the total's place, when every thread's last entry is a real one)
+    s.item0[E] = ix;
+    s.tile0[E] = tx;
+    if (write) {
+      p.item0[E] = ix;
+      p.tile0[E] = tx;
+    }
+  }
+  __syncthreads();
+}
+
+// A walk along a worker's tiles.
+struct TileCursor {
+  int e, item, rt, kvh, j, kt;  // entry, item (over all entries), row tile, kv head, key tile of kt
+  SP_DEVINL void set_item(const PlanShared& s, const PlanArgs& p, int Hkv) {
+    const int in = item - s.item0[e];
+    rt = in / Hkv;
+    kvh = in - rt * Hkv;
+    kt = (s.keys[e] + (1 << p.key_shift) - 1) >> p.key_shift;
+  }
+  // the entry that holds tile t (entries without tiles are passed over)
+  SP_DEVINL void seek(const PlanShared& s, const PlanArgs& p, int E, int Hkv, long long t) {
+    int lo = 0, hi = E - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (s.tile0[mid] <= t) lo = mid; else hi = mid - 1;
+    }
+    e = lo;
+    const int k = (s.keys[e] + (1 << p.key_shift) - 1) >> p.key_shift;
+    const int in = (int)((t - s.tile0[e]) / k);
+    item = s.item0[e] + in;
+    j = (int)((t - s.tile0[e]) - (long long)in * k);
+    set_item(s, p, Hkv);
+  }
+  // to the next tile, which exists
+  SP_DEVINL void next(const PlanShared& s, const PlanArgs& p, int Hkv) {
+    if (++j < kt) return;
+    j = 0;
+    ++item;
+    while (item >= s.item0[e + 1] || s.tile0[e + 1] == s.tile0[e]) {
+      ++e;
+      item = s.item0[e];
+    }
+    set_item(s, p, Hkv);
+  }
+};
+
+}  // namespace sp
+
+namespace sp {
+
+// Workspace of a call (host arithmetic on what the host knows).
+struct PrefixLayout {
+  PlanArgs warp;
+  size_t slots;
+  size_t off_tile0, off_item0, off_ml, off_o, bytes;
+};
+PrefixLayout prefix_layout(int T_cap, int B, int n_groups, int Hq, int Hkv, int dh);
+cudaError_t prefix_attention_launch(const PrefixArgs& a, int dh, void* ws, cudaStream_t st);
+
+}  // namespace sp
