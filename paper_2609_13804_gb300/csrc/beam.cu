@@ -15,7 +15,11 @@ namespace sp {
 
 namespace {
 
-constexpr int BS_NT = 256, BS_WARPS = BS_NT / 32, BS_MAX_OUT = 32;
+constexpr int BS_NT = 256, BS_WARPS = BS_NT / 32, BS_MAX_OUT = 2 * SP_MAX_BEAMS;
+constexpr int BS_LOADS = 4;                 // 16-byte loads per thread and tile
+constexpr int BS_BLOCK = 16;                // tiles of a block
+constexpr int BS_CAP = 128;                 // candidates a warp keeps at most
+constexpr int BS_LIST = 256;                // slices x n_out of a row, at most (one warp's join)
 constexpr float kLog2e = 1.44269504088896341f;
 
 SP_DEVINL float ex2(float x) {
@@ -26,7 +30,7 @@ SP_DEVINL float ex2(float x) {
 
 // A logit and its token as one key that sorts by (logit, lower token first); 0: none.
 SP_DEVINL unsigned long long cand_key(float x, int v) {
-  const uint32_t u = __float_as_uint(x);
+  const uint32_t u = __float_as_uint(x + 0.f);  // (-0 is 0)
   const uint32_t s = (u & 0x80000000u) ? ~u : (u | 0x80000000u);
   return ((unsigned long long)s << 32) | (uint32_t)~v;
 }
@@ -47,255 +51,392 @@ struct MaxSum {
   }
 };
 
-// The n largest keys seen by a warp, one per lane in descending order.
-struct WarpTop {
-  unsigned long long key;  // lane i: the i-th largest (0: none)
-  unsigned long long least;  // the n-th largest: what a new key has to exceed
-  SP_DEVINL void offer(unsigned long long k, int n, int lane) {
-    unsigned int some = __ballot_sync(0xffffffffu, k > least);
-    while (some) {
-      const int src = __ffs(some) - 1;
-      some &= some - 1;
-      const unsigned long long c = __shfl_sync(0xffffffffu, k, src);
-      if (c <= least) continue;
-      const int at = __popc(__ballot_sync(0xffffffffu, key > c));
-      const unsigned long long up = __shfl_up_sync(0xffffffffu, key, 1);
-      if (lane == at) key = c;
-      else if (lane > at) key = up;
-      if (lane >= n) key = 0;
-      least = __shfl_sync(0xffffffffu, key, n - 1);
-    }
-  }
-};
-
 template <bool F32>
 struct Chunk;  // 16 bytes of logits
 template <>
 struct Chunk<true> {
   static constexpr int N = 4;
-  SP_DEVINL static void unpack(const uint4& u, float (&x)[4]) {
-    x[0] = __uint_as_float(u.x);
-    x[1] = __uint_as_float(u.y);
-    x[2] = __uint_as_float(u.z);
-    x[3] = __uint_as_float(u.w);
+  static constexpr uint32_t kNone = 0xff800000u;  // a word of -infinity
+  SP_DEVINL static float at(const uint4& u, int k) {
+    return __uint_as_float(k == 0 ? u.x : k == 1 ? u.y : k == 2 ? u.z : u.w);
+  }
+  SP_DEVINL static float top(const uint4& u) {  // (fmaxf passes over NaN)
+    return fmaxf(fmaxf(__uint_as_float(u.x), __uint_as_float(u.y)), fmaxf(__uint_as_float(u.z), __uint_as_float(u.w)));
   }
   SP_DEVINL static float one(const void* row, int v) { return __ldg(static_cast<const float*>(row) + v); }
 };
 template <>
 struct Chunk<false> {
   static constexpr int N = 8;
-  SP_DEVINL static void unpack(const uint4& u, float (&x)[8]) {
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(w[i] << 16);
-      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
+  static constexpr uint32_t kNone = 0xff80ff80u;
+  SP_DEVINL static float at(const uint4& u, int k) {
+    const uint32_t w = k < 2 ? u.x : k < 4 ? u.y : k < 6 ? u.z : u.w;
+    return __uint_as_float((k & 1) ? (w & 0xffff0000u) : (w << 16));
+  }
+  SP_DEVINL static float top(const uint4& u) {
+    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&u);
+    const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));  // (NaN passed over)
+    return fmaxf(__low2float(m), __high2float(m));
   }
   SP_DEVINL static float one(const void* row, int v) {
     return __bfloat162float(static_cast<const __nv_bfloat16*>(row)[v]);
   }
 };
 
-// One CTA: a slice of one row.  Its (m, sum) and n_out largest keys to part.
+// Two fp32 numbers as one operand of Blackwell's packed arithmetic
+SP_DEVINL unsigned long long pack2(float lo, float hi) {
+  unsigned long long r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+SP_DEVINL void unpack2(unsigned long long v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+SP_DEVINL unsigned long long add2(unsigned long long a, unsigned long long b) {
+  unsigned long long r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+SP_DEVINL unsigned long long mul2(unsigned long long a, unsigned long long b) {
+  unsigned long long r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+// The n_out largest of a warp's list of n (at most BS_CAP) to its front, in order, by counting the larger ones
+// of each; returns how many there are.  (A function of its own: its registers are not the scan's.)
+__device__ __noinline__ int cut_list(unsigned long long* list, int n, int n_out) {
+  const int lane = threadIdx.x & 31;
+  unsigned long long mine[BS_CAP / 32];
+  int rank[BS_CAP / 32];
+#pragma unroll
+  for (int q = 0; q < BS_CAP / 32; ++q) {
+    const int i = q * 32 + lane;
+    mine[q] = i < n ? list[i] : 0ull;
+    rank[q] = 0;
+  }
+  for (int i = 0; i < n; ++i) {
+    const unsigned long long u = list[i];
+#pragma unroll
+    for (int q = 0; q < BS_CAP / 32; ++q)
+      if (q * 32 < n) rank[q] += u > mine[q];
+  }
+  __syncwarp();
+#pragma unroll
+  for (int q = 0; q < BS_CAP / 32; ++q)
+    if (mine[q] != 0 && rank[q] < n_out) list[rank[q]] = mine[q];
+  __syncwarp();
+  return min(n, n_out);
+}
+
+// One CTA: a slice of one row.  The slice goes by in blocks of tiles (a tile: 4 loads of every thread).  First a
+// block's share of (m, sum), every thread noting the maximum of each of its tiles; nothing is selected on the way,
+// which would cost more than the sums.  Then a bound T below which n_out of the slice are known not to lie: the
+// least, over the warps, of the ceil(n_out / warps)-th largest thread maximum of the block (n_out threads hold
+// something at or above it, and only about 2.7 n_out logits of the block lie there).  Then the few threads whose
+// tiles reach T load those again (from L2) and put what lies above T into their warp's list.  A list that could
+// overflow is cut down to its n_out largest and T raised to the last of them, so any order of logits, and any
+// number of equal ones (keys tell them apart by token), is taken exactly.  At the end the lists' n_out largest,
+// in order, and (m, sum) go to part.
 template <bool F32>
-__global__ void __launch_bounds__(BS_NT)
+__global__ void __launch_bounds__(BS_NT, 4)
 beam_scan_kernel(const void* __restrict__ logits, long long ld, int V, const float* __restrict__ cum,
                  const unsigned char* __restrict__ done, int n_out, int slice, float2* __restrict__ part_ms,
                  unsigned long long* __restrict__ part_key) {
   using K = Chunk<F32>;
-  __shared__ unsigned long long top_s[BS_WARPS * BS_MAX_OUT];
+  __shared__ unsigned long long list_s[BS_WARPS][BS_CAP];
   __shared__ float2 ms_s[BS_WARPS];
+  __shared__ float tile_max[BS_BLOCK][BS_NT];
+  __shared__ uint32_t bound_s[2][BS_WARPS];
+  __shared__ int events[BS_WARPS][64];
+  __shared__ int n_s[BS_WARPS];
   pdl_wait();
   pdl_trigger();
-  const int row = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if ((done && done[row]) || !(cum[row] > -INFINITY)) return;  // (the join reads nothing of such a beam's row)
-  const char* base = static_cast<const char*>(logits) + row * ld * (F32 ? 4 : 2);
+  const int row = blockIdx.y, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const float cw = __ldg(cum + row);
+  const bool over = done && __ldg(done + row);
+  constexpr int esz = F32 ? 4 : 2, PER = BS_LOADS * K::N;  // logits per thread and tile: one to a lane at most
+  static_assert(PER <= 32 && BS_BLOCK % 2 == 0, "");
+  const char* base = static_cast<const char*>(logits) + row * ld * esz;
   const int v0 = min(blockIdx.x * slice, V), v1 = min(v0 + slice, V);
   // whole 16-byte chunks of the slice; what is before and behind them goes one by one
-  const int esz = F32 ? 4 : 2;
   const int head = min((int)((16 - (reinterpret_cast<uintptr_t>(base + (size_t)v0 * esz) & 15)) & 15) / esz, v1 - v0);
   const int c0 = v0 + head, chunks = (v1 - c0) / K::N, c1 = c0 + chunks * K::N;
+  unsigned long long* list = list_s[warp];
+  int n = 0;
   MaxSum ms{-INFINITY, 0.f};
-  WarpTop top{0ull, 0ull};
-  auto single = [&](float x, int v, bool in) {
-    in = in && x > -INFINITY;  // (NaN and -infinity are no candidates and have no weight)
-    if (in) ms.add(x, 1.f);
-    top.offer(in ? cand_key(x, v) : 0ull, n_out, lane);
-  };
-  if (warp == 0 && head > 0) {
-    const bool in = lane < head;
-    single(in ? K::one(base, v0 + lane) : 0.f, v0 + lane, in);
-  }
-  if (warp == 1 && c1 < v1) {
-    const bool in = lane < v1 - c1;
-    single(in ? K::one(base, c1 + lane) : 0.f, c1 + lane, in);
+  if (warp == 0) {
+    const bool in = lane < head + (v1 - c1);  // (fewer than 16)
+    const int v = lane < head ? v0 + lane : c1 + lane - head;
+    const float x = in ? K::one(base, v) : -INFINITY;
+    const bool some = x > -INFINITY;  // (NaN and -infinity are no candidates and have no weight)
+    const unsigned int all = __ballot_sync(0xffffffffu, some);
+    if (some) {
+      ms.m = x;
+      ms.s = 1.f;
+      list[__popc(all & ((1u << lane) - 1u))] = cand_key(x, v);
+    }
+    n = __popc(all);
   }
   const uint4* src = reinterpret_cast<const uint4*>(base + (size_t)c0 * esz);
-  const int steps = (chunks + BS_NT - 1) / BS_NT;
-  for (int i = 0; i < steps; ++i) {
-    const int c = i * BS_NT + threadIdx.x;
-    const bool in = c < chunks;
-    float x[K::N];
-    if (in) {
-      K::unpack(__ldg(src + c), x);
-    } else {
+  unsigned long long T = 0;  // keys above T are candidates
+  const int tile_chunks = BS_NT * BS_LOADS;
+  auto load = [&](int t, uint4 (&u)[BS_LOADS]) {
 #pragma unroll
-      for (int k = 0; k < K::N; ++k) x[k] = -INFINITY;
+    for (int q = 0; q < BS_LOADS; ++q) {
+      const int c = t * tile_chunks + q * BS_NT + tid;
+      u[q] = make_uint4(K::kNone, K::kNone, K::kNone, K::kNone);
+      if (c < chunks) u[q] = __ldg(src + c);
     }
-    float cm = -INFINITY;
+  };
+  const int tiles = (chunks + tile_chunks - 1) / tile_chunks;
+  float bm = -INFINITY;  // the thread's maximum of the block
+  auto take = [&](const uint4 (&u)[BS_LOADS], int place) {
+    float lm = -INFINITY;
 #pragma unroll
-    for (int k = 0; k < K::N; ++k) cm = fmaxf(cm, x[k]);  // (fmaxf passes over NaN)
-    if (cm > -INFINITY) {
-      if (cm > ms.m) {
-        ms.s = ms.m == -INFINITY ? 0.f : ms.s * ex2((ms.m - cm) * kLog2e);
-        ms.m = cm;
+    for (int q = 0; q < BS_LOADS; ++q) lm = fmaxf(lm, K::top(u[q]));
+    tile_max[place][tid] = lm;
+    bm = fmaxf(bm, lm);
+    if (lm == -INFINITY) return;
+    if (lm > ms.m) {
+      ms.s = ms.m == -INFINITY ? 0.f : ms.s * ex2((ms.m - lm) * kLog2e);
+      ms.m = lm;
+    }
+    // (x - m first, exactly where it matters, then log2 e: m log2 e rounded would shift the whole sum)
+    const unsigned long long nm = pack2(-ms.m, -ms.m), l2 = pack2(kLog2e, kLog2e);
+    unsigned long long sum[2] = {0ull, 0ull};
+#pragma unroll
+    for (int q = 0; q < BS_LOADS; ++q)
+#pragma unroll
+      for (int k = 0; k < K::N; k += 2) {
+        float a, b;
+        unpack2(mul2(add2(pack2(K::at(u[q], k), K::at(u[q], k + 1)), nm), l2), a, b);
+        sum[(k >> 1) & 1] = add2(sum[(k >> 1) & 1], pack2(ex2(a), ex2(b)));
       }
-      if (ms.m == INFINITY) {
+    float sa, sb;
+    unpack2(add2(sum[0], sum[1]), sa, sb);
+    float ts = sa + sb;
+    if (ts != ts) {  // a NaN, or infinity less infinity, among them
+      ts = 0.f;
+      for (int i = 0; i < PER; ++i) {
+        float x = 0.f;
 #pragma unroll
-        for (int k = 0; k < K::N; ++k) ms.s += x[k] == INFINITY ? 1.f : 0.f;
-      } else {
+        for (int q = 0; q < BS_LOADS; ++q)
 #pragma unroll
-        for (int k = 0; k < K::N; ++k) {
-          const float d = x[k] == x[k] ? x[k] : -INFINITY;
-          ms.s += ex2((d - ms.m) * kLog2e);
+          for (int k = 0; k < K::N; ++k)
+            if (i == q * K::N + k) x = K::at(u[q], k);
+        if (x == ms.m) ts += 1.f;
+        else if (x < ms.m) ts += ex2((x - ms.m) * kLog2e);
+      }
+    }
+    ms.s += ts;
+  };
+  uint4 ua[BS_LOADS], ub[BS_LOADS];  // a tile ahead
+  load(0, ua);
+  if (over || !(cw > -INFINITY)) return;  // (the join reads nothing of such a beam's row)
+  for (int tb = 0, block = 0; tb < tiles; tb += BS_BLOCK, ++block) {
+    const int te = min(tb + BS_BLOCK, tiles);  // (BS_BLOCK is even: tile tb + an even number is in ua)
+    bm = -INFINITY;
+    for (int t = tb; t < te; t += 2) {
+      load(t + 1, ub);
+      take(ua, t - tb);
+      if (t + 1 < te) {
+        load(t + 2, ua);
+        take(ub, t + 1 - tb);
+      }
+    }
+    // the block's bound
+    uint32_t rest = bm > -INFINITY ? (uint32_t)(cand_key(bm, 0) >> 32) : 0u, hi = 0;
+    for (int r = 0; r < n_out; r += BS_WARPS) {
+      hi = __reduce_max_sync(0xffffffffu, rest);
+      if (lane == __ffs(__ballot_sync(0xffffffffu, rest == hi)) - 1) rest = 0;
+    }
+    if (lane == 0) bound_s[block & 1][warp] = hi;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < BS_WARPS; ++w) hi = min(hi, bound_s[block & 1][w]);
+    if (hi != 0 && ((unsigned long long)hi << 32) - 1 > T) T = ((unsigned long long)hi << 32) - 1;
+    float Tf = T == 0 ? -INFINITY : key_logit(T);  // (a little below T: keys decide)
+    unsigned int who = __ballot_sync(0xffffffffu, bm >= Tf && bm > -INFINITY);
+    int* ev = events[warp];
+    while (who) {
+      // tiles of threads of the warp that reach T, 64 at most at a time
+      int ne = 0;
+      for (; who && ne <= 64 - BS_BLOCK; who &= who - 1) {
+        const int other = __ffs(who) - 1;
+        const bool reach = lane < te - tb && tile_max[lane & (BS_BLOCK - 1)][(warp << 5) + other] >= Tf;
+        const unsigned int all = __ballot_sync(0xffffffffu, reach);
+        if (reach) ev[ne + __popc(all & ((1u << lane) - 1u))] = (lane << 5) + other;
+        ne += __popc(all);
+      }
+      __syncwarp();
+      for (int e0 = 0; e0 < ne; e0 += 4) {  // each tile's logits, one to a lane; four tiles' loads at once
+        float x[4];
+        int v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int code = ev[min(e0 + i, ne - 1)];
+          const int q = lane / K::N, c = (tb + (code >> 5)) * tile_chunks + q * BS_NT + (warp << 5) + (code & 31);
+          v[i] = c0 + c * K::N + lane % K::N;
+          x[i] = e0 + i < ne && q < BS_LOADS && c < chunks ? K::one(base, v[i]) : -INFINITY;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const unsigned long long key = cand_key(x[i], v[i]);
+          const bool in = x[i] > -INFINITY && key > T;
+          const unsigned int all = __ballot_sync(0xffffffffu, in);
+          if (in) list[n + __popc(all & ((1u << lane) - 1u))] = key;
+          n += __popc(all);
+          __syncwarp();
+          if (n > BS_CAP - 32) {
+            n = cut_list(list, n, n_out);
+            if (list[n_out - 1] - 1 > T) T = list[n_out - 1] - 1;
+            Tf = key_logit(T);
+          }
         }
       }
-    }
-    if (__any_sync(0xffffffffu, cm > -INFINITY && cand_key(cm, 0) > top.least)) {
-#pragma unroll
-      for (int k = 0; k < K::N; ++k)
-        top.offer(x[k] > -INFINITY ? cand_key(x[k], c0 + c * K::N + k) : 0ull, n_out, lane);
+      __syncwarp();
     }
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const float m2 = __shfl_xor_sync(0xffffffffu, ms.m, o), s2 = __shfl_xor_sync(0xffffffffu, ms.s, o);
-    ms.add(m2, s2);
+  const float mw = warp_max(ms.m);
+  const float sw = warp_sum(ms.m == mw ? ms.s : ms.m > -INFINITY ? ms.s * ex2((ms.m - mw) * kLog2e) : 0.f);
+  if (n > 32) n = cut_list(list, n, n_out);
+  if (lane == 0) {
+    ms_s[warp] = make_float2(mw, sw);
+    n_s[warp] = n;
   }
-  if (lane < n_out) top_s[warp * n_out + lane] = top.key;
-  if (lane == 0) ms_s[warp] = make_float2(ms.m, ms.s);
   __syncthreads();
+  // every candidate's place: how many are larger
   const size_t at = (size_t)row * gridDim.x + blockIdx.x;
-  const int n = BS_WARPS * n_out;
-  if (threadIdx.x < n) {  // rank of every warp's keys among all (no two are equal, but for the empty ones)
-    const unsigned long long k = top_s[threadIdx.x];
-    int rank = 0;
-    for (int i = 0; i < n; ++i) {
-      const unsigned long long u = top_s[i];
-      rank += u > k || (u == k && i < threadIdx.x);
+  int total = 0, rank = 0;
+  const unsigned long long k = lane < n ? list[lane] : 0ull;
+  for (int w = 0; w < BS_WARPS; ++w) {
+    const int nw = n_s[w];
+    total += nw;
+    if (n > 0) {
+#pragma unroll 4
+      for (int i = 0; i < nw; ++i) rank += list_s[w][i] > k;
     }
-    if (rank < n_out) part_key[at * n_out + rank] = k;
   }
-  if (threadIdx.x == 0) {
+  if (k != 0 && rank < n_out) part_key[at * n_out + rank] = k;
+  if (tid < n_out && tid >= total) part_key[at * n_out + tid] = 0ull;
+  if (tid == 0) {
+    ms = MaxSum{ms_s[0].x, ms_s[0].y};
     for (int w = 1; w < BS_WARPS; ++w) ms.add(ms_s[w].x, ms_s[w].y);
     part_ms[at] = make_float2(ms.m, ms.s);
   }
 }
 
-SP_DEVINL double shfl_xor_d(double v, int o) { return __shfl_xor_sync(0xffffffffu, v, o); }
+// The bits of a double so that they sort as it does.
+SP_DEVINL unsigned long long order_bits(double v) {
+  const unsigned long long u = (unsigned long long)__double_as_longlong(v + 0.0);
+  return (u >> 63) ? ~u : (u | 0x8000000000000000ull);
+}
 
-// One CTA per element, a warp per beam: the slices' lists joined into the beam's n_out best, their scores in
-// 64 bits, then one warp takes the n_out best over the beams.
-__global__ void __launch_bounds__(512)
+// One CTA per element, a warp per beam: the beam's n_out best of its slices' lists by counting, for each, the
+// larger ones; their scores in 64 bits; then the same over the beams.  Comparisons are of integers (the 64-bit
+// floating-point pipe is slow here).  log(sum) is e log 2 + log f with sum = 2^e f: exact in e, and log f, below
+// 0.7, is good to 2^-24 in fp32, as are the sums that go into it.
+__global__ void __launch_bounds__(32 * SP_MAX_BEAMS)
 beam_join_kernel(int W, int V, int S, const float* __restrict__ cum, const unsigned char* __restrict__ done, int eos,
                  int n_out, const float2* __restrict__ part_ms, const unsigned long long* __restrict__ part_key,
                  float* __restrict__ score, int* __restrict__ parent, int* __restrict__ token) {
-  __shared__ double sc_s[16 * BS_MAX_OUT];
-  __shared__ int tk_s[16 * BS_MAX_OUT];
+  extern __shared__ unsigned long long rows_s[];  // [W][S n_out] the beams' lists
+  __shared__ unsigned long long sc_s[SP_MAX_BEAMS * BS_MAX_OUT];  // order_bits of the score, 0: none
+  __shared__ double val_s[SP_MAX_BEAMS * BS_MAX_OUT];
+  __shared__ int tk_s[SP_MAX_BEAMS * BS_MAX_OUT];
   pdl_wait();
   pdl_trigger();
   const int e = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (warp < W) {
-    const int row = e * W + warp;
-    const float cw = cum[row];
-    double sc = -INFINITY;
-    int tk = -1;
-    if (!(cw > -INFINITY)) {
-    } else if (done && done[row]) {
-      if (lane == 0) {
-        sc = cw;
-        tk = eos;
-      }
+  const int row = e * W + warp, n = S * n_out;
+  unsigned long long* sc = sc_s + warp * n_out;
+  if (lane < n_out) sc[lane] = 0;
+  // (a beam that was not scanned has nothing there: what is loaded for it is not used)
+  unsigned long long mine[BS_LIST / 32];
+  float2 ms[BS_LIST / 32];
+  const float cw = __ldg(cum + row);
+  const bool over = done && __ldg(done + row);
+#pragma unroll
+  for (int q = 0; q < BS_LIST / 32; ++q) {
+    const int i = q * 32 + lane;
+    mine[q] = i < n ? __ldcg(part_key + (size_t)row * n + i) : 0ull;
+    ms[q] = i < S ? __ldcg(part_ms + (size_t)row * S + i) : make_float2(-INFINITY, 0.f);
+  }
+  __syncwarp();
+  if (!(cw > -INFINITY)) {
+  } else if (over) {
+    if (lane == 0) {
+      sc[0] = order_bits((double)cw);
+      val_s[warp * n_out] = cw;
+      tk_s[warp * n_out] = eos;
+    }
+  } else {
+    unsigned long long* keys = rows_s + (size_t)warp * n;
+    int rank[BS_LIST / 32];
+    float m = -INFINITY;
+#pragma unroll
+    for (int q = 0; q < BS_LIST / 32; ++q) {
+      rank[q] = 0;
+      m = fmaxf(m, ms[q].x);
+    }
+    m = warp_max(m);
+    float sum = 0.f;
+#pragma unroll
+    for (int q = 0; q < BS_LIST / 32; ++q) {
+      if (ms[q].x == m) sum += ms[q].y;
+      else if (ms[q].x > -INFINITY) sum += ms[q].y * ex2((ms[q].x - m) * kLog2e);
+    }
+    sum = warp_sum(sum);
+#pragma unroll
+    for (int q = 0; q < BS_LIST / 32; ++q)
+      if (q * 32 + lane < n) keys[q * 32 + lane] = mine[q];
+    __syncwarp();
+    if (n <= 32) {
+#pragma unroll 8
+      for (int i = 0; i < n; ++i) rank[0] += keys[i] > mine[0];
     } else {
-      float m = -INFINITY;
-      for (int s = lane; s < S; s += 32) m = fmaxf(m, __ldcg(part_ms + (size_t)row * S + s).x);
-      m = warp_max(m);
-      double sum = 0.0;
-      for (int s = lane; s < S; s += 32) {
-        const float2 u = __ldcg(part_ms + (size_t)row * S + s);
-        if (u.x == m) sum += u.y;
-        else if (u.x > -INFINITY) sum += (double)u.y * exp((double)u.x - (double)m);
-      }
+#pragma unroll 2
+      for (int i = 0; i < n; ++i) {
+        const unsigned long long u = keys[i];
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) sum += shfl_xor_d(sum, o);
-      const double lsum = log(sum);
-      // S sorted lists: a lane holds the heads of lists lane, lane + 32, ... one after the other
-      const unsigned long long* keys = part_key + (size_t)row * S * n_out;
-      unsigned long long mine = 0, best = 0;
-      for (int l0 = 0; l0 < S; l0 += 32) {  // 32 lists at a time into the running n_out best
-        int head = 0;
-        const int l = l0 + lane;
-        unsigned long long h = l < S ? __ldcg(keys + (size_t)l * n_out) : 0ull;
-        unsigned long long old = mine;  // the best so far, in lane order: a 33rd list
-        int taken = 0;                  // of them
-        mine = 0;
-        for (int r = 0; r < n_out; ++r) {
-          const unsigned long long o33 = __shfl_sync(0xffffffffu, old, taken);
-          best = h;
-#pragma unroll
-          for (int o = 16; o > 0; o >>= 1) {
-            const unsigned long long u = __shfl_xor_sync(0xffffffffu, best, o);
-            if (u > best) best = u;
-          }
-          if (o33 >= best) {
-            best = o33;
-            ++taken;
-          } else if (h == best) {
-            ++head;
-            h = head < n_out ? __ldcg(keys + (size_t)l * n_out + head) : 0ull;
-          }
-          if (lane == r) mine = best;
-        }
-      }
-      if (mine != 0 && lane < n_out) {
-        const float x = key_logit(mine);
-        const double d = x == m ? 0.0 : (double)x - (double)m;  // (m = +infinity: its tokens alone have weight)
-        sc = (double)cw + (d - lsum);
-        tk = key_token(mine);
+        for (int q = 0; q < BS_LIST / 32; ++q) rank[q] += u > mine[q];
       }
     }
-    if (lane < n_out) {
-      sc_s[warp * n_out + lane] = sc;
-      tk_s[warp * n_out + lane] = tk;
+    int ex = 0;
+    const float f = frexpf(sum, &ex) * 2.f;  // sum = f 2^(ex - 1), f in [1, 2)
+    const double lsum = (double)(ex - 1) * 0.69314718055994530942 + (double)logf(f);
+#pragma unroll
+    for (int q = 0; q < BS_LIST / 32; ++q) {
+      if (mine[q] == 0 || rank[q] >= n_out) continue;
+      const float x = key_logit(mine[q]);
+      const double d = x == m ? 0.0 : (double)x - (double)m;  // (m = +infinity: its tokens alone have weight)
+      const double v = (double)cw + (d - lsum);
+      if (v > -INFINITY) {
+        sc[rank[q]] = order_bits(v);
+        val_s[warp * n_out + rank[q]] = v;
+        tk_s[warp * n_out + rank[q]] = key_token(mine[q]);
+      }
     }
   }
   __syncthreads();
-  if (warp != 0) return;
-  int head = 0;  // lane w: the head of beam w's list
-  for (int r = 0; r < n_out; ++r) {
-    double s = -INFINITY;
-    int t = -1;
-    if (lane < W && head < n_out) {
-      s = sc_s[lane * n_out + head];
-      t = tk_s[lane * n_out + head];
+  // over the beams: place in (beam, rank) order breaks ties
+  const int total = W * n_out, t = threadIdx.x;
+  if (t < total) {
+    const unsigned long long s = sc_s[t];
+    int rank = 0, have = 0;
+#pragma unroll 8
+    for (int i = 0; i < total; ++i) {
+      const unsigned long long u = sc_s[i];
+      rank += u > s || (u == s && i < t);
+      have += u != 0;
     }
-    int from = lane;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      const double s2 = shfl_xor_d(s, o);
-      const int t2 = __shfl_xor_sync(0xffffffffu, t, o), f2 = __shfl_xor_sync(0xffffffffu, from, o);
-      if (t2 >= 0 && (t < 0 || s2 > s || (s2 == s && f2 < from))) {
-        s = s2;
-        t = t2;
-        from = f2;
-      }
+    if (s != 0 && rank < n_out) {
+      score[(size_t)e * n_out + rank] = (float)val_s[t];
+      parent[(size_t)e * n_out + rank] = t / n_out;
+      token[(size_t)e * n_out + rank] = tk_s[t];
     }
-    if (t >= 0 && from == lane) ++head;
-    if (lane == 0) {
-      score[(size_t)e * n_out + r] = t >= 0 ? (float)s : -INFINITY;
-      parent[(size_t)e * n_out + r] = t >= 0 ? from : -1;
-      token[(size_t)e * n_out + r] = t;
+    if (t < n_out && t >= have) {
+      score[(size_t)e * n_out + t] = -INFINITY;
+      parent[(size_t)e * n_out + t] = -1;
+      token[(size_t)e * n_out + t] = -1;
     }
   }
 }
@@ -376,34 +517,32 @@ beam_reorder_kernel(uint4* __restrict__ kv, int planes, int n_pages, int page_sh
 
 }  // namespace
 
-int beam_slices(int rows, int V) {
-  // slices of a row: enough CTAs for four per SM, of at least 2,048 logits each
-  const int want = (device_sm_count() * 4 + rows - 1) / rows;
-  return std::max(1, std::min(want, (V + 2047) / 2048));
+// Slices of a row: about four CTAs per SM, of at least 4,096 logits each, and no more lists than a warp joins.
+static int beam_slices(int rows, int V, int n_out) {
+  const int want = (device_sm_count() * 4 + rows / 2) / rows;
+  return std::max(1, std::min(std::min(want, BS_LIST / n_out), (V + 4095) / 4096));
 }
 
 size_t beam_select_bytes(int rows, int V, int n_out) {
-  const size_t n = (size_t)rows * beam_slices(rows, V);
+  const size_t n = (size_t)rows * beam_slices(rows, V, n_out);
   return ((n * 8 + 255) & ~size_t(255)) + n * n_out * 8;
 }
 
 cudaError_t beam_select_launch(const void* logits, bool f32, long long ld, int B, int W, int V, const float* cum,
                                const unsigned char* done, int eos, int n_out, void* ws, float* score, int* parent,
                                int* token, cudaStream_t st) {
-  const int rows = B * W, S = beam_slices(rows, V);
+  const int rows = B * W, S = beam_slices(rows, V, n_out);
   const int slice = (((V + S - 1) / S) + 7) & ~7;
   auto* ms = static_cast<float2*>(ws);
   auto* key = reinterpret_cast<unsigned long long*>(static_cast<char*>(ws) + (((size_t)rows * S * 8 + 255) & ~size_t(255)));
   prof_begin_launch(st);
-  cudaError_t r = f32 ? launch_pdl(beam_scan_kernel<true>, dim3(S, rows), dim3(BS_NT), 0, st, logits, ld, V, cum, done,
-                                   n_out, slice, ms, key)
-                      : launch_pdl(beam_scan_kernel<false>, dim3(S, rows), dim3(BS_NT), 0, st, logits, ld, V, cum, done,
-                                   n_out, slice, ms, key);
+  cudaError_t r = launch_pdl(f32 ? beam_scan_kernel<true> : beam_scan_kernel<false>, dim3(S, rows), dim3(BS_NT), 0, st,
+                             logits, ld, V, cum, done, n_out, slice, ms, key);
   prof_end_launch(st, SP_K_MISC, 0.0, (double)rows * V * (f32 ? 4 : 2));
   if (r != cudaSuccess) return r;
   prof_begin_launch(st);
-  r = launch_pdl(beam_join_kernel, dim3(B), dim3(W * 32), 0, st, W, V, S, cum, done, eos, n_out,
-                 (const float2*)ms, (const unsigned long long*)key, score, parent, token);
+  r = launch_pdl(beam_join_kernel, dim3(B), dim3(W * 32), (size_t)W * S * n_out * 8, st, W, V, S, cum, done, eos,
+                 n_out, (const float2*)ms, (const unsigned long long*)key, score, parent, token);
   prof_end_launch(st, SP_K_MISC, 0.0, 0.0);
   return r;
 }
