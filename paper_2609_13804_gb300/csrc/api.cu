@@ -140,6 +140,19 @@ bool encode_tmap_2d(CUtensorMap* map, const void* ptr, bool f32, uint64_t rows, 
   return true;
 }
 
+bool encode_tmap_rows3(CUtensorMap* map, const void* ptr, uint64_t inner, uint64_t mid, uint64_t rows, uint64_t ld,
+                       uint32_t box_inner, uint32_t box_mid, uint32_t box_rows) {
+  EncodeTiledFn fn = encode_fn(nullptr);
+  if (!fn) return false;
+  cuuint64_t dims[3] = {inner, mid, rows ? rows : 1};
+  cuuint64_t strides[2] = {inner * 2, ld * 2};
+  cuuint32_t box[3] = {box_inner, box_mid, box_rows};
+  cuuint32_t es[3] = {1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, es,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // ------------------------------------------------------------------ profiling
 
 namespace {

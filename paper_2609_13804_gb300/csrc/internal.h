@@ -63,6 +63,10 @@ bool encode_tmap_bf16(CUtensorMap* map, const void* ptr, uint64_t rows, uint64_t
 bool encode_tmap_2d(CUtensorMap* map, const void* ptr, bool f32, uint64_t rows, uint64_t cols,
                     uint32_t box_cols, uint32_t box_rows, std::string* msg);
 
+// 3-D map over bf16 rows ld elements apart, each `mid` pieces of `inner` elements; 128-byte swizzle.
+bool encode_tmap_rows3(CUtensorMap* map, const void* ptr, uint64_t inner, uint64_t mid, uint64_t rows, uint64_t ld,
+                       uint32_t box_inner, uint32_t box_mid, uint32_t box_rows);
+
 // ------------------------------------------------------------- tcgen05 GEMM
 enum EpiKind {
   EPI_BF16 = 0,         // out bf16 = acc

@@ -291,7 +291,7 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(const PrefixArgs a, c
     for (int side = 0; side < 2; ++side) {
       const PlanArgs& p = side == 0 ? pp : po;
       const int e = side == 0 ? g : a.n_groups + b;
-      if (e < 0) continue;
+      if (e < 0 || !(side == 0 ? p.prefix : p.own)) continue;
       const long long N = __ldcg(p.tile0 + E), e0 = __ldcg(p.tile0 + e), e1 = __ldcg(p.tile0 + e + 1);
       const int i0 = __ldcg(p.item0 + e), n_items = __ldcg(p.item0 + e + 1) - i0;
       if (e1 <= e0) continue;
@@ -300,7 +300,7 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(const PrefixArgs a, c
       const int mv = (row - r0) * G + h % G;
       const int rt = mv / p.tile_rows, mr = mv - rt * p.tile_rows;
       const int in = rt * a.Hkv + h / G;
-      if (in < 0 || in >= n_items) continue;  // (row offsets that do not ascend)
+      if (row < r0 || in >= n_items) continue;  // (row offsets that do not ascend)
       const long long t0 = e0 + in * kt;
       const int P = plan_workers(N, p.workers, p.min_tiles);
       const int w0 = part_of(N, P, t0), w1 = part_of(N, P, t0 + kt - 1);
@@ -334,66 +334,84 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(const PrefixArgs a, c
 
 }  // namespace
 
-// Rows of an item's slot and slots of one launch at most, from what the host knows.
-static size_t plan_slots(const PlanArgs& p, int T_cap, int B, int n_groups, int G, int Hkv) {
-  size_t items = 0;
-  const size_t full = ((size_t)T_cap * G) / p.tile_rows;
-  if (p.prefix) items += (full + n_groups) * Hkv;
-  if (p.own) items += (full + B) * Hkv;
-  return items + p.workers;
-}
+// Vectors per entry from which its products go to prefix_tc_kernel.
+constexpr int kTcVectors = 32;
 
-PrefixLayout prefix_layout(int T_cap, int B, int n_groups, int Hq, int Hkv, int dh) {
-  PrefixLayout L;
-  const int G = Hq / Hkv;
-  const int sms = device_sm_count();
-  PlanArgs& p = L.warp;
-  p = PlanArgs();
-  p.tile_rows = WK_ROWS;
-  p.key_shift = 4;
-  p.min_tiles = 2;
-  p.workers = sms * WK_WARPS;
-  p.prefix = n_groups > 0;
-  p.own = true;
-  p.slot_rows = (int)std::min<size_t>(WK_ROWS, (size_t)T_cap * G);
-  L.slots = plan_slots(p, T_cap, B, n_groups, G, Hkv);
-  const size_t E = (size_t)n_groups + B + 1;
+// A plan's arrays in its part of the workspace (base NULL: sizes only); returns its bytes.
+static size_t plan_carve(PlanArgs* p, char* base, int T_cap, int B, int n_groups, int G, int Hkv, int dh) {
+  const size_t full = ((size_t)T_cap * G) / p->tile_rows;  // row tiles besides each entry's last
+  const size_t items = ((p->prefix ? full + n_groups : 0) + (p->own ? full + B : 0)) * Hkv;
+  p->max_items = (int)items;
+  const size_t rows = (items + p->workers) * p->slot_rows, E = (size_t)n_groups + B + 1;
   size_t off = 0;
   auto take = [&](size_t bytes) {
-    const size_t at = off;
+    char* at = base + off;
     off = (off + bytes + 255) & ~size_t(255);
     return at;
   };
-  L.off_tile0 = take(E * 8);
-  L.off_item0 = take(E * 4);
-  L.off_ml = take(L.slots * p.slot_rows * 8);
-  L.off_o = take(L.slots * p.slot_rows * dh * 4);
-  L.bytes = off;
+  p->tile0 = reinterpret_cast<long long*>(take(E * 8));
+  p->item0 = reinterpret_cast<int*>(take(E * 4));
+  p->part_ml = reinterpret_cast<float2*>(take(rows * 8));
+  p->part_o = reinterpret_cast<float*>(take(rows * dh * 4));
+  return off;
+}
+
+PrefixLayout prefix_layout(int T_cap, int B, int n_groups, int Hq, int Hkv, int dh) {
+  PrefixLayout L = {};
+  const int G = Hq / Hkv, sms = device_sm_count();
+  const bool fits = G <= 128;
+  const bool tc_prefix = fits && n_groups > 0 && (long long)T_cap * G >= (long long)kTcVectors * n_groups;
+  const bool tc_own = fits && (long long)T_cap * G >= (long long)kTcVectors * B;
+  L.warp.tile_rows = WK_ROWS;
+  L.warp.key_shift = 4;
+  L.warp.min_tiles = 2;
+  L.warp.prefix = n_groups > 0 && !tc_prefix;
+  L.warp.own = !tc_own;
+  L.warp.workers = L.warp.prefix || L.warp.own ? sms * WK_WARPS : 0;
+  L.warp.slot_rows = (int)std::min<size_t>(WK_ROWS, (size_t)T_cap * G);
+  L.tc.tile_rows = fits ? 128 / G * G : 128;
+  L.tc.key_shift = 6;
+  L.tc.min_tiles = 2;
+  L.tc.prefix = tc_prefix;
+  L.tc.own = tc_own;
+  L.tc.workers = tc_prefix || tc_own ? sms * 2 : 0;
+  L.tc.slot_rows = (int)std::min<size_t>(L.tc.tile_rows, (size_t)T_cap * G);
+  L.off_warp = 0;
+  if (L.warp.workers) L.bytes = plan_carve(&L.warp, nullptr, T_cap, B, n_groups, G, Hkv, dh);
+  L.off_tc = L.bytes;
+  if (L.tc.workers) L.bytes += plan_carve(&L.tc, nullptr, T_cap, B, n_groups, G, Hkv, dh);
   return L;
 }
 
 cudaError_t prefix_attention_launch(const PrefixArgs& a, int dh, void* ws, cudaStream_t st) {
   if (a.T_cap == 0) return cudaSuccess;
   PrefixLayout L = prefix_layout(a.T_cap, a.B, a.n_groups, a.Hq, a.Hkv, dh);
+  const int sms = device_sm_count(), G = a.Hq / a.Hkv;
   char* base = static_cast<char*>(ws);
-  PlanArgs p = L.warp;
-  p.tile0 = reinterpret_cast<long long*>(base + L.off_tile0);
-  p.item0 = reinterpret_cast<int*>(base + L.off_item0);
-  p.part_ml = reinterpret_cast<float2*>(base + L.off_ml);
-  p.part_o = reinterpret_cast<float*>(base + L.off_o);
-  const int sms = device_sm_count();
-  const size_t smem = dh == 128 ? WkCfg<128>::SMEM : WkCfg<64>::SMEM;
-  auto* kern = dh == 128 ? prefix_warp_kernel<128> : prefix_warp_kernel<64>;
-  cudaError_t r = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (r != cudaSuccess) return r;
-  prof_begin_launch(st);
-  r = launch_pdl(kern, dim3(sms), dim3(WK_NT), smem, st, a, p);
-  prof_end_launch(st, SP_K_ATTN, 0.0, 0.0);
-  if (r != cudaSuccess) return r;
+  cudaError_t r;
+  if (L.tc.workers) {
+    plan_carve(&L.tc, base + L.off_tc, a.T_cap, a.B, a.n_groups, G, a.Hkv, dh);
+    prof_begin_launch(st);
+    r = prefix_tc_launch(a, L.tc, dh, st);
+    prof_end_launch(st, SP_K_ATTN, 0.0, 0.0);
+    if (r != cudaSuccess) return r;
+  }
+  if (L.warp.workers) {
+    plan_carve(&L.warp, base + L.off_warp, a.T_cap, a.B, a.n_groups, G, a.Hkv, dh);
+    const size_t smem = dh == 128 ? WkCfg<128>::SMEM : WkCfg<64>::SMEM;
+    auto* kern = dh == 128 ? prefix_warp_kernel<128> : prefix_warp_kernel<64>;
+    r = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (r != cudaSuccess) return r;
+    prof_begin_launch(st);
+    r = launch_pdl(kern, dim3(sms), dim3(WK_NT), smem, st, a, L.warp);
+    prof_end_launch(st, SP_K_ATTN, 0.0, 0.0);
+    if (r != cudaSuccess) return r;
+  }
   const long long warps = (long long)a.T_cap * a.Hq;
   const int grid = (int)std::min<long long>((warps + 7) / 8, (long long)sms * 8);
   prof_begin_launch(st);
-  r = launch_pdl(dh == 128 ? prefix_merge_kernel<128> : prefix_merge_kernel<64>, dim3(grid), dim3(256), 0, st, a, p, p);
+  r = launch_pdl(dh == 128 ? prefix_merge_kernel<128> : prefix_merge_kernel<64>, dim3(grid), dim3(256), 0, st, a,
+                 L.tc.prefix ? L.tc : L.warp, L.tc.own ? L.tc : L.warp);
   prof_end_launch(st, SP_K_ATTN, 0.0, 0.0);
   return r;
 }

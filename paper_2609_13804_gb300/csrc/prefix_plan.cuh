@@ -46,6 +46,7 @@ struct PlanArgs {
   int key_shift;           // log2 of the keys of a key tile
   int min_tiles;           // key tiles a worker takes at least (while there are enough)
   int workers;
+  int max_items;           // items there is room for: no more exist while row and group offsets ascend
   bool prefix, own;        // which entries this launch covers
   long long* tile0;        // [n_groups + B + 1] first tile of each entry, then N      (written for the merge)
   int* item0;              // [n_groups + B + 1] first item of each entry, then the item count
@@ -64,7 +65,7 @@ struct PlanShared {
   int item0[kPlanEntries + 1];
   int row0[kPlanEntries], rows[kPlanEntries], keys[kPlanEntries];
   long long wsum_t[32];
-  int wsum_i[32];
+  int wsum_i[32];  // (a CTA has 32 warps at most)
 };
 
 SP_DEVINL int plan_workers(long long N, int workers, int min_tiles) {
@@ -136,26 +137,26 @@ SP_DEVINL void build_plan(const PrefixArgs& a, const PlanArgs& p, PlanShared& s,
     ix += s.wsum_i[w];
     tx += s.wsum_t[w];
   }
+  int total = 0;
+  for (int w = 0; w < NT / 32; ++w) total += s.wsum_i[w];
+  const bool fits = total <= p.max_items;
+  if (!fits && write && tid == 0) set_error(a.err, SP_DEVERR_INDEX);
 #pragma unroll
-  for (int k = 0; k < PER; ++k) {
+  for (int k = 0; k <= PER; ++k) {  // (the total's place follows the last entry, maybe another thread's first)
     const int e = tid * PER + k;
-    if (e <= E) {
-      s.item0[e] = ix;
-      s.tile0[e] = tx;
+    if (k < PER ? e <= E : (e == E && tid == NT - 1)) {
+      const int i = fits ? ix : 0;
+      const long long t = fits ? tx : 0;
+      s.item0[e] = i;
+      s.tile0[e] = t;
       if (write) {
-        p.item0[e] = ix;
-        p.tile0[e] = tx;
+        p.item0[e] = i;
+        p.tile0[e] = t;
       }
     }
-    ix += il[k];
-    tx += tl[k];
-  }
-  if (tid == NT - 1 && E == NT * PER) {  // (the total's place, when every thread's last entry is a real one)
-    s.item0[E] = ix;
-    s.tile0[E] = tx;
-    if (write) {
-      p.item0[E] = ix;
-      p.tile0[E] = tx;
+    if (k < PER) {
+      ix += il[k];
+      tx += tl[k];
     }
   }
   __syncthreads();
@@ -201,13 +202,14 @@ struct TileCursor {
 
 namespace sp {
 
-// Workspace of a call (host arithmetic on what the host knows).
+// What a call launches, from what the host knows, and its workspace.
 struct PrefixLayout {
-  PlanArgs warp;
-  size_t slots;
-  size_t off_tile0, off_item0, off_ml, off_o, bytes;
+  PlanArgs warp, tc;       // the kernel for few vectors per entry, the one for many (workers 0: not launched)
+  size_t off_warp, off_tc; // their parts of the workspace
+  size_t bytes;
 };
 PrefixLayout prefix_layout(int T_cap, int B, int n_groups, int Hq, int Hkv, int dh);
 cudaError_t prefix_attention_launch(const PrefixArgs& a, int dh, void* ws, cudaStream_t st);
+cudaError_t prefix_tc_launch(const PrefixArgs& a, const PlanArgs& p, int dh, cudaStream_t st);
 
 }  // namespace sp

@@ -518,3 +518,23 @@ def test_binding_refuses_wrong_tensors(sp):
     for bad in (dict(head_dim=32, n_heads=2, n_kv_heads=2), dict(scale=-1.0), dict(ws=torch.empty(256, dtype=torch.uint8, device=DEV))):
         with pytest.raises(sp.SPError):
             call(**bad)
+
+
+def test_attention_reports_offsets_that_do_not_ascend(sp):
+    """Group and row offsets that run back: nothing outside the buffers is touched.  The workspace has room for
+    floor(40 / 16) + 6 row tiles of prefixes and floor(40 / 16) + 4 of own keys, 14; the first offsets ask for
+    3 x 3 + 2 x 3 = 15, which the error word reports, the second for 3 x 3 + 4 = 13, which fit."""
+    g = gen(14)
+    kv = normal(g, 2, 8, 16, 64)
+    q = normal(g, 40, 64)
+    ws = sp.prefix_attention_workspace(T_cap=40, B=4, n_heads=1, n_kv_heads=1, head_dim=64, n_groups=6)
+    n = ws.numel()
+    big = torch.full((n + (1 << 20),), 7, dtype=torch.uint8, device=DEV)
+    groups = [0, 4, 0, 4, 0, 4, 0]
+    for cu, err in (([0, 40, 0, 40, 40], 2), ([0, 10, 20, 30, 40], 0)):
+        out = torch.full((44, 64), 7.0, dtype=torch.bfloat16, device=DEV)
+        r = sp.sp_prefix_attention(q=q, kv=kv, table=ints([[0], [1], [2], [3]]), lens=ints([16, 16, 16, 16]), n_heads=1,
+                                   n_kv_heads=1, head_dim=64, cu_rows=ints(cu), prefix_table=ints([[4, 5]] * 6),
+                                   prefix_lens=ints([32] * 6), group_cu=ints(groups), out=out[:40], ws=big[:n])
+        assert int(r["err"].item()) == err
+        assert (out[40:] == 7).all() and (big[n:] == 7).all()
