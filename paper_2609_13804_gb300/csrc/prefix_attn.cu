@@ -73,21 +73,21 @@ __global__ void __launch_bounds__(WK_NT, 1) prefix_warp_kernel(const PrefixArgs 
   pdl_wait();
   pdl_trigger();
   build_plan<WK_NT>(a, p, plan, blockIdx.x == 0);
-  const long long N = plan.tile0[E];
+  const int N = plan.unit0[E];
   if (N == 0) return;
-  const int P = plan_workers(N, p.workers, p.min_tiles);
+  const int P = plan_workers(p, N);
   const int w = blockIdx.x + warp * gridDim.x;  // (a short list goes to different SMs first)
   if (w >= P) return;
-  const long long t0 = part_begin(N, P, w), t1 = part_begin(N, P, w + 1);
-  if (t0 >= t1) return;
+  const int t1 = part_begin(N, P, w + 1);
+  TileCursor put, get;
+  bool more = get.seek(plan, p, E, a.Hkv, part_begin(N, P, w), t1);
+  if (!more) return;
+  put = get;
+  bool more_put = true;
 
   const uint32_t ring = smem_u32(ring_all) + warp * C::NS * C::STAGE;
   const size_t W = (size_t)a.Hkv * DH;
   const size_t plane = ((size_t)a.n_pages << a.page_shift) * W;
-
-  TileCursor put, get;
-  put.seek(plan, p, E, a.Hkv, t0);
-  get = put;
 
   // one tile into ring slot `slot`: lane = 16-byte chunk of a row, rows in turn; rows past the keys are zeros
   auto load_tile = [&](int slot) {
@@ -116,12 +116,11 @@ __global__ void __launch_bounds__(WK_NT, 1) prefix_warp_kernel(const PrefixArgs 
     }
   };
 
-  long long t_put = t0;
 #pragma unroll
   for (int s = 0; s < C::NS - 1; ++s) {
-    if (t_put < t1) {
+    if (more_put) {
       load_tile(s);
-      if (++t_put < t1) put.next(plan, p, a.Hkv);
+      more_put = put.next(plan, p, a.Hkv, t1);
     }
     cp_async_commit();
   }
@@ -134,7 +133,7 @@ __global__ void __launch_bounds__(WK_NT, 1) prefix_warp_kernel(const PrefixArgs 
   int slot = 0, slot_put = C::NS - 1;
   const int row_a = lane >> 2, col = (lane & 3) * 2;
 
-  for (long long t = t0; t < t1; ++t) {
+  while (more) {
     if (fresh) {  // a new segment: its query vectors, empty statistics
       const int M = plan.rows[get.e] * G;
       const int keys = plan.keys[get.e], R = plan.rows[get.e];
@@ -160,9 +159,9 @@ __global__ void __launch_bounds__(WK_NT, 1) prefix_warp_kernel(const PrefixArgs 
         for (int c = 0; c < 4; ++c) o[n][c] = 0.f;
       fresh = false;
     }
-    if (t_put < t1) {
+    if (more_put) {
       load_tile(slot_put);
-      if (++t_put < t1) put.next(plan, p, a.Hkv);
+      more_put = put.next(plan, p, a.Hkv, t1);
     }
     cp_async_commit();
     if (++slot_put == C::NS) slot_put = 0;
@@ -231,16 +230,18 @@ __global__ void __launch_bounds__(WK_NT, 1) prefix_warp_kernel(const PrefixArgs 
     __syncwarp();  // the tile is read before a lane's next copies overwrite it
     if (++slot == C::NS) slot = 0;
 
-    if (t + 1 == t1 || get.j + 1 == get.kt) {  // the segment ends
-      const int M = plan.rows[get.e] * G;
-      const size_t base = ((size_t)get.item + w) * p.slot_rows;
+    const TileCursor now = get;
+    more = get.next(plan, p, a.Hkv, t1);
+    if (!more || get.item != now.item) {  // the segment ends
+      const int M = plan.rows[now.e] * G;
+      const size_t base = ((size_t)now.item + w) * p.slot_rows;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         float sum = l[h];
         sum += __shfl_xor_sync(0xffffffffu, sum, 1);
         sum += __shfl_xor_sync(0xffffffffu, sum, 2);
         const int mr = row_a + 8 * h;
-        if (get.rt * WK_ROWS + mr < M) {
+        if (now.rt * WK_ROWS + mr < M) {
           float* po = p.part_o + (base + mr) * DH + col;
 #pragma unroll
           for (int n = 0; n < DH / 8; ++n)
@@ -250,86 +251,108 @@ __global__ void __launch_bounds__(WK_NT, 1) prefix_warp_kernel(const PrefixArgs 
       }
       fresh = true;
     }
-    if (t + 1 < t1) get.next(plan, p, a.Hkv);
   }
   cp_async_wait<0>();
 }
 
 // --------------------------------------------------------------- joining the segments
-// One warp per (row, query head): the segments of its prefix item and of its own item, in key order.
+// One CTA per row and eight of its query heads, a warp each: the segments of the row's prefix item and of its own
+// item, in key order.  What the heads share (sequence, group, where the items lie) is found by all threads at once;
+// the segments' (max, sum) are read a lane each, then their values with the weights known, so that one access's
+// latency is paid once and not per segment.
+struct MergeSide {
+  int unit0;               // the entry's first unit
+  int N, len, items, item0, P;
+  int mv;                  // the row's first query vector in the entry
+};
+
 template <int DH>
 __global__ void __launch_bounds__(256) prefix_merge_kernel(const PrefixArgs a, const PlanArgs pp, const PlanArgs po) {
+  __shared__ MergeSide side_s[2];
   pdl_wait();
   pdl_trigger();
-  const int lane = threadIdx.x & 31;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int E = a.n_groups + a.B, G = a.Hq / a.Hkv;
-  const long long rows = row_begin(a, a.B);
-  const long long first = row_begin(a, 0);
-  for (long long i = blockIdx.x * 8ll + (threadIdx.x >> 5); i < (rows - first) * a.Hq; i += gridDim.x * 8ll) {
-    const int row = (int)(first + i / a.Hq), h = (int)(i % a.Hq);
-    int lo = 0, hi = a.B - 1;
-    while (lo < hi) {  // the row's sequence
-      const int mid = (lo + hi + 1) >> 1;
-      if (row_begin(a, mid) <= row) lo = mid; else hi = mid - 1;
-    }
-    const int b = lo;
-    int g = -1;
-    if (a.n_groups > 0) {  // its group, if it is in one
-      lo = 0;
-      hi = a.n_groups - 1;
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (__ldg(a.group_cu + mid) <= b) lo = mid; else hi = mid - 1;
-      }
-      if (__ldg(a.group_cu + lo) <= b && b < __ldg(a.group_cu + lo + 1)) g = lo;
-    }
-    constexpr int V = DH / 32;
-    float acc[V], mm = -INFINITY, ll = 0.f;
-#pragma unroll
-    for (int v = 0; v < V; ++v) acc[v] = 0.f;
-#pragma unroll
-    for (int side = 0; side < 2; ++side) {
-      const PlanArgs& p = side == 0 ? pp : po;
-      const int e = side == 0 ? g : a.n_groups + b;
-      if (e < 0 || !(side == 0 ? p.prefix : p.own)) continue;
-      const long long N = __ldcg(p.tile0 + E), e0 = __ldcg(p.tile0 + e), e1 = __ldcg(p.tile0 + e + 1);
-      const int i0 = __ldcg(p.item0 + e), n_items = __ldcg(p.item0 + e + 1) - i0;
-      if (e1 <= e0) continue;
-      const long long kt = (e1 - e0) / n_items;
-      const int r0 = side == 0 ? row_begin(a, __ldg(a.group_cu + g)) : row_begin(a, b);
-      const int mv = (row - r0) * G + h % G;
-      const int rt = mv / p.tile_rows, mr = mv - rt * p.tile_rows;
-      const int in = rt * a.Hkv + h / G;
-      if (row < r0 || in >= n_items) continue;  // (row offsets that do not ascend)
-      const long long t0 = e0 + in * kt;
-      const int P = plan_workers(N, p.workers, p.min_tiles);
-      const int w0 = part_of(N, P, t0), w1 = part_of(N, P, t0 + kt - 1);
-      for (int w = w0; w <= w1; ++w) {
-        const size_t at = ((size_t)(i0 + in) + w) * p.slot_rows + mr;
-        const float2 ml = __ldcg(p.part_ml + at);
-        if (ml.x == -INFINITY) continue;
-        const float mn = fmaxf(mm, ml.x);
-        const float ca = ex2(mm - mn), cb = ex2(ml.x - mn);
-        const float* x = p.part_o + at * DH + lane * V;
-        float y[V];
-        if (V == 4) *reinterpret_cast<float4*>(y) = __ldcg(reinterpret_cast<const float4*>(x));
-        else *reinterpret_cast<float2*>(y) = __ldcg(reinterpret_cast<const float2*>(x));
-#pragma unroll
-        for (int v = 0; v < V; ++v) acc[v] = acc[v] * ca + y[v] * cb;
-        ll = ll * ca + ml.y * cb;
-        mm = mn;
+  const int row = blockIdx.x;
+  const int first = row_begin(a, 0), last = row_begin(a, a.B);
+  static_assert(SP_MAX_BATCH <= 256, "a thread per sequence");
+  if (row < first || row >= last) return;
+  const int b = __syncthreads_count(tid < a.B && row_begin(a, min(tid, a.B)) <= row) - 1;
+  // its group, if it is in one
+  int g = __syncthreads_count(tid < a.n_groups && __ldg(a.group_cu + min(tid, a.n_groups)) <= b) - 1;
+  if (tid < 2) {
+    const PlanArgs& p = tid == 0 ? pp : po;
+    if (tid == 0 && g >= 0 && b >= __ldg(a.group_cu + g + 1)) g = -1;
+    const int e = tid == 0 ? g : a.n_groups + b;
+    MergeSide m = {};
+    if (e >= 0 && (tid == 0 ? p.prefix : p.own)) {
+      const int e0 = __ldcg(p.unit0 + e), e1 = __ldcg(p.unit0 + e + 1);
+      const int i0 = __ldcg(p.item0 + e), i1 = __ldcg(p.item0 + e + 1);
+      const int r0 = tid == 0 ? row_begin(a, min(max(__ldg(a.group_cu + g), 0), a.B)) : row_begin(a, b);
+      m.N = __ldcg(p.unit0 + E);
+      if (e1 > e0 && row >= r0) {
+        m.unit0 = e0;
+        m.items = i1 - i0;
+        m.item0 = i0;
+        m.len = (e1 - e0) / m.items;
+        m.P = plan_workers(p, m.N);
+        m.mv = (row - r0) * G;
       }
     }
-    const float inv = ll > 0.f ? 1.f / ll : 0.f;
-    __nv_bfloat16* d = a.out + row * a.ld_out + (long long)h * DH + lane * V;
-    if (V == 4)
-      *reinterpret_cast<uint2*>(d) = make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv),
-                                                pack_bf16x2(acc[V - 2] * inv, acc[V - 1] * inv));
-    else
-      *reinterpret_cast<uint32_t*>(d) = pack_bf16x2(acc[0] * inv, acc[1] * inv);
-    if (a.lse && lane == 0)
-      a.lse[(size_t)row * a.Hq + h] = ll > 0.f ? (mm + log2f(ll)) * 0.69314718055994531f : -INFINITY;
+    side_s[tid] = m;
   }
+  __syncthreads();
+  const int h = blockIdx.y * 8 + warp;
+  if (h >= a.Hq) return;
+  constexpr int V = DH / 32;
+  float acc[V], mm = -INFINITY, ll = 0.f;
+#pragma unroll
+  for (int v = 0; v < V; ++v) acc[v] = 0.f;
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+    const PlanArgs& p = side == 0 ? pp : po;
+    const MergeSide m = side_s[side];
+    if (m.items == 0) continue;
+    const int mv = m.mv + h % G;
+    const int rt = mv / p.tile_rows, mr = mv - rt * p.tile_rows;
+    const int in = rt * a.Hkv + h / G;
+    if (in >= m.items) continue;  // (row offsets that do not ascend)
+    const int u0 = m.unit0 + in * m.len;
+    const int w0 = part_of(m.N, m.P, u0 + p.over), w1 = part_of(m.N, m.P, u0 + m.len - 1);
+    const size_t at0 = ((size_t)(m.item0 + in) + w0) * p.slot_rows + mr;
+    const int n = w1 - w0 + 1;
+    for (int s0 = 0; s0 < n; s0 += 32) {
+      float2 ml = make_float2(-INFINITY, 0.f);
+      if (s0 + lane < n) ml = __ldcg(p.part_ml + at0 + (size_t)(s0 + lane) * p.slot_rows);
+      const float mn = fmaxf(mm, warp_max(ml.x));
+      if (mn == -INFINITY) continue;
+      const float ca = ex2(mm - mn), cb = ex2(ml.x - mn);
+      ll = ll * ca + warp_sum(ml.y * cb);
+#pragma unroll
+      for (int v = 0; v < V; ++v) acc[v] *= ca;
+      mm = mn;
+      const float* x = p.part_o + (at0 + (size_t)s0 * p.slot_rows) * DH + lane * V;
+#pragma unroll 4
+      for (int s = 0; s < min(32, n - s0); ++s) {
+        const float c = __shfl_sync(0xffffffffu, cb, s);
+        float y[V];
+        const float* xs = x + (size_t)s * p.slot_rows * DH;
+        if (V == 4) *reinterpret_cast<float4*>(y) = __ldcg(reinterpret_cast<const float4*>(xs));
+        else *reinterpret_cast<float2*>(y) = __ldcg(reinterpret_cast<const float2*>(xs));
+#pragma unroll
+        for (int v = 0; v < V; ++v) acc[v] += y[v] * c;
+      }
+    }
+  }
+  const float inv = ll > 0.f ? 1.f / ll : 0.f;
+  __nv_bfloat16* d = a.out + row * a.ld_out + (long long)h * DH + lane * V;
+  if (V == 4)
+    *reinterpret_cast<uint2*>(d) = make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv),
+                                              pack_bf16x2(acc[V - 2] * inv, acc[V - 1] * inv));
+  else
+    *reinterpret_cast<uint32_t*>(d) = pack_bf16x2(acc[0] * inv, acc[1] * inv);
+  if (a.lse && lane == 0)
+    a.lse[(size_t)row * a.Hq + h] = ll > 0.f ? (mm + log2f(ll)) * 0.69314718055994531f : -INFINITY;
 }
 
 }  // namespace
@@ -349,7 +372,7 @@ static size_t plan_carve(PlanArgs* p, char* base, int T_cap, int B, int n_groups
     off = (off + bytes + 255) & ~size_t(255);
     return at;
   };
-  p->tile0 = reinterpret_cast<long long*>(take(E * 8));
+  p->unit0 = reinterpret_cast<int*>(take(E * 4));
   p->item0 = reinterpret_cast<int*>(take(E * 4));
   p->part_ml = reinterpret_cast<float2*>(take(rows * 8));
   p->part_o = reinterpret_cast<float*>(take(rows * dh * 4));
@@ -364,17 +387,19 @@ PrefixLayout prefix_layout(int T_cap, int B, int n_groups, int Hq, int Hkv, int 
   const bool tc_own = fits && (long long)T_cap * G >= (long long)kTcVectors * B;
   L.warp.tile_rows = WK_ROWS;
   L.warp.key_shift = 4;
-  L.warp.min_tiles = 2;
+  L.warp.over = 2;
+  L.warp.min_units = 4;
   L.warp.prefix = n_groups > 0 && !tc_prefix;
   L.warp.own = !tc_own;
   L.warp.workers = L.warp.prefix || L.warp.own ? sms * WK_WARPS : 0;
   L.warp.slot_rows = (int)std::min<size_t>(WK_ROWS, (size_t)T_cap * G);
   L.tc.tile_rows = fits ? 128 / G * G : 128;
-  L.tc.key_shift = 6;
-  L.tc.min_tiles = 2;
+  L.tc.key_shift = 7;
+  L.tc.over = 2;
+  L.tc.min_units = 4;
   L.tc.prefix = tc_prefix;
   L.tc.own = tc_own;
-  L.tc.workers = tc_prefix || tc_own ? sms * 2 : 0;
+  L.tc.workers = tc_prefix || tc_own ? sms : 0;
   L.tc.slot_rows = (int)std::min<size_t>(L.tc.tile_rows, (size_t)T_cap * G);
   L.off_warp = 0;
   if (L.warp.workers) L.bytes = plan_carve(&L.warp, nullptr, T_cap, B, n_groups, G, Hkv, dh);
@@ -407,10 +432,9 @@ cudaError_t prefix_attention_launch(const PrefixArgs& a, int dh, void* ws, cudaS
     prof_end_launch(st, SP_K_ATTN, 0.0, 0.0);
     if (r != cudaSuccess) return r;
   }
-  const long long warps = (long long)a.T_cap * a.Hq;
-  const int grid = (int)std::min<long long>((warps + 7) / 8, (long long)sms * 8);
+  const dim3 grid(a.T_cap, (a.Hq + 7) / 8);
   prof_begin_launch(st);
-  r = launch_pdl(dh == 128 ? prefix_merge_kernel<128> : prefix_merge_kernel<64>, dim3(grid), dim3(256), 0, st, a,
+  r = launch_pdl(dh == 128 ? prefix_merge_kernel<128> : prefix_merge_kernel<64>, grid, dim3(256), 0, st, a,
                  L.tc.prefix ? L.tc : L.warp, L.tc.own ? L.tc : L.warp);
   prof_end_launch(st, SP_K_ATTN, 0.0, 0.0);
   return r;

@@ -4,11 +4,12 @@
 // group's sequences; entry n_groups + b is sequence b's own keys, read by its rows.  For one key / value
 // head the G = Hq / Hkv query heads of a row read the same keys, so an entry with R rows is a product of
 // M = R G query vectors (vector m: row m / G, head m % G of the kv head's G) with the entry's keys.  The M
-// vectors are cut into row tiles, the keys into key tiles; an item is (entry, row tile, kv head) and the
-// items' key tiles, one after the other, are one list of N tiles.  P workers (warps, or the two pipelines
-// of a CTA) take equal consecutive parts of it, whatever the entries' lengths: worker w the tiles
-// [w N / P, (w + 1) N / P).  The part of an item that one worker takes is a segment; a segment writes its
-// running max, sum and weighted values in 32 bits to slot (item index + worker index), which is its own:
+// vectors are cut into row tiles, the keys into key tiles; an item is (entry, row tile, kv head).  An item
+// counts `over` units for what it costs whatever its length (its query vectors in, its result out) and one
+// for each of its key tiles, and the items' units, one after the other, are one list of N.  P workers (warps,
+// or the two pipelines of a CTA) take equal consecutive parts of it, whatever the entries' lengths: worker w
+// the units [w N / P, (w + 1) N / P).  The key tiles of an item that one worker takes are a segment; it writes
+// its running max, sum and weighted values in 32 bits to slot (item index + worker index), which is its own:
 // going along the list, each next segment has the next item or the next worker.  prefix_merge_kernel joins
 // every row's segments.  All lengths are read on the device; every CTA builds the same plan from them.
 #pragma once
@@ -44,11 +45,13 @@ struct PrefixArgs {
 struct PlanArgs {
   int tile_rows;           // query vectors of a row tile
   int key_shift;           // log2 of the keys of a key tile
-  int min_tiles;           // key tiles a worker takes at least (while there are enough)
+  int over;                // units of an item besides its key tiles
+  int min_units;           // units a worker takes at least (while there are enough)
   int workers;
-  int max_items;           // items there is room for: no more exist while row and group offsets ascend
+  int max_items;           // items there is room for: no more exist while row and group offsets ascend (else, and
+                           // beyond 2^31 - 1 units, the launch covers nothing and reports SP_DEVERR_INDEX)
   bool prefix, own;        // which entries this launch covers
-  long long* tile0;        // [n_groups + B + 1] first tile of each entry, then N      (written for the merge)
+  int* unit0;              // [n_groups + B + 1] first unit of each entry, then N      (written for the merge)
   int* item0;              // [n_groups + B + 1] first item of each entry, then the item count
   float* part_o;           // [slots][slot_rows][DH]
   float2* part_ml;         // [slots][slot_rows] (max in log2 units, sum)
@@ -61,21 +64,26 @@ SP_DEVINL int row_begin(const PrefixArgs& a, int b) {
 }
 
 struct PlanShared {
-  long long tile0[kPlanEntries + 1];
+  int unit0[kPlanEntries + 1];
   int item0[kPlanEntries + 1];
   int row0[kPlanEntries], rows[kPlanEntries], keys[kPlanEntries];
   long long wsum_t[32];
   int wsum_i[32];  // (a CTA has 32 warps at most)
 };
 
-SP_DEVINL int plan_workers(long long N, int workers, int min_tiles) {
-  const long long most = (N + min_tiles - 1) / min_tiles;
-  return (int)(most < workers ? (most < 1 ? 1 : most) : workers);
+SP_DEVINL int plan_workers(const PlanArgs& p, int N) { return max(min(p.workers, (N + p.min_units - 1) / p.min_units), 1); }
+// First unit of worker w's part, floor(w N / P), without products over 32 bits (P is below 2^15).
+SP_DEVINL int part_begin(int N, int P, int w) {
+  const int q = N / P, r = N - q * P;
+  return w * q + w * r / P;
 }
-// First tile of worker w's part.
-SP_DEVINL long long part_begin(long long N, int P, int w) { return (long long)w * N / P; }
-// The worker whose part holds tile t: the largest w with floor(w N / P) <= t.
-SP_DEVINL int part_of(long long N, int P, long long t) { return (int)(((t + 1) * P - 1) / N); }
+// The worker whose part holds unit t: the largest w with part_begin(w) <= t.
+SP_DEVINL int part_of(int N, int P, int t) {
+  int w = min((int)((float)t / (float)N * (float)P), P - 1);
+  while (w > 0 && part_begin(N, P, w) > t) --w;
+  while (w + 1 < P && part_begin(N, P, w + 1) <= t) ++w;
+  return w;
+}
 
 // Called by all NT threads of the CTA (a multiple of 32, at most 1,024).
 template <int NT>
@@ -107,7 +115,8 @@ SP_DEVINL void build_plan(const PrefixArgs& a, const PlanArgs& p, PlanShared& s,
       s.keys[e] = keys;
       if (pre ? p.prefix : p.own) {
         items = (r * G + p.tile_rows - 1) / p.tile_rows * a.Hkv;
-        tiles = (long long)items * ((keys + (1 << p.key_shift) - 1) >> p.key_shift);
+        const int kt = (keys + (1 << p.key_shift) - 1) >> p.key_shift;
+        tiles = kt ? (long long)items * (kt + p.over) : 0;
       }
     }
     il[k] = items;
@@ -139,19 +148,21 @@ SP_DEVINL void build_plan(const PrefixArgs& a, const PlanArgs& p, PlanShared& s,
   }
   int total = 0;
   for (int w = 0; w < NT / 32; ++w) total += s.wsum_i[w];
-  const bool fits = total <= p.max_items;
+  long long units = 0;
+  for (int w = 0; w < NT / 32; ++w) units += s.wsum_t[w];
+  const bool fits = total <= p.max_items && units <= 0x7fffffff;
   if (!fits && write && tid == 0) set_error(a.err, SP_DEVERR_INDEX);
 #pragma unroll
   for (int k = 0; k <= PER; ++k) {  // (the total's place follows the last entry, maybe another thread's first)
     const int e = tid * PER + k;
     if (k < PER ? e <= E : (e == E && tid == NT - 1)) {
       const int i = fits ? ix : 0;
-      const long long t = fits ? tx : 0;
+      const int t = fits ? (int)tx : 0;
       s.item0[e] = i;
-      s.tile0[e] = t;
+      s.unit0[e] = t;
       if (write) {
         p.item0[e] = i;
-        p.tile0[e] = t;
+        p.unit0[e] = t;
       }
     }
     if (k < PER) {
@@ -162,45 +173,47 @@ SP_DEVINL void build_plan(const PrefixArgs& a, const PlanArgs& p, PlanShared& s,
   __syncthreads();
 }
 
-// A walk along a worker's tiles.
+// A walk along the key tiles of a worker's part, which ends at unit t1.
 struct TileCursor {
   int e, item, rt, kvh, j, kt;  // entry, item (over all entries), row tile, kv head, key tile of kt
+  int u;                        // the key tile's unit
   SP_DEVINL void set_item(const PlanShared& s, const PlanArgs& p, int Hkv) {
     const int in = item - s.item0[e];
     rt = in / Hkv;
     kvh = in - rt * Hkv;
     kt = (s.keys[e] + (1 << p.key_shift) - 1) >> p.key_shift;
   }
-  // the entry that holds tile t (entries without tiles are passed over)
-  SP_DEVINL void seek(const PlanShared& s, const PlanArgs& p, int E, int Hkv, long long t) {
-    int lo = 0, hi = E - 1;
+  // to the first key tile at or behind unit t < t1; false: there is none before t1
+  SP_DEVINL bool seek(const PlanShared& s, const PlanArgs& p, int E, int Hkv, int t, int t1) {
+    int lo = 0, hi = E - 1;  // the entry that holds unit t (entries without units are passed over)
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if (s.tile0[mid] <= t) lo = mid; else hi = mid - 1;
+      if (s.unit0[mid] <= t) lo = mid; else hi = mid - 1;
     }
     e = lo;
-    const int k = (s.keys[e] + (1 << p.key_shift) - 1) >> p.key_shift;
-    const int in = (int)((t - s.tile0[e]) / k);
+    const int len = ((s.keys[e] + (1 << p.key_shift) - 1) >> p.key_shift) + p.over;
+    const int off = t - s.unit0[e], in = off / len;
     item = s.item0[e] + in;
-    j = (int)((t - s.tile0[e]) - (long long)in * k);
+    j = max(off - in * len - p.over, 0);
+    u = s.unit0[e] + in * len + p.over + j;
     set_item(s, p, Hkv);
+    return u < t1;
   }
-  // to the next tile, which exists
-  SP_DEVINL void next(const PlanShared& s, const PlanArgs& p, int Hkv) {
-    if (++j < kt) return;
+  // to the next key tile; false: there is none before t1
+  SP_DEVINL bool next(const PlanShared& s, const PlanArgs& p, int Hkv, int t1) {
+    if (++u >= t1) return false;  // (else there are units behind this one)
+    if (++j < kt) return true;
     j = 0;
     ++item;
-    while (item >= s.item0[e + 1] || s.tile0[e + 1] == s.tile0[e]) {
+    while (item >= s.item0[e + 1] || s.unit0[e + 1] == s.unit0[e]) {
       ++e;
       item = s.item0[e];
     }
     set_item(s, p, Hkv);
+    u += p.over;
+    return u < t1;
   }
 };
-
-}  // namespace sp
-
-namespace sp {
 
 // What a call launches, from what the host knows, and its workspace.
 struct PrefixLayout {
