@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Dict, List, Optional, Sequence
 
 import numpy as np
@@ -203,12 +204,12 @@ def lib():
         "sp_soft_topk": (C.c_int, [C.c_int, IP, C.c_int, P, P, C.c_float, P, P, P]),
         "sp_vp_gate": (C.c_int, [C.c_int, C.c_int, P, P, P, P, P]),
         "sp_mrope_positions": (C.c_int, [C.c_int, IP, IP, IP, P, C.c_int, P, P, C.c_int, P, P]),
-        "sp_paged_append": (C.c_int, [C.POINTER(sp_paged_append_io), P]),
+        "sp_paged_append": (C.c_int, [P, P]),
         "sp_prefix_attention_workspace": (C.c_size_t, [C.c_int] * 6),
-        "sp_prefix_attention": (C.c_int, [C.POINTER(sp_prefix_attention_io), P, C.c_size_t, P]),
+        "sp_prefix_attention": (C.c_int, [P, P, C.c_size_t, P]),
         "sp_beam_select_workspace": (C.c_size_t, [C.c_int] * 4),
-        "sp_beam_select": (C.c_int, [C.POINTER(sp_beam_select_io), P, C.c_size_t, P]),
-        "sp_beam_reorder": (C.c_int, [C.POINTER(sp_beam_reorder_io), P]),
+        "sp_beam_select": (C.c_int, [P, P, C.c_size_t, P]),
+        "sp_beam_reorder": (C.c_int, [P, P]),
         "sp_wait_probe": (C.c_int, [P, C.c_uint, C.c_int, P, P, P]),
         "sp_profile_begin": (C.c_int, [C.c_int]),
         "sp_profile_end": (C.c_int, [C.POINTER(C.c_double), C.POINTER(C.c_longlong), C.POINTER(C.c_double),
@@ -609,44 +610,89 @@ def sp_mrope_positions(n_vis, n_txt, grid_w, *, idx, count, k_cap, T_cap, stream
 
 
 # ----------------------------------------------------------------------------- paged cache, shared prefixes, beams
+#
+# A generation step makes these calls for every layer, and most take the GPU a few microseconds: the arguments are
+# checked with few Python operations and packed by `struct` (an argument struct filled by ctypes costs as much as
+# the launch).
 
-class _On:
-    """The device that a call's tensors lie on, current for the call; checks the tensors handed to it."""
+def _packer(cls):
+    """struct.Struct of a ctypes Structure's fields (nested ones in place), with the C layout."""
+    code = {C.c_int: "i", P: "P", C.c_longlong: "q", C.c_float: "f"}
 
-    def __init__(self, who: str, first):
-        torch = _torch()
-        if not first.is_cuda:
-            raise ValueError(f"{who}: tensors must be on a CUDA device")
-        self.who, self.dev = who, first.device
-        self._guard = torch.cuda.device(self.dev) if torch.cuda.current_device() != self.dev.index else None
+    def fields(c):
+        out = ""
+        for _, t in c._fields_:
+            if isinstance(t, type) and issubclass(t, C.Structure):
+                out += fields(t)
+            elif hasattr(t, "_length_"):
+                out += code[t._type_] * t._length_
+            else:
+                out += code[t]
+        return out + "0P"  # (a struct with pointers ends on a pointer's boundary)
 
-    def __enter__(self):
-        if self._guard is not None:
-            self._guard.__enter__()
-        return self
+    s = struct.Struct("@" + fields(cls))
+    if s.size != C.sizeof(cls):
+        raise TypeError(f"{cls.__name__}: packed {s.size} bytes, C has {C.sizeof(cls)}")
+    return s.pack
 
-    def __exit__(self, *a):
-        if self._guard is not None:
-            self._guard.__exit__(*a)
 
-    def ptr(self, name, t, dtype, shape, optional=False):
-        """Address of a contiguous tensor of this type and shape (None in a shape: any size)."""
-        if t is None:
-            if optional:
-                return None
-            raise ValueError(f"{self.who}: {name} is required")
-        if (t.dtype is not dtype or t.device != self.dev or t.dim() != len(shape) or not t.is_contiguous()
-                or any(n is not None and n != m for n, m in zip(shape, t.shape))):
-            raise ValueError(f"{self.who}: {name} must be contiguous {dtype} {tuple('?' if n is None else n for n in shape)} "
-                             f"on {self.dev}, got {t.dtype} {tuple(t.shape)} on {t.device}")
-        return t.data_ptr()
+_pack_append = _packer(sp_paged_append_io)
+_pack_attention = _packer(sp_prefix_attention_io)
+_pack_select = _packer(sp_beam_select_io)
+_pack_reorder = _packer(sp_beam_reorder_io)
 
-    def rows(self, name, t, width):
-        """(address, row stride) of bf16 rows of `width` elements, which may lie apart."""
-        torch = _torch()
-        if t is None or t.dtype is not torch.bfloat16 or t.device != self.dev or t.dim() != 2 or t.shape[1] != width or t.stride(1) != 1:
-            raise ValueError(f"{self.who}: {name} must be bf16 rows of {width} elements on {self.dev}")
-        return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else max(t.stride(0), width))
+
+def _enter(who: str, t):
+    """(device index, guard): makes the tensor's device current where it is not; leave() with the guard."""
+    torch = _torch()
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError(f"{who}: tensors must be on a CUDA device")
+    if torch.cuda.current_device() == dev:
+        return dev, None
+    guard = torch.cuda.device(dev)
+    guard.__enter__()
+    return dev, guard
+
+
+def _leave(guard):
+    if guard is not None:
+        guard.__exit__(None, None, None)
+
+
+def _raw_stream(stream, dev: int) -> int:
+    if stream is None:
+        return _torch()._C._cuda_getCurrentRawStream(dev)
+    return stream if isinstance(stream, int) else stream.cuda_stream
+
+
+def _arg(who, name, t, dtype, dev, shape) -> int:
+    """Address of a contiguous tensor of exactly this type and shape on the device."""
+    if t is None or t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        got = "None" if t is None else f"{t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}"
+        raise ValueError(f"{who}: {name} must be contiguous {dtype} {tuple(shape)} on device {dev}, got {got}")
+    return t.data_ptr()
+
+
+def _opt(who, name, t, dtype, dev, shape) -> int:
+    return 0 if t is None else _arg(who, name, t, dtype, dev, shape)
+
+
+def _rows(who, name, t, dtype, dev, width):
+    """(address, row stride) of rows of `width` elements, which may lie apart."""
+    if t is None or t.dtype is not dtype or t.dim() != 2 or t.shape[1] != width or t.get_device() != dev or t.stride(1) != 1:
+        raise ValueError(f"{who}: {name} must be {dtype} rows of {width} elements on device {dev}")
+    ld = t.stride(0)
+    return t.data_ptr(), ld if ld >= width or t.shape[0] > 1 else width
+
+
+def _pool(who, kv, dev, width):
+    """(address, pages, page size) of one layer's pool."""
+    torch = _torch()
+    if kv is None or kv.dim() != 4:
+        raise ValueError(f"{who}: kv must be one layer's pool [2, n_pages, page_size, {width}]")
+    _, pages, page, _ = kv.shape
+    return _arg(who, "kv", kv, torch.bfloat16, dev, (2, pages, page, width)), pages, page
 
 
 def rope_table(max_pos: int, head_dim: int, theta: float = 10000.0, device="cuda"):
@@ -663,14 +709,6 @@ def paged_pool(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, n_l
     return torch.zeros((n_layers, 2, n_pages, page_size, n_kv_heads * head_dim), dtype=torch.bfloat16, device=device)
 
 
-def _cache(on: _On, kv, table, lens, B, width, lens_optional=False):
-    torch = _torch()
-    k = on.ptr("kv", kv, torch.bfloat16, (2, None, None, width))
-    t = on.ptr("table", table, torch.int32, (B, None))
-    return sp_paged_kv(k, kv.shape[1], kv.shape[2], t, table.shape[1],
-                       on.ptr("lens", lens, torch.int32, (B,), optional=lens_optional))
-
-
 def sp_paged_append(*, qkv, kv, table, n_heads, n_kv_heads, head_dim, lens=None, cu_rows=None, rope=None, pos=None,
                     pos3=None, mrope_section=None, q_out=None, keys_only=False, err=None, stream=None) -> Dict:
     """Rows q | k | v [T, (n_heads + 2 n_kv_heads) head_dim] into the pages of kv (one layer's pool): row j of
@@ -678,33 +716,41 @@ def sp_paged_append(*, qkv, kv, table, n_heads, n_kv_heads, head_dim, lens=None,
     is sequence b's).  rope (rope_table) rotates queries and keys at pos [T] or pos3 [T, 4] (mrope_section); None
     leaves them as they are.  The queries go to q_out (new when None; a view of qkv's first columns rotates in
     place; keys_only: nowhere).  Returns q and err."""
-    torch = _torch()
-    with _On("sp_paged_append", qkv) as on:
-        B = int(table.shape[0])
-        x, ld = on.rows("qkv", qkv, (n_heads + 2 * n_kv_heads) * head_dim)
-        T = int(qkv.shape[0])
-        if q_out is None and not keys_only:
-            q_out = torch.empty((T, n_heads * head_dim), dtype=torch.bfloat16, device=on.dev)
-        q, ld_q = on.rows("q_out", q_out, n_heads * head_dim) if not keys_only else (None, 0)
-        if q_out is not None and not keys_only and q_out.shape[0] != T:
-            raise ValueError("sp_paged_append: q_out must have qkv's rows")
+    torch, who = _torch(), "sp_paged_append"
+    dev, guard = _enter(who, qkv)
+    try:
+        i32, bf16 = torch.int32, torch.bfloat16
+        T, B, mp = qkv.shape[0], table.shape[0], table.shape[-1]
+        x, ld = _rows(who, "qkv", qkv, bf16, dev, (n_heads + 2 * n_kv_heads) * head_dim)
+        q = ld_q = 0
+        if not keys_only:
+            if q_out is None:
+                q_out = torch.empty((T, n_heads * head_dim), dtype=bf16, device=qkv.device)
+            q, ld_q = _rows(who, "q_out", q_out, bf16, dev, n_heads * head_dim)
+            if q_out.shape[0] != T:
+                raise ValueError("sp_paged_append: q_out must have qkv's rows")
         if err is None:
-            err = torch.zeros(1, dtype=torch.int32, device=on.dev)
-        sec = (C.c_int * 3)(*(mrope_section or (0, 0, 0)))
-        io = sp_paged_append_io(B, T, on.ptr("cu_rows", cu_rows, torch.int32, (B + 1,), optional=True), x, ld, q, ld_q,
-                                n_heads, n_kv_heads, head_dim,
-                                on.ptr("rope", rope, torch.float32, (None, head_dim // 2, 2), optional=True),
-                                int(rope.shape[0]) if rope is not None else 0,
-                                on.ptr("pos", pos, torch.int32, (T,), optional=True),
-                                on.ptr("pos3", pos3, torch.int32, (T, 4), optional=True), sec,
-                                _cache(on, kv, table, lens, B, n_kv_heads * head_dim, lens_optional=True),
-                                on.ptr("err", err, torch.int32, (1,)))
-        _check(lib().sp_paged_append(C.byref(io), _stream(stream)), "sp_paged_append")
+            err = torch.zeros(1, dtype=i32, device=qkv.device)
+        k, pages, page = _pool(who, kv, dev, n_kv_heads * head_dim)
+        n_pos = 0
+        if rope is not None:
+            n_pos = rope.shape[0]
+        s0, s1, s2 = mrope_section or (0, 0, 0)
+        io = _pack_append(B, T, _opt(who, "cu_rows", cu_rows, i32, dev, (B + 1,)), x, ld, q, ld_q, n_heads, n_kv_heads,
+                          head_dim, _opt(who, "rope", rope, torch.float32, dev, (n_pos, head_dim // 2, 2)), n_pos,
+                          _opt(who, "pos", pos, i32, dev, (T,)), _opt(who, "pos3", pos3, i32, dev, (T, 4)), s0, s1, s2,
+                          k, pages, page, _arg(who, "table", table, i32, dev, (B, mp)), mp,
+                          _opt(who, "lens", lens, i32, dev, (B,)), _arg(who, "err", err, i32, dev, (1,)))
+        st = lib().sp_paged_append(io, _raw_stream(stream, dev))
+        if st:
+            _check(st, who)
+    finally:
+        _leave(guard)
     return {"q": q_out, "err": err}
 
 
 def prefix_attention_workspace(*, T_cap, B, n_heads, n_kv_heads, head_dim, n_groups=0, device="cuda"):
-    """A workspace for sp_prefix_attention calls of up to these sizes."""
+    """A workspace for sp_prefix_attention calls of these sizes."""
     with _torch().cuda.device(device):
         n = lib().sp_prefix_attention_workspace(int(T_cap), int(B), int(n_groups), int(n_heads), int(n_kv_heads),
                                                 int(head_dim))
@@ -720,33 +766,40 @@ def sp_prefix_attention(*, q, kv, table, lens, n_heads, n_kv_heads, head_dim, pr
     group_cu[g+1] - 1 share prefix_table[g], prefix_lens[g] positions) and, causally, over their sequence's own
     pages (table, lens: positions with these rows' own).  Returns out [T, n_heads head_dim] bf16, lse (the given
     [T, n_heads] fp32 tensor or None) and err."""
-    torch = _torch()
-    with _On("sp_prefix_attention", q) as on:
-        B, T = int(table.shape[0]), int(q.shape[0])
-        x, ld_q = on.rows("q", q, n_heads * head_dim)
+    torch, who = _torch(), "sp_prefix_attention"
+    dev, guard = _enter(who, q)
+    try:
+        i32, bf16 = torch.int32, torch.bfloat16
+        T, B, mp = q.shape[0], table.shape[0], table.shape[-1]
+        x, ld_q = _rows(who, "q", q, bf16, dev, n_heads * head_dim)
         if out is None:
-            out = torch.empty((T, n_heads * head_dim), dtype=torch.bfloat16, device=on.dev)
-        o, ld_out = on.rows("out", out, n_heads * head_dim)
+            out = torch.empty((T, n_heads * head_dim), dtype=bf16, device=q.device)
+        o, ld_out = _rows(who, "out", out, bf16, dev, n_heads * head_dim)
         if out.shape[0] != T:
             raise ValueError("sp_prefix_attention: out must have q's rows")
         if err is None:
-            err = torch.zeros(1, dtype=torch.int32, device=on.dev)
-        groups = int(prefix_table.shape[0]) if prefix_table is not None else 0
+            err = torch.zeros(1, dtype=i32, device=q.device)
+        groups = pmp = pt = gc = pl = 0
+        if prefix_table is not None and prefix_table.shape[0] > 0:
+            groups, pmp = prefix_table.shape[0], prefix_table.shape[-1]
+            pt = _arg(who, "prefix_table", prefix_table, i32, dev, (groups, pmp))
+            gc = _arg(who, "group_cu", group_cu, i32, dev, (groups + 1,))
+            pl = _arg(who, "prefix_lens", prefix_lens, i32, dev, (groups,))
         if ws is None:
             ws = prefix_attention_workspace(T_cap=T, B=B, n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim,
-                                            n_groups=groups, device=on.dev)
-        some = groups > 0
-        io = sp_prefix_attention_io(
-            B, T, on.ptr("cu_rows", cu_rows, torch.int32, (B + 1,), optional=True), x, ld_q, o, ld_out,
-            on.ptr("lse", lse, torch.float32, (T, n_heads), optional=True), n_heads, n_kv_heads, head_dim, float(scale),
-            _cache(on, kv, table, lens, B, n_kv_heads * head_dim), groups,
-            on.ptr("group_cu", group_cu, torch.int32, (groups + 1,)) if some else None,
-            on.ptr("prefix_table", prefix_table, torch.int32, (groups, None)) if some else None,
-            int(prefix_table.shape[1]) if some else 0,
-            on.ptr("prefix_lens", prefix_lens, torch.int32, (groups,)) if some else None,
-            on.ptr("err", err, torch.int32, (1,)))
-        _check(lib().sp_prefix_attention(C.byref(io), on.ptr("ws", ws, torch.uint8, (None,)), ws.numel(),
-                                         _stream(stream)), "sp_prefix_attention")
+                                            n_groups=groups, device=q.device)
+        k, pages, page = _pool(who, kv, dev, n_kv_heads * head_dim)
+        n = ws.numel()
+        io = _pack_attention(B, T, _opt(who, "cu_rows", cu_rows, i32, dev, (B + 1,)), x, ld_q, o, ld_out,
+                             _opt(who, "lse", lse, torch.float32, dev, (T, n_heads)), n_heads, n_kv_heads, head_dim, scale,
+                             k, pages, page, _arg(who, "table", table, i32, dev, (B, mp)), mp,
+                             _arg(who, "lens", lens, i32, dev, (B,)), groups, gc, pt, pmp, pl,
+                             _arg(who, "err", err, i32, dev, (1,)))
+        st = lib().sp_prefix_attention(io, _arg(who, "ws", ws, torch.uint8, dev, (n,)), n, _raw_stream(stream, dev))
+        if st:
+            _check(st, who)
+    finally:
+        _leave(guard)
     return {"out": out, "lse": lse, "err": err, "_ws": ws}
 
 
@@ -764,30 +817,43 @@ def sp_beam_select(*, logits, cum, n_out, done=None, eos=0, score=None, parent=N
     """The n_out best continuations of every element's beams: logits [B, W, V] fp32 or bf16 (rows may lie apart),
     cum [B, W] fp32, done [B, W] bool or None (a finished beam proposes itself with token eos).  Returns score,
     parent (beam) and token [B, n_out], best first; places without a continuation hold -infinity, -1, -1."""
-    torch = _torch()
-    with _On("sp_beam_select", logits) as on:
-        if logits.dim() != 3 or logits.dtype not in (torch.float32, torch.bfloat16) or (logits.shape[2] > 1 and logits.stride(2) != 1):
-            raise ValueError("sp_beam_select: logits must be [B, W, V] fp32 or bf16, tokens next to each other")
-        B, W, V = (int(n) for n in logits.shape)
-        ld = logits.stride(1) if W > 1 else logits.stride(0) if B > 1 else V
-        if B > 1 and W > 1 and logits.stride(0) != W * ld:
-            raise ValueError("sp_beam_select: the rows of logits must lie evenly apart")
+    torch, who = _torch(), "sp_beam_select"
+    dev, guard = _enter(who, logits)
+    try:
+        f32, i32 = torch.float32, torch.int32
+        is_f32 = logits.dtype is f32
+        if logits.dim() != 3 or not (is_f32 or logits.dtype is torch.bfloat16):
+            raise ValueError("sp_beam_select: logits must be [B, W, V] fp32 or bf16")
+        B, W, V = logits.shape
+        if logits.is_contiguous():
+            ld = V
+        else:
+            sb, ld, sv = logits.stride()
+            if W == 1:
+                ld = sb if B > 1 else V
+            if sv != 1 and V > 1:
+                raise ValueError("sp_beam_select: the tokens of logits must lie next to each other")
+            if B > 1 and sb != W * ld:
+                raise ValueError("sp_beam_select: the rows of logits must lie evenly apart")
+        shape = (B, n_out)
         if score is None:
-            score = torch.empty((B, n_out), dtype=torch.float32, device=on.dev)
+            score = torch.empty(shape, dtype=f32, device=logits.device)
         if parent is None:
-            parent = torch.empty((B, n_out), dtype=torch.int32, device=on.dev)
+            parent = torch.empty(shape, dtype=i32, device=logits.device)
         if token is None:
-            token = torch.empty((B, n_out), dtype=torch.int32, device=on.dev)
+            token = torch.empty(shape, dtype=i32, device=logits.device)
         if ws is None:
-            ws = beam_select_workspace(B=B, W=W, V=V, n_out=n_out, device=on.dev)
-        io = sp_beam_select_io(B, W, V, logits.data_ptr(), 1 if logits.dtype is torch.float32 else 0, ld,
-                               on.ptr("cum", cum, torch.float32, (B, W)),
-                               on.ptr("done", done, torch.bool, (B, W), optional=True), int(eos), int(n_out),
-                               on.ptr("score", score, torch.float32, (B, n_out)),
-                               on.ptr("parent", parent, torch.int32, (B, n_out)),
-                               on.ptr("token", token, torch.int32, (B, n_out)))
-        _check(lib().sp_beam_select(C.byref(io), on.ptr("ws", ws, torch.uint8, (None,)), ws.numel(), _stream(stream)),
-               "sp_beam_select")
+            ws = beam_select_workspace(B=B, W=W, V=V, n_out=n_out, device=logits.device)
+        n = ws.numel()
+        io = _pack_select(B, W, V, logits.data_ptr(), is_f32, ld, _arg(who, "cum", cum, f32, dev, (B, W)),
+                          _opt(who, "done", done, torch.bool, dev, (B, W)), eos, n_out,
+                          _arg(who, "score", score, f32, dev, shape), _arg(who, "parent", parent, i32, dev, shape),
+                          _arg(who, "token", token, i32, dev, shape))
+        st = lib().sp_beam_select(io, _arg(who, "ws", ws, torch.uint8, dev, (n,)), n, _raw_stream(stream, dev))
+        if st:
+            _check(st, who)
+    finally:
+        _leave(guard)
     return {"score": score, "parent": parent, "token": token, "_ws": ws}
 
 
@@ -795,23 +861,29 @@ def sp_beam_reorder(*, kv, table, own_table, lens, parent, err=None, stream=None
     """Puts the cache into the beams' new order: table rows and the rows of the partly filled pages of all layers
     (kv [n_layers, 2, n_pages, page_size, width]) follow parent [B, W or more] (its first W columns); table is
     updated in place.  Returns err."""
-    torch = _torch()
-    with _On("sp_beam_reorder", kv) as on:
-        if parent.dim() != 2 or parent.shape[0] < 1 or table.dim() != 2 or table.shape[0] % parent.shape[0] != 0:
-            raise ValueError("sp_beam_reorder: table must have the beams of parent's elements")
-        B, R = int(parent.shape[0]), int(table.shape[0])
-        if parent.dtype is not torch.int32 or parent.device != on.dev or parent.shape[1] < R // B or parent.stride(1) != 1:
-            raise ValueError(f"sp_beam_reorder: parent must be int32 [{B}, at least {R // B}]")
+    torch, who = _torch(), "sp_beam_reorder"
+    dev, guard = _enter(who, kv)
+    try:
+        i32 = torch.int32
+        if kv.dim() != 5 or parent.dim() != 2 or table.dim() != 2:
+            raise ValueError("sp_beam_reorder: kv [n_layers, 2, n_pages, page_size, width], parent [B, W], table [B W, pages]")
+        B, (R, mp) = parent.shape[0], table.shape
+        W = R // B if B > 0 else 0
+        if W < 1 or W * B != R or parent.dtype is not i32 or parent.get_device() != dev or parent.shape[1] < W or parent.stride(1) != 1:
+            raise ValueError("sp_beam_reorder: parent must be int32 [B, at least W], table have its B W beams")
         if err is None:
-            err = torch.zeros(1, dtype=torch.int32, device=on.dev)
-        k = on.ptr("kv", kv, torch.bfloat16, (None, 2, None, None, None))
-        io = sp_beam_reorder_io(B, R // B, kv.shape[0], k, kv.shape[2], kv.shape[3], kv.shape[4],
-                                on.ptr("table", table, torch.int32, (R, None)),
-                                on.ptr("own_table", own_table, torch.int32, (R, table.shape[1])), table.shape[1],
-                                on.ptr("lens", lens, torch.int32, (R,)), parent.data_ptr(),
-                                parent.stride(0) if B > 1 else max(parent.stride(0), R // B),
-                                on.ptr("err", err, torch.int32, (1,)))
-        _check(lib().sp_beam_reorder(C.byref(io), _stream(stream)), "sp_beam_reorder")
+            err = torch.zeros(1, dtype=i32, device=kv.device)
+        layers, _, pages, page, width = kv.shape
+        io = _pack_reorder(B, W, layers, _arg(who, "kv", kv, torch.bfloat16, dev, (layers, 2, pages, page, width)), pages,
+                           page, width, _arg(who, "table", table, i32, dev, (R, mp)),
+                           _arg(who, "own_table", own_table, i32, dev, (R, mp)), mp,
+                           _arg(who, "lens", lens, i32, dev, (R,)), parent.data_ptr(),
+                           parent.stride(0) if B > 1 else parent.shape[1], _arg(who, "err", err, i32, dev, (1,)))
+        st = lib().sp_beam_reorder(io, _raw_stream(stream, dev))
+        if st:
+            _check(st, who)
+    finally:
+        _leave(guard)
     return err
 
 

@@ -73,6 +73,7 @@ __global__ void __launch_bounds__(WK_NT, 1) prefix_warp_kernel(const PrefixArgs 
   pdl_wait();
   pdl_trigger();
   build_plan<WK_NT>(a, p, plan, blockIdx.x == 0);
+  if (warp == WK_WARPS - 1) write_rows(a, p, plan, lane, 32);  // (the warp with the least to do)
   const int N = plan.unit0[E];
   if (N == 0) return;
   const int P = plan_workers(p, N);
@@ -140,9 +141,9 @@ __global__ void __launch_bounds__(WK_NT, 1) prefix_warp_kernel(const PrefixArgs 
       const bool pre = get.e < a.n_groups;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int mv = get.rt * WK_ROWS + row_a + 8 * h;
+        const int mr = row_a + 8 * h, mv = get.rt * p.tile_rows + mr;
         const int r = mv / G, g = mv - r * G;
-        const bool have = mv < M;
+        const bool have = mr < p.tile_rows && mv < M;
         lim[h] = have ? (pre ? keys : min(max(keys - R + r + 1, 0), keys)) : 0;
         const __nv_bfloat16* qr = a.q + (have ? (plan.row0[get.e] + r) * a.ld_q + (get.kvh * G + g) * DH : 0) + col;
 #pragma unroll
@@ -241,7 +242,7 @@ __global__ void __launch_bounds__(WK_NT, 1) prefix_warp_kernel(const PrefixArgs 
         sum += __shfl_xor_sync(0xffffffffu, sum, 1);
         sum += __shfl_xor_sync(0xffffffffu, sum, 2);
         const int mr = row_a + 8 * h;
-        if (now.rt * WK_ROWS + mr < M) {
+        if (mr < p.tile_rows && now.rt * p.tile_rows + mr < M) {
           float* po = p.part_o + (base + mr) * DH + col;
 #pragma unroll
           for (int n = 0; n < DH / 8; ++n)
@@ -256,92 +257,87 @@ __global__ void __launch_bounds__(WK_NT, 1) prefix_warp_kernel(const PrefixArgs 
 }
 
 // --------------------------------------------------------------- joining the segments
-// One CTA per row and eight of its query heads, a warp each: the segments of the row's prefix item and of its own
-// item, in key order.  What the heads share (sequence, group, where the items lie) is found by all threads at once;
-// the segments' (max, sum) are read a lane each, then their values with the weights known, so that one access's
-// latency is paid once and not per segment.
-struct MergeSide {
-  int unit0;               // the entry's first unit
-  int N, len, items, item0, P;
-  int mv;                  // the row's first query vector in the entry
-};
-
+// One warp per row and query head: the segments of the row's prefix item and of its own item, in key order, up to 32
+// of them at a time.  Bound by latency, so the chain of dependent accesses is short: where the row's items lie (both
+// at once), every segment's (max, sum), a lane each, then the values with the weights known.
 template <int DH>
 __global__ void __launch_bounds__(256) prefix_merge_kernel(const PrefixArgs a, const PlanArgs pp, const PlanArgs po) {
-  __shared__ MergeSide side_s[2];
   pdl_wait();
   pdl_trigger();
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int lane = threadIdx.x & 31;
   const int E = a.n_groups + a.B, G = a.Hq / a.Hkv;
-  const int row = blockIdx.x;
-  const int first = row_begin(a, 0), last = row_begin(a, a.B);
-  static_assert(SP_MAX_BATCH <= 256, "a thread per sequence");
-  if (row < first || row >= last) return;
-  const int b = __syncthreads_count(tid < a.B && row_begin(a, min(tid, a.B)) <= row) - 1;
-  // its group, if it is in one
-  int g = __syncthreads_count(tid < a.n_groups && __ldg(a.group_cu + min(tid, a.n_groups)) <= b) - 1;
-  if (tid < 2) {
-    const PlanArgs& p = tid == 0 ? pp : po;
-    if (tid == 0 && g >= 0 && b >= __ldg(a.group_cu + g + 1)) g = -1;
-    const int e = tid == 0 ? g : a.n_groups + b;
-    MergeSide m = {};
-    if (e >= 0 && (tid == 0 ? p.prefix : p.own)) {
-      const int e0 = __ldcg(p.unit0 + e), e1 = __ldcg(p.unit0 + e + 1);
-      const int i0 = __ldcg(p.item0 + e), i1 = __ldcg(p.item0 + e + 1);
-      const int r0 = tid == 0 ? row_begin(a, min(max(__ldg(a.group_cu + g), 0), a.B)) : row_begin(a, b);
-      m.N = __ldcg(p.unit0 + E);
-      if (e1 > e0 && row >= r0) {
-        m.unit0 = e0;
-        m.items = i1 - i0;
-        m.item0 = i0;
-        m.len = (e1 - e0) / m.items;
-        m.P = plan_workers(p, m.N);
-        m.mv = (row - r0) * G;
-      }
-    }
-    side_s[tid] = m;
-  }
-  __syncthreads();
-  const int h = blockIdx.y * 8 + warp;
+  const int row = blockIdx.x, h = blockIdx.y * 8 + (threadIdx.x >> 5);
   if (h >= a.Hq) return;
+  int4 place[2];
+  int total[2];
+  place[0] = pp.prefix ? __ldcg(pp.rows_prefix + row) : make_int4(0, 0, 0, 0);
+  place[1] = po.own ? __ldcg(po.rows_own + row) : make_int4(0, 0, 0, 0);
+  total[0] = pp.prefix ? __ldcg(pp.unit0 + E) : 0;
+  total[1] = po.own ? __ldcg(po.unit0 + E) : 0;
+  if (row < row_begin(a, 0) || row >= row_begin(a, a.B)) return;
+  const int kvh = h / G, g = h - kvh * G;
+  int n[2];           // segments of the prefix item, of the own item
+  size_t first[2];    // slot row of the first one's vector
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+    const PlanArgs& p = side == 0 ? pp : po;
+    const int unit0 = place[side].x, len = place[side].y, N = total[side];
+    n[side] = 0;
+    first[side] = 0;
+    if (len == 0) continue;
+    const int mv = place[side].w + g;
+    const int rt = mv / p.tile_rows, mr = mv - rt * p.tile_rows;
+    const int in = rt * a.Hkv + kvh;
+    // the workers that have key tiles of the item, units u0 .. u1: a lane tries each of 32 candidates, from a little
+    // before where u0's worker is estimated
+    const int u0 = unit0 + in * len + p.over, u1 = unit0 + in * len + len - 1;
+    const int P = plan_workers(p, N);
+    int from = max((int)((float)u0 / (float)N * (float)P) - 2, 0);
+    while (from > 0 && part_begin(N, P, from) > u0) --from;
+    int w0 = from, w1 = from;
+    for (int c = from;; c += 32) {
+      const int begin = c + lane < P ? part_begin(N, P, c + lane) : 0x7fffffff;
+      const unsigned int upto0 = __ballot_sync(0xffffffffu, begin <= u0), upto1 = __ballot_sync(0xffffffffu, begin <= u1);
+      if (upto0) w0 = c + 31 - __clz(upto0);
+      if (upto1) w1 = c + 31 - __clz(upto1);
+      if (upto1 != 0xffffffffu) break;
+    }
+    n[side] = w1 - w0 + 1;
+    first[side] = ((size_t)(place[side].z + in) + w0) * p.slot_rows + mr;
+  }
   constexpr int V = DH / 32;
   float acc[V], mm = -INFINITY, ll = 0.f;
 #pragma unroll
   for (int v = 0; v < V; ++v) acc[v] = 0.f;
+  for (int s0 = 0; s0 < n[0] + n[1]; s0 += 32) {
+    const int s = s0 + lane, there = min(32, n[0] + n[1] - s0);
+    float2 ml = make_float2(-INFINITY, 0.f);
+    const float* o = nullptr;
+    if (s < n[0]) {
+      const size_t at = first[0] + (size_t)s * pp.slot_rows;
+      ml = __ldcg(pp.part_ml + at);
+      o = pp.part_o + at * DH;
+    } else if (s < n[0] + n[1]) {
+      const size_t at = first[1] + (size_t)(s - n[0]) * po.slot_rows;
+      ml = __ldcg(po.part_ml + at);
+      o = po.part_o + at * DH;
+    }
+    const float mn = fmaxf(mm, warp_max(ml.x));
+    if (mn == -INFINITY) continue;
+    const float ca = ex2(mm - mn), cb = ex2(ml.x - mn);
+    ll = ll * ca + warp_sum(ml.y * cb);
 #pragma unroll
-  for (int side = 0; side < 2; ++side) {
-    const PlanArgs& p = side == 0 ? pp : po;
-    const MergeSide m = side_s[side];
-    if (m.items == 0) continue;
-    const int mv = m.mv + h % G;
-    const int rt = mv / p.tile_rows, mr = mv - rt * p.tile_rows;
-    const int in = rt * a.Hkv + h / G;
-    if (in >= m.items) continue;  // (row offsets that do not ascend)
-    const int u0 = m.unit0 + in * m.len;
-    const int w0 = part_of(m.N, m.P, u0 + p.over), w1 = part_of(m.N, m.P, u0 + m.len - 1);
-    const size_t at0 = ((size_t)(m.item0 + in) + w0) * p.slot_rows + mr;
-    const int n = w1 - w0 + 1;
-    for (int s0 = 0; s0 < n; s0 += 32) {
-      float2 ml = make_float2(-INFINITY, 0.f);
-      if (s0 + lane < n) ml = __ldcg(p.part_ml + at0 + (size_t)(s0 + lane) * p.slot_rows);
-      const float mn = fmaxf(mm, warp_max(ml.x));
-      if (mn == -INFINITY) continue;
-      const float ca = ex2(mm - mn), cb = ex2(ml.x - mn);
-      ll = ll * ca + warp_sum(ml.y * cb);
-#pragma unroll
-      for (int v = 0; v < V; ++v) acc[v] *= ca;
-      mm = mn;
-      const float* x = p.part_o + (at0 + (size_t)s0 * p.slot_rows) * DH + lane * V;
+    for (int v = 0; v < V; ++v) acc[v] *= ca;
+    mm = mn;
 #pragma unroll 4
-      for (int s = 0; s < min(32, n - s0); ++s) {
-        const float c = __shfl_sync(0xffffffffu, cb, s);
-        float y[V];
-        const float* xs = x + (size_t)s * p.slot_rows * DH;
-        if (V == 4) *reinterpret_cast<float4*>(y) = __ldcg(reinterpret_cast<const float4*>(xs));
-        else *reinterpret_cast<float2*>(y) = __ldcg(reinterpret_cast<const float2*>(xs));
+    for (int i = 0; i < there; ++i) {
+      const float c = __shfl_sync(0xffffffffu, cb, i);
+      const float* x = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(o), i)) + lane * V;
+      float y[V];
+      if (V == 4) *reinterpret_cast<float4*>(y) = __ldcg(reinterpret_cast<const float4*>(x));
+      else *reinterpret_cast<float2*>(y) = __ldcg(reinterpret_cast<const float2*>(x));
 #pragma unroll
-        for (int v = 0; v < V; ++v) acc[v] += y[v] * c;
-      }
+      for (int v = 0; v < V; ++v) acc[v] += y[v] * c;
     }
   }
   const float inv = ll > 0.f ? 1.f / ll : 0.f;
@@ -374,6 +370,8 @@ static size_t plan_carve(PlanArgs* p, char* base, int T_cap, int B, int n_groups
   };
   p->unit0 = reinterpret_cast<int*>(take(E * 4));
   p->item0 = reinterpret_cast<int*>(take(E * 4));
+  p->rows_prefix = reinterpret_cast<int4*>(take(p->prefix ? (size_t)T_cap * 16 : 0));
+  p->rows_own = reinterpret_cast<int4*>(take(p->own ? (size_t)T_cap * 16 : 0));
   p->part_ml = reinterpret_cast<float2*>(take(rows * 8));
   p->part_o = reinterpret_cast<float*>(take(rows * dh * 4));
   return off;
@@ -385,14 +383,14 @@ PrefixLayout prefix_layout(int T_cap, int B, int n_groups, int Hq, int Hkv, int 
   const bool fits = G <= 128;
   const bool tc_prefix = fits && n_groups > 0 && (long long)T_cap * G >= (long long)kTcVectors * n_groups;
   const bool tc_own = fits && (long long)T_cap * G >= (long long)kTcVectors * B;
-  L.warp.tile_rows = WK_ROWS;
+  L.warp.tile_rows = G <= WK_ROWS ? WK_ROWS / G * G : WK_ROWS;  // (whole rows where they fit)
   L.warp.key_shift = 4;
   L.warp.over = 2;
   L.warp.min_units = 4;
   L.warp.prefix = n_groups > 0 && !tc_prefix;
   L.warp.own = !tc_own;
   L.warp.workers = L.warp.prefix || L.warp.own ? sms * WK_WARPS : 0;
-  L.warp.slot_rows = (int)std::min<size_t>(WK_ROWS, (size_t)T_cap * G);
+  L.warp.slot_rows = (int)std::min<size_t>(L.warp.tile_rows, (size_t)T_cap * G);
   L.tc.tile_rows = fits ? 128 / G * G : 128;
   L.tc.key_shift = 7;
   L.tc.over = 2;
@@ -432,10 +430,10 @@ cudaError_t prefix_attention_launch(const PrefixArgs& a, int dh, void* ws, cudaS
     prof_end_launch(st, SP_K_ATTN, 0.0, 0.0);
     if (r != cudaSuccess) return r;
   }
-  const dim3 grid(a.T_cap, (a.Hq + 7) / 8);
+  const PlanArgs &pp = L.tc.prefix ? L.tc : L.warp, &po = L.tc.own ? L.tc : L.warp;
   prof_begin_launch(st);
-  r = launch_pdl(dh == 128 ? prefix_merge_kernel<128> : prefix_merge_kernel<64>, grid, dim3(256), 0, st, a,
-                 L.tc.prefix ? L.tc : L.warp, L.tc.own ? L.tc : L.warp);
+  r = launch_pdl(dh == 128 ? prefix_merge_kernel<128> : prefix_merge_kernel<64>, dim3(a.T_cap, (a.Hq + 7) / 8), dim3(256),
+                 0, st, a, pp, po);
   prof_end_launch(st, SP_K_ATTN, 0.0, 0.0);
   return r;
 }

@@ -5,8 +5,8 @@
 // One CTA per SM is a worker of the plan; a key tile is 128 keys.
 //
 //   warp 0        Q and K by TMA: the Q tile once per segment, then per key tile its K rows, one box per page
-//                 (and 64 columns), into a three-slot ring
-//   warp 3        V by TMA into a two-slot ring.  Rows past the entry's keys are not to be multiplied: a zero
+//                 (and 64 columns), into a two-slot ring
+//   warp 3        V by TMA into a three-slot ring.  Rows past the entry's keys are not to be multiplied: a zero
 //                 weight times what lies there (NaN, say) is no zero, so the warp clears those rows in shared
 //                 memory behind the copy.
 //   warp 1        issues the scores S = Q K^T (M 128, N 128) into one of three S / P buffers of tensor memory
@@ -35,7 +35,7 @@ namespace sp {
 
 namespace {
 
-constexpr int TC_KV = 128, TC_NT = 384, NSB = 3, NVS = 2;
+constexpr int TC_KV = 128, TC_NT = 384, NSB = 3, NKS = 2, NVS = 3;
 constexpr float kRescaleLog2 = 8.f;
 
 template <int DH>
@@ -43,8 +43,8 @@ struct TcCfg {
   static constexpr uint32_t BOX = 128 * 128;               // 128 rows x 64 elements
   static constexpr uint32_t TILE = DH / 64 * BOX;          // a Q tile or a K / V tile
   static constexpr uint32_t OFF_Q = 0;
-  static constexpr uint32_t OFF_K = TILE;                  // [NSB]
-  static constexpr uint32_t OFF_V = OFF_K + NSB * TILE;    // [NVS]
+  static constexpr uint32_t OFF_K = TILE;                  // [NKS]
+  static constexpr uint32_t OFF_V = OFF_K + NKS * TILE;    // [NVS]
   static constexpr uint32_t OFF_M = OFF_V + NVS * TILE;    // running max by tile parity: [2][128] floats
   static constexpr uint32_t OFF_L = OFF_M + 2 * 128 * 4;   // sums: [segment parity][stream][128] floats
   static constexpr uint32_t OFF_STG = OFF_L + 4 * 128 * 4; // output stage: [8 warps][32 rows][64 B]
@@ -55,7 +55,7 @@ struct TcCfg {
   static constexpr uint32_t T_O = 384;
 };
 
-// X + s for slot / buffer s.  K_FULL counts the copies of K (with their bytes) and the end of O += P V three tiles
+// X + s for S / P buffer s (tile % 3).  K_FULL counts the copies of K (with their bytes) and the end of O += P V three tiles
 // before, the last reader of the S / P buffer that the scores will overwrite (the loader arrives twice for the
 // first three tiles); P_FULL the stream's four warps and the copies of V.  A K slot is free when its scores are
 // done (S_FULL), a V slot when its product is (PV_DONE).  V_TAIL: the copies of a tile whose rows are cleared next;
@@ -144,6 +144,11 @@ prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     tmem_alloc(tslot, 512);
     tmem_relinquish();
   }
+  if (threadIdx.x == 96) {
+    tma_prefetch_desc(&tmQ);
+    tma_prefetch_desc(&tmK);
+    tma_prefetch_desc(&tmV);
+  }
   // vectors behind a tile's last row are multiplied too (to nothing): let them be zeros, not what was there
   for (uint32_t i = threadIdx.x * 16; i < C::TILE; i += TC_NT * 16)
     *reinterpret_cast<uint4*>(sm + C::OFF_Q + i) = make_uint4(0u, 0u, 0u, 0u);
@@ -212,10 +217,10 @@ prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         };
         const uint32_t sb = g % NSB;
         if (!is_v) {
-          uint8_t* s = sm + C::OFF_K + sb * C::TILE;
+          uint8_t* s = sm + C::OFF_K + (g % NKS) * C::TILE;
           uint64_t* full = &bar[K_FULL + sb];
-          // the slot last held tile g - 3: free once its scores are done
-          if (g >= NSB && !mbar_wait_warp(&bar[S_FULL + sb], ((g / NSB) & 1) ^ 1u, a.err)) { ok = false; break; }
+          // the slot last held tile g - 2: free once its scores are done
+          if (g >= NKS && !mbar_wait_warp(&bar[S_FULL + (g - NKS) % NSB], ((g - NKS) / NSB) & 1, a.err)) { ok = false; break; }
           if (bad) {
             clear_bad(s);
             fence_proxy_async_smem();
@@ -234,7 +239,7 @@ prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         } else {
           uint8_t* s = sm + C::OFF_V + (g % NVS) * C::TILE;
           uint64_t* full = &bar[P_FULL + sb];
-          // the slot last held tile g - 2: free once its product is done
+          // the slot last held tile g - 3: free once its product is done
           if (g >= NVS && !mbar_wait_warp(&bar[PV_DONE + (g - NVS) % NSB], ((g - NVS) / NSB) & 1, a.err)) { ok = false; break; }
           const bool tail = here < TC_KV || bad;
           uint64_t* land = tail ? &bar[V_TAIL] : full;
@@ -282,7 +287,7 @@ prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
 #pragma unroll
             for (int kk = 0; kk < DH / 16; ++kk)
               umma_bf16(tmem + sb * TC_KV, dQ + (((kk >> 2) * C::BOX + (kk & 3) * 32) >> 4),
-                        dK + sb * slot16 + (((kk >> 2) * C::BOX + (kk & 3) * 32) >> 4), IDESC_S, kk ? 1u : 0u);
+                        dK + (gg % NKS) * slot16 + (((kk >> 2) * C::BOX + (kk & 3) * 32) >> 4), IDESC_S, kk ? 1u : 0u);
             umma_commit(&bar[S_FULL + sb]);
             if (j + 1 == sg.n) umma_commit(&bar[Q_EMPTY]);
           }
@@ -319,6 +324,7 @@ prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     const uint32_t s = (uint32_t)(warp - 4) >> 2;
     const int r0 = (warp & 3) * 32, r = r0 + lane;
     const uint32_t trow = tmem + ((uint32_t)r0 << 16);
+    write_rows(a, p, plan, threadIdx.x - 128, TC_NT - 128);
     float* mchain = reinterpret_cast<float*>(sm + C::OFF_M);
     float* lsum = reinterpret_cast<float*>(sm + C::OFF_L);
     while (ok && more) {

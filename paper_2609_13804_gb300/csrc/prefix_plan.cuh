@@ -53,6 +53,8 @@ struct PlanArgs {
   bool prefix, own;        // which entries this launch covers
   int* unit0;              // [n_groups + B + 1] first unit of each entry, then N      (written for the merge)
   int* item0;              // [n_groups + B + 1] first item of each entry, then the item count
+  int4* rows_prefix;       // [T_cap] where a row's prefix items lie (if this launch covers prefixes): the entry's first
+  int4* rows_own;          // unit, units per item (0: none), first item, the row's first vector; its own items likewise
   float* part_o;           // [slots][slot_rows][DH]
   float2* part_ml;         // [slots][slot_rows] (max in log2 units, sum)
   int slot_rows;
@@ -77,14 +79,6 @@ SP_DEVINL int part_begin(int N, int P, int w) {
   const int q = N / P, r = N - q * P;
   return w * q + w * r / P;
 }
-// The worker whose part holds unit t: the largest w with part_begin(w) <= t.
-SP_DEVINL int part_of(int N, int P, int t) {
-  int w = min((int)((float)t / (float)N * (float)P), P - 1);
-  while (w > 0 && part_begin(N, P, w) > t) --w;
-  while (w + 1 < P && part_begin(N, P, w + 1) <= t) ++w;
-  return w;
-}
-
 // Called by all NT threads of the CTA (a multiple of 32, at most 1,024).
 template <int NT>
 SP_DEVINL void build_plan(const PrefixArgs& a, const PlanArgs& p, PlanShared& s, bool write) {
@@ -94,7 +88,20 @@ SP_DEVINL void build_plan(const PrefixArgs& a, const PlanArgs& p, PlanShared& s,
   long long t_sum = 0;
   int i_sum = 0;
   long long tl[PER];
-  int il[PER];
+  int il[PER], r0[PER], r1[PER], len[PER];
+  // every thread's loads at once, first those that others depend on (entries beyond the last: the last's again)
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const int e = min(tid * PER + k, E - 1), b = e - a.n_groups;
+    r0[k] = b < 0 ? __ldg(a.group_cu + e) : b;
+    r1[k] = b < 0 ? __ldg(a.group_cu + e + 1) : b + 1;
+    len[k] = __ldg(b < 0 ? a.plens + e : a.lens + b);
+  }
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    r0[k] = row_begin(a, min(max(r0[k], 0), a.B));
+    r1[k] = row_begin(a, min(max(r1[k], 0), a.B));
+  }
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
     const int e = tid * PER + k;
@@ -102,15 +109,11 @@ SP_DEVINL void build_plan(const PrefixArgs& a, const PlanArgs& p, PlanShared& s,
     long long tiles = 0;
     if (e < E) {
       const bool pre = e < a.n_groups;
-      const int b = e - a.n_groups;
-      const int b0 = pre ? min(max(__ldg(a.group_cu + e), 0), a.B) : b;
-      const int b1 = pre ? min(max(__ldg(a.group_cu + e + 1), 0), a.B) : b + 1;
-      const int r0 = row_begin(a, b0), r = max(row_begin(a, b1) - r0, 0);
-      const int L = pre ? __ldg(a.plens + e) : __ldg(a.lens + b);
+      const int r = max(r1[k] - r0[k], 0);
       const int cap = (pre ? a.pmax_pages : a.max_pages) << a.page_shift;
-      if ((L < 0 || L > cap) && write) set_error(a.err, SP_DEVERR_INDEX);
-      const int keys = min(max(L, 0), cap);
-      s.row0[e] = r0;
+      if ((len[k] < 0 || len[k] > cap) && write) set_error(a.err, SP_DEVERR_INDEX);
+      const int keys = min(max(len[k], 0), cap);
+      s.row0[e] = r0[k];
       s.rows[e] = r;
       s.keys[e] = keys;
       if (pre ? p.prefix : p.own) {
@@ -171,6 +174,27 @@ SP_DEVINL void build_plan(const PrefixArgs& a, const PlanArgs& p, PlanShared& s,
     }
   }
   __syncthreads();
+}
+
+// Where row `row`'s items lie, of the entries e0 .. e1 - 1 (whose rows ascend).
+SP_DEVINL int4 find_row(const PlanShared& s, int e0, int e1, int row, int G) {
+  int lo = e0, hi = e1 - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (s.row0[mid] <= row) lo = mid; else hi = mid - 1;
+  }
+  const int in = row - s.row0[lo], items = s.item0[lo + 1] - s.item0[lo], units = s.unit0[lo + 1] - s.unit0[lo];
+  if (in < 0 || in >= s.rows[lo] || units == 0) return make_int4(0, 0, 0, 0);
+  return make_int4(s.unit0[lo], units / items, s.item0[lo], in * G);
+}
+
+// The merge's table of rows, by `threads` threads of every CTA (thread t of them).
+SP_DEVINL void write_rows(const PrefixArgs& a, const PlanArgs& p, const PlanShared& s, int t, int threads) {
+  const int G = a.Hq / a.Hkv;
+  for (int row = blockIdx.x * threads + t; row < a.T_cap; row += gridDim.x * threads) {
+    if (p.prefix) p.rows_prefix[row] = find_row(s, 0, a.n_groups, row, G);
+    if (p.own) p.rows_own[row] = find_row(s, a.n_groups, a.n_groups + a.B, row, G);
+  }
 }
 
 // A walk along the key tiles of a worker's part, which ends at unit t1.
