@@ -63,28 +63,27 @@ struct WkCfg {
 };
 
 template <int DH>
-__global__ void __launch_bounds__(WK_NT, 1) prefix_warp_kernel(const PrefixArgs a, const PlanArgs p) {
+__global__ void __launch_bounds__(WK_NT, 1) prefix_warp_kernel(const PrefixArgs a, const PlanArgs p, int late) {
   using C = WkCfg<DH>;
   constexpr int CPR = DH / 8;  // 16-byte chunks of a row
   extern __shared__ __align__(128) uint8_t ring_all[];
   __shared__ PlanShared plan;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int E = a.n_groups + a.B, G = a.Hq / a.Hkv;
-  pdl_wait();
+  // Behind prefix_tc_kernel (late) nothing here reads or overwrites what that writes, and what came before it was
+  // complete when it let this kernel start: only the merge has to find both complete, so the wait is at the end and
+  // SMs that the other kernel has left are used meanwhile.
+  if (!late) pdl_wait();
   pdl_trigger();
   build_plan<WK_NT>(a, p, plan, blockIdx.x == 0);
   if (warp == WK_WARPS - 1) write_rows(a, p, plan, lane, 32);  // (the warp with the least to do)
-  const int N = plan.unit0[E];
-  if (N == 0) return;
-  const int P = plan_workers(p, N);
+  const int N = plan.unit0[E], P = N > 0 ? plan_workers(p, N) : 0;
   const int w = blockIdx.x + warp * gridDim.x;  // (a short list goes to different SMs first)
-  if (w >= P) return;
-  const int t1 = part_begin(N, P, w + 1);
+  const int t1 = w < P ? part_begin(N, P, w + 1) : 0;
   TileCursor put, get;
-  bool more = get.seek(plan, p, E, a.Hkv, part_begin(N, P, w), t1);
-  if (!more) return;
+  bool more = w < P && get.seek(plan, p, E, a.Hkv, part_begin(N, P, w), t1);
   put = get;
-  bool more_put = true;
+  bool more_put = more;
 
   const uint32_t ring = smem_u32(ring_all) + warp * C::NS * C::STAGE;
   const size_t W = (size_t)a.Hkv * DH;
@@ -254,6 +253,7 @@ __global__ void __launch_bounds__(WK_NT, 1) prefix_warp_kernel(const PrefixArgs 
     }
   }
   cp_async_wait<0>();
+  if (late) pdl_wait();
 }
 
 // --------------------------------------------------------------- joining the segments
@@ -426,7 +426,7 @@ cudaError_t prefix_attention_launch(const PrefixArgs& a, int dh, void* ws, cudaS
     r = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (r != cudaSuccess) return r;
     prof_begin_launch(st);
-    r = launch_pdl(kern, dim3(sms), dim3(WK_NT), smem, st, a, L.warp);
+    r = launch_pdl(kern, dim3(sms), dim3(WK_NT), smem, st, a, L.warp, L.tc.workers ? 1 : 0);
     prof_end_launch(st, SP_K_ATTN, 0.0, 0.0);
     if (r != cudaSuccess) return r;
   }
