@@ -79,9 +79,10 @@ __global__ void __launch_bounds__(WK_NT, 1) prefix_warp_kernel(const PrefixArgs 
   if (warp == WK_WARPS - 1) write_rows(a, p, plan, lane, 32);  // (the warp with the least to do)
   const int N = plan.unit0[E], P = N > 0 ? plan_workers(p, N) : 0;
   const int w = blockIdx.x + warp * gridDim.x;  // (a short list goes to different SMs first)
-  const int t1 = w < P ? part_begin(N, P, w + 1) : 0;
+  int t0 = 0, t1 = 0;
+  if (w < P) part_of_worker(N, P, w, t0, t1);
   TileCursor put, get;
-  bool more = w < P && get.seek(plan, p, E, a.Hkv, part_begin(N, P, w), t1);
+  bool more = w < P && get.seek(plan, p, E, a.Hkv, t0, t1);
   put = get;
   bool more_put = more;
 
@@ -89,39 +90,54 @@ __global__ void __launch_bounds__(WK_NT, 1) prefix_warp_kernel(const PrefixArgs 
   const size_t W = (size_t)a.Hkv * DH;
   const size_t plane = ((size_t)a.n_pages << a.page_shift) * W;
 
-  // one tile into ring slot `slot`: lane = 16-byte chunk of a row, rows in turn; rows past the keys are zeros
-  auto load_tile = [&](int slot) {
+  // A tile to be loaded: its page is looked up when the one before it is loaded, which hides the lookup.
+  struct Ahead {
+    int page, row, n, kvh;  // page, its first key's row there, keys, kv head
+    bool some;
+  };
+  auto look = [&]() {
+    Ahead h;
+    h.some = more_put;
+    if (!more_put) return h;
     const bool pre = put.e < a.n_groups;
     const int k0 = put.j * WK_KEYS;
-    const int n = min(WK_KEYS, plan.keys[put.e] - k0);
     const int* tb = pre ? a.ptable + (size_t)put.e * a.pmax_pages : a.table + (size_t)(put.e - a.n_groups) * a.max_pages;
-    int page = __ldg(tb + (k0 >> a.page_shift));
-    bool ok = page >= 0 && page < a.n_pages;
+    h.page = __ldg(tb + (k0 >> a.page_shift));
+    h.row = k0 & ((1 << a.page_shift) - 1);
+    h.n = min(WK_KEYS, plan.keys[put.e] - k0);
+    h.kvh = put.kvh;
+    more_put = put.next(plan, p, a.Hkv, t1);
+    return h;
+  };
+  // one tile into ring slot `slot`: lane = 16-byte chunk of a row, rows in turn; rows past the keys are zeros
+  auto load_tile = [&](const Ahead& h, int slot) {
+    int page = h.page;
+    const bool ok = page >= 0 && page < a.n_pages;
     if (!ok) {
       if (lane == 0) set_error(a.err, SP_DEVERR_INDEX);
       page = 0;
     }
-    const __nv_bfloat16* src =
-        a.kv + (((size_t)page << a.page_shift) + (k0 & ((1 << a.page_shift) - 1))) * W + put.kvh * DH;
     const uint32_t dst = ring + slot * C::STAGE;
     const int c = lane % CPR;
+    const __nv_bfloat16* src = a.kv + (((size_t)page << a.page_shift) + h.row) * W + h.kvh * DH + c * 8;
 #pragma unroll
     for (int r0 = 0; r0 < WK_KEYS; r0 += 32 / CPR) {
       const int r = r0 + lane / CPR;
-      const bool in = ok && r < n;
-      const __nv_bfloat16* s = src + (in ? r : 0) * W + c * 8;
+      const bool in = ok && r < h.n;
+      const __nv_bfloat16* s = src + (in ? r : 0) * W;
       const uint32_t d = dst + r * C::ROW + ((c ^ (r & 7)) << 4);
       cp_async16(d, s, in ? 16 : 0);
       cp_async16(d + WK_KEYS * C::ROW, s + plane, in ? 16 : 0);
     }
   };
 
+  Ahead first[C::NS - 1], ahead;
+#pragma unroll
+  for (int s = 0; s < C::NS - 1; ++s) first[s] = look();
+  ahead = look();
 #pragma unroll
   for (int s = 0; s < C::NS - 1; ++s) {
-    if (more_put) {
-      load_tile(s);
-      more_put = put.next(plan, p, a.Hkv, t1);
-    }
+    if (first[s].some) load_tile(first[s], s);
     cp_async_commit();
   }
 
@@ -159,9 +175,9 @@ __global__ void __launch_bounds__(WK_NT, 1) prefix_warp_kernel(const PrefixArgs 
         for (int c = 0; c < 4; ++c) o[n][c] = 0.f;
       fresh = false;
     }
-    if (more_put) {
-      load_tile(slot_put);
-      more_put = put.next(plan, p, a.Hkv, t1);
+    if (ahead.some) {
+      load_tile(ahead, slot_put);
+      ahead = look();
     }
     cp_async_commit();
     if (++slot_put == C::NS) slot_put = 0;
@@ -386,7 +402,7 @@ PrefixLayout prefix_layout(int T_cap, int B, int n_groups, int Hq, int Hkv, int 
   L.warp.tile_rows = G <= WK_ROWS ? WK_ROWS / G * G : WK_ROWS;  // (whole rows where they fit)
   L.warp.key_shift = 4;
   L.warp.over = 2;
-  L.warp.min_units = 4;
+  L.warp.min_shift = 2;
   L.warp.prefix = n_groups > 0 && !tc_prefix;
   L.warp.own = !tc_own;
   L.warp.workers = L.warp.prefix || L.warp.own ? sms * WK_WARPS : 0;
@@ -394,7 +410,7 @@ PrefixLayout prefix_layout(int T_cap, int B, int n_groups, int Hq, int Hkv, int 
   L.tc.tile_rows = fits ? 128 / G * G : 128;
   L.tc.key_shift = 7;
   L.tc.over = 2;
-  L.tc.min_units = 4;
+  L.tc.min_shift = 2;
   L.tc.prefix = tc_prefix;
   L.tc.own = tc_own;
   L.tc.workers = tc_prefix || tc_own ? sms : 0;

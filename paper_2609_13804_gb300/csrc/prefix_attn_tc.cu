@@ -101,8 +101,9 @@ struct SegWalk {
     if (N == 0) return false;
     const int P = plan_workers(p, N);
     if (w >= P) return false;
-    t1 = part_begin(N, P, w + 1);
-    if (!c.seek(s, p, E, Hkv, part_begin(N, P, w), t1)) return false;
+    int t0;
+    part_of_worker(N, P, w, t0, t1);
+    if (!c.seek(s, p, E, Hkv, t0, t1)) return false;
     size();
     return true;
   }

@@ -46,7 +46,7 @@ struct PlanArgs {
   int tile_rows;           // query vectors of a row tile
   int key_shift;           // log2 of the keys of a key tile
   int over;                // units of an item besides its key tiles
-  int min_units;           // units a worker takes at least (while there are enough)
+  int min_shift;           // log2 of the units a worker takes at least (while there are enough)
   int workers;
   int max_items;           // items there is room for: no more exist while row and group offsets ascend (else, and
                            // beyond 2^31 - 1 units, the launch covers nothing and reports SP_DEVERR_INDEX)
@@ -73,12 +73,19 @@ struct PlanShared {
   int wsum_i[32];  // (a CTA has 32 warps at most)
 };
 
-SP_DEVINL int plan_workers(const PlanArgs& p, int N) { return max(min(p.workers, (N + p.min_units - 1) / p.min_units), 1); }
+SP_DEVINL int plan_workers(const PlanArgs& p, int N) { return max(min(p.workers, (N + (1 << p.min_shift) - 1) >> p.min_shift), 1); }
 // First unit of worker w's part, floor(w N / P), without products over 32 bits (P is below 2^15).
 SP_DEVINL int part_begin(int N, int P, int w) {
   const int q = N / P, r = N - q * P;
   return w * q + w * r / P;
 }
+// Worker w's units [t0, t1).
+SP_DEVINL void part_of_worker(int N, int P, int w, int& t0, int& t1) {
+  const int q = N / P, r = N - q * P, a = w * r, f = a / P;
+  t0 = w * q + f;
+  t1 = t0 + q + (a - f * P + r >= P ? 1 : 0);
+}
+
 // Called by all NT threads of the CTA (a multiple of 32, at most 1,024).
 template <int NT>
 SP_DEVINL void build_plan(const PrefixArgs& a, const PlanArgs& p, PlanShared& s, bool write) {
