@@ -634,6 +634,46 @@ SP_API sp_status sp_prefix_attention(const sp_prefix_attention_io* io, void* wor
                                      sp_stream stream);
 
 /*
+ * The model over a paged cache.  pools is the pools of all layers one after the
+ * other (kv [n_layers][2][n_pages][page_size][n_kv_heads * head_dim]), lens is
+ * ignored.
+ * sp_prefill_paged: sp_prefill (workspace and results are its) with the keys and
+ * values put into pages: row j of sequence b at position j of table row b;
+ * io.kv must be NULL.
+ */
+SP_API sp_status sp_prefill_paged(const sp_model* m, const sp_prefill_io* io, const sp_paged_kv* pools, void* workspace,
+                                  size_t workspace_bytes, sp_stream stream);
+
+/*
+ * One generation step over pages, sequences sharing prefixes: the layers of
+ * sp_decode applied to the new token x[b] of every sequence, its keys and values
+ * appended at the sequence's own position lens[b] (sp_paged_append) and its
+ * attention over its group's prefix and its own pages (sp_prefix_attention).
+ * lens and rope_pos are then incremented on the device, so steps chain.  (After a
+ * prefix of L positions rope_pos starts at L, after an mRoPE prefix at the
+ * position its next text token takes.)  A position outside the table sets
+ * SP_DEVERR_INDEX and is not written.
+ */
+typedef struct {
+  int B;                    /* sequences, 1..SP_MAX_BATCH */
+  const void* x;            /* DEVICE [B, d] bf16: the new token of each sequence */
+  int* lens;                /* DEVICE [B] own cached positions; incremented */
+  int* rope_pos;            /* DEVICE [B] rotary position of each new token; incremented */
+  sp_paged_kv cache;        /* pools of all layers; table [B, max_pages]: the sequences' own pages; lens ignored */
+  int n_groups;             /* as in sp_prefix_attention_io */
+  const int* group_cu;
+  const int* prefix_table;
+  int prefix_max_pages;
+  const int* prefix_lens;
+  float* hidden;            /* DEVICE [B, d] fp32 output */
+  int* err;                 /* DEVICE error word or NULL */
+} sp_decode_paged_io;
+
+SP_API size_t sp_decode_paged_workspace(const sp_model* m, int B, int n_groups);
+SP_API sp_status sp_decode_paged(const sp_model* m, const sp_decode_paged_io* io, void* workspace,
+                                 size_t workspace_bytes, sp_stream stream);
+
+/*
  * Beam search's selection: of the W beams of each of B elements and the V
  * tokens, the n_out continuations with the largest
  *   cum[w] + log softmax(logits[w])[v],

@@ -38,7 +38,7 @@ EXPORTS = [
     "sp_decode_workspace", "sp_decode", "sp_select_train", "sp_soft_topk", "sp_vp_gate",
     "sp_mrope_positions", "sp_wait_probe",
     "sp_paged_append", "sp_prefix_attention_workspace", "sp_prefix_attention", "sp_beam_select_workspace",
-    "sp_beam_select", "sp_beam_reorder",
+    "sp_beam_select", "sp_beam_reorder", "sp_prefill_paged", "sp_decode_paged_workspace", "sp_decode_paged",
 ]
 SP_SELECT_NOALLOC_SCRATCH_BYTES = 64 << 20
 
@@ -142,6 +142,12 @@ class sp_prefix_attention_io(C.Structure):
                 ("group_cu", P), ("prefix_table", P), ("prefix_max_pages", C.c_int), ("prefix_lens", P), ("err", P)]
 
 
+class sp_decode_paged_io(C.Structure):
+    _fields_ = [("B", C.c_int), ("x", P), ("lens", P), ("rope_pos", P), ("cache", sp_paged_kv), ("n_groups", C.c_int),
+                ("group_cu", P), ("prefix_table", P), ("prefix_max_pages", C.c_int), ("prefix_lens", P), ("hidden", P),
+                ("err", P)]
+
+
 class sp_beam_select_io(C.Structure):
     _fields_ = [("B", C.c_int), ("W", C.c_int), ("V", C.c_int), ("logits", P), ("logits_f32", C.c_int),
                 ("ld", C.c_longlong), ("cum", P), ("done", P), ("eos", C.c_int), ("n_out", C.c_int), ("score", P),
@@ -210,6 +216,9 @@ def lib():
         "sp_beam_select_workspace": (C.c_size_t, [C.c_int] * 4),
         "sp_beam_select": (C.c_int, [P, P, C.c_size_t, P]),
         "sp_beam_reorder": (C.c_int, [P, P]),
+        "sp_prefill_paged": (C.c_int, [P, C.POINTER(sp_prefill_io), C.POINTER(sp_paged_kv), P, C.c_size_t, P]),
+        "sp_decode_paged_workspace": (C.c_size_t, [P, C.c_int, C.c_int]),
+        "sp_decode_paged": (C.c_int, [P, P, P, C.c_size_t, P]),
         "sp_wait_probe": (C.c_int, [P, C.c_uint, C.c_int, P, P, P]),
         "sp_profile_begin": (C.c_int, [C.c_int]),
         "sp_profile_end": (C.c_int, [C.POINTER(C.c_double), C.POINTER(C.c_longlong), C.POINTER(C.c_double),
@@ -640,6 +649,7 @@ _pack_append = _packer(sp_paged_append_io)
 _pack_attention = _packer(sp_prefix_attention_io)
 _pack_select = _packer(sp_beam_select_io)
 _pack_reorder = _packer(sp_beam_reorder_io)
+_pack_decode = _packer(sp_decode_paged_io)
 
 
 def _enter(who: str, t):
@@ -801,6 +811,74 @@ def sp_prefix_attention(*, q, kv, table, lens, n_heads, n_kv_heads, head_dim, pr
     finally:
         _leave(guard)
     return {"out": out, "lse": lse, "err": err, "_ws": ws}
+
+
+def sp_prefill_paged(model: Model, *, x, cu_seqlens, pos, B, T_cap, max_seqlen_cap, kv, table, residual=None,
+                     stream=None, ws=None, hidden=None, pos3=None, err=None) -> Dict:
+    """sp_prefill with the keys and values put into pages: kv [n_layers, 2, n_pages, page_size, width] (paged_pool),
+    table [B, pages] int32."""
+    torch, who, m = _torch(), "sp_prefill_paged", model.shape
+    dev, guard = _enter(who, x)
+    try:
+        if kv.dim() != 5:
+            raise ValueError("sp_prefill_paged: kv must be the pools of all layers")
+        _, _, pages, page, width = kv.shape
+        k = _arg(who, "kv", kv, torch.bfloat16, dev, (m.n_layers, 2, pages, page, m.n_kv_heads * m.head_dim))
+        t = _arg(who, "table", table, torch.int32, dev, (B, table.shape[-1]))
+        if hidden is None:
+            hidden = torch.zeros((max(T_cap, 1), m.d), dtype=torch.float32, device=x.device)
+        if err is None:
+            err = torch.zeros(1, dtype=torch.int32, device=x.device)
+        io = sp_prefill_io(int(B), int(T_cap), int(max_seqlen_cap), ptr(x), ptr(cu_seqlens), ptr(pos), ptr(hidden),
+                           ptr(residual), ptr(err), None, 0, ptr(pos3))
+        pools = sp_paged_kv(k, pages, page, t, table.shape[-1], None)
+        if ws is None:
+            ws = workspace(lib().sp_prefill_workspace(model.handle, int(T_cap), int(max_seqlen_cap)), x.device)
+        _check(lib().sp_prefill_paged(model.handle, C.byref(io), C.byref(pools), ptr(ws), ws.numel(),
+                                      _raw_stream(stream, dev)), who)
+    finally:
+        _leave(guard)
+    return {"hidden": hidden, "err": err, "_ws": ws}
+
+
+def sp_decode_paged(model: Model, *, x, lens, rope_pos, kv, table, prefix_table=None, prefix_lens=None, group_cu=None,
+                    hidden=None, ws=None, err=None, stream=None) -> Dict:
+    """One generation step over pages: x [B, d] bf16 new tokens, lens / rope_pos [B] int32 own cached positions and
+    rotary positions (both incremented on the device), kv [n_layers, 2, n_pages, page_size, width], table [B, pages]
+    the sequences' own pages; sequences group_cu[g] .. group_cu[g+1] - 1 share prefix_table[g], prefix_lens[g]."""
+    torch, who, m = _torch(), "sp_decode_paged", model.shape
+    dev, guard = _enter(who, x)
+    try:
+        i32 = torch.int32
+        B, mp = x.shape[0], table.shape[-1]
+        if kv.dim() != 5:
+            raise ValueError("sp_decode_paged: kv must be the pools of all layers")
+        _, _, pages, page, _ = kv.shape
+        groups = pmp = pt = gc = pl = 0
+        if prefix_table is not None and prefix_table.shape[0] > 0:
+            groups, pmp = prefix_table.shape[0], prefix_table.shape[-1]
+            pt = _arg(who, "prefix_table", prefix_table, i32, dev, (groups, pmp))
+            gc = _arg(who, "group_cu", group_cu, i32, dev, (groups + 1,))
+            pl = _arg(who, "prefix_lens", prefix_lens, i32, dev, (groups,))
+        if hidden is None:
+            hidden = torch.empty((B, m.d), dtype=torch.float32, device=x.device)
+        if err is None:
+            err = torch.zeros(1, dtype=i32, device=x.device)
+        if ws is None:
+            ws = workspace(lib().sp_decode_paged_workspace(model.handle, B, groups), x.device)
+        n = ws.numel()
+        io = _pack_decode(B, _arg(who, "x", x, torch.bfloat16, dev, (B, m.d)), _arg(who, "lens", lens, i32, dev, (B,)),
+                          _arg(who, "rope_pos", rope_pos, i32, dev, (B,)),
+                          _arg(who, "kv", kv, torch.bfloat16, dev, (m.n_layers, 2, pages, page, m.n_kv_heads * m.head_dim)),
+                          pages, page, _arg(who, "table", table, i32, dev, (B, mp)), mp, 0, groups, gc, pt, pmp, pl,
+                          _arg(who, "hidden", hidden, torch.float32, dev, (B, m.d)), _arg(who, "err", err, i32, dev, (1,)))
+        st = lib().sp_decode_paged(model.handle, io, _arg(who, "ws", ws, torch.uint8, dev, (n,)), n,
+                                   _raw_stream(stream, dev))
+        if st:
+            _check(st, who)
+    finally:
+        _leave(guard)
+    return {"hidden": hidden, "err": err, "_ws": ws}
 
 
 def beam_select_workspace(*, B, W, V, n_out, device="cuda"):

@@ -1107,9 +1107,55 @@ size_t sp_prefill_workspace(const sp_model* m, int T_cap, int max_seqlen_cap) {
   return prefill_ws(m, T_cap, true, cv, nullptr) + 256;
 }
 
-static sp_status prefill_impl(const sp_model* m, const sp_prefill_io* io, void* ws, size_t ws_bytes, cudaStream_t st) {
+// The paged pools of every layer: sizes and pointers, as sp_paged_kv for one layer.
+static sp_status check_pools(const char* who, const sp_model_cfg& c, const sp_paged_kv* pg) {
+  if (!pg->kv || !pg->table) return fail(SP_ERR_INVALID_ARG, "%s: kv and table required", who);
+  if (pg->page_size < 16 || pg->page_size > 1024 || (pg->page_size & (pg->page_size - 1)))
+    return fail(SP_ERR_SHAPE, "%s: page_size must be a power of two in 16..1024", who);
+  if (pg->n_pages < 1 || (long long)pg->n_pages * pg->page_size > (1ll << 30) || pg->max_pages < 1 ||
+      (long long)pg->max_pages * pg->page_size > (1ll << 30))
+    return fail(SP_ERR_SHAPE, "%s: n_pages and max_pages must be at least 1 and at most 2^30 positions", who);
+  if (!al16(pg->kv)) return fail(SP_ERR_ALIGN, "%s: kv must be 16-byte aligned", who);
+  return SP_OK;
+}
+
+// Layer l's pool.
+static __nv_bfloat16* pool_of(const sp_model_cfg& c, const sp_paged_kv& pg, int l) {
+  return static_cast<__nv_bfloat16*>(pg.kv) + (size_t)l * 2 * pg.n_pages * pg.page_size * c.n_kv_heads * c.head_dim;
+}
+
+// What the paged append of a model's rows has in common for all layers (kv is set per layer).
+static PagedAppendArgs append_args(const sp_model* m, const sp_paged_kv& pg, void* qkv, int B, int T_cap, const int* cu_rows,
+                                   const int* lens, int* err) {
+  const sp_model_cfg& c = m->cfg;
+  PagedAppendArgs a = {};
+  a.qkv = static_cast<const __nv_bfloat16*>(qkv);
+  a.ld = (c.n_heads + 2 * c.n_kv_heads) * c.head_dim;
+  a.n_pages = pg.n_pages;
+  a.page_shift = __builtin_ctz(pg.page_size);
+  a.table = pg.table;
+  a.max_pages = pg.max_pages;
+  a.lens = lens;
+  a.cu_rows = cu_rows;
+  a.B = B;
+  a.T_cap = T_cap;
+  a.Hq = c.n_heads;
+  a.Hkv = c.n_kv_heads;
+  a.dh = c.head_dim;
+  a.err = err;
+  return a;
+}
+
+// pg (may be NULL): keys and values go to pages instead of io->kv.
+static sp_status prefill_impl(const sp_model* m, const sp_prefill_io* io, void* ws, size_t ws_bytes, cudaStream_t st,
+                              const sp_paged_kv* pg = nullptr) {
   if (!m || !io) return fail(SP_ERR_INVALID_ARG, "sp_prefill: NULL argument");
   const sp_model_cfg& c = m->cfg;
+  if (pg) {
+    if (io->kv) return fail(SP_ERR_INVALID_ARG, "sp_prefill_paged: io.kv must be NULL");
+    const sp_status s = check_pools("sp_prefill_paged", c, pg);
+    if (s != SP_OK) return s;
+  }
   if (io->B < 1 || io->B > SP_MAX_BATCH || io->T_cap < 0 || io->max_seqlen_cap < 0)
     return fail(SP_ERR_SHAPE, "sp_prefill: bad B / T_cap / max_seqlen_cap");
   const bool mrope = c.mrope_section[0] + c.mrope_section[1] + c.mrope_section[2] > 0;
@@ -1166,6 +1212,11 @@ static sp_status prefill_impl(const sp_model* m, const sp_prefill_io* io, void* 
       SP_CUDA(kv_store(p.qkv, io->cu_seqlens, io->pos, io->B, T_cap, c.n_heads, c.n_kv_heads, c.head_dim, kv_l,
                        io->kv_S_cap, io->err, st), "kv cache");
     }
+    if (pg) {  // (the rows are rotated already)
+      PagedAppendArgs pa = append_args(m, *pg, p.qkv, io->B, T_cap, io->cu_seqlens, nullptr, io->err);
+      pa.kv = pool_of(c, *pg, l);
+      SP_CUDA(paged_append_launch(pa, st), "paged cache");
+    }
     SP_CUDA(attention_varlen(p.qkv, p.ob, io->cu_seqlens, io->B, io->max_seqlen_cap, T_cap, c.n_heads, c.n_kv_heads,
                              c.head_dim, true, gs.attn_sched, io->err, st), "attention");
     GemmEpi er;
@@ -1188,6 +1239,12 @@ static sp_status prefill_impl(const sp_model* m, const sp_prefill_io* io, void* 
 
 sp_status sp_prefill(const sp_model* m, const sp_prefill_io* io, void* ws, size_t ws_bytes, sp_stream stream) {
   return prefill_impl(m, io, ws, ws_bytes, (cudaStream_t)stream);
+}
+
+sp_status sp_prefill_paged(const sp_model* m, const sp_prefill_io* io, const sp_paged_kv* pools, void* ws, size_t ws_bytes,
+                           sp_stream stream) {
+  if (!pools) return fail(SP_ERR_INVALID_ARG, "sp_prefill_paged: NULL argument");
+  return prefill_impl(m, io, ws, ws_bytes, (cudaStream_t)stream, pools);
 }
 
 sp_status sp_mrope_positions(int B, const int* n_vis, const int* n_txt, const int* grid_w, const int* idx, int k_cap,
@@ -1236,6 +1293,47 @@ size_t sp_decode_workspace(const sp_model* m, int B) {
   return decode_ws(m, B, cv, nullptr) + 256;
 }
 
+extern "C++" {
+// One generation step through the layers: rows x [B, d] to hidden.  qkv_epi describes the QKV product's epilogue;
+// attend(l) takes p.qkv to p.ob (the attention, with the cache of layer l).
+template <class Attend>
+static sp_status decode_layers(const sp_model* m, int B, const void* x, float* hidden, const PrefillParts& p,
+                               const GemmEpi& qkv_epi, int* err, cudaStream_t st, Attend attend) {
+  const sp_model_cfg& c = m->cfg;
+  const int dq = c.n_heads * c.head_dim, qkvw = (c.n_heads + 2 * c.n_kv_heads) * c.head_dim;
+  std::string msg;
+  CUtensorMap tX, tO, tA, tX16, tO16, tA16;  // box rows 128 / 16 (weight-streaming GEMMs)
+  if (!encode_tmap_bf16(&tX, p.xb, B, c.d, 128, &msg) || !encode_tmap_bf16(&tO, p.ob, B, dq, 128, &msg) ||
+      !encode_tmap_bf16(&tA, p.act, B, c.ffn, 128, &msg) || !encode_tmap_bf16(&tX16, p.xb, B, c.d, 16, &msg) ||
+      !encode_tmap_bf16(&tO16, p.ob, B, dq, 16, &msg) || !encode_tmap_bf16(&tA16, p.act, B, c.ffn, 16, &msg))
+    return fail(SP_ERR_CUDA, "%s", msg.c_str());
+  GemmScratch gs;
+  gs.splitk = p.splitk;
+  gs.splitk_floats = p.splitk_floats;
+  SP_CUDA(bf16_to_f32(x, p.h32, B, nullptr, c.d, st), "embed");
+  for (int l = 0; l < c.n_layers; ++l) {
+    SP_CUDA(rmsnorm_f32_to_bf16(p.h32, m->w.attn_norm[l], p.xb, B, nullptr, c.d, c.rms_eps, st), "attn norm");
+    SP_CUDA(gemm_bf16(tX, B, nullptr, m->qkv[l], qkvw, qkv_epi, err, st, &gs, nullptr, &tX16), "qkv");
+    SP_CUDA(attend(l), "decode attention");
+    GemmEpi er;
+    er.kind = EPI_F32_ACC;
+    er.out = p.h32;
+    er.ldo = c.d;
+    SP_CUDA(gemm_bf16(tO, B, nullptr, m->o[l], c.d, er, err, st, &gs, nullptr, &tO16), "o");
+    SP_CUDA(rmsnorm_f32_to_bf16(p.h32, m->w.mlp_norm[l], p.xb, B, nullptr, c.d, c.rms_eps, st), "mlp norm");
+    GemmEpi eg;
+    eg.kind = EPI_SWIGLU_BF16;
+    eg.out = p.act;
+    eg.ldo = c.ffn;
+    eg.up_off = c.ffn;
+    SP_CUDA(gemm_bf16(tX, B, nullptr, m->gu[l], 2 * c.ffn, eg, err, st, &gs, nullptr, &tX16), "gate/up");
+    SP_CUDA(gemm_bf16(tA, B, nullptr, m->down[l], c.d, er, err, st, &gs, nullptr, &tA16), "down");
+  }
+  SP_CUDA(rmsnorm_f32_to_f32(p.h32, m->w.final_norm, hidden, B, nullptr, c.d, c.rms_eps, st), "final norm");
+  return SP_OK;
+}
+}  // extern "C++"
+
 static sp_status decode_impl(const sp_model* m, const sp_decode_io* io, void* ws, size_t ws_bytes, cudaStream_t st) {
   if (!m || !io) return fail(SP_ERR_INVALID_ARG, "sp_decode: NULL argument");
   const sp_model_cfg& c = m->cfg;
@@ -1253,57 +1351,122 @@ static sp_status decode_impl(const sp_model* m, const sp_decode_io* io, void* ws
   if (!ws || ws_bytes < need) return fail(SP_ERR_WORKSPACE, "sp_decode: workspace %zu < %zu bytes", ws_bytes, need);
   if (!al16(ws)) return fail(SP_ERR_ALIGN, "sp_decode: workspace must be 16-byte aligned");
   const int B = io->B;
-  const int dq = c.n_heads * c.head_dim, qkvw = (c.n_heads + 2 * c.n_kv_heads) * c.head_dim;
   const size_t layer_elems = (size_t)2 * B * io->kv_S_cap * c.n_kv_heads * c.head_dim;
-  std::string msg;
-  CUtensorMap tX, tO, tA, tX16, tO16, tA16;  // box rows 128 / 16 (weight-streaming GEMMs)
-  if (!encode_tmap_bf16(&tX, p.xb, B, c.d, 128, &msg) || !encode_tmap_bf16(&tO, p.ob, B, dq, 128, &msg) ||
-      !encode_tmap_bf16(&tA, p.act, B, c.ffn, 128, &msg) || !encode_tmap_bf16(&tX16, p.xb, B, c.d, 16, &msg) ||
-      !encode_tmap_bf16(&tO16, p.ob, B, dq, 16, &msg) || !encode_tmap_bf16(&tA16, p.act, B, c.ffn, 16, &msg))
-    return fail(SP_ERR_CUDA, "%s", msg.c_str());
-  GemmScratch gs;
-  gs.splitk = p.splitk;
-  gs.splitk_floats = p.splitk_floats;
   SP_CUDA(cudaMemsetAsync(p.dcnt, 0, sizeof(int) * (size_t)c.n_layers * B * c.n_kv_heads, st), "decode counters");
-  SP_CUDA(bf16_to_f32(io->x, p.h32, B, nullptr, c.d, st), "embed");
-  for (int l = 0; l < c.n_layers; ++l) {
+  GemmEpi eq;
+  eq.kind = EPI_BF16_ROPE;
+  eq.out = p.qkv;
+  eq.ldo = (c.n_heads + 2 * c.n_kv_heads) * c.head_dim;
+  eq.rope = m->rope;
+  eq.pos = io->rope_pos ? io->rope_pos : io->lens;  // default: the cached length
+  eq.max_pos = c.max_pos;
+  eq.head_dim = c.head_dim;
+  eq.rope_cols = (c.n_heads + c.n_kv_heads) * c.head_dim;
+  const sp_status s = decode_layers(m, B, io->x, io->hidden, p, eq, io->err, st, [&](int l) {
     void* kv_l = static_cast<uint16_t*>(io->kv) + (size_t)l * layer_elems;
-    SP_CUDA(rmsnorm_f32_to_bf16(p.h32, m->w.attn_norm[l], p.xb, B, nullptr, c.d, c.rms_eps, st), "attn norm");
-    GemmEpi eq;
-    eq.kind = EPI_BF16_ROPE;
-    eq.out = p.qkv;
-    eq.ldo = qkvw;
-    eq.rope = m->rope;
-    eq.pos = io->rope_pos ? io->rope_pos : io->lens;  // default: the cached length
-    eq.max_pos = c.max_pos;
-    eq.head_dim = c.head_dim;
-    eq.rope_cols = (c.n_heads + c.n_kv_heads) * c.head_dim;
-    SP_CUDA(gemm_bf16(tX, B, nullptr, m->qkv[l], qkvw, eq, io->err, st, &gs, nullptr, &tX16), "qkv");
-    SP_CUDA(decode_attention(p.qkv, kv_l, io->kv_S_cap, io->lens, B, c.n_heads, c.n_kv_heads, c.head_dim,
-                             io->max_len_cap, p.dattn, kDecodeSplits, p.dcnt + (size_t)l * B * c.n_kv_heads, p.ob,
-                             io->err, st),
-            "decode attention");
-    GemmEpi er;
-    er.kind = EPI_F32_ACC;
-    er.out = p.h32;
-    er.ldo = c.d;
-    SP_CUDA(gemm_bf16(tO, B, nullptr, m->o[l], c.d, er, io->err, st, &gs, nullptr, &tO16), "o");
-    SP_CUDA(rmsnorm_f32_to_bf16(p.h32, m->w.mlp_norm[l], p.xb, B, nullptr, c.d, c.rms_eps, st), "mlp norm");
-    GemmEpi eg;
-    eg.kind = EPI_SWIGLU_BF16;
-    eg.out = p.act;
-    eg.ldo = c.ffn;
-    eg.up_off = c.ffn;
-    SP_CUDA(gemm_bf16(tX, B, nullptr, m->gu[l], 2 * c.ffn, eg, io->err, st, &gs, nullptr, &tX16), "gate/up");
-    SP_CUDA(gemm_bf16(tA, B, nullptr, m->down[l], c.d, er, io->err, st, &gs, nullptr, &tA16), "down");
-  }
-  SP_CUDA(rmsnorm_f32_to_f32(p.h32, m->w.final_norm, io->hidden, B, nullptr, c.d, c.rms_eps, st), "final norm");
+    return decode_attention(p.qkv, kv_l, io->kv_S_cap, io->lens, B, c.n_heads, c.n_kv_heads, c.head_dim, io->max_len_cap,
+                            p.dattn, kDecodeSplits, p.dcnt + (size_t)l * B * c.n_kv_heads, p.ob, io->err, st);
+  });
+  if (s != SP_OK) return s;
   SP_CUDA(lens_increment(io->lens, io->rope_pos, B, io->kv_S_cap, st), "lens");
   return SP_OK;
 }
 
 sp_status sp_decode(const sp_model* m, const sp_decode_io* io, void* ws, size_t ws_bytes, sp_stream stream) {
   return decode_impl(m, io, ws, ws_bytes, (cudaStream_t)stream);
+}
+
+// ------------------------------------------------------------------ decode over pages
+
+struct PagedDecodeParts {
+  int* lens1;   // [B] positions with the new token
+  void* attn;   // the attention's workspace
+};
+
+static size_t decode_paged_ws(const sp_model* m, int B, int n_groups, Carve& cv, PrefillParts* p, PagedDecodeParts* q) {
+  const sp_model_cfg& c = m->cfg;
+  decode_ws(m, B, cv, p);
+  PagedDecodeParts d;
+  d.lens1 = cv.take<int>(B);
+  d.attn = cv.take<char>(prefix_attention_bytes(B, B, n_groups, c.n_heads, c.n_kv_heads, c.head_dim));
+  if (q) *q = d;
+  return cv.off;
+}
+
+size_t sp_decode_paged_workspace(const sp_model* m, int B, int n_groups) {
+  if (!m || B < 1 || B > SP_MAX_BATCH || n_groups < 0 || n_groups > SP_MAX_BATCH) return 0;
+  Carve cv(nullptr);
+  return decode_paged_ws(m, B, n_groups, cv, nullptr, nullptr) + 256;
+}
+
+static sp_status decode_paged_impl(const sp_model* m, const sp_decode_paged_io* io, void* ws, size_t ws_bytes, cudaStream_t st) {
+  const char* who = "sp_decode_paged";
+  if (!m || !io) return fail(SP_ERR_INVALID_ARG, "%s: NULL argument", who);
+  const sp_model_cfg& c = m->cfg;
+  const sp_paged_kv& pg = io->cache;
+  if (io->B < 1 || io->B > SP_MAX_BATCH) return fail(SP_ERR_SHAPE, "%s: B must be in 1..SP_MAX_BATCH", who);
+  const sp_status s0 = check_pools(who, c, &pg);
+  if (s0 != SP_OK) return s0;
+  if (!io->x || !io->lens || !io->rope_pos || !io->hidden)
+    return fail(SP_ERR_INVALID_ARG, "%s: x, lens, rope_pos, hidden required", who);
+  if (io->n_groups < 0 || io->n_groups > SP_MAX_BATCH || (io->n_groups > 0 && io->prefix_max_pages < 1) ||
+      (long long)io->prefix_max_pages * pg.page_size > (1ll << 30))
+    return fail(SP_ERR_SHAPE, "%s: n_groups must be in 0..SP_MAX_BATCH, prefix_max_pages at least 1 with groups", who);
+  if (io->n_groups > 0 && (!io->group_cu || !io->prefix_table || !io->prefix_lens))
+    return fail(SP_ERR_INVALID_ARG, "%s: groups need group_cu, prefix_table and prefix_lens", who);
+  if (!al16(io->x) || !al16(io->hidden)) return fail(SP_ERR_ALIGN, "%s: x and hidden must be 16-byte aligned", who);
+  const int B = io->B;
+  Carve cv(ws);
+  PrefillParts p;
+  PagedDecodeParts q;
+  const size_t need = decode_paged_ws(m, B, io->n_groups, cv, &p, &q) + 256;
+  if (!ws || ws_bytes < need) return fail(SP_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", who, ws_bytes, need);
+  if (!al16(ws)) return fail(SP_ERR_ALIGN, "%s: workspace must be 16-byte aligned", who);
+  const int qkvw = (c.n_heads + 2 * c.n_kv_heads) * c.head_dim;
+  SP_CUDA(lens_plus_one(io->lens, q.lens1, B, st), "lens");
+  GemmEpi eq;
+  eq.kind = EPI_BF16;
+  eq.out = p.qkv;
+  eq.ldo = qkvw;
+  PagedAppendArgs pa = append_args(m, pg, p.qkv, B, B, nullptr, io->lens, io->err);
+  pa.q_out = static_cast<__nv_bfloat16*>(p.qkv);  // (queries in place)
+  pa.ld_q = qkvw;
+  pa.rope = m->rope;
+  pa.max_pos = c.max_pos;
+  pa.pos = io->rope_pos;
+  PrefixAttention at = {};
+  at.q = p.qkv;
+  at.ld_q = qkvw;
+  at.out = p.ob;
+  at.ld_out = c.n_heads * c.head_dim;
+  at.n_pages = pg.n_pages;
+  at.page_size = pg.page_size;
+  at.table = pg.table;
+  at.max_pages = pg.max_pages;
+  at.lens = q.lens1;
+  at.ptable = io->prefix_table;
+  at.pmax_pages = io->n_groups > 0 ? io->prefix_max_pages : 0;
+  at.plens = io->prefix_lens;
+  at.group_cu = io->group_cu;
+  at.n_groups = io->n_groups;
+  at.B = at.T_cap = B;
+  at.Hq = c.n_heads;
+  at.Hkv = c.n_kv_heads;
+  at.dh = c.head_dim;
+  at.err = io->err;
+  const sp_status s = decode_layers(m, B, io->x, io->hidden, p, eq, io->err, st, [&](int l) {
+    pa.kv = pool_of(c, pg, l);
+    at.kv = pa.kv;
+    const cudaError_t r = paged_append_launch(pa, st);
+    return r != cudaSuccess ? r : prefix_attention(at, q.attn, st);
+  });
+  if (s != SP_OK) return s;
+  SP_CUDA(lens_increment(io->lens, io->rope_pos, B, pg.max_pages * pg.page_size, st), "lens");
+  return SP_OK;
+}
+
+sp_status sp_decode_paged(const sp_model* m, const sp_decode_paged_io* io, void* ws, size_t ws_bytes, sp_stream stream) {
+  return decode_paged_impl(m, io, ws, ws_bytes, (cudaStream_t)stream);
 }
 
 // ------------------------------------------------------------------ pipeline

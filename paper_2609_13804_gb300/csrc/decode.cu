@@ -296,6 +296,11 @@ cudaError_t dispatch_decode_attn(int G, dim3 grid, cudaStream_t st, const __nv_b
 #undef SP_DEC_G
 }
 
+__global__ void lens_plus_one_kernel(const int* lens, int* out, int B) {
+  const int b = blockIdx.x * blockDim.x + threadIdx.x;
+  if (b < B) out[b] = lens[b] + 1;
+}
+
 __global__ void lens_increment_kernel(int* lens, int* rope_pos, int B, int S_cap) {
   const int b = blockIdx.x * blockDim.x + threadIdx.x;
   if (b < B && lens[b] < S_cap) {
@@ -347,6 +352,11 @@ cudaError_t decode_attention(const void* qkv, void* kv_l, int S_cap, const int* 
     return cudaErrorInvalidValue;
   prof_end_launch(st, SP_K_ATTN, 0.0, 0.0);
   if (r != cudaSuccess) return r;
+  return cudaGetLastError();
+}
+
+cudaError_t lens_plus_one(const int* lens, int* out, int B, cudaStream_t st) {
+  lens_plus_one_kernel<<<(B + 127) / 128, 128, 0, st>>>(lens, out, B);
   return cudaGetLastError();
 }
 

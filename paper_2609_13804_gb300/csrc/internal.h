@@ -205,6 +205,7 @@ size_t decode_attention_floats(int B, int Hq, int dh, int max_splits);
 cudaError_t decode_attention(const void* qkv, void* kv_l, int S_cap, const int* lens, int B, int Hq, int Hkv, int dh,
                              int max_len, float* part, int max_splits, int* cnt, void* out, int* err,
                              cudaStream_t st);
+cudaError_t lens_plus_one(const int* lens, int* out, int B, cudaStream_t st);
 cudaError_t lens_increment(int* lens, int* rope_pos, int B, int S_cap, cudaStream_t st);
 
 // ------------------------------------------------------------- attention
@@ -327,6 +328,31 @@ struct PagedAppendArgs {
   int* err;
 };
 cudaError_t paged_append_launch(const PagedAppendArgs& a, cudaStream_t st);
+// Attention over shared prefixes (sp_prefix_attention_io's fields, checked); ws: prefix_attention_bytes() bytes,
+// 256-byte aligned.
+struct PrefixAttention {
+  const void* q;
+  long long ld_q;
+  void* out;
+  long long ld_out;
+  float* lse;
+  const void* kv;
+  int n_pages, page_size;
+  const int* table;
+  int max_pages;
+  const int* lens;
+  const int* ptable;
+  int pmax_pages;
+  const int* plens;
+  const int* group_cu;
+  int n_groups;
+  const int* cu_rows;
+  int B, T_cap, Hq, Hkv, dh;
+  float scale;  // 0: 1 / sqrt(dh)
+  int* err;
+};
+size_t prefix_attention_bytes(int T_cap, int B, int n_groups, int Hq, int Hkv, int dh);
+cudaError_t prefix_attention(const PrefixAttention& x, void* ws, cudaStream_t st);
 size_t beam_select_bytes(int rows, int V, int n_out);
 cudaError_t beam_select_launch(const void* logits, bool f32, long long ld, int B, int W, int V, const float* cum,
                                const unsigned char* done, int eos, int n_out, void* ws, float* score, int* parent,

@@ -3,7 +3,6 @@
 #include <cmath>
 
 #include "internal.h"
-#include "prefix_plan.cuh"
 
 using namespace sp;
 
@@ -98,7 +97,7 @@ size_t sp_prefix_attention_workspace(int T_cap, int B, int n_groups, int n_heads
   if (T_cap < 0 || B < 1 || B > SP_MAX_BATCH || n_groups < 0 || n_groups > SP_MAX_BATCH ||
       check_heads("sp_prefix_attention_workspace", n_heads, n_kv_heads, head_dim) != SP_OK)
     return 0;
-  return prefix_layout(T_cap, B, n_groups, n_heads, n_kv_heads, head_dim).bytes + 256;
+  return prefix_attention_bytes(T_cap, B, n_groups, n_heads, n_kv_heads, head_dim) + 256;
 }
 
 sp_status sp_prefix_attention(const sp_prefix_attention_io* io, void* workspace, size_t workspace_bytes,
@@ -128,19 +127,19 @@ sp_status sp_prefix_attention(const sp_prefix_attention_io* io, void* workspace,
   if (!(io->scale >= 0.f) || !std::isfinite(io->scale))
     return report(SP_ERR_INVALID_ARG, "%s: scale must be finite and not negative", who);
   const size_t need =
-      prefix_layout(io->T_cap, io->B, io->n_groups, io->n_heads, io->n_kv_heads, io->head_dim).bytes + 256;
+      prefix_attention_bytes(io->T_cap, io->B, io->n_groups, io->n_heads, io->n_kv_heads, io->head_dim) + 256;
   if (!workspace || workspace_bytes < need)
     return report(SP_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", who, workspace_bytes, need);
   if (!al(workspace, 16)) return report(SP_ERR_ALIGN, "%s: workspace must be 16-byte aligned", who);
-  PrefixArgs a;
-  a.q = static_cast<const __nv_bfloat16*>(io->q);
+  PrefixAttention a;
+  a.q = io->q;
   a.ld_q = io->ld_q;
-  a.out = static_cast<__nv_bfloat16*>(io->out);
+  a.out = io->out;
   a.ld_out = io->ld_out;
   a.lse = io->lse;
-  a.kv = static_cast<const __nv_bfloat16*>(io->cache.kv);
+  a.kv = io->cache.kv;
   a.n_pages = io->cache.n_pages;
-  a.page_shift = page_shift_of(io->cache.page_size);
+  a.page_size = io->cache.page_size;
   a.table = io->cache.table;
   a.max_pages = io->cache.max_pages;
   a.lens = io->cache.lens;
@@ -154,10 +153,11 @@ sp_status sp_prefix_attention(const sp_prefix_attention_io* io, void* workspace,
   a.T_cap = io->T_cap;
   a.Hq = io->n_heads;
   a.Hkv = io->n_kv_heads;
-  a.scale_log2 = (io->scale > 0.f ? io->scale : 1.f / sqrtf((float)io->head_dim)) * 1.4426950408889634f;
+  a.dh = io->head_dim;
+  a.scale = io->scale;
   a.err = io->err;
   void* base = reinterpret_cast<void*>((reinterpret_cast<uintptr_t>(workspace) + 255) & ~uintptr_t(255));
-  SP_PG_CUDA(prefix_attention_launch(a, io->head_dim, base, (cudaStream_t)stream), who);
+  SP_PG_CUDA(prefix_attention(a, base, (cudaStream_t)stream), who);
   return SP_OK;
 }
 

@@ -8,6 +8,7 @@
 // scores.  P is rounded to bf16 for the second product (relative 2^-9 of each weight, the operand's type),
 // the sum l takes the unrounded weights.  A row without a visible key has l = 0: zeros out, lse -infinity.
 #include <algorithm>
+#include <cmath>
 
 #include "internal.h"
 #include "prefix_plan.cuh"
@@ -369,6 +370,13 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(const PrefixArgs a, c
 
 }  // namespace
 
+// What a call launches, from what the host knows, and its workspace.
+struct PrefixLayout {
+  PlanArgs warp, tc;       // the kernel for few vectors per entry, the one for many (workers 0: not launched)
+  size_t off_warp, off_tc; // their parts of the workspace
+  size_t bytes;
+};
+
 // Vectors per entry from which its products go to prefix_tc_kernel.
 constexpr int kTcVectors = 32;
 
@@ -393,7 +401,7 @@ static size_t plan_carve(PlanArgs* p, char* base, int T_cap, int B, int n_groups
   return off;
 }
 
-PrefixLayout prefix_layout(int T_cap, int B, int n_groups, int Hq, int Hkv, int dh) {
+static PrefixLayout prefix_layout(int T_cap, int B, int n_groups, int Hq, int Hkv, int dh) {
   PrefixLayout L = {};
   const int G = Hq / Hkv, sms = device_sm_count();
   const bool fits = G <= 128;
@@ -422,7 +430,7 @@ PrefixLayout prefix_layout(int T_cap, int B, int n_groups, int Hq, int Hkv, int 
   return L;
 }
 
-cudaError_t prefix_attention_launch(const PrefixArgs& a, int dh, void* ws, cudaStream_t st) {
+static cudaError_t prefix_attention_launch(const PrefixArgs& a, int dh, void* ws, cudaStream_t st) {
   if (a.T_cap == 0) return cudaSuccess;
   PrefixLayout L = prefix_layout(a.T_cap, a.B, a.n_groups, a.Hq, a.Hkv, dh);
   const int sms = device_sm_count(), G = a.Hq / a.Hkv;
@@ -452,6 +460,38 @@ cudaError_t prefix_attention_launch(const PrefixArgs& a, int dh, void* ws, cudaS
                  0, st, a, pp, po);
   prof_end_launch(st, SP_K_ATTN, 0.0, 0.0);
   return r;
+}
+
+size_t prefix_attention_bytes(int T_cap, int B, int n_groups, int Hq, int Hkv, int dh) {
+  return prefix_layout(T_cap, B, n_groups, Hq, Hkv, dh).bytes;
+}
+
+cudaError_t prefix_attention(const PrefixAttention& x, void* ws, cudaStream_t st) {
+  PrefixArgs a;
+  a.q = static_cast<const __nv_bfloat16*>(x.q);
+  a.ld_q = x.ld_q;
+  a.out = static_cast<__nv_bfloat16*>(x.out);
+  a.ld_out = x.ld_out;
+  a.lse = x.lse;
+  a.kv = static_cast<const __nv_bfloat16*>(x.kv);
+  a.n_pages = x.n_pages;
+  a.page_shift = __builtin_ctz(x.page_size);
+  a.table = x.table;
+  a.max_pages = x.max_pages;
+  a.lens = x.lens;
+  a.ptable = x.ptable;
+  a.pmax_pages = x.pmax_pages;
+  a.plens = x.plens;
+  a.group_cu = x.group_cu;
+  a.n_groups = x.n_groups;
+  a.cu_rows = x.cu_rows;
+  a.B = x.B;
+  a.T_cap = x.T_cap;
+  a.Hq = x.Hq;
+  a.Hkv = x.Hkv;
+  a.scale_log2 = (x.scale > 0.f ? x.scale : 1.f / sqrtf((float)x.dh)) * 1.4426950408889634f;
+  a.err = x.err;
+  return prefix_attention_launch(a, x.dh, ws, st);
 }
 
 }  // namespace sp

@@ -246,14 +246,6 @@ struct TileCursor {
   }
 };
 
-// What a call launches, from what the host knows, and its workspace.
-struct PrefixLayout {
-  PlanArgs warp, tc;       // the kernel for few vectors per entry, the one for many (workers 0: not launched)
-  size_t off_warp, off_tc; // their parts of the workspace
-  size_t bytes;
-};
-PrefixLayout prefix_layout(int T_cap, int B, int n_groups, int Hq, int Hkv, int dh);
-cudaError_t prefix_attention_launch(const PrefixArgs& a, int dh, void* ws, cudaStream_t st);
 cudaError_t prefix_tc_launch(const PrefixArgs& a, const PlanArgs& p, int dh, cudaStream_t st);
 
 }  // namespace sp

@@ -107,6 +107,27 @@ def test_reorder_refusals(L, want, change):
     assert L.sp_beam_reorder(C.byref(reorder(**change)), None) == want
 
 
+def test_decode_paged_layout_and_null(L):
+    assert C.sizeof(b.sp_decode_paged_io) == 8 * 4 + 40 + 4 + 4 + 8 * 2 + 4 + 4 + 8 * 3
+    assert L.sp_decode_paged(None, None, None, 0, None) == INVALID
+    assert L.sp_prefill_paged(None, None, None, None, 0, None) == INVALID
+    assert L.sp_decode_paged_workspace(None, 4, 0) == 0
+
+
+def test_packed_arguments_are_the_structs(L):
+    """The binding packs arguments with struct: the bytes are those of the ctypes structures."""
+    io = reorder()
+    packed = b._pack_reorder(2, 3, 2, OK, 9, 16, 64, OK, 512, 3, OK, OK, 3, 0)
+    assert packed == bytes(io)
+    io = attend(scale=0.5, n_groups=3, group_cu=OK, prefix_table=OK, prefix_max_pages=7, prefix_lens=OK)
+    packed = b._pack_attention(2, 2, 0, OK, 256, 512, 256, 0, 4, 2, 64, 0.5, OK, 8, 16, OK, 4, OK, 3, OK, OK, 7, OK, 0)
+    assert packed == bytes(io)
+    io = append(mrope_section=(C.c_int * 3)(1, 2, 3))
+    packed = b._pack_append(2, 2, 0, OK, 512, OK, 256, 4, 2, 64, OK, 9, OK, 0, 1, 2, 3, OK, 8, 16, OK, 4, OK, 0)
+    assert packed == bytes(io)
+    assert b._pack_select(2, 3, 100, OK, True, 100, OK, 0, 0, 3, OK, OK, OK) == bytes(select())
+
+
 def test_null_and_workspace_queries(L):
     assert L.sp_paged_append(None, None) == INVALID
     assert L.sp_prefix_attention(None, None, 0, None) == INVALID
