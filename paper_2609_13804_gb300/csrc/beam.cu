@@ -17,9 +17,10 @@ namespace {
 
 constexpr int BS_NT = 256, BS_WARPS = BS_NT / 32, BS_MAX_OUT = 2 * SP_MAX_BEAMS;
 constexpr int BS_LOADS = 4;                 // 16-byte loads per thread and tile
+constexpr int BS_RING = 3;                  // tiles in flight
 constexpr int BS_BLOCK = 16;                // tiles of a block
 constexpr int BS_CAP = 128;                 // candidates a warp keeps at most
-constexpr int BS_LIST = 256;                // slices x n_out of a row, at most (one warp's join)
+constexpr int BS_LIST = 256;                // slices x n_out of a row, at most (shared memory of the join)
 constexpr float kLog2e = 1.44269504088896341f;
 
 SP_DEVINL float ex2(float x) {
@@ -137,24 +138,24 @@ __device__ __noinline__ int cut_list(unsigned long long* list, int n, int n_out)
 // number of equal ones (keys tell them apart by token), is taken exactly.  At the end the lists' n_out largest,
 // in order, and (m, sum) go to part.
 template <bool F32>
-__global__ void __launch_bounds__(BS_NT, 4)
+__global__ void __launch_bounds__(BS_NT, 3)
 beam_scan_kernel(const void* __restrict__ logits, long long ld, int V, const float* __restrict__ cum,
                  const unsigned char* __restrict__ done, int n_out, int slice, float2* __restrict__ part_ms,
                  unsigned long long* __restrict__ part_key) {
   using K = Chunk<F32>;
   __shared__ unsigned long long list_s[BS_WARPS][BS_CAP];
+  extern __shared__ uint4 ring[];  // [BS_RING][BS_LOADS][BS_NT]: a thread's own loads, read by itself only
   __shared__ float2 ms_s[BS_WARPS];
   __shared__ float tile_max[BS_BLOCK][BS_NT];
   __shared__ uint32_t bound_s[2][BS_WARPS];
   __shared__ int events[BS_WARPS][64];
   __shared__ int n_s[BS_WARPS];
   pdl_wait();
-  pdl_trigger();
   const int row = blockIdx.y, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const float cw = __ldg(cum + row);
   const bool over = done && __ldg(done + row);
   constexpr int esz = F32 ? 4 : 2, PER = BS_LOADS * K::N;  // logits per thread and tile: one to a lane at most
-  static_assert(PER <= 32 && BS_BLOCK % 2 == 0, "");
+  static_assert(PER <= 32, "");
   const char* base = static_cast<const char*>(logits) + row * ld * esz;
   const int v0 = min(blockIdx.x * slice, V), v1 = min(v0 + slice, V);
   // whole 16-byte chunks of the slice; what is before and behind them goes one by one
@@ -179,13 +180,15 @@ beam_scan_kernel(const void* __restrict__ logits, long long ld, int V, const flo
   const uint4* src = reinterpret_cast<const uint4*>(base + (size_t)c0 * esz);
   unsigned long long T = 0;  // keys above T are candidates
   const int tile_chunks = BS_NT * BS_LOADS;
-  auto load = [&](int t, uint4 (&u)[BS_LOADS]) {
+  auto load = [&](int t) {  // (what lies past the slice is not loaded, and read as -infinity)
+    uint4* to = ring + (t % BS_RING) * (BS_LOADS * BS_NT) + tid;
 #pragma unroll
     for (int q = 0; q < BS_LOADS; ++q) {
       const int c = t * tile_chunks + q * BS_NT + tid;
-      u[q] = make_uint4(K::kNone, K::kNone, K::kNone, K::kNone);
-      if (c < chunks) u[q] = __ldg(src + c);
+      if (c < chunks)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to + q * BS_NT)), "l"(src + c) : "memory");
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
   };
   const int tiles = (chunks + tile_chunks - 1) / tile_chunks;
   float bm = -INFINITY;  // the thread's maximum of the block
@@ -229,19 +232,28 @@ beam_scan_kernel(const void* __restrict__ logits, long long ld, int V, const flo
     }
     ms.s += ts;
   };
-  uint4 ua[BS_LOADS], ub[BS_LOADS];  // a tile ahead
-  load(0, ua);
-  if (over || !(cw > -INFINITY)) return;  // (the join reads nothing of such a beam's row)
+#pragma unroll
+  for (int t = 0; t < BS_RING - 1; ++t) load(t);
+  if (over || !(cw > -INFINITY)) {  // (the join reads nothing of such a beam's row)
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    return;
+  }
   for (int tb = 0, block = 0; tb < tiles; tb += BS_BLOCK, ++block) {
-    const int te = min(tb + BS_BLOCK, tiles);  // (BS_BLOCK is even: tile tb + an even number is in ua)
+    const int te = min(tb + BS_BLOCK, tiles);
     bm = -INFINITY;
-    for (int t = tb; t < te; t += 2) {
-      load(t + 1, ub);
-      take(ua, t - tb);
-      if (t + 1 < te) {
-        load(t + 2, ua);
-        take(ub, t + 1 - tb);
+    for (int t = tb; t < te; ++t) {
+      load(t + BS_RING - 1);
+      asm volatile("cp.async.wait_group %0;" ::"n"(BS_RING - 1) : "memory");
+      const uint4* from = ring + (t % BS_RING) * (BS_LOADS * BS_NT) + tid;
+      uint4 u[BS_LOADS];
+#pragma unroll
+      for (int q = 0; q < BS_LOADS; ++q) u[q] = from[q * BS_NT];
+      if (t == tiles - 1) {
+#pragma unroll
+        for (int q = 0; q < BS_LOADS; ++q)
+          if (t * tile_chunks + q * BS_NT + tid >= chunks) u[q] = make_uint4(K::kNone, K::kNone, K::kNone, K::kNone);
       }
+      take(u, t - tb);
     }
     // the block's bound
     uint32_t rest = bm > -INFINITY ? (uint32_t)(cand_key(bm, 0) >> 32) : 0u, hi = 0;
@@ -296,6 +308,7 @@ beam_scan_kernel(const void* __restrict__ logits, long long ld, int V, const flo
       __syncwarp();
     }
   }
+  pdl_trigger();  // (not before: CTAs of the join would sit on the SMs that slices still need)
   const float mw = warp_max(ms.m);
   const float sw = warp_sum(ms.m == mw ? ms.s : ms.m > -INFINITY ? ms.s * ex2((ms.m - mw) * kLog2e) : 0.f);
   if (n > 32) n = cut_list(list, n, n_out);
@@ -331,112 +344,90 @@ SP_DEVINL unsigned long long order_bits(double v) {
   return (u >> 63) ? ~u : (u | 0x8000000000000000ull);
 }
 
-// One CTA per element, a warp per beam: the beam's n_out best of its slices' lists by counting, for each, the
-// larger ones; their scores in 64 bits; then the same over the beams.  Comparisons are of integers (the 64-bit
-// floating-point pipe is slow here).  log(sum) is e log 2 + log f with sum = 2^e f: exact in e, and log f, below
-// 0.7, is good to 2^-24 in fp32, as are the sums that go into it.
+// The largest of the lanes' values.
+SP_DEVINL unsigned long long warp_max64(unsigned long long v) {
+  const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(v >> 32));
+  const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(v >> 32) == hi ? (uint32_t)v : 0u);
+  return ((unsigned long long)hi << 32) | lo;
+}
+
+// One CTA per element, a warp per beam: the n_out best of the beam's lists, which are in order (a lane holds a list's
+// next key, the largest of them is taken n_out times); their scores in 64 bits; then the same over the beams'
+// lists.  Comparisons are of integers (the 64-bit floating-point pipe is slow here).  log(sum) is e log 2 + log f with
+// sum = 2^e f: exact in e, and log f, below 0.7, is good to 2^-24 in fp32, as are the sums that go into it.
 __global__ void __launch_bounds__(32 * SP_MAX_BEAMS)
-beam_join_kernel(int W, int V, int S, const float* __restrict__ cum, const unsigned char* __restrict__ done, int eos,
-                 int n_out, const float2* __restrict__ part_ms, const unsigned long long* __restrict__ part_key,
+beam_join_kernel(int W, int S, const float* __restrict__ cum, const unsigned char* __restrict__ done, int eos, int n_out,
+                 const float2* __restrict__ part_ms, const unsigned long long* __restrict__ part_key,
                  float* __restrict__ score, int* __restrict__ parent, int* __restrict__ token) {
   extern __shared__ unsigned long long rows_s[];  // [W][S n_out] the beams' lists
   __shared__ unsigned long long sc_s[SP_MAX_BEAMS * BS_MAX_OUT];  // order_bits of the score, 0: none
-  __shared__ double val_s[SP_MAX_BEAMS * BS_MAX_OUT];
+  __shared__ float val_s[SP_MAX_BEAMS * BS_MAX_OUT];
   __shared__ int tk_s[SP_MAX_BEAMS * BS_MAX_OUT];
   pdl_wait();
   pdl_trigger();
   const int e = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int row = e * W + warp, n = S * n_out;
-  unsigned long long* sc = sc_s + warp * n_out;
-  if (lane < n_out) sc[lane] = 0;
   // (a beam that was not scanned has nothing there: what is loaded for it is not used)
-  unsigned long long mine[BS_LIST / 32];
-  float2 ms[BS_LIST / 32];
+  unsigned long long* keys = rows_s + (size_t)warp * n;
   const float cw = __ldg(cum + row);
   const bool over = done && __ldg(done + row);
-#pragma unroll
-  for (int q = 0; q < BS_LIST / 32; ++q) {
-    const int i = q * 32 + lane;
-    mine[q] = i < n ? __ldcg(part_key + (size_t)row * n + i) : 0ull;
-    ms[q] = i < S ? __ldcg(part_ms + (size_t)row * S + i) : make_float2(-INFINITY, 0.f);
-  }
+  const float2 ms = lane < S ? __ldcg(part_ms + (size_t)row * S + lane) : make_float2(-INFINITY, 0.f);
+  for (int i = lane; i < n; i += 32) keys[i] = __ldcg(part_key + (size_t)row * n + i);
   __syncwarp();
+  unsigned long long sc = 0;
+  float val = 0.f;
+  int tk = 0;
   if (!(cw > -INFINITY)) {
   } else if (over) {
     if (lane == 0) {
-      sc[0] = order_bits((double)cw);
-      val_s[warp * n_out] = cw;
-      tk_s[warp * n_out] = eos;
+      sc = order_bits((double)cw);
+      val = cw;
+      tk = eos;
     }
   } else {
-    unsigned long long* keys = rows_s + (size_t)warp * n;
-    int rank[BS_LIST / 32];
-    float m = -INFINITY;
-#pragma unroll
-    for (int q = 0; q < BS_LIST / 32; ++q) {
-      rank[q] = 0;
-      m = fmaxf(m, ms[q].x);
-    }
-    m = warp_max(m);
-    float sum = 0.f;
-#pragma unroll
-    for (int q = 0; q < BS_LIST / 32; ++q) {
-      if (ms[q].x == m) sum += ms[q].y;
-      else if (ms[q].x > -INFINITY) sum += ms[q].y * ex2((ms[q].x - m) * kLog2e);
-    }
-    sum = warp_sum(sum);
-#pragma unroll
-    for (int q = 0; q < BS_LIST / 32; ++q)
-      if (q * 32 + lane < n) keys[q * 32 + lane] = mine[q];
-    __syncwarp();
-    if (n <= 32) {
-#pragma unroll 8
-      for (int i = 0; i < n; ++i) rank[0] += keys[i] > mine[0];
-    } else {
-#pragma unroll 2
-      for (int i = 0; i < n; ++i) {
-        const unsigned long long u = keys[i];
-#pragma unroll
-        for (int q = 0; q < BS_LIST / 32; ++q) rank[q] += u > mine[q];
-      }
+    const float m = warp_max(ms.x);
+    const float sum = warp_sum(ms.x == m ? ms.y : ms.x > -INFINITY ? ms.y * ex2((ms.x - m) * kLog2e) : 0.f);
+    unsigned long long next = lane < S ? keys[lane * n_out] : 0ull, mine = 0;
+    int at = 0;
+    for (int r = 0; r < n_out; ++r) {
+      const unsigned long long best = warp_max64(next);
+      if (best == 0) break;
+      if (lane == r) mine = best;
+      if (next == best) next = ++at < n_out ? keys[lane * n_out + at] : 0ull;  // (no two keys are equal)
     }
     int ex = 0;
     const float f = frexpf(sum, &ex) * 2.f;  // sum = f 2^(ex - 1), f in [1, 2)
-    const double lsum = (double)(ex - 1) * 0.69314718055994530942 + (double)logf(f);
-#pragma unroll
-    for (int q = 0; q < BS_LIST / 32; ++q) {
-      if (mine[q] == 0 || rank[q] >= n_out) continue;
-      const float x = key_logit(mine[q]);
+    if (mine != 0) {
+      const double lsum = (double)(ex - 1) * 0.69314718055994530942 + (double)logf(f);
+      const float x = key_logit(mine);
       const double d = x == m ? 0.0 : (double)x - (double)m;  // (m = +infinity: its tokens alone have weight)
       const double v = (double)cw + (d - lsum);
       if (v > -INFINITY) {
-        sc[rank[q]] = order_bits(v);
-        val_s[warp * n_out + rank[q]] = v;
-        tk_s[warp * n_out + rank[q]] = key_token(mine[q]);
+        sc = order_bits(v);
+        val = (float)v;
+        tk = key_token(mine);
       }
     }
   }
+  if (lane < n_out) {
+    sc_s[warp * n_out + lane] = sc;
+    val_s[warp * n_out + lane] = val;
+    tk_s[warp * n_out + lane] = tk;
+  }
   __syncthreads();
-  // over the beams: place in (beam, rank) order breaks ties
-  const int total = W * n_out, t = threadIdx.x;
-  if (t < total) {
-    const unsigned long long s = sc_s[t];
-    int rank = 0, have = 0;
-#pragma unroll 8
-    for (int i = 0; i < total; ++i) {
-      const unsigned long long u = sc_s[i];
-      rank += u > s || (u == s && i < t);
-      have += u != 0;
-    }
-    if (s != 0 && rank < n_out) {
-      score[(size_t)e * n_out + rank] = (float)val_s[t];
-      parent[(size_t)e * n_out + rank] = t / n_out;
-      token[(size_t)e * n_out + rank] = tk_s[t];
-    }
-    if (t < n_out && t >= have) {
-      score[(size_t)e * n_out + t] = -INFINITY;
-      parent[(size_t)e * n_out + t] = -1;
-      token[(size_t)e * n_out + t] = -1;
+  if (warp != 0) return;
+  unsigned long long next = lane < W ? sc_s[lane * n_out] : 0ull;
+  int at = 0;
+  for (int r = 0; r < n_out; ++r) {
+    const unsigned long long best = warp_max64(next);
+    const int from = __ffs(__ballot_sync(0xffffffffu, next == best)) - 1;  // (equal scores: the lower beam)
+    if (lane == from) {
+      const size_t o = (size_t)e * n_out + r;
+      const int i = lane * n_out + at;
+      score[o] = best ? val_s[i] : -INFINITY;
+      parent[o] = best ? lane : -1;
+      token[o] = best ? tk_s[i] : -1;
+      if (best) next = ++at < n_out ? sc_s[lane * n_out + at] : 0ull;
     }
   }
 }
@@ -517,10 +508,11 @@ beam_reorder_kernel(uint4* __restrict__ kv, int planes, int n_pages, int page_sh
 
 }  // namespace
 
-// Slices of a row: about four CTAs per SM, of at least 4,096 logits each, and no more lists than a warp joins.
+// Slices of a row: about four CTAs per SM, of at least 4,096 logits each, and no more lists than lanes to join them
+// (and keys than BS_LIST).
 static int beam_slices(int rows, int V, int n_out) {
-  const int want = (device_sm_count() * 4 + rows / 2) / rows;
-  return std::max(1, std::min(std::min(want, BS_LIST / n_out), (V + 4095) / 4096));
+  const int want = (device_sm_count() * 3 + rows / 2) / rows;
+  return std::max(1, std::min(std::min(want, std::min(32, BS_LIST / n_out)), (V + 4095) / 4096));
 }
 
 size_t beam_select_bytes(int rows, int V, int n_out) {
@@ -536,12 +528,15 @@ cudaError_t beam_select_launch(const void* logits, bool f32, long long ld, int B
   auto* ms = static_cast<float2*>(ws);
   auto* key = reinterpret_cast<unsigned long long*>(static_cast<char*>(ws) + (((size_t)rows * S * 8 + 255) & ~size_t(255)));
   prof_begin_launch(st);
-  cudaError_t r = launch_pdl(f32 ? beam_scan_kernel<true> : beam_scan_kernel<false>, dim3(S, rows), dim3(BS_NT), 0, st,
-                             logits, ld, V, cum, done, n_out, slice, ms, key);
+  auto* scan = f32 ? beam_scan_kernel<true> : beam_scan_kernel<false>;
+  constexpr int ring = BS_RING * BS_LOADS * BS_NT * 16;
+  cudaError_t r = cudaFuncSetAttribute(scan, cudaFuncAttributeMaxDynamicSharedMemorySize, ring);
+  if (r == cudaSuccess)
+    r = launch_pdl(scan, dim3(S, rows), dim3(BS_NT), (size_t)ring, st, logits, ld, V, cum, done, n_out, slice, ms, key);
   prof_end_launch(st, SP_K_MISC, 0.0, (double)rows * V * (f32 ? 4 : 2));
   if (r != cudaSuccess) return r;
   prof_begin_launch(st);
-  r = launch_pdl(beam_join_kernel, dim3(B), dim3(W * 32), (size_t)W * S * n_out * 8, st, W, V, S, cum, done, eos,
+  r = launch_pdl(beam_join_kernel, dim3(B), dim3(W * 32), (size_t)W * S * n_out * 8, st, W, S, cum, done, eos,
                  n_out, (const float2*)ms, (const unsigned long long*)key, score, parent, token);
   prof_end_launch(st, SP_K_MISC, 0.0, 0.0);
   return r;
