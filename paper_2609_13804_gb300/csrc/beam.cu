@@ -144,6 +144,7 @@ beam_scan_kernel(const void* __restrict__ logits, long long ld, int V, const flo
                  unsigned long long* __restrict__ part_key) {
   using K = Chunk<F32>;
   __shared__ unsigned long long list_s[BS_WARPS][BS_CAP];
+  __shared__ unsigned long long list_all[BS_WARPS * 32];
   extern __shared__ uint4 ring[];  // [BS_RING][BS_LOADS][BS_NT]: a thread's own loads, read by itself only
   __shared__ float2 ms_s[BS_WARPS];
   __shared__ float tile_max[BS_BLOCK][BS_NT];
@@ -317,19 +318,25 @@ beam_scan_kernel(const void* __restrict__ logits, long long ld, int V, const flo
     n_s[warp] = n;
   }
   __syncthreads();
-  // every candidate's place: how many are larger
+  // the warps' candidates side by side, then every one's place: how many are larger
   const size_t at = (size_t)row * gridDim.x + blockIdx.x;
-  int total = 0, rank = 0;
-  const unsigned long long k = lane < n ? list[lane] : 0ull;
+  int total = 0, before = 0;
+#pragma unroll
   for (int w = 0; w < BS_WARPS; ++w) {
     const int nw = n_s[w];
+    before += w < warp ? nw : 0;
     total += nw;
-    if (n > 0) {
-#pragma unroll 4
-      for (int i = 0; i < nw; ++i) rank += list_s[w][i] > k;
-    }
   }
-  if (k != 0 && rank < n_out) part_key[at * n_out + rank] = k;
+  unsigned long long* all = &list_all[0];
+  if (lane < n) all[before + lane] = list[lane];
+  __syncthreads();
+  if (tid < total) {
+    const unsigned long long k = all[tid];
+    int rank = 0;
+#pragma unroll 8
+    for (int i = 0; i < total; ++i) rank += all[i] > k;
+    if (rank < n_out) part_key[at * n_out + rank] = k;
+  }
   if (tid < n_out && tid >= total) part_key[at * n_out + tid] = 0ull;
   if (tid == 0) {
     ms = MaxSum{ms_s[0].x, ms_s[0].y};
@@ -351,9 +358,8 @@ SP_DEVINL unsigned long long warp_max64(unsigned long long v) {
   return ((unsigned long long)hi << 32) | lo;
 }
 
-// One CTA per element, a warp per beam: the n_out best of the beam's lists, which are in order (a lane holds a list's
-// next key, the largest of them is taken n_out times); their scores in 64 bits; then the same over the beams'
-// lists.  Comparisons are of integers (the 64-bit floating-point pipe is slow here).  log(sum) is e log 2 + log f with
+// One CTA per element, a warp per beam: the n_out best of the beam's lists, their scores in 64 bits, then the n_out
+// best over the beams.  Comparisons are of integers (the 64-bit floating-point pipe is slow here).  log(sum) is e log 2 + log f with
 // sum = 2^e f: exact in e, and log f, below 0.7, is good to 2^-24 in fp32, as are the sums that go into it.
 __global__ void __launch_bounds__(32 * SP_MAX_BEAMS)
 beam_join_kernel(int W, int S, const float* __restrict__ cum, const unsigned char* __restrict__ done, int eos, int n_out,
@@ -377,6 +383,8 @@ beam_join_kernel(int W, int S, const float* __restrict__ cum, const unsigned cha
   unsigned long long sc = 0;
   float val = 0.f;
   int tk = 0;
+  unsigned long long* best = sc_s + warp * n_out;  // (its scores' place: the keys are read before)
+  if (lane < n_out) best[lane] = 0;
   if (!(cw > -INFINITY)) {
   } else if (over) {
     if (lane == 0) {
@@ -387,13 +395,30 @@ beam_join_kernel(int W, int S, const float* __restrict__ cum, const unsigned cha
   } else {
     const float m = warp_max(ms.x);
     const float sum = warp_sum(ms.x == m ? ms.y : ms.x > -INFINITY ? ms.y * ex2((ms.x - m) * kLog2e) : 0.f);
-    unsigned long long next = lane < S ? keys[lane * n_out] : 0ull, mine = 0;
-    int at = 0;
-    for (int r = 0; r < n_out; ++r) {
-      const unsigned long long best = warp_max64(next);
-      if (best == 0) break;
-      if (lane == r) mine = best;
-      if (next == best) next = ++at < n_out ? keys[lane * n_out + at] : 0ull;  // (no two keys are equal)
+    unsigned long long mine = 0;  // lane r: the r-th best
+    if (n <= 64) {  // by counting the larger ones of each: two keys per lane
+      const unsigned long long k0 = lane < n ? keys[lane] : 0ull, k1 = lane + 32 < n ? keys[lane + 32] : 0ull;
+      int r0 = 0, r1 = 0;
+#pragma unroll 8
+      for (int i = 0; i < n; ++i) {
+        const unsigned long long u = keys[i];
+        r0 += u > k0;
+        r1 += u > k1;
+      }
+      __syncwarp();
+      if (k0 != 0 && r0 < n_out) best[r0] = k0;
+      if (k1 != 0 && r1 < n_out) best[r1] = k1;
+      __syncwarp();
+      if (lane < n_out) mine = best[lane];
+    } else {  // a lane holds a list's next key: the largest, n_out times
+      unsigned long long next = lane < S ? keys[lane * n_out] : 0ull;
+      int at = 0;
+      for (int r = 0; r < n_out; ++r) {
+        const unsigned long long most = warp_max64(next);
+        if (most == 0) break;
+        if (lane == r) mine = most;
+        if (next == most) next = ++at < n_out ? keys[lane * n_out + at] : 0ull;  // (no two keys are equal)
+      }
     }
     int ex = 0;
     const float f = frexpf(sum, &ex) * 2.f;  // sum = f 2^(ex - 1), f in [1, 2)
@@ -415,20 +440,27 @@ beam_join_kernel(int W, int S, const float* __restrict__ cum, const unsigned cha
     tk_s[warp * n_out + lane] = tk;
   }
   __syncthreads();
-  if (warp != 0) return;
-  unsigned long long next = lane < W ? sc_s[lane * n_out] : 0ull;
-  int at = 0;
-  for (int r = 0; r < n_out; ++r) {
-    const unsigned long long best = warp_max64(next);
-    const int from = __ffs(__ballot_sync(0xffffffffu, next == best)) - 1;  // (equal scores: the lower beam)
-    if (lane == from) {
-      const size_t o = (size_t)e * n_out + r;
-      const int i = lane * n_out + at;
-      score[o] = best ? val_s[i] : -INFINITY;
-      parent[o] = best ? lane : -1;
-      token[o] = best ? tk_s[i] : -1;
-      if (best) next = ++at < n_out ? sc_s[lane * n_out + at] : 0ull;
-    }
+  // over the beams: how many are better; (beam, rank) breaks ties
+  const int total = W * n_out, t = threadIdx.x;
+  if (t >= total) return;
+  const unsigned long long s = sc_s[t];
+  int rank = 0, have = 0;
+#pragma unroll 8
+  for (int i = 0; i < total; ++i) {
+    const unsigned long long u = sc_s[i];
+    rank += u > s || (u == s && i < t);
+    have += u != 0;
+  }
+  const size_t o = (size_t)e * n_out;
+  if (s != 0 && rank < n_out) {
+    score[o + rank] = val_s[t];
+    parent[o + rank] = t / n_out;
+    token[o + rank] = tk_s[t];
+  }
+  if (t < n_out && t >= have) {
+    score[o + t] = -INFINITY;
+    parent[o + t] = -1;
+    token[o + t] = -1;
   }
 }
 
@@ -508,10 +540,11 @@ beam_reorder_kernel(uint4* __restrict__ kv, int planes, int n_pages, int page_sh
 
 }  // namespace
 
-// Slices of a row: about four CTAs per SM, of at least 4,096 logits each, and no more lists than lanes to join them
+// Slices of a row: about two CTAs per SM (what a CTA does besides reading, some 3 us, is not hidden by more: four
+// took 25.4 us instead of 23.1 for 256 rows of 152,064 bf16 logits), of at least 4,096 logits each, and no more lists than lanes to join them
 // (and keys than BS_LIST).
 static int beam_slices(int rows, int V, int n_out) {
-  const int want = (device_sm_count() * 3 + rows / 2) / rows;
+  const int want = (device_sm_count() * 2 + rows / 2) / rows;
   return std::max(1, std::min(std::min(want, std::min(32, BS_LIST / n_out)), (V + 4095) / 4096));
 }
 
