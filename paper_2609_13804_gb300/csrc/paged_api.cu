@@ -51,6 +51,7 @@ sp_status sp_paged_append(const sp_paged_append_io* io, sp_stream stream) {
   const int qkvw = (io->n_heads + 2 * io->n_kv_heads) * io->head_dim;
   if (io->B < 1 || io->B > SP_MAX_BATCH || io->T_cap < 0 || (!io->cu_rows && io->T_cap != io->B))
     return report(SP_ERR_SHAPE, "%s: B must be in 1..SP_MAX_BATCH and T_cap >= 0 (= B without cu_rows)", who);
+  if (io->T_cap == 0) return SP_OK;  // nothing to do
   if (!io->qkv) return report(SP_ERR_INVALID_ARG, "%s: qkv required", who);
   if (io->ld < qkvw || io->ld % 8 != 0 || (io->q_out && (io->ld_q < io->n_heads * io->head_dim || io->ld_q % 8 != 0)))
     return report(SP_ERR_SHAPE, "%s: row strides must be multiples of 8 and hold a row", who);
@@ -116,6 +117,7 @@ sp_status sp_prefix_attention(const sp_prefix_attention_io* io, void* workspace,
     return report(SP_ERR_SHAPE, "%s: n_groups must be in 0..SP_MAX_BATCH, prefix_max_pages at least 1 with groups", who);
   if ((long long)io->T_cap * io->n_heads > (1ll << 28))
     return report(SP_ERR_SHAPE, "%s: T_cap * n_heads must be at most 2^28", who);
+  if (io->T_cap == 0) return SP_OK;  // nothing to do
   if (!io->q || !io->out || !io->cache.lens)
     return report(SP_ERR_INVALID_ARG, "%s: q, out and cache.lens required", who);
   if (io->n_groups > 0 && (!io->group_cu || !io->prefix_table || !io->prefix_lens))

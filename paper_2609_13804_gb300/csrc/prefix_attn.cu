@@ -274,17 +274,18 @@ __global__ void __launch_bounds__(WK_NT, 1) prefix_warp_kernel(const PrefixArgs 
 }
 
 // --------------------------------------------------------------- joining the segments
-// One warp per row and query head: the segments of the row's prefix item and of its own item, in key order, up to 32
-// of them at a time.  Bound by latency, so the chain of dependent accesses is short: where the row's items lie (both
-// at once), every segment's (max, sum), a lane each, then the values with the weights known.
-template <int DH>
+// One warp per row and VC query heads of a kv head: the segments of their prefix item and of their own item, in key
+// order, up to 32 of them at a time.  Bound by latency, so the chain of dependent accesses is short: where the
+// row's items lie (both at once), every segment's (max, sum), a lane each, then the values with the weights known.
+template <int DH, int VC>
 __global__ void __launch_bounds__(256) prefix_merge_kernel(const PrefixArgs a, const PlanArgs pp, const PlanArgs po) {
   pdl_wait();
   pdl_trigger();
   const int lane = threadIdx.x & 31;
   const int E = a.n_groups + a.B, G = a.Hq / a.Hkv;
-  const int row = blockIdx.x, h = blockIdx.y * 8 + (threadIdx.x >> 5);
-  if (h >= a.Hq) return;
+  const int per = (G + VC - 1) / VC;  // warps per kv head
+  const int row = blockIdx.x, task = blockIdx.y * 8 + (threadIdx.x >> 5);
+  if (task >= a.Hkv * per) return;
   int4 place[2];
   int total[2];
   place[0] = pp.prefix ? __ldcg(pp.rows_prefix + row) : make_int4(0, 0, 0, 0);
@@ -292,9 +293,9 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(const PrefixArgs a, c
   total[0] = pp.prefix ? __ldcg(pp.unit0 + E) : 0;
   total[1] = po.own ? __ldcg(po.unit0 + E) : 0;
   if (row < row_begin(a, 0) || row >= row_begin(a, a.B)) return;
-  const int kvh = h / G, g = h - kvh * G;
+  const int kvh = task / per, g0 = (task - kvh * per) * VC, nv = min(VC, G - g0);
   int n[2];           // segments of the prefix item, of the own item
-  size_t first[2];    // slot row of the first one's vector
+  size_t first[2];    // slot row of the first one's first vector
 #pragma unroll
   for (int side = 0; side < 2; ++side) {
     const PlanArgs& p = side == 0 ? pp : po;
@@ -302,7 +303,7 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(const PrefixArgs a, c
     n[side] = 0;
     first[side] = 0;
     if (len == 0) continue;
-    const int mv = place[side].w + g;
+    const int mv = place[side].w + g0;
     const int rt = mv / p.tile_rows, mr = mv - rt * p.tile_rows;
     const int in = rt * a.Hkv + kvh;
     // the workers that have key tiles of the item, units u0 .. u1: a lane tries each of 32 candidates, from a little
@@ -323,49 +324,90 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(const PrefixArgs a, c
     first[side] = ((size_t)(place[side].z + in) + w0) * p.slot_rows + mr;
   }
   constexpr int V = DH / 32;
-  float acc[V], mm = -INFINITY, ll = 0.f;
+  float acc[VC][V], mm[VC], ll[VC];
 #pragma unroll
-  for (int v = 0; v < V; ++v) acc[v] = 0.f;
+  for (int x = 0; x < VC; ++x) {
+    mm[x] = -INFINITY;
+    ll[x] = 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) acc[x][v] = 0.f;
+  }
   for (int s0 = 0; s0 < n[0] + n[1]; s0 += 32) {
     const int s = s0 + lane, there = min(32, n[0] + n[1] - s0);
-    float2 ml = make_float2(-INFINITY, 0.f);
-    const float* o = nullptr;
+    const float* o = nullptr;  // the lane's segment: values and (max, sum) of the first vector
+    const float2* ml_at = nullptr;
     if (s < n[0]) {
       const size_t at = first[0] + (size_t)s * pp.slot_rows;
-      ml = __ldcg(pp.part_ml + at);
+      ml_at = pp.part_ml + at;
       o = pp.part_o + at * DH;
     } else if (s < n[0] + n[1]) {
       const size_t at = first[1] + (size_t)(s - n[0]) * po.slot_rows;
-      ml = __ldcg(po.part_ml + at);
+      ml_at = po.part_ml + at;
       o = po.part_o + at * DH;
     }
-    const float mn = fmaxf(mm, warp_max(ml.x));
-    if (mn == -INFINITY) continue;
-    const float ca = ex2(mm - mn), cb = ex2(ml.x - mn);
-    ll = ll * ca + warp_sum(ml.y * cb);
+    float2 ml[VC];
+    float cb[VC];
 #pragma unroll
-    for (int v = 0; v < V; ++v) acc[v] *= ca;
-    mm = mn;
-#pragma unroll 4
+    for (int x = 0; x < VC; ++x) {
+      ml[x] = make_float2(-INFINITY, 0.f);
+      if (ml_at && x < nv) ml[x] = __ldcg(ml_at + x);
+    }
+#pragma unroll
+    for (int x = 0; x < VC; ++x) {
+      const float mn = fmaxf(mm[x], warp_max(ml[x].x));
+      const float mz = mn == -INFINITY ? 0.f : mn;
+      const float ca = ex2(mm[x] - mz);  // (0 while mm is -infinity)
+      cb[x] = ex2(ml[x].x - mz);
+      ll[x] = ll[x] * ca + warp_sum(ml[x].y * cb[x]);
+#pragma unroll
+      for (int v = 0; v < V; ++v) acc[x][v] *= ca;
+      mm[x] = mn;
+    }
+#pragma unroll(VC == 1 ? 4 : 2)
     for (int i = 0; i < there; ++i) {
-      const float c = __shfl_sync(0xffffffffu, cb, i);
-      const float* x = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(o), i)) + lane * V;
-      float y[V];
-      if (V == 4) *reinterpret_cast<float4*>(y) = __ldcg(reinterpret_cast<const float4*>(x));
-      else *reinterpret_cast<float2*>(y) = __ldcg(reinterpret_cast<const float2*>(x));
+      const float* src = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(o), i)) + lane * V;
+      float y[VC][V];
 #pragma unroll
-      for (int v = 0; v < V; ++v) acc[v] += y[v] * c;
+      for (int x = 0; x < VC; ++x) {
+        if (x >= nv) continue;
+        if (V == 4) *reinterpret_cast<float4*>(y[x]) = __ldcg(reinterpret_cast<const float4*>(src + x * DH));
+        else *reinterpret_cast<float2*>(y[x]) = __ldcg(reinterpret_cast<const float2*>(src + x * DH));
+      }
+#pragma unroll
+      for (int x = 0; x < VC; ++x) {
+        const float c = __shfl_sync(0xffffffffu, cb[x], i);
+        if (x >= nv) continue;
+        if (c != 0.f) {  // (a segment that saw no key of this vector may hold anything)
+#pragma unroll
+          for (int v = 0; v < V; ++v) acc[x][v] += y[x][v] * c;
+        }
+      }
     }
   }
-  const float inv = ll > 0.f ? 1.f / ll : 0.f;
-  __nv_bfloat16* d = a.out + row * a.ld_out + (long long)h * DH + lane * V;
-  if (V == 4)
-    *reinterpret_cast<uint2*>(d) = make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv),
-                                              pack_bf16x2(acc[V - 2] * inv, acc[V - 1] * inv));
-  else
-    *reinterpret_cast<uint32_t*>(d) = pack_bf16x2(acc[0] * inv, acc[1] * inv);
-  if (a.lse && lane == 0)
-    a.lse[(size_t)row * a.Hq + h] = ll > 0.f ? (mm + log2f(ll)) * 0.69314718055994531f : -INFINITY;
+#pragma unroll
+  for (int x = 0; x < VC; ++x) {
+    if (x >= nv) continue;
+    const int h = kvh * G + g0 + x;
+    const float inv = ll[x] == 0.f ? 0.f : 1.f / ll[x];  // (NaN stays NaN)
+    __nv_bfloat16* d = a.out + row * a.ld_out + (long long)h * DH + lane * V;
+    if (V == 4)
+      *reinterpret_cast<uint2*>(d) = make_uint2(pack_bf16x2(acc[x][0] * inv, acc[x][1] * inv),
+                                                pack_bf16x2(acc[x][V - 2] * inv, acc[x][V - 1] * inv));
+    else
+      *reinterpret_cast<uint32_t*>(d) = pack_bf16x2(acc[x][0] * inv, acc[x][1] * inv);
+    if (a.lse && lane == 0)
+      a.lse[(size_t)row * a.Hq + h] = ll[x] == 0.f ? -INFINITY : (mm[x] + log2f(ll[x])) * 0.69314718055994531f;
+  }
+}
+
+template <int DH>
+cudaError_t launch_merge(const PrefixArgs& a, const PlanArgs& pp, const PlanArgs& po, cudaStream_t st) {
+  // four heads per warp where there are warps enough all the same (24 per SM): fewer chains; above 16 heads per kv
+  // head a row's vectors may lie in two row tiles, so one
+  const int G = a.Hq / a.Hkv, four = (G + 3) / 4;
+  const bool many = G > 1 && G <= 16 && (long long)a.T_cap * a.Hkv * four >= 24ll * device_sm_count();
+  const dim3 grid(a.T_cap, (a.Hkv * (many ? four : G) + 7) / 8);
+  return launch_pdl(many ? prefix_merge_kernel<DH, 4> : prefix_merge_kernel<DH, 1>, grid, dim3(256), 0, st, a, pp, po);
 }
 
 }  // namespace
@@ -456,8 +498,7 @@ static cudaError_t prefix_attention_launch(const PrefixArgs& a, int dh, void* ws
   }
   const PlanArgs &pp = L.tc.prefix ? L.tc : L.warp, &po = L.tc.own ? L.tc : L.warp;
   prof_begin_launch(st);
-  r = launch_pdl(dh == 128 ? prefix_merge_kernel<128> : prefix_merge_kernel<64>, dim3(a.T_cap, (a.Hq + 7) / 8), dim3(256),
-                 0, st, a, pp, po);
+  r = dh == 128 ? launch_merge<128>(a, pp, po, st) : launch_merge<64>(a, pp, po, st);
   prof_end_launch(st, SP_K_ATTN, 0.0, 0.0);
   return r;
 }

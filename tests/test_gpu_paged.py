@@ -295,6 +295,91 @@ def test_attention_reports_a_page_outside_the_pool(sp):
     assert int(r["err"].item()) == 2
 
 
+@pytest.mark.parametrize("G,n", [(2, 3), (4, 64)])  # few query vectors per prefix, many
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("page", [16, 64, 256])
+def test_attention_counts_a_bad_page_as_zeros(sp, G, n, dh, page):
+    """Pages outside the pool inside a prefix and at its end: their keys and values are zeros, the error word says so."""
+    g = gen(page + n)
+    pages = -(-300 // page)
+    kv = normal(g, 2, pages + 3, page, 2 * dh)
+    q = normal(g, n, 2 * G * dh)
+    ids = torch.randperm(pages, device=DEV, generator=g).to(torch.int32)
+    good = torch.full((1, pages), pages, dtype=torch.int32, device=DEV)  # page `pages` of the pool: zeros
+    kv[:, pages] = 0
+    bad = good.clone()
+    keep = [i for i in range(pages) if i not in (1, pages - 1)]
+    for t in (good, bad):
+        t[0, keep] = ids[keep]
+    bad[0, 1 % pages], bad[0, pages - 1] = -1, pages + 3
+    args = dict(q=q, kv=kv, lens=ints([0] * n), table=torch.full((n, 1), -1, dtype=torch.int32, device=DEV), n_heads=2 * G,
+                n_kv_heads=2, head_dim=dh, prefix_lens=ints([300]), group_cu=ints([0, n]))
+    a = sp.sp_prefix_attention(prefix_table=good, **args)
+    b = sp.sp_prefix_attention(prefix_table=bad, **args)
+    assert int(a["err"].item()) == 0 and int(b["err"].item()) == 2
+    assert torch.equal(a["out"], b["out"])
+
+
+@pytest.mark.parametrize("n", [3, 64])
+def test_attention_nan_stays_in_its_row(sp, n):
+    g = gen(n)
+    kv = normal(g, 2, 30, 16, 128)
+    q = normal(g, n, 4 * 128)
+    args = dict(kv=kv, lens=ints([5] * n), table=ints([[20]] * n), n_heads=4, n_kv_heads=1, head_dim=128,
+                prefix_table=torch.arange(20, device=DEV, dtype=torch.int32)[None], prefix_lens=ints([311]), group_cu=ints([0, n]))
+    ref = sp.sp_prefix_attention(q=q, **args)["out"].clone()
+    q[1, 128:256] = torch.nan  # one head of one row
+    got = sp.sp_prefix_attention(q=q, lse=(lse := torch.zeros((n, 4), device=DEV)), **args)["out"]
+    assert torch.isnan(got[1, 128:256]).all() and torch.isnan(lse[1, 1])
+    got[1, 128:256] = ref[1, 128:256]
+    assert torch.equal(got, ref) and int(torch.isnan(lse).sum()) == 1
+    kv[1, 3, 5, 7] = torch.nan  # a value that all rows see
+    got = sp.sp_prefix_attention(q=ref.new_zeros(n, 512), **args)["out"].view(n, 4, 128)
+    assert torch.isnan(got[..., 7]).all() and torch.isfinite(got[..., :7]).all() and torch.isfinite(got[..., 8:]).all()
+
+
+def test_attention_130_query_heads_of_one(sp):
+    attention_case(sp, 15, (130, 1, 64), 16, [1, 2, 1], [9, 30, 1], [2, 1], [33, 64])
+    attention_case(sp, 16, (48, 2, 128), 16, [1, 7], [9, 30], [2], [133])
+
+
+def test_offsets_beyond_32_bits(sp):
+    """A pool of more than 2^32 elements, pages at both ends of it: append, attention by both kernels, reordering."""
+    g = gen(17)
+    Hq, Hkv, dh, page = 32, 8, 128, 16
+    pages = 140_000  # 2 x 140,000 x 16 x 1,024 elements
+    kv = torch.empty((1, 2, pages, page, Hkv * dh), dtype=torch.bfloat16, device=DEV)
+    table = ints([[0, pages - 1], [pages - 2, 1], [pages - 3, pages - 4]])
+    kv[:, :, [0, 1, 2, pages - 1, pages - 2, pages - 3, pages - 4]] = normal(g, 1, 2, 7, page, Hkv * dh)
+    qkv = normal(g, 3, (Hq + 2 * Hkv) * dh)
+    sp.sp_paged_append(qkv=qkv, kv=kv[0], table=table, lens=ints([17, 15, 31]), n_heads=Hq, n_kv_heads=Hkv, head_dim=dh)
+    for b, (p, r) in enumerate(((pages - 1, 1), (pages - 2, 15), (pages - 4, 15))):
+        assert torch.equal(kv[0, :, p, r].reshape(-1), qkv[b, Hq * dh:])
+    for n in (3, 40):
+        q = normal(g, n, Hq * dh)
+        r = sp.sp_prefix_attention(q=q, kv=kv[0], table=table[:1].expand(n, 2).contiguous(), lens=ints([18] * n), n_heads=Hq, n_kv_heads=Hkv,
+                                   head_dim=dh, prefix_table=table[1:], prefix_lens=ints([20, 32]), group_cu=ints([0, n - 1, n]))
+        few = torch.cat((kv[0, :, [0, 1]], kv[0, :, pages - 4:]), dim=1)  # the same pages in a small pool
+        at = lambda t: torch.where(t > 1, t - (pages - 4) + 2, t).to(torch.int32)  # noqa: E731
+        s = sp.sp_prefix_attention(q=q, kv=few, table=at(table[:1]).expand(n, 2).contiguous(), lens=ints([18] * n), n_heads=Hq, n_kv_heads=Hkv,
+                                   head_dim=dh, prefix_table=at(table[1:]), prefix_lens=ints([20, 32]), group_cu=ints([0, n - 1, n]))
+        assert int(r["err"].item()) == 0 and torch.equal(r["out"], s["out"])
+    own = ints([[0, pages - 1], [pages - 2, pages - 3]])
+    t = own.clone()
+    src = kv[0, :, pages - 1, :5].clone()
+    err = sp.sp_beam_reorder(kv=kv, table=t, own_table=own, lens=ints([21, 21]), parent=ints([[0, 0]]))
+    assert int(err.item()) == 0 and torch.equal(kv[0, :, pages - 3, :5], src)
+    assert t.tolist() == [[0, pages - 1], [0, pages - 3]]
+
+
+def test_calls_without_rows(sp):
+    kv = sp.paged_pool(2, 16, 1, 64)[0]
+    args = dict(kv=kv, table=ints([[0]]), lens=ints([3]), cu_rows=ints([0, 0]), n_heads=1, n_kv_heads=1, head_dim=64)
+    q = torch.empty((0, 64), dtype=torch.bfloat16, device=DEV)
+    assert sp.sp_prefix_attention(q=q, **args)["out"].shape == (0, 64)
+    assert sp.sp_paged_append(qkv=torch.empty((0, 192), dtype=torch.bfloat16, device=DEV), **args)["q"].shape == (0, 64)
+
+
 # ----------------------------------------------------------------------------- beam selection
 
 def plain_select(logits, cum, n_out, done, eos):

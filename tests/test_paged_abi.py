@@ -128,6 +128,11 @@ def test_packed_arguments_are_the_structs(L):
     assert b._pack_select(2, 3, 100, OK, True, 100, OK, 0, 0, 3, OK, OK, OK) == bytes(select())
 
 
+def test_no_rows_is_nothing_to_do(L):
+    assert L.sp_paged_append(C.byref(append(T_cap=0, cu_rows=OK, qkv=None, q_out=None)), None) == 0
+    assert L.sp_prefix_attention(C.byref(attend(T_cap=0, cu_rows=OK, q=None, out=None)), None, 0, None) == 0
+
+
 def test_null_and_workspace_queries(L):
     assert L.sp_paged_append(None, None) == INVALID
     assert L.sp_prefix_attention(None, None, 0, None) == INVALID
