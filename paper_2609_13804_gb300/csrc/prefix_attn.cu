@@ -459,7 +459,7 @@ static PrefixLayout prefix_layout(int T_cap, int B, int n_groups, int Hq, int Hk
   L.warp.slot_rows = (int)std::min<size_t>(L.warp.tile_rows, (size_t)T_cap * G);
   L.tc.tile_rows = fits ? 128 / G * G : 128;
   L.tc.key_shift = 7;
-  L.tc.over = 2;
+  L.tc.over = 4;     // (a segment of one tile takes as long as four more tiles in a row)
   L.tc.min_shift = 2;
   L.tc.prefix = tc_prefix;
   L.tc.own = tc_own;

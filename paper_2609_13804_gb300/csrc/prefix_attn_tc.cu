@@ -77,6 +77,24 @@ SP_DEVINL float max3(float a, float b, float c) {
   return r;
 }
 
+// Two fp32 numbers as one operand of the packed arithmetic: half the instructions of the exponents and sums.
+SP_DEVINL unsigned long long pack2(float lo, float hi) {
+  unsigned long long r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+SP_DEVINL void unpack2(unsigned long long v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+SP_DEVINL unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+SP_DEVINL unsigned long long add2(unsigned long long a, unsigned long long b) {
+  unsigned long long r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
 // Orders later uses of registers written by tcgen05.ld behind the tcgen05.wait::ld before this call.
 template <int N>
 SP_DEVINL void loaded(float (&r)[N]) {
@@ -331,7 +349,9 @@ prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     while (ok && more) {
       const int M = plan.rows[sg.c.e] * G, keys = plan.keys[sg.c.e], m0 = sg.c.rt * p.tile_rows;
       const int rows = min(p.tile_rows, M - m0);  // vectors of the tile
-      int row_lim = 0;                            // keys [0, row_lim) are visible
+      // keys [0, row_lim) are visible; a lane without a vector masks nothing (its results go nowhere, and the one
+      // masked lane would cost its warp the masking of every tile)
+      int row_lim = 0x7fffffff;
       if (r < rows)
         row_lim = sg.c.e < a.n_groups ? keys : min(max(keys - plan.rows[sg.c.e] + (m0 + r) / G + 1, 0), keys);
       float mlast = -INFINITY;             // m of this stream's latest tile
@@ -386,23 +406,26 @@ prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
           ms = m;
         }
         const float nm = m == -INFINITY ? 0.f : -m;
-        float rs[8];
+        const unsigned long long sc2 = pack2(a.scale_log2, a.scale_log2), nm2 = pack2(nm, nm);
+        unsigned long long rs[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) rs[e] = 0.f;
+        for (int e = 0; e < 4; ++e) rs[e] = 0ull;
 #pragma unroll
         for (int c = 0; c < TC_KV / 32; ++c) {
           float pk[16];  // bf16 pairs
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const float p0 = ex2(fmaf(v[c * 32 + 2 * e], a.scale_log2, nm));
-            const float p1 = ex2(fmaf(v[c * 32 + 2 * e + 1], a.scale_log2, nm));
-            rs[(2 * e) & 7] += p0;
-            rs[(2 * e + 1) & 7] += p1;
+            float x0, x1;
+            unpack2(fma2(pack2(v[c * 32 + 2 * e], v[c * 32 + 2 * e + 1]), sc2, nm2), x0, x1);
+            const float p0 = ex2(x0), p1 = ex2(x1);
+            rs[e & 3] = add2(rs[e & 3], pack2(p0, p1));
             pk[e] = __uint_as_float(pack_bf16x2(p0, p1));
           }
           tmem_st_cols<16>(trow + sb * TC_KV + c * 16, pk);
         }
-        ls += ((rs[0] + rs[1]) + (rs[2] + rs[3])) + ((rs[4] + rs[5]) + (rs[6] + rs[7]));
+        float sum0, sum1;
+        unpack2(add2(add2(rs[0], rs[1]), add2(rs[2], rs[3])), sum0, sum1);
+        ls += sum0 + sum1;
         if (__any_sync(0xffffffffu, moved)) {
           // the product of the tile before is done with O before it is rescaled
           const uint32_t pb = gg - 1;
