@@ -563,7 +563,8 @@ cudaError_t beam_select_launch(const void* logits, bool f32, long long ld, int B
   prof_begin_launch(st);
   auto* scan = f32 ? beam_scan_kernel<true> : beam_scan_kernel<false>;
   constexpr int ring = BS_RING * BS_LOADS * BS_NT * 16;
-  cudaError_t r = cudaFuncSetAttribute(scan, cudaFuncAttributeMaxDynamicSharedMemorySize, ring);
+  static std::atomic<unsigned long long> allowed[2];
+  cudaError_t r = allow_smem(scan, ring, allowed[f32]);
   if (r == cudaSuccess)
     r = launch_pdl(scan, dim3(S, rows), dim3(BS_NT), (size_t)ring, st, logits, ld, V, cum, done, n_out, slice, ms, key);
   prof_end_launch(st, SP_K_MISC, 0.0, (double)rows * V * (f32 ? 4 : 2));

@@ -489,7 +489,8 @@ static cudaError_t prefix_attention_launch(const PrefixArgs& a, int dh, void* ws
     plan_carve(&L.warp, base + L.off_warp, a.T_cap, a.B, a.n_groups, G, a.Hkv, dh);
     const size_t smem = dh == 128 ? WkCfg<128>::SMEM : WkCfg<64>::SMEM;
     auto* kern = dh == 128 ? prefix_warp_kernel<128> : prefix_warp_kernel<64>;
-    r = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    static std::atomic<unsigned long long> allowed[2];
+    r = allow_smem(kern, smem, allowed[dh == 128]);
     if (r != cudaSuccess) return r;
     prof_begin_launch(st);
     r = launch_pdl(kern, dim3(sms), dim3(WK_NT), smem, st, a, L.warp, L.tc.workers ? 1 : 0);

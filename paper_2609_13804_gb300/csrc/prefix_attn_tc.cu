@@ -519,8 +519,8 @@ cudaError_t launch_tc(const PrefixArgs& a, const PlanArgs& p, cudaStream_t st) {
       !encode_tmap_2d(&tk, a.kv, false, rows, W, 64, brows, nullptr) ||
       !encode_tmap_2d(&tv, a.kv + rows * W, false, rows, W, 64, brows, nullptr))
     return cudaErrorInvalidValue;
-  const cudaError_t r =
-      cudaFuncSetAttribute(prefix_tc_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM);
+  static std::atomic<unsigned long long> allowed;
+  const cudaError_t r = allow_smem(prefix_tc_kernel<DH>, C::SMEM, allowed);
   if (r != cudaSuccess) return r;
   return launch_pdl(prefix_tc_kernel<DH>, dim3(p.workers), dim3(TC_NT), C::SMEM, st, tq, tk, tv, a, p);
 }
