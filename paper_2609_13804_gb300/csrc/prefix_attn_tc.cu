@@ -53,6 +53,7 @@ struct TcCfg {
   // more than half of the shared memory: a second CTA would only wait for the tensor memory
   static constexpr size_t SMEM = SMEM_USED > 116 * 1024 ? SMEM_USED : 116 * 1024;
   static constexpr uint32_t T_O = 384;
+  static_assert(SMEM + sizeof(PlanShared) <= 227 * 1024, "a CTA's shared memory");
 };
 
 // X + s for S / P buffer s (tile % 3).  K_FULL counts the copies of K (with their bytes) and the end of O += P V three tiles

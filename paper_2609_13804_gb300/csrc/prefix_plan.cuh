@@ -49,7 +49,8 @@ struct PlanArgs {
   int min_shift;           // log2 of the units a worker takes at least (while there are enough)
   int workers;
   int max_items;           // items there is room for: no more exist while row and group offsets ascend (else, and
-                           // beyond 2^31 - 1 units, the launch covers nothing and reports SP_DEVERR_INDEX)
+                           // where an entry has over 2^31 / entries units, the launch covers nothing and reports
+                           // SP_DEVERR_INDEX)
   bool prefix, own;        // which entries this launch covers
   int* unit0;              // [n_groups + B + 1] first unit of each entry, then N      (written for the merge)
   int* item0;              // [n_groups + B + 1] first item of each entry, then the item count
@@ -69,8 +70,7 @@ struct PlanShared {
   int unit0[kPlanEntries + 1];
   int item0[kPlanEntries + 1];
   int row0[kPlanEntries], rows[kPlanEntries], keys[kPlanEntries];
-  long long wsum_t[32];
-  int wsum_i[32];  // (a CTA has 32 warps at most)
+  int2 wsum[32];  // a warp's items and units (a CTA has 32 warps at most)
 };
 
 SP_DEVINL int plan_workers(const PlanArgs& p, int N) { return max(min(p.workers, (N + (1 << p.min_shift) - 1) >> p.min_shift), 1); }
@@ -92,9 +92,9 @@ SP_DEVINL void build_plan(const PrefixArgs& a, const PlanArgs& p, PlanShared& s,
   const int E = a.n_groups + a.B, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int G = a.Hq / a.Hkv;
   constexpr int PER = (kPlanEntries + NT - 1) / NT;
-  long long t_sum = 0;
-  int i_sum = 0;
-  long long tl[PER];
+  int t_sum = 0, i_sum = 0;
+  bool over = false;  // an entry with more units than its share of 2^31
+  int tl[PER];
   int il[PER], r0[PER], r1[PER], len[PER];
   // every thread's loads at once, first those that others depend on (entries beyond the last: the last's again)
 #pragma unroll
@@ -112,8 +112,7 @@ SP_DEVINL void build_plan(const PrefixArgs& a, const PlanArgs& p, PlanShared& s,
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
     const int e = tid * PER + k;
-    int items = 0;
-    long long tiles = 0;
+    int items = 0, units = 0;
     if (e < E) {
       const bool pre = e < a.n_groups;
       const int r = max(r1[k] - r0[k], 0);
@@ -126,48 +125,45 @@ SP_DEVINL void build_plan(const PrefixArgs& a, const PlanArgs& p, PlanShared& s,
       if (pre ? p.prefix : p.own) {
         items = (r * G + p.tile_rows - 1) / p.tile_rows * a.Hkv;
         const int kt = (keys + (1 << p.key_shift) - 1) >> p.key_shift;
-        tiles = kt ? (long long)items * (kt + p.over) : 0;
+        const long long n = kt ? (long long)items * (kt + p.over) : 0;
+        if (n * E > 0x7fffffffll) over = true;
+        else units = (int)n;
       }
     }
     il[k] = items;
-    tl[k] = tiles;
+    tl[k] = units;
     i_sum += items;
-    t_sum += tiles;
+    t_sum += units;
   }
-  int ix = i_sum;
-  long long tx = t_sum;
+  int ix = i_sum, tx = t_sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int iu = __shfl_up_sync(0xffffffffu, ix, o);
-    const long long tu = __shfl_up_sync(0xffffffffu, tx, o);
+    const int iu = __shfl_up_sync(0xffffffffu, ix, o), tu = __shfl_up_sync(0xffffffffu, tx, o);
     if (lane >= o) {
       ix += iu;
       tx += tu;
     }
   }
-  if (lane == 31) {
-    s.wsum_i[warp] = ix;
-    s.wsum_t[warp] = tx;
-  }
-  __syncthreads();
+  if (lane == 31) s.wsum[warp] = make_int2(ix, tx);
+  over = __syncthreads_or(over);
   ix -= i_sum;
   tx -= t_sum;
-  for (int w = 0; w < warp; ++w) {
-    ix += s.wsum_i[w];
-    tx += s.wsum_t[w];
-  }
   int total = 0;
-  for (int w = 0; w < NT / 32; ++w) total += s.wsum_i[w];
-  long long units = 0;
-  for (int w = 0; w < NT / 32; ++w) units += s.wsum_t[w];
-  const bool fits = total <= p.max_items && units <= 0x7fffffff;
+#pragma unroll
+  for (int w = 0; w < NT / 32; ++w) {
+    const int2 x = s.wsum[w];
+    total += x.x;
+    ix += w < warp ? x.x : 0;
+    tx += w < warp ? x.y : 0;
+  }
+  const bool fits = total <= p.max_items && !over;
   if (!fits && write && tid == 0) set_error(a.err, SP_DEVERR_INDEX);
 #pragma unroll
   for (int k = 0; k <= PER; ++k) {  // (the total's place follows the last entry, maybe another thread's first)
     const int e = tid * PER + k;
     if (k < PER ? e <= E : (e == E && tid == NT - 1)) {
       const int i = fits ? ix : 0;
-      const int t = fits ? (int)tx : 0;
+      const int t = fits ? tx : 0;
       s.item0[e] = i;
       s.unit0[e] = t;
       if (write) {
@@ -214,14 +210,16 @@ struct TileCursor {
     kvh = in - rt * Hkv;
     kt = (s.keys[e] + (1 << p.key_shift) - 1) >> p.key_shift;
   }
-  // to the first key tile at or behind unit t < t1; false: there is none before t1
+  // to the first key tile at or behind unit t < t1; false: there is none before t1 (called by whole warps)
   SP_DEVINL bool seek(const PlanShared& s, const PlanArgs& p, int E, int Hkv, int t, int t1) {
-    int lo = 0, hi = E - 1;  // the entry that holds unit t (entries without units are passed over)
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (s.unit0[mid] <= t) lo = mid; else hi = mid - 1;
-    }
-    e = lo;
+    // the entry that holds unit t (entries without units are passed over), by the whole warp: every step-th entry,
+    // then those between
+    const int lane = threadIdx.x & 31, step = (E + 31) >> 5;
+    static_assert(kPlanEntries <= 32 * 32, "two rounds of 32");
+    const unsigned int coarse = __ballot_sync(0xffffffffu, lane * step < E && s.unit0[min(lane * step, E)] <= t);
+    const int from = (31 - __clz(coarse)) * step;
+    const unsigned int fine = __ballot_sync(0xffffffffu, lane < step && from + lane < E && s.unit0[min(from + lane, E)] <= t);
+    e = from + 31 - __clz(fine);
     const int len = ((s.keys[e] + (1 << p.key_shift) - 1) >> p.key_shift) + p.over;
     const int off = t - s.unit0[e], in = off / len;
     item = s.item0[e] + in;
