@@ -18,6 +18,9 @@
  *   sp_prefill   the LM prefill over the packed prefix (hidden states after the
  *                final RMSNorm).
  *   sp_pipeline  all four, back to back on one stream.
+ * and the generation after it: sp_decode over a cache per sequence, and over
+ * pages that sequences share (sp_prefill_paged, sp_decode_paged and the
+ * operators they and beam search are made of).
  *
  * Conventions (all entry points):
  *   - Pointers marked DEVICE are device memory owned by the caller; HOST marks

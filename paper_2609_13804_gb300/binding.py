@@ -914,19 +914,27 @@ def sp_beam_select(*, logits, cum, n_out, done=None, eos=0, score=None, parent=N
             if B > 1 and sb != W * ld:
                 raise ValueError("sp_beam_select: the rows of logits must lie evenly apart")
         shape = (B, n_out)
+        where = logits.device
         if score is None:
-            score = torch.empty(shape, dtype=f32, device=logits.device)
+            score = torch.empty(shape, dtype=f32, device=where)
+            s = score.data_ptr()
+        else:
+            s = _arg(who, "score", score, f32, dev, shape)
         if parent is None:
-            parent = torch.empty(shape, dtype=i32, device=logits.device)
+            parent = torch.empty(shape, dtype=i32, device=where)
+            p = parent.data_ptr()
+        else:
+            p = _arg(who, "parent", parent, i32, dev, shape)
         if token is None:
-            token = torch.empty(shape, dtype=i32, device=logits.device)
+            token = torch.empty(shape, dtype=i32, device=where)
+            t = token.data_ptr()
+        else:
+            t = _arg(who, "token", token, i32, dev, shape)
         if ws is None:
             ws = beam_select_workspace(B=B, W=W, V=V, n_out=n_out, device=logits.device)
         n = ws.numel()
         io = _pack_select(B, W, V, logits.data_ptr(), is_f32, ld, _arg(who, "cum", cum, f32, dev, (B, W)),
-                          _opt(who, "done", done, torch.bool, dev, (B, W)), eos, n_out,
-                          _arg(who, "score", score, f32, dev, shape), _arg(who, "parent", parent, i32, dev, shape),
-                          _arg(who, "token", token, i32, dev, shape))
+                          _opt(who, "done", done, torch.bool, dev, (B, W)), eos, n_out, s, p, t)
         st = lib().sp_beam_select(io, _arg(who, "ws", ws, torch.uint8, dev, (n,)), n, _raw_stream(stream, dev))
         if st:
             _check(st, who)
