@@ -606,7 +606,8 @@ SP_API sp_status sp_paged_append(const sp_paged_append_io* io, sp_stream stream)
  * A prefix is read once for all rows that share it.  Scores, statistics and
  * sums are fp32; the weights are rounded to bf16 for the product with V.
  * Lengths are read on the device (they may change between replays of a graph);
- * the workspace depends on the arguments of its query alone and keeps nothing.
+ * the workspace depends on the arguments of its query alone and keeps nothing
+ * (calls whose GPU work overlaps need one each).
  * Rows outside cu_rows[0] .. cu_rows[B] - 1 are left as they were.  The result
  * does not depend on timing (no atomics); it is summed in an order that depends
  * on the lengths of the whole batch.
@@ -688,7 +689,8 @@ SP_API sp_status sp_decode_paged(const sp_model* m, const sp_decode_paged_io* io
  *   - NaN and -infinity logits have no weight and are never chosen; a row with
  *     +infinity spreads its weight over them (the softmax's limit).
  * Places for which no continuation is left get score -infinity, parent and
- * token -1.
+ * token -1.  The workspace keeps nothing; calls whose GPU work overlaps need one
+ * each.
  */
 typedef struct {
   int B, W, V;              /* 1..SP_MAX_BATCH, 1..SP_MAX_BEAMS, 1..2^24 */

@@ -692,8 +692,7 @@ def _rows(who, name, t, dtype, dev, width):
     """(address, row stride) of rows of `width` elements, which may lie apart."""
     if t is None or t.dtype is not dtype or t.dim() != 2 or t.shape[1] != width or t.get_device() != dev or t.stride(1) != 1:
         raise ValueError(f"{who}: {name} must be {dtype} rows of {width} elements on device {dev}")
-    ld = t.stride(0)
-    return t.data_ptr(), ld if ld >= width or t.shape[0] > 1 else width
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else width
 
 
 def _pool(who, kv, dev, width):

@@ -137,6 +137,8 @@ __device__ __noinline__ int cut_list(unsigned long long* list, int n, int n_out)
 // overflow is cut down to its n_out largest and T raised to the last of them, so any order of logits, and any
 // number of equal ones (keys tell them apart by token), is taken exactly.  At the end the lists' n_out largest,
 // in order, and (m, sum) go to part.
+// Bound by issue (some 6 instructions a logit with the exponential's) and by what a slice costs besides, about 3 us:
+// 256 rows of 152,064 bf16 logits, a fifth of them finished, 62 MB, 18 us (3.4 TB/s); 4 rows of 32,000 fp32 3.5 us.
 template <bool F32>
 __global__ void __launch_bounds__(BS_NT, 3)
 beam_scan_kernel(const void* __restrict__ logits, long long ld, int V, const float* __restrict__ cum,
@@ -469,7 +471,8 @@ beam_join_kernel(int W, int S, const float* __restrict__ cum, const unsigned cha
 // table takes p(w)'s entries.  The partly filled page is copied: every beam has a page of its own for each
 // place of its table (own_table), the only ones it ever writes, so the rows of own[p(w)] go to own[w], in
 // place for all beams at once: a thread reads its 16 bytes of every parent before it writes any.
-// blockIdx.y: a plane (layer, K or V), or behind the last the tables; bound by the copied rows' bytes.
+// blockIdx.y: a plane (layer, K or V), or behind the last the tables.  Bound by the copied rows' bytes (66 MB of 16 x 4
+// beams, 28 layers, in 14.2 us, 4.7 TB/s read and written), for few of them by the chain length -> pages -> rows.
 constexpr int BR_NT = 256;
 
 template <int WMAX>
