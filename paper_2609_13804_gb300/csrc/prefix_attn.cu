@@ -84,7 +84,8 @@ __global__ void __maxnreg__(200) prefix_warp_kernel(const PrefixArgs a, const Pl
   build_plan<WK_NT>(a, p, plan, blockIdx.x == 0);
   if (warp == WK_WARPS - 1) write_rows(a, p, plan, lane, 32);  // (the warp with the least to do)
   const int N = plan.unit0[E], P = N > 0 ? plan_workers(p, N) : 0;
-  const int w = blockIdx.x + warp * gridDim.x;  // (a short list goes to different SMs first)
+  // a short list goes to different SMs first; behind the other kernel to few, those that one has left idle
+  const int w = late ? blockIdx.x * WK_WARPS + warp : blockIdx.x + warp * gridDim.x;
   int t0 = 0, t1 = 0;
   if (w < P) part_of_worker(N, P, w, t0, t1);
   TileCursor put, get;
