@@ -682,7 +682,10 @@ SP_API sp_status sp_decode_paged(const sp_model* m, const sp_decode_paged_io* io
  * tokens, the n_out continuations with the largest
  *   cum[w] + log softmax(logits[w])[v],
  * best first.  Scores are compared in 64 bits; equal ones go to the lower beam,
- * then the lower token (within a beam the order is that of the logits).
+ * then the lower token (within a beam the order is that of the logits).  A
+ * row's sum is taken in fp32, in an order that depends on its first logit's
+ * place within 16 bytes: rows of equal logits have equal scores when they lie
+ * alike (ld and logits multiples of 16 bytes), else to that sum's rounding.
  *   - A beam with cum -infinity (or NaN) is not alive: it proposes nothing.
  *   - A finished beam (done != 0) proposes only itself: token eos, score cum;
  *     its logits are not read.

@@ -480,6 +480,39 @@ def test_select_finished_beams_and_rows_apart(sp):
         select_case(sp, full.to(torch.bfloat16)[..., 1:V], cum, 6, done, eos=0)
 
 
+@pytest.mark.parametrize("W,n_out", [(16, 32), (16, 5), (9, 8), (12, 17)])
+def test_select_among_many_beams(sp, W, n_out):
+    """Equal scores across all beams, far apart ones, and beams that offer one continuation or none."""
+    g = gen(W + n_out)
+    x = torch.randn((6, W, 700), device=DEV, generator=g)
+    cum = torch.zeros((6, W), device=DEV)
+    done = torch.zeros((6, W), dtype=torch.bool, device=DEV)
+    x[0] = x[0, :1]                           # every score W times
+    x[1] = 0
+    cum[2] = -4 * torch.arange(W, device=DEV)[torch.randperm(W, generator=g, device=DEV)]
+    cum[3, 1:] = -torch.inf                   # one beam left
+    done[4, ::2] = True
+    cum[4, 1::4] = -torch.inf
+    done[5] = True                            # W candidates in all
+    select_case(sp, x, cum, n_out, done, eos=3)
+    # Rows of 1,400 bytes start at 0 or 8 bytes past a multiple of 16, and with that the sum of 700 terms is taken in
+    # one order or another.  The sums of equal rows then differ by fp32's rounding of their additions (a thread adds no
+    # more than 36 terms, 8 additions and 3 scalings join the threads: below 48 halves of an ulp, 48 x 2^-24 < 2^-18),
+    # so such scores are equal within the bound and no more, and any of them may stand before another.
+    x16 = x.to(torch.bfloat16)
+    r = sp.sp_beam_select(logits=x16, cum=cum, n_out=n_out, done=done, eos=3)
+    tol = 2.0 ** -18
+    for b, cand in enumerate(plain_select(x16, cum, W * 700, done, 3)):
+        of = {(w, v): a for a, w, v, _ in cand if w >= 0}
+        best = (sorted(of.values(), reverse=True) + [-np.inf] * n_out)[:n_out]
+        got = list(zip(*(r[k][b].cpu().tolist() for k in ("parent", "token", "score"))))
+        named = [(w, v) for w, v, _ in got if w >= 0]
+        assert len(set(named)) == len(named)
+        for (w, v, s), a in zip(got, best):
+            assert (w, v, s) == (-1, -1, -np.inf) if a == -np.inf else abs(s - a) <= tol and abs(s - of[w, v]) <= tol
+        assert [s for _, _, s in got] == sorted((s for _, _, s in got), reverse=True)
+
+
 # ----------------------------------------------------------------------------- reordering
 
 @pytest.mark.parametrize("W", [1, 3, 4, 8, 16])
