@@ -426,8 +426,15 @@ struct PrefixLayout {
   size_t bytes;
 };
 
-// Vectors per entry from which its products go to prefix_tc_kernel.
+// Vectors per entry from which its products can go to prefix_tc_kernel.
 constexpr int kTcVectors = 32;
+// They stay with prefix_warp_kernel, whose start is shorter, while that has no more than kFewTiles key tiles of 16
+// vectors per warp of the GPU, taking every sequence and prefix as long as the tables can hold and the rows as evenly
+// spread, and none has more than kFewKeys keys (whose many segments cost the merge more).  Us of a call with that
+// kernel and with prefix_tc_kernel: 64 rows x 28 heads of 128, 4 kv heads, in 4 prefixes of 250 keys (3.8 tiles per
+// warp) 17 and 19, of 1,000 (15) 30 and 22; 32 rows x 32 heads, one prefix of 250 keys (0.8) 12.1 and 18.1, of 1,000
+// (3.3) 16.5 and 22.1, of 4,000 (13) 32.3 and 31.3; 5 rows x 28 heads, one prefix of 4,000 keys (2.5) 19.9 and 18.8.
+constexpr int kFewTiles = 7, kFewKeys = 2048;
 
 // A plan's arrays in its part of the workspace (base NULL: sizes only); returns its bytes.
 static size_t plan_carve(PlanArgs* p, char* base, int T_cap, int B, int n_groups, int G, int Hkv, int dh) {
@@ -450,12 +457,20 @@ static size_t plan_carve(PlanArgs* p, char* base, int T_cap, int B, int n_groups
   return off;
 }
 
-static PrefixLayout prefix_layout(int T_cap, int B, int n_groups, int Hq, int Hkv, int dh) {
+// keys_prefix, keys_own: what the tables can hold of a prefix, of a sequence.
+static PrefixLayout prefix_layout(int T_cap, int B, int n_groups, int Hq, int Hkv, int dh, long long keys_prefix,
+                                  long long keys_own) {
   PrefixLayout L = {};
   const int G = Hq / Hkv, sms = device_sm_count();
   const bool fits = G <= 128;
-  const bool tc_prefix = fits && n_groups > 0 && (long long)T_cap * G >= (long long)kTcVectors * n_groups;
-  const bool tc_own = fits && (long long)T_cap * G >= (long long)kTcVectors * B;
+  bool tc_prefix = fits && n_groups > 0 && (long long)T_cap * G >= (long long)kTcVectors * n_groups;
+  bool tc_own = fits && (long long)T_cap * G >= (long long)kTcVectors * B;
+  auto tiles = [&](int entries, long long keys) {
+    return ((long long)T_cap * G / WK_ROWS + entries) * Hkv * ((keys + WK_KEYS - 1) / WK_KEYS);
+  };
+  if (std::max(tc_prefix ? keys_prefix : 0, tc_own ? keys_own : 0) <= kFewKeys &&
+      (tc_prefix ? tiles(n_groups, keys_prefix) : 0) + (tc_own ? tiles(B, keys_own) : 0) <= (long long)kFewTiles * sms * WK_WARPS)
+    tc_prefix = tc_own = false;
   L.warp.tile_rows = G <= WK_ROWS ? WK_ROWS / G * G : WK_ROWS;  // (whole rows where they fit)
   L.warp.key_shift = 4;
   L.warp.over = 2;
@@ -481,7 +496,8 @@ static PrefixLayout prefix_layout(int T_cap, int B, int n_groups, int Hq, int Hk
 
 static cudaError_t prefix_attention_launch(const PrefixArgs& a, int dh, void* ws, cudaStream_t st) {
   if (a.T_cap == 0) return cudaSuccess;
-  PrefixLayout L = prefix_layout(a.T_cap, a.B, a.n_groups, a.Hq, a.Hkv, dh);
+  PrefixLayout L = prefix_layout(a.T_cap, a.B, a.n_groups, a.Hq, a.Hkv, dh, (long long)a.pmax_pages << a.page_shift,
+                                 (long long)a.max_pages << a.page_shift);
   const int sms = device_sm_count(), G = a.Hq / a.Hkv;
   char* base = static_cast<char*>(ws);
   cudaError_t r;
@@ -512,7 +528,9 @@ static cudaError_t prefix_attention_launch(const PrefixArgs& a, int dh, void* ws
 }
 
 size_t prefix_attention_bytes(int T_cap, int B, int n_groups, int Hq, int Hkv, int dh) {
-  return prefix_layout(T_cap, B, n_groups, Hq, Hkv, dh).bytes;
+  // (for tables of any width)
+  return std::max(prefix_layout(T_cap, B, n_groups, Hq, Hkv, dh, 0, 0).bytes,
+                  prefix_layout(T_cap, B, n_groups, Hq, Hkv, dh, kFewKeys + 1, kFewKeys + 1).bytes);
 }
 
 cudaError_t prefix_attention(const PrefixAttention& x, void* ws, cudaStream_t st) {

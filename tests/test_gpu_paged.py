@@ -63,6 +63,13 @@ def tables(g, lens, page, extra_pages=2, extra_columns=1):
     return t, sum(need) + extra_pages
 
 
+def widen(t, page):
+    """The same table with room for more than 2,048 keys, which takes many vectors of an entry to the tensor kernel."""
+    wide = torch.full((t.shape[0], max(t.shape[1], 2048 // page + 1)), -1, dtype=torch.int32, device=DEV)
+    wide[:, :t.shape[1]] = t
+    return wide
+
+
 # ----------------------------------------------------------------------------- append
 
 def plain_append(qkv, lens, rows, table, page, heads, theta, pos, section):
@@ -189,9 +196,15 @@ def plain_attention(q, kv, page, heads, rows, table, lens, group_cu, ptable, ple
     return torch.stack(outs), torch.stack(lses), torch.stack(sizes)
 
 
-def attention_case(sp, seed, heads, page, rows, lens, groups, plens, *, std=1.0, scale=None, strided=False, garbage=True,
-                   graph=False):
-    """Runs one call and compares it with the plain form; groups: sequences per group (the rest have no prefix)."""
+def attention_case(sp, seed, heads, page, rows, lens, groups, plens, **options):
+    """Runs one call with narrow and wide tables and compares it with the plain form."""
+    for wide in (False, True):
+        attention_call(sp, seed, heads, page, rows, lens, groups, plens, wide=wide, **options)
+
+
+def attention_call(sp, seed, heads, page, rows, lens, groups, plens, *, std=1.0, scale=None, strided=False, garbage=True,
+                   graph=False, wide=False):
+    """groups: sequences per group (the rest have no prefix)."""
     Hq, Hkv, dh = heads
     g = gen(seed)
     T = sum(rows)
@@ -215,6 +228,8 @@ def attention_case(sp, seed, heads, page, rows, lens, groups, plens, *, std=1.0,
     lse = torch.full((q.shape[0], Hq), 7.0, device=DEV)
     group_cu = [sum(groups[:i]) for i in range(len(groups) + 1)]
     some = len(groups) > 0
+    if wide:
+        table, ptable = widen(table, page), widen(ptable, page)
     args = dict(q=q, kv=kv, table=table, lens=ints(lens), cu_rows=cu, n_heads=Hq, n_kv_heads=Hkv, head_dim=dh,
                 prefix_table=ptable if some else None, prefix_lens=ints(plens) if some else None,
                 group_cu=ints(group_cu) if some else None, scale=scale or 0.0, out=out[:, :Hq * dh], lse=lse)
@@ -298,7 +313,8 @@ def test_attention_reports_a_page_outside_the_pool(sp):
 @pytest.mark.parametrize("G,n", [(2, 3), (4, 64)])  # few query vectors per prefix, many
 @pytest.mark.parametrize("dh", [64, 128])
 @pytest.mark.parametrize("page", [16, 64, 256])
-def test_attention_counts_a_bad_page_as_zeros(sp, G, n, dh, page):
+@pytest.mark.parametrize("wide", [False, True])
+def test_attention_counts_a_bad_page_as_zeros(sp, G, n, dh, page, wide):
     """Pages outside the pool inside a prefix and at its end: their keys and values are zeros, the error word says so."""
     g = gen(page + n)
     pages = -(-300 // page)
@@ -312,6 +328,8 @@ def test_attention_counts_a_bad_page_as_zeros(sp, G, n, dh, page):
     for t in (good, bad):
         t[0, keep] = ids[keep]
     bad[0, 1 % pages], bad[0, pages - 1] = -1, pages + 3
+    if wide:
+        good, bad = widen(good, page), widen(bad, page)
     args = dict(q=q, kv=kv, lens=ints([0] * n), table=torch.full((n, 1), -1, dtype=torch.int32, device=DEV), n_heads=2 * G,
                 n_kv_heads=2, head_dim=dh, prefix_lens=ints([300]), group_cu=ints([0, n]))
     a = sp.sp_prefix_attention(prefix_table=good, **args)
@@ -321,12 +339,15 @@ def test_attention_counts_a_bad_page_as_zeros(sp, G, n, dh, page):
 
 
 @pytest.mark.parametrize("n", [3, 64])
-def test_attention_nan_stays_in_its_row(sp, n):
+@pytest.mark.parametrize("wide", [False, True])
+def test_attention_nan_stays_in_its_row(sp, n, wide):
     g = gen(n)
     kv = normal(g, 2, 30, 16, 128)
     q = normal(g, n, 4 * 128)
     args = dict(kv=kv, lens=ints([5] * n), table=ints([[20]] * n), n_heads=4, n_kv_heads=1, head_dim=128,
                 prefix_table=torch.arange(20, device=DEV, dtype=torch.int32)[None], prefix_lens=ints([311]), group_cu=ints([0, n]))
+    if wide:
+        args["prefix_table"] = widen(args["prefix_table"], 16)
     ref = sp.sp_prefix_attention(q=q, **args)["out"].clone()
     q[1, 128:256] = torch.nan  # one head of one row
     got = sp.sp_prefix_attention(q=q, lse=(lse := torch.zeros((n, 4), device=DEV)), **args)["out"]
@@ -355,14 +376,15 @@ def test_offsets_beyond_32_bits(sp):
     sp.sp_paged_append(qkv=qkv, kv=kv[0], table=table, lens=ints([17, 15, 31]), n_heads=Hq, n_kv_heads=Hkv, head_dim=dh)
     for b, (p, r) in enumerate(((pages - 1, 1), (pages - 2, 15), (pages - 4, 15))):
         assert torch.equal(kv[0, :, p, r].reshape(-1), qkv[b, Hq * dh:])
-    for n in (3, 40):
+    for n, room in ((3, 2), (40, 2), (40, 129)):  # (129 pages of 16: over 2,048 keys)
         q = normal(g, n, Hq * dh)
+        fit = lambda t: t if room == 2 else widen(t, page)  # noqa: E731
         r = sp.sp_prefix_attention(q=q, kv=kv[0], table=table[:1].expand(n, 2).contiguous(), lens=ints([18] * n), n_heads=Hq, n_kv_heads=Hkv,
-                                   head_dim=dh, prefix_table=table[1:], prefix_lens=ints([20, 32]), group_cu=ints([0, n - 1, n]))
+                                   head_dim=dh, prefix_table=fit(table[1:]), prefix_lens=ints([20, 32]), group_cu=ints([0, n - 1, n]))
         few = torch.cat((kv[0, :, [0, 1]], kv[0, :, pages - 4:]), dim=1)  # the same pages in a small pool
         at = lambda t: torch.where(t > 1, t - (pages - 4) + 2, t).to(torch.int32)  # noqa: E731
         s = sp.sp_prefix_attention(q=q, kv=few, table=at(table[:1]).expand(n, 2).contiguous(), lens=ints([18] * n), n_heads=Hq, n_kv_heads=Hkv,
-                                   head_dim=dh, prefix_table=at(table[1:]), prefix_lens=ints([20, 32]), group_cu=ints([0, n - 1, n]))
+                                   head_dim=dh, prefix_table=fit(at(table[1:])), prefix_lens=ints([20, 32]), group_cu=ints([0, n - 1, n]))
         assert int(r["err"].item()) == 0 and torch.equal(r["out"], s["out"])
     own = ints([[0, pages - 1], [pages - 2, pages - 3]])
     t = own.clone()
@@ -600,7 +622,8 @@ def test_generation_steps_of_beams_together(sp):
         hist = [hist[e * W + int(s["parent"][e, w])].clone() for e in range(E) for w in range(W)]
 
 
-def test_calls_on_another_stream_and_two_at_once(sp):
+@pytest.mark.parametrize("wide", [False, True])
+def test_calls_on_another_stream_and_two_at_once(sp, wide):
     """Two calls with workspaces of their own on two streams give what they give one after the other."""
     g = gen(31)
     Hq, Hkv, dh, page = 28, 4, 128, 16
@@ -610,6 +633,8 @@ def test_calls_on_another_stream_and_two_at_once(sp):
         sets.append(dict(q=normal(g, 20, Hq * dh), kv=normal(g, 2, pages, page, Hkv * dh), table=table[:20].contiguous(),
                          lens=ints([100] * 20), prefix_table=table[20:].contiguous(), prefix_lens=ints([900]),
                          group_cu=ints([0, 20]), n_heads=Hq, n_kv_heads=Hkv, head_dim=dh))
+        if wide:
+            sets[-1]["prefix_table"] = widen(sets[-1]["prefix_table"], page)
     ref = [sp.sp_prefix_attention(**s)["out"].clone() for s in sets]
     torch.cuda.synchronize()
     streams = [torch.cuda.Stream() for _ in sets]
