@@ -1,7 +1,7 @@
 // Attention of rows that share a prefix, over a paged cache: every row of a sequence reads its group's
 // prefix and, causally, its sequence's own keys; grouped-query heads map query head i to kv head
-// i / (Hq / Hkv).  prefix_plan.cuh says how the work is cut; here are the kernel for few query vectors
-// per entry and the kernel that joins the segments.
+// i / (Hq / Hkv).  prefix_plan.cuh says how the work of larger calls is cut; here are the kernel for few query
+// vectors per entry, the kernel that joins the segments, and the kernel that takes single tokens by itself.
 //
 // Score s_k = scale <q, K_k>, m = max s_k, l = sum exp(s_k - m), o = sum exp(s_k - m) V_k / l, one pass over
 // the keys with the running m, l and o in fp32; exponentials in base 2 with scale log2(e) folded into the
@@ -67,7 +67,7 @@ struct WkCfg {
 };
 
 // (200 registers a thread leave room for a CTA of the merge beside this kernel's, which then waits on the SM instead
-// of being launched when it ends: 11.3 us instead of 12.6 for four beams)
+// of being launched when it ends: 11.3 us instead of 12.6 for four beams, when they went this way)
 template <int DH>
 __global__ void __maxnreg__(200) prefix_warp_kernel(const PrefixArgs a, const PlanArgs p, int late) {
   using C = WkCfg<DH>;
@@ -417,6 +417,283 @@ cudaError_t launch_merge(const PrefixArgs& a, const PlanArgs& pp, const PlanArgs
   return launch_pdl(many ? prefix_merge_kernel<DH, 4> : prefix_merge_kernel<DH, 1>, grid, dim3(256), 0, st, a, pp, po);
 }
 
+// --------------------------------------------------------------- rows of one token each, joined in a CTA
+// One CTA per R consecutive rows and kv head, its warps in turn over the 16-key tiles of the rows' prefixes (one that
+// several of the rows share is read once for them) and own keys, and the join in shared memory: one launch, no plan,
+// no workspace.  The R G <= 8 query vectors are the product's N: S^T = K Q^T and O^T = V^T P^T, so half the registers
+// of the other form hold Q and O; a tile counts for the vectors of its rows.
+// Measured: four beams (32 heads of 128, 240 + 20 keys) 5.8 us instead of 11.1 by plan and merge; 64 beams of 16 prefixes
+// of 300 keys (89 MB) 20.5 instead of 28.5.  With few CTAs bound by the chain of a tile, some 330 instructions that a warp
+// issues at 0.47 a cycle and scheduler together with 2 or 3 others (a tile takes a warp 1 us); 14 warps with two tiles in
+// flight each fill the shared memory and the registers (nine with three took 31 us where these take 24: 4,000 keys).
+// With many CTAs bound by HBM: 64 rows of 500 keys of their own, 540 MB, 95.7 us (5.6 TB/s).
+constexpr int RK_VECS = 8, RK_NS = 2;  // vectors; tiles of a warp in flight
+
+template <int DH>
+struct RkCfg {
+  static constexpr int ROW = DH * 2, HALF = WK_KEYS * ROW, STAGE = 2 * HALF;  // K tile, V tile
+  static constexpr int WARPS = DH == 128 ? 14 : 12;                           // of a CTA at most
+  static constexpr int SM_WARPS = DH == 128 ? 14 : 24;                        // of an SM, by shared memory and registers
+};
+
+SP_DEVINL uint32_t transpose8(uint32_t x) {  // an 8 x 8 matrix of 16-bit elements, a row's pair per lane
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+
+template <int DH>
+__global__ void __launch_bounds__(RkCfg<DH>::WARPS * 32, RkCfg<DH>::SM_WARPS / RkCfg<DH>::WARPS)
+prefix_row_kernel(const PrefixArgs a, int R, int rows) {
+  using C = RkCfg<DH>;
+  constexpr int CPR = DH / 8;
+  extern __shared__ __align__(256) uint8_t row_ring[];  // [warps][RK_NS][STAGE]; then the warps' O, [8][DH] each
+  __shared__ float2 ml_s[C::WARPS][RK_VECS];
+  static_assert(RK_VECS * DH * 4 <= RK_NS * C::STAGE, "a warp's O in its ring");
+  pdl_wait();
+  pdl_trigger();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  const int G = a.Hq / a.Hkv, kvh = blockIdx.x, r0 = blockIdx.y * R, nr = min(R, rows - r0);  // row = its sequence
+  const int cap = a.max_pages << a.page_shift, pcap = a.pmax_pages << a.page_shift;
+  const bool report = kvh == 0 && warp == 0;
+  // Lane i < 8 stands for the prefix that row r0 + i is the first of the rows to read, lane 8 + i for row r0 + i's own
+  // keys.
+  const int my = r0 + min(lane & 7, nr - 1);
+  const bool live = lane < 16 && (lane & 7) < nr;
+  const int own_len = __ldg(a.lens + my);
+  int g = -1;  // row my's group: the last that begins at or before it, if it reaches it
+  for (int g0 = 0; g0 < a.n_groups; g0 += 32) {
+    const int i = g0 + lane;
+    const int from = i < a.n_groups ? __ldg(a.group_cu + i) : 0, to = i < a.n_groups ? __ldg(a.group_cu + i + 1) : 0;
+    for (int j = 0; j < nr; ++j) {
+      const unsigned int all = __ballot_sync(0xffffffffu, from <= r0 + j && r0 + j < to);
+      if (all && my == r0 + j) g = g0 + 31 - __clz(all);
+    }
+    if (report && r0 == 0 && i < a.n_groups) {
+      const int n = __ldg(a.plens + i);
+      if (n < 0 || n > pcap) set_error(a.err, SP_DEVERR_INDEX);
+    }
+  }
+  if (report && live && (own_len < 0 || own_len > cap)) set_error(a.err, SP_DEVERR_INDEX);
+  const int g_before = __shfl_up_sync(0xffffffffu, g, 1);
+  const bool first = live && lane < 8 && (lane == 0 || g != g_before);
+  const unsigned int firsts = __ballot_sync(0xffffffffu, first);
+  int keys = 0, cols = 0;  // the lane's keys; its vectors, begin | end << 8
+  const int* tab = a.table + (size_t)my * a.max_pages;
+  if (live && lane >= 8) {
+    keys = min(max(own_len, 0), cap);
+    cols = (lane - 8) * G | (lane - 7) * G << 8;
+  } else if (first && g >= 0) {
+    const unsigned int behind = firsts & ~((2u << lane) - 1u);
+    keys = min(max(__ldg(a.plens + g), 0), pcap);
+    cols = lane * G | (behind ? __ffs(behind) - 1 : nr) * G << 8;
+    tab = a.ptable + (size_t)g * a.pmax_pages;
+  }
+  const int mine = (keys + WK_KEYS - 1) / WK_KEYS;
+  int upto = mine;  // tiles of the lanes up to this one
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) {
+    const int u = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += u;
+  }
+  const int tiles = __shfl_sync(0xffffffffu, upto, 15);
+  const size_t W = (size_t)a.Hkv * DH;
+  const size_t plane = ((size_t)a.n_pages << a.page_shift) * W;
+  const uint32_t ring = smem_u32(row_ring) + warp * RK_NS * C::STAGE;
+
+  struct Tile {
+    int page, row, n, cols;  // page, its first key's row there, keys (0: there is no such tile), vectors
+  };
+  // The lane whose tiles come next: its first tile and the one behind its last, keys, vectors, table.  (Every warp looks
+  // at its tiles in order.)
+  int seg_from = 0, seg_to = 0, seg_keys = 0, seg_cols = 0;
+  const int* seg_tab = nullptr;
+  auto look = [&](int t) {
+    Tile x;
+    x.page = x.row = x.n = x.cols = 0;
+    if (t >= tiles) return x;
+    if (t >= seg_to) {
+      const int from = __popc(__ballot_sync(0xffffffffu, lane < 16 && upto <= t));
+      seg_from = __shfl_sync(0xffffffffu, upto - mine, from);
+      seg_to = seg_from + __shfl_sync(0xffffffffu, mine, from);
+      seg_keys = __shfl_sync(0xffffffffu, keys, from);
+      seg_cols = __shfl_sync(0xffffffffu, cols, from);
+      seg_tab = reinterpret_cast<const int*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(tab), from));
+    }
+    const int k0 = (t - seg_from) * WK_KEYS;
+    x.n = min(WK_KEYS, seg_keys - k0);
+    x.cols = seg_cols;
+    x.row = k0 & ((1 << a.page_shift) - 1);
+    x.page = __ldg(seg_tab + (k0 >> a.page_shift));
+    return x;
+  };
+  // A tile's rows: lane = 16-byte piece, rows in turn, pieces exchanged so that reading them meets no bank twice.  Rows
+  // past the keys are zeros.
+  constexpr int STEP = 32 / CPR;
+  const int piece = lane % CPR, row_in = lane / CPR;
+  const uint32_t put = row_in * C::ROW + ((piece ^ row_in) << 4);
+  auto load = [&](const Tile& x, int slot) {
+    const bool ok = x.page >= 0 && x.page < a.n_pages;
+    if (!ok && lane == 0) set_error(a.err, SP_DEVERR_INDEX);
+    const __nv_bfloat16* src = a.kv + ((((size_t)(ok ? x.page : 0)) << a.page_shift) + x.row) * W + kvh * DH + piece * 8;
+    const uint32_t dst = ring + slot * C::STAGE;
+    if (ok && x.n == WK_KEYS) {
+      const __nv_bfloat16 *k = src + row_in * W, *v = k + plane;
+#pragma unroll
+      for (int i = 0; i < WK_KEYS; i += STEP) {
+        const uint32_t to = dst + (put ^ ((i & 7) << 4)) + i * C::ROW;
+        cp_async16(to, k, 16);
+        cp_async16(to + C::HALF, v, 16);
+        k += STEP * W;
+        v += STEP * W;
+      }
+    } else {
+      const int n = ok ? x.n : 0;
+#pragma unroll 1
+      for (int i = 0; i < WK_KEYS; i += STEP) {
+        const int r = i + row_in;
+        const __nv_bfloat16* from = src + (r < n ? r : 0) * W;
+        const uint32_t to = dst + (put ^ ((i & 7) << 4)) + i * C::ROW;
+        cp_async16(to, from, r < n ? 16 : 0);
+        cp_async16(to + C::HALF, from + plane, r < n ? 16 : 0);
+      }
+    }
+  };
+
+  Tile q[RK_NS];  // the tile at hand, those in flight, and the one to be loaded next
+#pragma unroll
+  for (int i = 0; i < RK_NS; ++i) q[i] = look(warp + i * warps);
+#pragma unroll
+  for (int i = 0; i < RK_NS - 1; ++i) {
+    if (q[i].n) load(q[i], i);
+    cp_async_commit();
+  }
+  // the query vectors: vector lane / 4
+  uint32_t qf[DH / 16][2];
+  {
+    const int vec = lane >> 2, r = min(vec / G, nr - 1);
+    const bool have = vec < nr * G;
+    const __nv_bfloat16* qr = a.q + (r0 + r) * a.ld_q + (kvh * G + (have ? vec - r * G : 0)) * DH + (lane & 3) * 2;
+#pragma unroll
+    for (int kk = 0; kk < DH / 16; ++kk)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) qf[kk][x] = have ? __ldg(reinterpret_cast<const unsigned int*>(qr + kk * 16 + x * 8)) : 0u;
+  }
+  float o[DH / 16][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};  // of vectors 2 (lane % 4) and the next
+#pragma unroll
+  for (int n = 0; n < DH / 16; ++n)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) o[n][c] = 0.f;
+  const int whole = nr * G << 8;
+  // a lane's address for the pieces 0 and 1 of K, of V transposed; pieces 2 i and 2 i + 1 are at it ^ (i << 5)
+  const uint32_t get_k = (lane & 15) * C::ROW + (((lane >> 4) ^ (lane & 7)) << 4);
+  const uint32_t get_v = ((lane >> 4) * 8 + (lane & 7)) * C::ROW + ((((lane >> 3) & 1) ^ (lane & 7)) << 4);
+  int slot = 0, slot_put = RK_NS - 1;
+  for (int t = warp; t < tiles; t += warps) {
+    const Tile now = q[0];
+    if (q[RK_NS - 1].n) load(q[RK_NS - 1], slot_put);
+    cp_async_commit();
+    if (++slot_put == RK_NS) slot_put = 0;
+#pragma unroll
+    for (int i = 0; i < RK_NS - 1; ++i) q[i] = q[i + 1];
+    q[RK_NS - 1] = look(t + RK_NS * warps);
+    cp_async_wait<RK_NS - 1>();
+    __syncwarp();  // every lane's copies have landed and are visible to the warp
+    const uint32_t ks = ring + slot * C::STAGE + get_k, vs = ring + slot * C::STAGE + C::HALF + get_v;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};  // keys lane / 4 and 8 on, two vectors each
+#pragma unroll
+    for (int kk = 0; kk < DH / 16; ++kk) {
+      uint32_t k[4];
+      ldsm4(ks ^ (kk << 5), k);
+      mma16816(s, k, qf[kk][0], qf[kk][1]);
+    }
+    float corr[2], x[4];
+    bool sees[2];
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+      const int vec = (lane & 3) * 2 + v;
+      sees[v] = vec >= (now.cols & 255) && vec < now.cols >> 8;
+      const int n = sees[v] ? now.n : 0;
+      x[v] = (lane >> 2) < n ? s[v] * a.scale_log2 : -INFINITY;
+      x[v + 2] = (lane >> 2) + 8 < n ? s[v + 2] * a.scale_log2 : -INFINITY;
+      float mx = fmaxf(x[v], x[v + 2]);
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+      const float mn = fmaxf(m[v], mx), mz = mn == -INFINITY ? 0.f : mn;
+      corr[v] = ex2(m[v] - mz);  // (0 while m is -infinity)
+      m[v] = mn;
+      x[v] = ex2(x[v] - mz);
+      x[v + 2] = ex2(x[v + 2] - mz);
+      l[v] = l[v] * corr[v] + (x[v] + x[v + 2]);
+    }
+    const uint32_t p0 = transpose8(pack_bf16x2(x[0], x[1])), p1 = transpose8(pack_bf16x2(x[2], x[3]));
+    if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
+#pragma unroll
+      for (int d = 0; d < DH / 16; ++d)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[d][c] *= corr[c & 1];
+    }
+    if (now.cols == whole) {
+#pragma unroll
+      for (int d = 0; d < DH / 16; ++d) {
+        uint32_t vt[4];
+        ldsm4_t(vs ^ (d << 5), vt);
+        mma16816(o[d], vt, p0, p1);
+      }
+    } else {  // (a zero weight times a NaN of another row's keys is no zero)
+#pragma unroll
+      for (int d = 0; d < DH / 16; ++d) {
+        uint32_t vt[4];
+        float y[4] = {0.f, 0.f, 0.f, 0.f};
+        ldsm4_t(vs ^ (d << 5), vt);
+        mma16816(y, vt, p0, p1);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[d][c] += sees[c & 1] ? y[c] : 0.f;
+      }
+    }
+    __syncwarp();  // the tile is read before a lane's next copies overwrite it
+    if (++slot == RK_NS) slot = 0;
+  }
+  // the join: every warp's (m, l) and, over its tiles, its O
+  float* os = reinterpret_cast<float*>(row_ring + (size_t)warp * RK_NS * C::STAGE);
+#pragma unroll
+  for (int v = 0; v < 2; ++v) {
+    l[v] += __shfl_xor_sync(0xffffffffu, l[v], 4);
+    l[v] += __shfl_xor_sync(0xffffffffu, l[v], 8);
+    l[v] += __shfl_xor_sync(0xffffffffu, l[v], 16);
+    const int vec = (lane & 3) * 2 + v;
+    if (lane < 4) ml_s[warp][vec] = make_float2(m[v], l[v]);
+    if (vec < nr * G) {
+#pragma unroll
+      for (int d = 0; d < DH / 16; ++d) {
+        os[vec * DH + d * 16 + (lane >> 2)] = o[d][v];
+        os[vec * DH + d * 16 + 8 + (lane >> 2)] = o[d][v + 2];
+      }
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < nr * G * (DH / 2); i += blockDim.x) {  // two values of a vector each
+    const int vec = i / (DH / 2), d = i % (DH / 2) * 2;
+    float mm = -INFINITY, ll = 0.f, y0 = 0.f, y1 = 0.f;
+    for (int w = 0; w < warps; ++w) mm = fmaxf(mm, ml_s[w][vec].x);
+    const float mz = mm == -INFINITY ? 0.f : mm;
+#pragma unroll 4
+    for (int w = 0; w < warps; ++w) {
+      const float2 ml = ml_s[w][vec];
+      const float c = ex2(ml.x - mz);
+      const float2 y = *reinterpret_cast<const float2*>(row_ring + (size_t)w * RK_NS * C::STAGE + (vec * DH + d) * 4);
+      ll += ml.y * c;
+      y0 += y.x * c;
+      y1 += y.y * c;
+    }
+    const int r = vec / G, h = kvh * G + vec - r * G;
+    const float inv = ll == 0.f ? 0.f : 1.f / ll;  // (NaN stays NaN)
+    *reinterpret_cast<uint32_t*>(a.out + (r0 + r) * a.ld_out + (long long)h * DH + d) = pack_bf16x2(y0 * inv, y1 * inv);
+    if (a.lse && d == 0) a.lse[(size_t)(r0 + r) * a.Hq + h] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * 0.69314718055994531f;
+  }
+}
+
 }  // namespace
 
 // What a call launches, from what the host knows, and its workspace.
@@ -494,8 +771,53 @@ static PrefixLayout prefix_layout(int T_cap, int B, int n_groups, int Hq, int Hk
   return L;
 }
 
+// Rows and warps of a CTA of prefix_row_kernel where a call goes to it (rows 0: it does not): single tokens of up to
+// RK_VECS heads per kv head, as long as a warp's share of the CTA's tiles, with tables as full as they can be, is short
+// (kRowTiles), or no prefix is read by two CTAs of a kv head and half the SMs have one (kRowTilesAlone).  Us with it and
+// without: four rows of 32 heads of 128 and one prefix of 240 keys (1.2 tiles a warp) 5.8 and 11.1, of 2,000 keys (9)
+// 13.9 and 16.1; 16 rows of 28 heads, 4 kv heads, 2,000 keys (9) 13.9 and 17.5; 4 rows, 4,000 keys (18) 22.3 and 19.3; 64
+// rows, one prefix of 2,944 keys (27) 33.0 and 23.3; without sharing, 8 rows of 32 heads and 4,000 keys (one CTA of 14
+// warps on two SMs of three; 36) 80 and 92; 64 rows and 500 (33, CTAs of one warp) 95.7 and 99.
+struct RowLayout {
+  int rows, warps;
+};
+constexpr int kRowTiles = 12, kRowTilesAlone = 36;
+// Rows of a CTA are doubled, up to the rows of a prefix, while the warps of the GPU would have more tiles than this each:
+// below that the SMs are better used by a row each.
+constexpr int kRowSpread = 2;
+static RowLayout row_layout(const PrefixArgs& a, int dh, int sms) {
+  const int G = a.Hq / a.Hkv, T = a.T_cap;
+  if (a.cu_rows || G > RK_VECS) return {0, 0};
+  const int share = a.n_groups > 0 ? std::max(1, T / a.n_groups) : 1;  // rows of a prefix
+  const long long pt = ((long long)a.pmax_pages << a.page_shift) / WK_KEYS, ot = ((long long)a.max_pages << a.page_shift) / WK_KEYS;
+  const int most = dh == 128 ? RkCfg<128>::WARPS : RkCfg<64>::WARPS;
+  const int warp_smem = RK_NS * (dh == 128 ? RkCfg<128>::STAGE : RkCfg<64>::STAGE);
+  const int sm_warps = dh == 128 ? RkCfg<128>::SM_WARPS : RkCfg<64>::SM_WARPS;
+  auto places = [&](int R) { return (long long)(T + R - 1) / R * a.Hkv; };
+  auto tiles = [&](int R) { return (R + share - 1) / share * pt + R * ot; };
+  int R = 1;
+  while (2 * R * G <= RK_VECS && R < share && places(R) * tiles(R) > (long long)kRowSpread * sms * sm_warps) R *= 2;
+  // as many warps as let all CTAs be there at once (2 KB: a CTA's other shared memory)
+  int warps = (int)std::max(1ll, std::min<long long>(most, tiles(R)));
+  while (warps > 1 && (227 * 1024) / (warps * warp_smem + 2048) * (long long)sms < places(R)) --warps;
+  const bool alone = R >= share && 2 * places(R) >= sms;
+  return tiles(R) <= (long long)(alone ? kRowTilesAlone : kRowTiles) * warps ? RowLayout{R, warps} : RowLayout{0, 0};
+}
+
 static cudaError_t prefix_attention_launch(const PrefixArgs& a, int dh, void* ws, cudaStream_t st) {
   if (a.T_cap == 0) return cudaSuccess;
+  if (const RowLayout x = row_layout(a, dh, device_sm_count()); x.rows) {
+    const size_t warp_smem = RK_NS * (dh == 128 ? RkCfg<128>::STAGE : RkCfg<64>::STAGE);
+    auto* kern = dh == 128 ? prefix_row_kernel<128> : prefix_row_kernel<64>;
+    static std::atomic<unsigned long long> allowed[2];
+    cudaError_t r = allow_smem(kern, warp_smem * (dh == 128 ? RkCfg<128>::WARPS : RkCfg<64>::WARPS), allowed[dh == 128]);
+    if (r != cudaSuccess) return r;
+    prof_begin_launch(st);
+    r = launch_pdl(kern, dim3(a.Hkv, (a.T_cap + x.rows - 1) / x.rows), dim3(x.warps * 32), warp_smem * x.warps, st, a,
+                   x.rows, a.T_cap);
+    prof_end_launch(st, SP_K_ATTN, 0.0, 0.0);
+    return r;
+  }
   PrefixLayout L = prefix_layout(a.T_cap, a.B, a.n_groups, a.Hq, a.Hkv, dh, (long long)a.pmax_pages << a.page_shift,
                                  (long long)a.max_pages << a.page_shift);
   const int sms = device_sm_count(), G = a.Hq / a.Hkv;

@@ -64,7 +64,8 @@ def tables(g, lens, page, extra_pages=2, extra_columns=1):
 
 
 def widen(t, page):
-    """The same table with room for more than 2,048 keys, which takes many vectors of an entry to the tensor kernel."""
+    """The same table with room for more than 2,048 keys: with the rows' offsets given too, many vectors of an entry go to
+    the tensor kernel then."""
     wide = torch.full((t.shape[0], max(t.shape[1], 2048 // page + 1)), -1, dtype=torch.int32, device=DEV)
     wide[:, :t.shape[1]] = t
     return wide
@@ -197,13 +198,13 @@ def plain_attention(q, kv, page, heads, rows, table, lens, group_cu, ptable, ple
 
 
 def attention_case(sp, seed, heads, page, rows, lens, groups, plens, **options):
-    """Runs one call with narrow and wide tables and compares it with the plain form."""
-    for wide in (False, True):
-        attention_call(sp, seed, heads, page, rows, lens, groups, plens, wide=wide, **options)
+    """Runs one call as each of the kernels takes it and compares it with the plain form."""
+    for wide, offsets in ((False, False), (False, True), (True, True)):
+        attention_call(sp, seed, heads, page, rows, lens, groups, plens, wide=wide, offsets=offsets, **options)
 
 
 def attention_call(sp, seed, heads, page, rows, lens, groups, plens, *, std=1.0, scale=None, strided=False, garbage=True,
-                   graph=False, wide=False):
+                   graph=False, wide=False, offsets=False):
     """groups: sequences per group (the rest have no prefix)."""
     Hq, Hkv, dh = heads
     g = gen(seed)
@@ -221,7 +222,7 @@ def attention_call(sp, seed, heads, page, rows, lens, groups, plens, *, std=1.0,
     full = normal(g, T + extra, Hq * dh + (16 if strided else 0), std=std)
     q = full[:, :Hq * dh]
     one = all(n == 1 for n in rows)
-    cu = None if one and not strided else starts(rows)
+    cu = None if one and not offsets else starts(rows)
     if cu is None:
         q = q[:T]
     out = torch.full((q.shape[0], Hq * dh + (8 if strided else 0)), 7.0, dtype=torch.bfloat16, device=DEV)
@@ -328,9 +329,10 @@ def test_attention_counts_a_bad_page_as_zeros(sp, G, n, dh, page, wide):
     for t in (good, bad):
         t[0, keep] = ids[keep]
     bad[0, 1 % pages], bad[0, pages - 1] = -1, pages + 3
+    cu = None
     if wide:
-        good, bad = widen(good, page), widen(bad, page)
-    args = dict(q=q, kv=kv, lens=ints([0] * n), table=torch.full((n, 1), -1, dtype=torch.int32, device=DEV), n_heads=2 * G,
+        good, bad, cu = widen(good, page), widen(bad, page), starts([1] * n)
+    args = dict(cu_rows=cu, q=q, kv=kv, lens=ints([0] * n), table=torch.full((n, 1), -1, dtype=torch.int32, device=DEV), n_heads=2 * G,
                 n_kv_heads=2, head_dim=dh, prefix_lens=ints([300]), group_cu=ints([0, n]))
     a = sp.sp_prefix_attention(prefix_table=good, **args)
     b = sp.sp_prefix_attention(prefix_table=bad, **args)
@@ -347,7 +349,7 @@ def test_attention_nan_stays_in_its_row(sp, n, wide):
     args = dict(kv=kv, lens=ints([5] * n), table=ints([[20]] * n), n_heads=4, n_kv_heads=1, head_dim=128,
                 prefix_table=torch.arange(20, device=DEV, dtype=torch.int32)[None], prefix_lens=ints([311]), group_cu=ints([0, n]))
     if wide:
-        args["prefix_table"] = widen(args["prefix_table"], 16)
+        args.update(prefix_table=widen(args["prefix_table"], 16), cu_rows=starts([1] * n))
     ref = sp.sp_prefix_attention(q=q, **args)["out"].clone()
     q[1, 128:256] = torch.nan  # one head of one row
     got = sp.sp_prefix_attention(q=q, lse=(lse := torch.zeros((n, 4), device=DEV)), **args)["out"]
@@ -357,6 +359,33 @@ def test_attention_nan_stays_in_its_row(sp, n, wide):
     kv[1, 3, 5, 7] = torch.nan  # a value that all rows see
     got = sp.sp_prefix_attention(q=ref.new_zeros(n, 512), **args)["out"].view(n, 4, 128)
     assert torch.isnan(got[..., 7]).all() and torch.isfinite(got[..., :7]).all() and torch.isfinite(got[..., 8:]).all()
+
+
+@pytest.mark.parametrize("heads", [(32, 32, 128), (64, 32, 128), (48, 48, 64)])
+def test_attention_rows_of_different_groups_together(sp, heads):
+    """Up to eight query vectors share a CTA: rows of one prefix, of several, and of none."""
+    for groups in ([8, 8], [3, 5, 1, 4], [1, 0, 2, 11]):
+        lens = [(11 * i) % 30 for i in range(16)]
+        attention_call(sp, 20, heads, 16, [1] * 16, lens, groups, [300, 17, 0, 290][:len(groups)])
+
+
+@pytest.mark.parametrize("heads", [(32, 32, 128), (64, 32, 128), (48, 48, 64)])
+def test_attention_nan_in_own_keys_stays_in_its_row(sp, heads):
+    Hq, Hkv, dh = heads
+    g = gen(21)
+    n = 16
+    kv = normal(g, 2, 20 + 2 * n, 16, Hkv * dh)
+    q = normal(g, n, Hq * dh)
+    args = dict(q=q, kv=kv, lens=ints([5 + i for i in range(n)]), table=ints([[20 + 2 * i, 21 + 2 * i] for i in range(n)]),
+                n_heads=Hq, n_kv_heads=Hkv, head_dim=dh, prefix_table=torch.arange(20, device=DEV, dtype=torch.int32)[None],
+                prefix_lens=ints([311]), group_cu=ints([0, n]))
+    ref = sp.sp_prefix_attention(**args)["out"].clone()
+    kv[:, 20 + 2 * 5, 3] = torch.nan   # a key and value of row 5, a value of row 6, an infinite value of row 7
+    kv[1, 20 + 2 * 6, 2] = torch.nan
+    kv[1, 20 + 2 * 7, 1] = torch.inf
+    got = sp.sp_prefix_attention(**args)["out"]
+    keep = [i for i in range(n) if i not in (5, 6, 7)]
+    assert torch.equal(got[keep], ref[keep]) and torch.isnan(got[5:7]).all() and torch.isinf(got[7]).all()
 
 
 def test_attention_130_query_heads_of_one(sp):
@@ -376,15 +405,16 @@ def test_offsets_beyond_32_bits(sp):
     sp.sp_paged_append(qkv=qkv, kv=kv[0], table=table, lens=ints([17, 15, 31]), n_heads=Hq, n_kv_heads=Hkv, head_dim=dh)
     for b, (p, r) in enumerate(((pages - 1, 1), (pages - 2, 15), (pages - 4, 15))):
         assert torch.equal(kv[0, :, p, r].reshape(-1), qkv[b, Hq * dh:])
-    for n, room in ((3, 2), (40, 2), (40, 129)):  # (129 pages of 16: over 2,048 keys)
+    for n, room in ((3, 2), (3, 129), (40, 2), (40, 129)):  # (129 pages of 16: over 2,048 keys)
         q = normal(g, n, Hq * dh)
         fit = lambda t: t if room == 2 else widen(t, page)  # noqa: E731
+        cu = None if room == 2 and n == 3 else starts([1] * n)
         r = sp.sp_prefix_attention(q=q, kv=kv[0], table=table[:1].expand(n, 2).contiguous(), lens=ints([18] * n), n_heads=Hq, n_kv_heads=Hkv,
-                                   head_dim=dh, prefix_table=fit(table[1:]), prefix_lens=ints([20, 32]), group_cu=ints([0, n - 1, n]))
+                                   head_dim=dh, cu_rows=cu, prefix_table=fit(table[1:]), prefix_lens=ints([20, 32]), group_cu=ints([0, n - 1, n]))
         few = torch.cat((kv[0, :, [0, 1]], kv[0, :, pages - 4:]), dim=1)  # the same pages in a small pool
         at = lambda t: torch.where(t > 1, t - (pages - 4) + 2, t).to(torch.int32)  # noqa: E731
         s = sp.sp_prefix_attention(q=q, kv=few, table=at(table[:1]).expand(n, 2).contiguous(), lens=ints([18] * n), n_heads=Hq, n_kv_heads=Hkv,
-                                   head_dim=dh, prefix_table=fit(at(table[1:])), prefix_lens=ints([20, 32]), group_cu=ints([0, n - 1, n]))
+                                   head_dim=dh, cu_rows=cu, prefix_table=fit(at(table[1:])), prefix_lens=ints([20, 32]), group_cu=ints([0, n - 1, n]))
         assert int(r["err"].item()) == 0 and torch.equal(r["out"], s["out"])
     own = ints([[0, pages - 1], [pages - 2, pages - 3]])
     t = own.clone()
@@ -634,7 +664,7 @@ def test_calls_on_another_stream_and_two_at_once(sp, wide):
                          lens=ints([100] * 20), prefix_table=table[20:].contiguous(), prefix_lens=ints([900]),
                          group_cu=ints([0, 20]), n_heads=Hq, n_kv_heads=Hkv, head_dim=dh))
         if wide:
-            sets[-1]["prefix_table"] = widen(sets[-1]["prefix_table"], page)
+            sets[-1].update(prefix_table=widen(sets[-1]["prefix_table"], page), cu_rows=starts([1] * 20))
     ref = [sp.sp_prefix_attention(**s)["out"].clone() for s in sets]
     torch.cuda.synchronize()
     streams = [torch.cuda.Stream() for _ in sets]
