@@ -199,7 +199,7 @@ def plain_attention(q, kv, page, heads, rows, table, lens, group_cu, ptable, ple
 
 def attention_case(sp, seed, heads, page, rows, lens, groups, plens, **options):
     """Runs one call as each of the kernels takes it and compares it with the plain form."""
-    for wide, offsets in ((False, False), (False, True), (True, True)):
+    for wide, offsets in ((False, False), (False, True), (True, True), (True, False)):
         attention_call(sp, seed, heads, page, rows, lens, groups, plens, wide=wide, offsets=offsets, **options)
 
 
@@ -314,8 +314,8 @@ def test_attention_reports_a_page_outside_the_pool(sp):
 @pytest.mark.parametrize("G,n", [(2, 3), (4, 64)])  # few query vectors per prefix, many
 @pytest.mark.parametrize("dh", [64, 128])
 @pytest.mark.parametrize("page", [16, 64, 256])
-@pytest.mark.parametrize("wide", [False, True])
-def test_attention_counts_a_bad_page_as_zeros(sp, G, n, dh, page, wide):
+@pytest.mark.parametrize("wide,offsets", [(False, False), (True, True), (True, False)])
+def test_attention_counts_a_bad_page_as_zeros(sp, G, n, dh, page, wide, offsets):
     """Pages outside the pool inside a prefix and at its end: their keys and values are zeros, the error word says so."""
     g = gen(page + n)
     pages = -(-300 // page)
@@ -329,9 +329,9 @@ def test_attention_counts_a_bad_page_as_zeros(sp, G, n, dh, page, wide):
     for t in (good, bad):
         t[0, keep] = ids[keep]
     bad[0, 1 % pages], bad[0, pages - 1] = -1, pages + 3
-    cu = None
+    cu = starts([1] * n) if offsets else None
     if wide:
-        good, bad, cu = widen(good, page), widen(bad, page), starts([1] * n)
+        good, bad = widen(good, page), widen(bad, page)
     args = dict(cu_rows=cu, q=q, kv=kv, lens=ints([0] * n), table=torch.full((n, 1), -1, dtype=torch.int32, device=DEV), n_heads=2 * G,
                 n_kv_heads=2, head_dim=dh, prefix_lens=ints([300]), group_cu=ints([0, n]))
     a = sp.sp_prefix_attention(prefix_table=good, **args)
@@ -341,15 +341,17 @@ def test_attention_counts_a_bad_page_as_zeros(sp, G, n, dh, page, wide):
 
 
 @pytest.mark.parametrize("n", [3, 64])
-@pytest.mark.parametrize("wide", [False, True])
-def test_attention_nan_stays_in_its_row(sp, n, wide):
+@pytest.mark.parametrize("wide,offsets", [(False, False), (True, True), (True, False)])
+def test_attention_nan_stays_in_its_row(sp, n, wide, offsets):
     g = gen(n)
     kv = normal(g, 2, 30, 16, 128)
     q = normal(g, n, 4 * 128)
     args = dict(kv=kv, lens=ints([5] * n), table=ints([[20]] * n), n_heads=4, n_kv_heads=1, head_dim=128,
                 prefix_table=torch.arange(20, device=DEV, dtype=torch.int32)[None], prefix_lens=ints([311]), group_cu=ints([0, n]))
     if wide:
-        args.update(prefix_table=widen(args["prefix_table"], 16), cu_rows=starts([1] * n))
+        args.update(prefix_table=widen(args["prefix_table"], 16))
+    if offsets:
+        args.update(cu_rows=starts([1] * n))
     ref = sp.sp_prefix_attention(q=q, **args)["out"].clone()
     q[1, 128:256] = torch.nan  # one head of one row
     got = sp.sp_prefix_attention(q=q, lse=(lse := torch.zeros((n, 4), device=DEV)), **args)["out"]
@@ -370,15 +372,19 @@ def test_attention_rows_of_different_groups_together(sp, heads):
 
 
 @pytest.mark.parametrize("heads", [(32, 32, 128), (64, 32, 128), (48, 48, 64)])
-def test_attention_nan_in_own_keys_stays_in_its_row(sp, heads):
+@pytest.mark.parametrize("wide", [False, True])
+def test_attention_nan_in_own_keys_stays_in_its_row(sp, heads, wide):
     Hq, Hkv, dh = heads
     g = gen(21)
-    n = 16
+    n = 34 if wide else 16
     kv = normal(g, 2, 20 + 2 * n, 16, Hkv * dh)
     q = normal(g, n, Hq * dh)
     args = dict(q=q, kv=kv, lens=ints([5 + i for i in range(n)]), table=ints([[20 + 2 * i, 21 + 2 * i] for i in range(n)]),
                 n_heads=Hq, n_kv_heads=Hkv, head_dim=dh, prefix_table=torch.arange(20, device=DEV, dtype=torch.int32)[None],
                 prefix_lens=ints([311]), group_cu=ints([0, n]))
+    args["lens"] = args["lens"].clamp(max=32)
+    if wide:
+        args["prefix_table"] = widen(args["prefix_table"], 16)
     ref = sp.sp_prefix_attention(**args)["out"].clone()
     kv[:, 20 + 2 * 5, 3] = torch.nan   # a key and value of row 5, a value of row 6, an infinite value of row 7
     kv[1, 20 + 2 * 6, 2] = torch.nan
@@ -405,10 +411,10 @@ def test_offsets_beyond_32_bits(sp):
     sp.sp_paged_append(qkv=qkv, kv=kv[0], table=table, lens=ints([17, 15, 31]), n_heads=Hq, n_kv_heads=Hkv, head_dim=dh)
     for b, (p, r) in enumerate(((pages - 1, 1), (pages - 2, 15), (pages - 4, 15))):
         assert torch.equal(kv[0, :, p, r].reshape(-1), qkv[b, Hq * dh:])
-    for n, room in ((3, 2), (3, 129), (40, 2), (40, 129)):  # (129 pages of 16: over 2,048 keys)
+    for n, room, offsets in ((3, 2, 0), (3, 129, 1), (40, 2, 1), (40, 129, 1), (40, 129, 0)):  # (129 pages of 16: over 2,048 keys)
         q = normal(g, n, Hq * dh)
         fit = lambda t: t if room == 2 else widen(t, page)  # noqa: E731
-        cu = None if room == 2 and n == 3 else starts([1] * n)
+        cu = starts([1] * n) if offsets else None
         r = sp.sp_prefix_attention(q=q, kv=kv[0], table=table[:1].expand(n, 2).contiguous(), lens=ints([18] * n), n_heads=Hq, n_kv_heads=Hkv,
                                    head_dim=dh, cu_rows=cu, prefix_table=fit(table[1:]), prefix_lens=ints([20, 32]), group_cu=ints([0, n - 1, n]))
         few = torch.cat((kv[0, :, [0, 1]], kv[0, :, pages - 4:]), dim=1)  # the same pages in a small pool
@@ -652,8 +658,8 @@ def test_generation_steps_of_beams_together(sp):
         hist = [hist[e * W + int(s["parent"][e, w])].clone() for e in range(E) for w in range(W)]
 
 
-@pytest.mark.parametrize("wide", [False, True])
-def test_calls_on_another_stream_and_two_at_once(sp, wide):
+@pytest.mark.parametrize("wide,offsets", [(False, False), (True, True), (True, False)])
+def test_calls_on_another_stream_and_two_at_once(sp, wide, offsets):
     """Two calls with workspaces of their own on two streams give what they give one after the other."""
     g = gen(31)
     Hq, Hkv, dh, page = 28, 4, 128, 16
@@ -664,7 +670,9 @@ def test_calls_on_another_stream_and_two_at_once(sp, wide):
                          lens=ints([100] * 20), prefix_table=table[20:].contiguous(), prefix_lens=ints([900]),
                          group_cu=ints([0, 20]), n_heads=Hq, n_kv_heads=Hkv, head_dim=dh))
         if wide:
-            sets[-1].update(prefix_table=widen(sets[-1]["prefix_table"], page), cu_rows=starts([1] * 20))
+            sets[-1].update(prefix_table=widen(sets[-1]["prefix_table"], page))
+        if offsets:
+            sets[-1].update(cu_rows=starts([1] * 20))
     ref = [sp.sp_prefix_attention(**s)["out"].clone() for s in sets]
     torch.cuda.synchronize()
     streams = [torch.cuda.Stream() for _ in sets]
