@@ -1,7 +1,7 @@
 // Attention of rows that share a prefix, over a paged cache: every row of a sequence reads its group's
 // prefix and, causally, its sequence's own keys; grouped-query heads map query head i to kv head
 // i / (Hq / Hkv).  prefix_plan.cuh says how the work of larger calls is cut; here are the kernel for few query
-// vectors per entry, the kernel that joins the segments, and the kernel that takes single tokens by itself.
+// vectors per entry, the kernel that joins the segments, and the kernel that takes smaller calls by itself.
 //
 // Score s_k = scale <q, K_k>, m = max s_k, l = sum exp(s_k - m), o = sum exp(s_k - m) V_k / l, one pass over
 // the keys with the running m, l and o in fp32; exponentials in base 2 with scale log2(e) folded into the
@@ -417,7 +417,7 @@ cudaError_t launch_merge(const PrefixArgs& a, const PlanArgs& pp, const PlanArgs
   return launch_pdl(many ? prefix_merge_kernel<DH, 4> : prefix_merge_kernel<DH, 1>, grid, dim3(256), 0, st, a, pp, po);
 }
 
-// --------------------------------------------------------------- rows of one token each, joined in a CTA
+// --------------------------------------------------------------- few tiles per row, joined in a CTA
 // One CTA per R consecutive rows and kv head, its warps in turn over the 16-key tiles of the rows' prefixes (one that
 // several of the rows share is read once for them) and own keys, and the join in shared memory: one launch, no plan,
 // no workspace.  The R G <= 8 query vectors are the product's N: S^T = K Q^T and O^T = V^T P^T, so half the registers
@@ -453,40 +453,66 @@ prefix_row_kernel(const PrefixArgs a, int R, int rows) {
   pdl_wait();
   pdl_trigger();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-  const int G = a.Hq / a.Hkv, kvh = blockIdx.x, r0 = blockIdx.y * R, nr = min(R, rows - r0);  // row = its sequence
+  const int G = a.Hq / a.Hkv, kvh = blockIdx.x, r0 = blockIdx.y * R, nr = min(R, rows - r0);
   const int cap = a.max_pages << a.page_shift, pcap = a.pmax_pages << a.page_shift;
-  const bool report = kvh == 0 && warp == 0;
-  // Lane i < 8 stands for the prefix that row r0 + i is the first of the rows to read, lane 8 + i for row r0 + i's own
-  // keys.
+  // Lane i < 8 stands for the prefix that row r0 + i is the first of the rows to read, lane 8 + i for the sequence whose
+  // first row here is r0 + i.  First lane i's and lane 8 + i's row, its sequence b (-1: none), that one's rows, its group g
+  // (-1: none): the last that begins at or before, if it reaches it.
   const int my = r0 + min(lane & 7, nr - 1);
-  const bool live = lane < 16 && (lane & 7) < nr;
-  const int own_len = __ldg(a.lens + my);
-  int g = -1;  // row my's group: the last that begins at or before it, if it reaches it
-  for (int g0 = 0; g0 < a.n_groups; g0 += 32) {
-    const int i = g0 + lane;
-    const int from = i < a.n_groups ? __ldg(a.group_cu + i) : 0, to = i < a.n_groups ? __ldg(a.group_cu + i + 1) : 0;
-    for (int j = 0; j < nr; ++j) {
-      const unsigned int all = __ballot_sync(0xffffffffu, from <= r0 + j && r0 + j < to);
-      if (all && my == r0 + j) g = g0 + 31 - __clz(all);
-    }
-    if (report && r0 == 0 && i < a.n_groups) {
-      const int n = __ldg(a.plens + i);
-      if (n < 0 || n > pcap) set_error(a.err, SP_DEVERR_INDEX);
-    }
+  int b = -1, g = -1, b_from = my, b_rows = 1;
+  // (A round's offsets are loaded in the one before it.)
+  int own_len = 0;
+  if (!a.cu_rows) {
+    if (my < a.B) own_len = __ldg(a.lens + (b = my));
   }
-  if (report && live && (own_len < 0 || own_len > cap)) set_error(a.err, SP_DEVERR_INDEX);
-  const int g_before = __shfl_up_sync(0xffffffffu, g, 1);
-  const bool first = live && lane < 8 && (lane == 0 || g != g_before);
-  const unsigned int firsts = __ballot_sync(0xffffffffu, first);
-  int keys = 0, cols = 0;  // the lane's keys; its vectors, begin | end << 8
-  const int* tab = a.table + (size_t)my * a.max_pages;
-  if (live && lane >= 8) {
-    keys = min(max(own_len, 0), cap);
-    cols = (lane - 8) * G | (lane - 7) * G << 8;
+  auto group_at = [&](int i) { return i <= a.n_groups ? __ldg(a.group_cu + i) : 0; };
+  int g_from = a.n_groups ? group_at(lane) : 0, g_to = a.n_groups ? group_at(lane + 1) : 0;
+  if (a.cu_rows) {
+    auto row_at = [&](int i) { return row_begin(a, min(i, a.B)); };
+    int from = row_at(lane), to = row_at(lane + 1);
+    for (int b0 = 0; b0 < a.B; b0 += 32) {
+      const int from_next = row_at(b0 + 32 + lane), to_next = row_at(b0 + 33 + lane);
+      for (int j = 0; j < nr; ++j) {
+        const unsigned int all = __ballot_sync(0xffffffffu, from <= r0 + j && r0 + j < to);
+        const int at = all ? 31 - __clz(all) : 0, f = __shfl_sync(0xffffffffu, from, at), n = __shfl_sync(0xffffffffu, to, at) - f;
+        if (all && my == r0 + j) {
+          b = b0 + at;
+          b_from = f;
+          b_rows = n;
+        }
+      }
+      from = from_next;
+      to = to_next;
+    }
+    if (b >= 0) own_len = __ldg(a.lens + b);
+  }
+  for (int g0 = 0; g0 < a.n_groups; g0 += 32) {
+    const int from_next = group_at(g0 + 32 + lane), to_next = group_at(g0 + 33 + lane);
+    for (int j = 0; j < nr; ++j) {
+      const int bj = __shfl_sync(0xffffffffu, b, j);
+      const unsigned int all = __ballot_sync(0xffffffffu, g0 + lane < a.n_groups && g_from <= bj && bj < g_to);
+      if (all && bj >= 0 && my == r0 + j) g = g0 + 31 - __clz(all);
+    }
+    g_from = from_next;
+    g_to = to_next;
+  }
+  const bool live = lane < 16 && (lane & 7) < nr && b >= 0;
+  const int own = live ? min(max(own_len, 0), cap) : 0;
+  const int see = min(max(own - b_rows + my - b_from + 1, 0), own);  // own keys that the row sees
+  const int b_before = __shfl_up_sync(0xffffffffu, b, 1), g_before = __shfl_up_sync(0xffffffffu, g, 1);
+  const bool first = live && ((lane & 7) == 0 || (lane < 8 ? g != g_before : b != b_before));
+  const unsigned int firsts = __ballot_sync(0xffffffffu, first || !live);  // (a row of none ends a run as well)
+  const int run = __ffs(firsts >> (lane & 31) >> 1 | 1u << (8 - (lane & 7) - 1));  // rows of the run that begins here
+  const int see_last = __shfl_sync(0xffffffffu, see, (lane + run - 1) & 31);
+  int keys = 0, cols = 0;  // the lane's keys; its vectors, begin | end << 8, and 1 << 16 for own keys
+  const int* tab = a.table;
+  if (first && lane >= 8) {
+    keys = see_last;
+    cols = (lane - 8) * G | (lane - 8 + run) * G << 8 | 1 << 16;
+    tab = a.table + (size_t)b * a.max_pages;
   } else if (first && g >= 0) {
-    const unsigned int behind = firsts & ~((2u << lane) - 1u);
     keys = min(max(__ldg(a.plens + g), 0), pcap);
-    cols = lane * G | (behind ? __ffs(behind) - 1 : nr) * G << 8;
+    cols = lane * G | (lane + run) * G << 8;
     tab = a.ptable + (size_t)g * a.pmax_pages;
   }
   const int mine = (keys + WK_KEYS - 1) / WK_KEYS;
@@ -497,12 +523,13 @@ prefix_row_kernel(const PrefixArgs a, int R, int rows) {
     if (lane >= o) upto += u;
   }
   const int tiles = __shfl_sync(0xffffffffu, upto, 15);
+  const unsigned int lives = __ballot_sync(0xffffffffu, live);
   const size_t W = (size_t)a.Hkv * DH;
   const size_t plane = ((size_t)a.n_pages << a.page_shift) * W;
   const uint32_t ring = smem_u32(row_ring) + warp * RK_NS * C::STAGE;
 
   struct Tile {
-    int page, row, n, cols;  // page, its first key's row there, keys (0: there is no such tile), vectors
+    int page, row, n, cols, k0;  // page, its first key's row there, keys (0: there is no such tile), vectors, first key
   };
   // The lane whose tiles come next: its first tile and the one behind its last, keys, vectors, table.  (Every warp looks
   // at its tiles in order.)
@@ -510,7 +537,7 @@ prefix_row_kernel(const PrefixArgs a, int R, int rows) {
   const int* seg_tab = nullptr;
   auto look = [&](int t) {
     Tile x;
-    x.page = x.row = x.n = x.cols = 0;
+    x.page = x.row = x.n = x.cols = x.k0 = 0;
     if (t >= tiles) return x;
     if (t >= seg_to) {
       const int from = __popc(__ballot_sync(0xffffffffu, lane < 16 && upto <= t));
@@ -523,6 +550,7 @@ prefix_row_kernel(const PrefixArgs a, int R, int rows) {
     const int k0 = (t - seg_from) * WK_KEYS;
     x.n = min(WK_KEYS, seg_keys - k0);
     x.cols = seg_cols;
+    x.k0 = k0;
     x.row = k0 & ((1 << a.page_shift) - 1);
     x.page = __ldg(seg_tab + (k0 >> a.page_shift));
     return x;
@@ -585,6 +613,9 @@ prefix_row_kernel(const PrefixArgs a, int R, int rows) {
 #pragma unroll
     for (int c = 0; c < 4; ++c) o[n][c] = 0.f;
   const int whole = nr * G << 8;
+  int limit[2];  // own keys of the rows of this lane's vectors
+#pragma unroll
+  for (int v = 0; v < 2; ++v) limit[v] = __shfl_sync(0xffffffffu, see, min(((lane & 3) * 2 + v) / G, nr - 1));
   // a lane's address for the pieces 0 and 1 of K, of V transposed; pieces 2 i and 2 i + 1 are at it ^ (i << 5)
   const uint32_t get_k = (lane & 15) * C::ROW + (((lane >> 4) ^ (lane & 7)) << 4);
   const uint32_t get_v = ((lane >> 4) * 8 + (lane & 7)) * C::ROW + ((((lane >> 3) & 1) ^ (lane & 7)) << 4);
@@ -612,8 +643,8 @@ prefix_row_kernel(const PrefixArgs a, int R, int rows) {
 #pragma unroll
     for (int v = 0; v < 2; ++v) {
       const int vec = (lane & 3) * 2 + v;
-      sees[v] = vec >= (now.cols & 255) && vec < now.cols >> 8;
-      const int n = sees[v] ? now.n : 0;
+      sees[v] = vec >= (now.cols & 255) && vec < (now.cols >> 8 & 255);
+      const int n = !sees[v] ? 0 : now.cols >> 16 ? min(now.n, limit[v] - now.k0) : now.n;
       x[v] = (lane >> 2) < n ? s[v] * a.scale_log2 : -INFINITY;
       x[v + 2] = (lane >> 2) + 8 < n ? s[v + 2] * a.scale_log2 : -INFINITY;
       float mx = fmaxf(x[v], x[v + 2]);
@@ -634,7 +665,7 @@ prefix_row_kernel(const PrefixArgs a, int R, int rows) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) o[d][c] *= corr[c & 1];
     }
-    if (now.cols == whole) {
+    if ((now.cols & 0xffff) == whole) {
 #pragma unroll
       for (int d = 0; d < DH / 16; ++d) {
         uint32_t vt[4];
@@ -675,6 +706,7 @@ prefix_row_kernel(const PrefixArgs a, int R, int rows) {
   __syncthreads();
   for (int i = threadIdx.x; i < nr * G * (DH / 2); i += blockDim.x) {  // two values of a vector each
     const int vec = i / (DH / 2), d = i % (DH / 2) * 2;
+    if (!(lives >> (vec / G) & 1)) continue;  // (a row of no sequence stays as it is)
     float mm = -INFINITY, ll = 0.f, y0 = 0.f, y1 = 0.f;
     for (int w = 0; w < warps; ++w) mm = fmaxf(mm, ml_s[w][vec].x);
     const float mz = mm == -INFINITY ? 0.f : mm;
@@ -692,6 +724,12 @@ prefix_row_kernel(const PrefixArgs a, int R, int rows) {
     *reinterpret_cast<uint32_t*>(a.out + (r0 + r) * a.ld_out + (long long)h * DH + d) = pack_bf16x2(y0 * inv, y1 * inv);
     if (a.lse && d == 0) a.lse[(size_t)(r0 + r) * a.Hq + h] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * 0.69314718055994531f;
   }
+  // lengths outside the tables, of all sequences and groups (last: nothing waits for it)
+  if (kvh == 0 && warp == 0)
+    for (int i = blockIdx.y * 32 + lane; i < a.B + a.n_groups; i += gridDim.y * 32) {
+      const int n = __ldg(i < a.B ? a.lens + i : a.plens + i - a.B);
+      if (n < 0 || n > (i < a.B ? cap : pcap)) set_error(a.err, SP_DEVERR_INDEX);
+    }
 }
 
 }  // namespace
@@ -771,13 +809,15 @@ static PrefixLayout prefix_layout(int T_cap, int B, int n_groups, int Hq, int Hk
   return L;
 }
 
-// Rows and warps of a CTA of prefix_row_kernel where a call goes to it (rows 0: it does not): single tokens of up to
-// RK_VECS heads per kv head, as long as a warp's share of the CTA's tiles, with tables as full as they can be, is short
+// Rows and warps of a CTA of prefix_row_kernel where a call goes to it (rows 0: it does not): up to RK_VECS heads per kv
+// head, as long as a warp's share of the CTA's tiles, with tables as full as they can be and rows evenly spread, is short
 // (kRowTiles), or no prefix is read by two CTAs of a kv head and half the SMs have one (kRowTilesAlone).  Us with it and
-// without: four rows of 32 heads of 128 and one prefix of 240 keys (1.2 tiles a warp) 5.8 and 11.1, of 2,000 keys (9)
-// 13.9 and 16.1; 16 rows of 28 heads, 4 kv heads, 2,000 keys (9) 13.9 and 17.5; 4 rows, 4,000 keys (18) 22.3 and 19.3; 64
-// rows, one prefix of 2,944 keys (27) 33.0 and 23.3; without sharing, 8 rows of 32 heads and 4,000 keys (one CTA of 14
-// warps on two SMs of three; 36) 80 and 92; 64 rows and 500 (33, CTAs of one warp) 95.7 and 99.
+// without, single tokens: four rows of 32 heads of 128 and one prefix of 240 keys (1.2 tiles a warp) 5.8 and 11.1, of
+// 2,000 keys (9) 13.9 and 16.1; 16 rows of 28 heads, 4 kv heads, 2,000 keys (9) 13.9 and 17.5; 4 rows, 4,000 keys (18) 22.3
+// and 19.3; 64 rows, one prefix of 2,944 keys (27) 33.0 and 23.3; without sharing, 64 rows of 32 heads and 500 keys (33,
+// CTAs of one warp) 95.7 and 99.  Questions: 3 rows of 28 heads and 250 keys 7.6 and 10.7, four of 16 rows and 1,000 keys
+// (11) 16.1 and 21.2, 16 of 48 rows without a prefix (6, CTAs of one warp) 23.5 and 28.1.  Not CTAs of one warp for few
+// rows of a sequence that lie in several: 128 of 4 rows 22.1 and 16.3.
 struct RowLayout {
   int rows, warps;
 };
@@ -787,20 +827,22 @@ constexpr int kRowTiles = 12, kRowTilesAlone = 36;
 constexpr int kRowSpread = 2;
 static RowLayout row_layout(const PrefixArgs& a, int dh, int sms) {
   const int G = a.Hq / a.Hkv, T = a.T_cap;
-  if (a.cu_rows || G > RK_VECS) return {0, 0};
-  const int share = a.n_groups > 0 ? std::max(1, T / a.n_groups) : 1;  // rows of a prefix
+  if (G > RK_VECS) return {0, 0};
+  const int per = std::max(1, T / a.B);  // rows of a sequence
+  const int share = a.n_groups > 0 ? std::max(1, T / a.n_groups) : per;  // rows of a prefix
   const long long pt = ((long long)a.pmax_pages << a.page_shift) / WK_KEYS, ot = ((long long)a.max_pages << a.page_shift) / WK_KEYS;
   const int most = dh == 128 ? RkCfg<128>::WARPS : RkCfg<64>::WARPS;
   const int warp_smem = RK_NS * (dh == 128 ? RkCfg<128>::STAGE : RkCfg<64>::STAGE);
   const int sm_warps = dh == 128 ? RkCfg<128>::SM_WARPS : RkCfg<64>::SM_WARPS;
   auto places = [&](int R) { return (long long)(T + R - 1) / R * a.Hkv; };
-  auto tiles = [&](int R) { return (R + share - 1) / share * pt + R * ot; };
+  auto tiles = [&](int R) { return (R + share - 1) / share * pt + (R + per - 1) / per * ot; };
   int R = 1;
   while (2 * R * G <= RK_VECS && R < share && places(R) * tiles(R) > (long long)kRowSpread * sms * sm_warps) R *= 2;
   // as many warps as let all CTAs be there at once (2 KB: a CTA's other shared memory)
   int warps = (int)std::max(1ll, std::min<long long>(most, tiles(R)));
   while (warps > 1 && (227 * 1024) / (warps * warp_smem + 2048) * (long long)sms < places(R)) --warps;
-  const bool alone = R >= share && 2 * places(R) >= sms;
+  if (places(R) > 64ll * sms || (warps == 1 && R < per && (long long)T * G < (long long)kTcVectors * a.B)) return {0, 0};
+  const bool alone = R % share == 0 && 2 * places(R) >= sms;
   return tiles(R) <= (long long)(alone ? kRowTilesAlone : kRowTiles) * warps ? RowLayout{R, warps} : RowLayout{0, 0};
 }
 
