@@ -746,9 +746,9 @@ constexpr int kTcVectors = 32;
 // They stay with prefix_warp_kernel, whose start is shorter, while that has no more than kFewTiles key tiles of 16
 // vectors per warp of the GPU, taking every sequence and prefix as long as the tables can hold and the rows as evenly
 // spread, and none has more than kFewKeys keys (whose many segments cost the merge more).  Us of a call with that
-// kernel and with prefix_tc_kernel: 64 rows x 28 heads of 128, 4 kv heads, in 4 prefixes of 250 keys (3.8 tiles per
-// warp) 17 and 19, of 1,000 (15) 30 and 22; 32 rows x 32 heads, one prefix of 250 keys (0.8) 12.1 and 18.1, of 1,000
-// (3.3) 16.5 and 22.1, of 4,000 (13) 32.3 and 31.3; 5 rows x 28 heads, one prefix of 4,000 keys (2.5) 19.9 and 18.8.
+// kernel and with prefix_tc_kernel, 40 heads of 128 and one kv head: 16 rows and a prefix of 250 keys (0.5 tiles per
+// warp) 11.6 and 15.8, of 2,000 (4) 18.8 and 18.1, 64 rows and 250 keys (2) 14.9 and 17.3; 64 heads, 4 kv heads, 64 rows
+// in 16 prefixes of 250 keys (3.4) 17.3 and 19.8; of 1,000 (13; 28 heads) 30 and 22.
 constexpr int kFewTiles = 7, kFewKeys = 2048;
 
 // A plan's arrays in its part of the workspace (base NULL: sizes only); returns its bytes.
