@@ -25,6 +25,15 @@ U = 2.0 ** -8
 HEADS = [(32, 32, 128), (28, 4, 128), (16, 16, 64), (6, 2, 64), (40, 1, 128)]
 
 
+@pytest.fixture(autouse=True)
+def single_precision():
+    """Tensors without a type of their own are fp32, whatever another module has set."""
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(before)
+
+
 @pytest.fixture(scope="module")
 def sp():
     if not torch.cuda.is_available():
