@@ -603,14 +603,15 @@ SP_API sp_status sp_paged_append(const sp_paged_append_io* io, sp_stream stream)
  * those up to lens[b] - n_b + j.  Sequences outside every group have no prefix.
  *   out = softmax(scale <q, k>) v over the visible keys, lse = log sum exp of
  *   the scaled scores; a row that sees no key gets zeros and lse -infinity.
- * A prefix is read once for all rows that share it.  Scores, statistics and
- * sums are fp32; the weights are rounded to bf16 for the product with V.
+ * A prefix is read once for all rows that share it (in small calls by several
+ * CTAs, from the L2 cache).  Scores, statistics and sums are fp32; the weights are rounded to bf16 for the product with V.
  * Lengths are read on the device (they may change between replays of a graph);
  * the workspace depends on the arguments of its query alone and keeps nothing
  * (calls whose GPU work overlaps need one each).
  * Rows outside cu_rows[0] .. cu_rows[B] - 1 are left as they were.  The result
  * does not depend on timing (no atomics); it is summed in an order that depends
- * on the lengths of the whole batch.
+ * on the lengths of the whole batch and on how wide the tables are (which also
+ * decide how the call is cut: tables much wider than their contents cost time).
  */
 typedef struct {
   int B;                    /* sequences, 1..SP_MAX_BATCH */

@@ -380,6 +380,33 @@ def test_attention_rows_of_different_groups_together(sp, heads):
         attention_call(sp, 20, heads, 16, [1] * 16, lens, groups, [300, 17, 0, 290][:len(groups)])
 
 
+@pytest.mark.parametrize("heads", [(4, 4, 128), (14, 2, 64), (40, 2, 128)])
+@pytest.mark.parametrize("wide", [False, True])
+def test_attention_rows_before_the_first_and_between_empty_sequences(sp, heads, wide):
+    """Row offsets that begin behind row 0, sequences without rows, a group that begins with one: as the same rows from 0."""
+    Hq, Hkv, dh = heads
+    g = gen(22)
+    kv = normal(g, 2, 12, 32, Hkv * dh)
+    q = normal(g, 14, Hq * dh)
+    table, prefix = ints([[0, 1], [2, 3], [4, 5], [6, 7]]), ints([[8, 9], [10, 11]])
+    if wide:
+        prefix = widen(prefix, 32)
+    args = dict(kv=kv, table=table, lens=ints([9, 3, 40, 33]), n_heads=Hq, n_kv_heads=Hkv, head_dim=dh, prefix_table=prefix,
+                prefix_lens=ints([50, 64]), group_cu=ints([0, 2, 4]))
+    ref = sp.sp_prefix_attention(q=q[3:11].contiguous(), cu_rows=ints([0, 3, 3, 7, 8]), **args)["out"]
+    out, lse = torch.full((14, Hq * dh), 7.0, dtype=torch.bfloat16, device=DEV), torch.full((14, Hq), 7.0, device=DEV)
+    r = sp.sp_prefix_attention(q=q, cu_rows=ints([3, 6, 6, 10, 11]), out=out, lse=lse, **args)
+    assert int(r["err"].item()) == 0
+    outside = [0, 1, 2, 11, 12, 13]
+    assert (out[outside] == 7).all() and (lse[outside] == 7).all()
+    # (cut into other tiles: both within attention_call's bound, where the weights' sum of |v| is at most the largest |v|)
+    a, b, most = out[3:11].double(), ref.double(), kv[1].abs().max().double()
+    assert ((a - b).abs() <= 2 * (U * torch.maximum(a.abs(), b.abs()) + (U + 2.0 ** -12) * most)).all()
+    for bad in ([51, 65 if not wide else 1 << 20], [-1, 3]):
+        r = sp.sp_prefix_attention(q=q, cu_rows=ints([3, 6, 6, 10, 11]), **dict(args, prefix_lens=ints(bad)))
+        assert int(r["err"].item()) == 2
+
+
 @pytest.mark.parametrize("heads", [(32, 32, 128), (64, 32, 128), (48, 48, 64)])
 @pytest.mark.parametrize("wide", [False, True])
 def test_attention_nan_in_own_keys_stays_in_its_row(sp, heads, wide):
