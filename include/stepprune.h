@@ -608,6 +608,9 @@ SP_API sp_status sp_paged_append(const sp_paged_append_io* io, sp_stream stream)
  * Lengths are read on the device (they may change between replays of a graph);
  * the workspace depends on the arguments of its query alone and keeps nothing
  * (calls whose GPU work overlaps need one each).
+ * A NaN or infinity in V at a sequence's own position can also reach that
+ * sequence's earlier rows of the same call (a weight of zero times it is NaN),
+ * never another sequence.
  * Rows outside cu_rows[0] .. cu_rows[B] - 1 are left as they were.  The result
  * does not depend on timing (no atomics); it is summed in an order that depends
  * on the lengths of the whole batch and on how wide the tables are (which also
