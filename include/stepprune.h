@@ -608,6 +608,8 @@ SP_API sp_status sp_paged_append(const sp_paged_append_io* io, sp_stream stream)
  * Lengths are read on the device (they may change between replays of a graph);
  * the workspace depends on the arguments of its query alone and keeps nothing
  * (calls whose GPU work overlaps need one each).
+ * A NaN in a query, or in a key that it sees, makes that query's output and lse
+ * NaN.
  * A NaN or infinity in V at a sequence's own position can also reach that
  * sequence's earlier rows of the same call (a weight of zero times it is NaN),
  * never another sequence.
