@@ -403,7 +403,7 @@ prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         if (lane == 0) mbar_arrive(&bar[M_FULL + (gg & 1)]);
         mlast = m;
         if (m != ms) {  // bring this stream's sum to the new reference (from -infinity: zero, or NaN, which stays)
-          ls *= ex2(ms - m);
+          ls *= ex2(ms == -INFINITY ? 0.f : ms - m);
           ms = m;
         }
         const float nm = m == -INFINITY ? 0.f : -m;
@@ -455,7 +455,8 @@ prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         if (!mbar_wait_warp(&bar[M_FULL + (last & 1)], (last >> 1) & 1, a.err)) { ok = false; break; }
         mlast = mchain[(last & 1) * 128 + r];
       }
-      const float lsc = ms == mlast ? ls : ls * ex2(ms - mlast);  // (scores that are all NaN leave m at -infinity)
+      // (scores that are all NaN leave m at -infinity: their sum is passed on)
+      const float lsc = (ms == -INFINITY || mlast == -INFINITY) ? ls : ls * ex2(ms - mlast);
       float* xl = lsum + (nseg & 1) * 256;
       xl[s * 128 + r] = lsc;
       __syncwarp();
