@@ -608,6 +608,10 @@ SP_API sp_status sp_paged_append(const sp_paged_append_io* io, sp_stream stream)
  * Lengths are read on the device (they may change between replays of a graph);
  * the workspace depends on the arguments of its query alone and keeps nothing
  * (calls whose GPU work overlaps need one each).
+ * A call may have as much work as the arguments' limits allow while the sum, over
+ * the prefixes and the sequences, of (rows * n_heads + 128 n_kv_heads) *
+ * (keys + 1024) is at most 2^38 (its rows are those that read these keys); a call
+ * of several times that sets SP_DEVERR_INDEX and gives zeros and lse -infinity.
  * A NaN in a query, or in a key that it sees, makes that query's output and lse
  * NaN.
  * A NaN or infinity in V at a sequence's own position can also reach that

@@ -18,6 +18,9 @@
 namespace sp {
 
 constexpr int kPlanEntries = 2 * SP_MAX_BATCH;
+// Units of a plan, at most: they are counted in 32 bits.  Whether an entry's or all entries' are more is told from
+// counts of kCoarse units, rounded up.
+constexpr int kCoarse = 1 << 16, kMaxUnits = 32000 * kCoarse;
 
 struct PrefixArgs {
   const __nv_bfloat16* q;
@@ -49,8 +52,7 @@ struct PlanArgs {
   int min_shift;           // log2 of the units a worker takes at least (while there are enough)
   int workers;
   int max_items;           // items there is room for: no more exist while row and group offsets ascend (else, and
-                           // where an entry has over 2^31 / entries units, the launch covers nothing and reports
-                           // SP_DEVERR_INDEX)
+                           // with over kMaxUnits units in all, the launch covers nothing and reports SP_DEVERR_INDEX)
   bool prefix, own;        // which entries this launch covers
   int* unit0;              // [n_groups + B + 1] first unit of each entry, then N      (written for the merge)
   int* item0;              // [n_groups + B + 1] first item of each entry, then the item count
@@ -70,9 +72,11 @@ struct PlanShared {
   int unit0[kPlanEntries + 1];
   int item0[kPlanEntries + 1];
   int row0[kPlanEntries], rows[kPlanEntries], keys[kPlanEntries];
-  int2 wsum[32];  // a warp's items and units (a CTA has 32 warps at most)
+  uint2 wsum[32];  // a warp's items and units (a CTA has 32 warps at most)
+  unsigned int wcoarse[32];  // and its units in kCoarse
 };
 
+// (N is at most kMaxUnits)
 SP_DEVINL int plan_workers(const PlanArgs& p, int N) { return max(min(p.workers, (N + (1 << p.min_shift) - 1) >> p.min_shift), 1); }
 // First unit of worker w's part, floor(w N / P), without products over 32 bits (P is below 2^15).
 SP_DEVINL int part_begin(int N, int P, int w) {
@@ -92,9 +96,10 @@ SP_DEVINL void build_plan(const PrefixArgs& a, const PlanArgs& p, PlanShared& s,
   const int E = a.n_groups + a.B, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int G = a.Hq / a.Hkv;
   constexpr int PER = (kPlanEntries + NT - 1) / NT;
-  int t_sum = 0, i_sum = 0;
-  bool over = false;  // an entry with more units than its share of 2^31
-  int tl[PER];
+  int i_sum = 0;
+  unsigned int t_sum = 0;  // (may wrap where there are too many)
+  unsigned int coarse = 0;  // units in kCoarse, an entry's up to kMaxUnits / kCoarse + 1 (so that all entries' fit)
+  unsigned int tl[PER];
   int il[PER], r0[PER], r1[PER], len[PER];
   // every thread's loads at once, first those that others depend on (entries beyond the last: the last's again)
 #pragma unroll
@@ -112,7 +117,8 @@ SP_DEVINL void build_plan(const PrefixArgs& a, const PlanArgs& p, PlanShared& s,
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
     const int e = tid * PER + k;
-    int items = 0, units = 0;
+    int items = 0;
+    unsigned int units = 0;
     if (e < E) {
       const bool pre = e < a.n_groups;
       const int r = max(r1[k] - r0[k], 0);
@@ -126,8 +132,8 @@ SP_DEVINL void build_plan(const PrefixArgs& a, const PlanArgs& p, PlanShared& s,
         items = (r * G + p.tile_rows - 1) / p.tile_rows * a.Hkv;
         const int kt = (keys + (1 << p.key_shift) - 1) >> p.key_shift;
         const long long n = kt ? (long long)items * (kt + p.over) : 0;
-        if (n * E > 0x7fffffffll) over = true;
-        else units = (int)n;
+        units = (unsigned int)min(n, (long long)kMaxUnits);
+        coarse += (unsigned int)min((n + kCoarse - 1) / kCoarse, (long long)(kMaxUnits / kCoarse + 1));
       }
     }
     il[k] = items;
@@ -135,35 +141,43 @@ SP_DEVINL void build_plan(const PrefixArgs& a, const PlanArgs& p, PlanShared& s,
     i_sum += items;
     t_sum += units;
   }
-  int ix = i_sum, tx = t_sum;
+  int ix = i_sum;
+  unsigned int tx = t_sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int iu = __shfl_up_sync(0xffffffffu, ix, o), tu = __shfl_up_sync(0xffffffffu, tx, o);
+    const int iu = __shfl_up_sync(0xffffffffu, ix, o);
+    const unsigned int tu = __shfl_up_sync(0xffffffffu, tx, o);
     if (lane >= o) {
       ix += iu;
       tx += tu;
     }
   }
-  if (lane == 31) s.wsum[warp] = make_int2(ix, tx);
-  over = __syncthreads_or(over);
+  coarse = __reduce_add_sync(0xffffffffu, coarse);
+  if (lane == 31) {
+    s.wsum[warp] = make_uint2(ix, tx);
+    s.wcoarse[warp] = coarse;
+  }
+  __syncthreads();
   ix -= i_sum;
   tx -= t_sum;
   int total = 0;
+  coarse = 0;
 #pragma unroll
   for (int w = 0; w < NT / 32; ++w) {
-    const int2 x = s.wsum[w];
-    total += x.x;
-    ix += w < warp ? x.x : 0;
+    const uint2 x = s.wsum[w];
+    total += (int)x.x;
+    coarse += s.wcoarse[w];
+    ix += w < warp ? (int)x.x : 0;
     tx += w < warp ? x.y : 0;
   }
-  const bool fits = total <= p.max_items && !over;
+  const bool fits = total <= p.max_items && coarse <= kMaxUnits / kCoarse;
   if (!fits && write && tid == 0) set_error(a.err, SP_DEVERR_INDEX);
 #pragma unroll
   for (int k = 0; k <= PER; ++k) {  // (the total's place follows the last entry, maybe another thread's first)
     const int e = tid * PER + k;
     if (k < PER ? e <= E : (e == E && tid == NT - 1)) {
       const int i = fits ? ix : 0;
-      const int t = fits ? tx : 0;
+      const int t = fits ? (int)tx : 0;
       s.item0[e] = i;
       s.unit0[e] = t;
       if (write) {

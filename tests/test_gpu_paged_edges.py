@@ -94,3 +94,34 @@ def test_a_nan_own_key_gives_nan_where_it_is_seen(sp, dh, wide):
     assert torch.isnan(got[5:12]).all() and torch.isnan(gl[5:12]).all()
     keep = list(range(5)) + list(range(12, 36))
     assert torch.equal(got[keep], ref[keep]) and torch.equal(gl[keep], rl[keep])
+
+
+# ----------------------------------------------------------------------------- lengths
+
+def test_one_long_sequence_among_255_short_ones(sp):
+    """2,100 rows of 32 heads over 32,768 own keys (8.7 million tiles of 16 vectors by 16 keys) beside 255 single rows.
+    A segment's sums take up to 2,048 tiles one after the other, a rounding (2^-23, the tensor core's may cut off) each: 2^-12
+    of the weights' sum and of sum w |v| at most, beside P's bound for scores as small as these."""
+    g = gen(41)
+    Hq, dh, page, rows, keys = 32, 64, 256, 2100, 32768
+    n = [rows] + [1] * 255
+    lens = [keys] + [1 + (5 * i) % 60 for i in range(255)]
+    kv = normal(g, 2, 64, page, Hq * dh)
+    table = torch.randint(0, 64, (256, keys // page), device=DEV, generator=g, dtype=torch.int32)
+    q = normal(g, sum(n), Hq * dh)
+    lse = torch.zeros((sum(n), Hq), device=DEV)
+    r = sp.sp_prefix_attention(q=q, kv=kv, table=table, lens=ints(lens), cu_rows=starts(n), n_heads=Hq, n_kv_heads=Hq,
+                               head_dim=dh, lse=lse)
+    assert int(r["err"].item()) == 0
+    k = torch.arange(keys, device=DEV)
+    for b, picked in [(0, [0, 1, 700, 1555, rows - 1])] + [(b, [0]) for b in range(1, 256)]:
+        at = table[b, k[:lens[b]] // page].long(), k[:lens[b]] % page
+        K, V = (x[at].double().view(-1, Hq, dh) for x in kv)
+        for j in picked:
+            row = j if b == 0 else rows + b - 1
+            see = lens[b] - n[b] + j + 1
+            z = torch.einsum("hd,khd->hk", q[row].double().view(Hq, dh), K[:see]) * dh ** -0.5
+            w = torch.softmax(z, dim=-1)
+            o, size = (torch.einsum("hk,khd->hd", w, x[:see]).reshape(-1) for x in (V, V.abs()))
+            assert ((r["out"][row].double() - o).abs() <= U * o.abs() + (U + 2.0 ** -11) * size).all(), (b, j)
+            assert ((lse[row].double() - torch.logsumexp(z, dim=-1)).abs() <= 2.0 ** -12).all()
