@@ -660,13 +660,14 @@ SP_API sp_status sp_prefill_paged(const sp_model* m, const sp_prefill_io* io, co
 
 /*
  * One generation step over pages, sequences sharing prefixes: the layers of
- * sp_decode applied to the new token x[b] of every sequence, its keys and values
- * appended at the sequence's own position lens[b] (sp_paged_append) and its
- * attention over its group's prefix and its own pages (sp_prefix_attention).
+ * sp_decode applied to the new token x[b] of every sequence (queries and keys
+ * rotated in fp32 and rounded once, as there), its keys and values appended at
+ * the sequence's own position lens[b] (sp_paged_append) and its attention over
+ * its group's prefix and its own pages (sp_prefix_attention).
  * lens and rope_pos are then incremented on the device, so steps chain.  (After a
  * prefix of L positions rope_pos starts at L, after an mRoPE prefix at the
- * position its next text token takes.)  A position outside the table sets
- * SP_DEVERR_INDEX and is not written.
+ * position its next text token takes.)  A position outside the table, or a rotary
+ * position outside 0..max_pos-1, sets SP_DEVERR_INDEX and is not written.
  */
 typedef struct {
   int B;                    /* sequences, 1..SP_MAX_BATCH */

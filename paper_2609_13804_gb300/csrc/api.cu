@@ -1425,14 +1425,16 @@ static sp_status decode_paged_impl(const sp_model* m, const sp_decode_paged_io* 
   const int qkvw = (c.n_heads + 2 * c.n_kv_heads) * c.head_dim;
   SP_CUDA(lens_plus_one(io->lens, q.lens1, B, st), "lens");
   GemmEpi eq;
-  eq.kind = EPI_BF16;
+  eq.kind = EPI_BF16_ROPE;  // (rotated in fp32 and rounded once, as in the prefill and the dense step)
   eq.out = p.qkv;
   eq.ldo = qkvw;
+  eq.rope = m->rope;
+  eq.pos = io->rope_pos;
+  eq.max_pos = c.max_pos;
+  eq.head_dim = c.head_dim;
+  eq.rope_cols = (c.n_heads + c.n_kv_heads) * c.head_dim;
   PagedAppendArgs pa = append_args(m, pg, p.qkv, B, B, nullptr, io->lens, io->err);
-  pa.q_out = static_cast<__nv_bfloat16*>(p.qkv);  // (queries in place)
-  pa.ld_q = qkvw;
-  pa.rope = m->rope;
-  pa.max_pos = c.max_pos;
+  pa.max_pos = c.max_pos;  // (a position outside the rotary table is not cached)
   pa.pos = io->rope_pos;
   PrefixAttention at = {};
   at.q = p.qkv;

@@ -334,7 +334,7 @@ struct PagedAppendArgs {
   int B, T_cap, Hq, Hkv, dh;
   const float2* rope;    // [max_pos, dh / 2] (cos, sin), NULL: no rotation
   int max_pos;
-  const int* pos;
+  const int* pos;        // rotary positions, checked against max_pos (without rope too); both NULL: none
   const int* pos3;       // [T_cap, 4]
   int sec1, sec2;        // pos3: pairs below sec1 take its first component, below sec2 its second
   int* err;

@@ -68,7 +68,7 @@ __global__ void __launch_bounds__(PA_NT) paged_append_kernel(const PagedAppendAr
     }
     dst += c * 8;
     uint4 olo = lo, ohi = hi;
-    if (a.rope) {  // (a value head checks the position too: a row is skipped whole)
+    if (a.pos || a.pos3) {  // (a value head checks the position too: a row is skipped whole)
       int pt, ph, pw;
       if (a.pos3) {
         const int4 q = __ldg(reinterpret_cast<const int4*>(a.pos3) + row);
@@ -80,7 +80,7 @@ __global__ void __launch_bounds__(PA_NT) paged_append_kernel(const PagedAppendAr
         if (c == 0) set_error(a.err, SP_DEVERR_INDEX);
         continue;
       }
-      if (head < a.Hq + a.Hkv) {
+      if (a.rope && head < a.Hq + a.Hkv) {
         const uint32_t xl[4] = {lo.x, lo.y, lo.z, lo.w}, xh[4] = {hi.x, hi.y, hi.z, hi.w};
         uint32_t yl[4], yh[4];
 #pragma unroll

@@ -85,8 +85,8 @@ sp_status sp_paged_append(const sp_paged_append_io* io, sp_stream stream) {
   a.dh = io->head_dim;
   a.rope = reinterpret_cast<const float2*>(io->rope);
   a.max_pos = io->max_pos;
-  a.pos = io->pos;
-  a.pos3 = io->pos3;
+  a.pos = io->rope ? io->pos : nullptr;
+  a.pos3 = io->rope ? io->pos3 : nullptr;
   a.sec1 = io->pos3 ? sec[0] : 0;
   a.sec2 = io->pos3 ? sec[0] + sec[1] : 0;
   a.err = io->err;

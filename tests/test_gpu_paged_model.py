@@ -1,10 +1,9 @@
 """The model over a paged cache: sp_prefill_paged and sp_decode_paged against sp_prefill and the oracle, and beams
 generated with them, sp_beam_select and sp_beam_reorder.
 
-sp_prefill_paged does the arithmetic of sp_prefill: equal bits.  sp_decode_paged rounds queries and keys to bf16
-before their rotation as well as after it: one more half step (2^-9 relative) of q and k than the oracle takes, which
-moves a score by at most 2^-8 sum |q_i k_i| scale and the hidden state by a like part of the attention's contribution,
-inside the bounds of hidden_close, which hold a whole layer's bf16 roundings."""
+sp_prefill_paged does the arithmetic of sp_prefill: equal bits.  sp_decode_paged does that of sp_decode up to the
+attention, which weighs and adds in another order; both are inside the bounds of hidden_close, which hold a whole
+layer's bf16 roundings."""
 import numpy as np
 import pytest
 

@@ -1,0 +1,46 @@
+"""The model over a paged cache, where test_gpu_paged_model.py does not reach: bits of the cached keys, wide tables."""
+import numpy as np
+import pytest
+
+from oracle import core as O
+from paper_2609_13804_gb300 import synth as S
+
+import _parity as PT
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from test_gpu_paged_model import B, DEV, _model, _prefill, ints, single_precision  # noqa: E402, F401
+
+
+@pytest.mark.parametrize("heads", [(4, 2, 64), (2, 2, 128)])
+def test_the_step_caches_the_dense_steps_keys(B, heads):
+    """The first layer's new keys and values are those of sp_decode to the bit: rotated before they are rounded."""
+    w, layers, head, model = _model(B, 15, *heads, n_layers=1)
+    m, page, lens = w.model, 16, [5, 16, 40]
+    _, _, _, kv, table, args, _ = _prefill(B, w, model, lens, page)
+    dense = B.kv_cache(model, 3, 80)
+    B.sp_prefill(model, kv=dense, **args)
+    x = B.dev_bf16(S.bf16_round(S.normal(w.seed, "new", (3, m.d), 0.5)), DEV)
+    B.sp_decode(model, x=x, lens=ints(lens), kv=dense, max_len_cap=80)
+    o = B.sp_decode_paged(model, x=x, lens=ints(lens), rope_pos=ints(lens), kv=kv, table=table)
+    assert int(o["err"].item()) == 0
+    for b, n in enumerate(lens):
+        assert torch.equal(kv[:, :, int(table[b, n // page]), n % page], dense[:, :, b, n])
+    model.close()
+
+
+def test_a_rotary_position_outside_the_table_leaves_the_cache(B):
+    w, layers, head, model = _model(B, 16, 4, 2, 64, max_pos=64)
+    m, page, lens = w.model, 16, [5, 16, 9]
+    _, _, _, kv, table, _, _ = _prefill(B, w, model, lens, page)
+    before = kv.clone()
+    x = B.dev_bf16(S.bf16_round(S.normal(w.seed, "new", (3, m.d), 0.5)), DEV)
+    o = B.sp_decode_paged(model, x=x, lens=ints(lens), rope_pos=ints([64, 16, -1]), kv=kv, table=table)
+    assert int(o["err"].item()) == 2
+    changed = [(int(table[1, 1]), 0)]
+    for pg, r in changed:
+        assert not torch.equal(kv[:, :, pg, r], before[:, :, pg, r])
+        before[:, :, pg, r] = kv[:, :, pg, r]
+    assert torch.equal(kv, before)
+    model.close()
