@@ -1,13 +1,15 @@
 """Thin ctypes binding of libstepprune (include/stepprune.h).
 
 Argument marshalling only: every computation runs in the library's CUDA
-kernels.  PyTorch supplies device memory and streams.  The library is loaded on
+kernels.  PyTorch supplies device memory and streams; what a call with a
+`stream` (a torch stream or its handle) returns was allocated on that stream.  The library is loaded on
 first use; if it has not been built (paper_2609_13804_gb300.build) the call
 raises instead of falling back to anything else.
 """
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 import struct
 from typing import Dict, List, Optional, Sequence
@@ -285,6 +287,24 @@ def _stream(stream) -> Optional[int]:
     return stream.cuda_stream
 
 
+def _on_its_stream(call):
+    """Makes the stream that a call is given torch's current one while the call runs: what it allocates and clears then
+    belongs to that stream, in order with its kernels."""
+    @functools.wraps(call)
+    def on_stream(*args, stream=None, **kw):
+        if stream is None:
+            return call(*args, **kw)
+        torch = _torch()
+        if not isinstance(stream, torch.cuda.Stream):
+            handle = stream if isinstance(stream, int) else stream.cuda_stream
+            dev = next((d for d in (getattr(a, "device", None) for a in (*args, *kw.values()))
+                        if getattr(d, "type", None) == "cuda"), None)
+            stream = torch.cuda.ExternalStream(handle, device=dev) if handle else torch.cuda.default_stream(dev)
+        with torch.cuda.stream(stream):
+            return call(*args, stream=stream, **kw)
+    return on_stream
+
+
 def workspace(nbytes: int, device):
     torch = _torch()
     return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
@@ -379,6 +399,7 @@ def _select_in(n_vis, n_txt, X, E_text, H, stop_bias, group_size, g, k_max, keep
                         int(group_size), int(g), int(k_max))
 
 
+@_on_its_stream
 def sp_select(sel: Selector, n_vis, n_txt, *, stop_bias, X=None, E_text=None, H=None, group_size=0, g=1,
               k_max=192, k_cap=None, traces=True, memory=False, stream=None, ws=None,
               no_alloc=False, train=None) -> Dict:
@@ -430,6 +451,7 @@ def sp_select(sel: Selector, n_vis, n_txt, *, stop_bias, X=None, E_text=None, H=
     return out
 
 
+@_on_its_stream
 def sp_soft_topk(n_vis, *, score, kbar, tau, group_size=0, stream=None, alpha=None) -> Dict:
     """Eq. 8 per image (k = the batch mean of the images' soft counts); returns
     alpha [sum N_b] fp32 and k [1] fp32 (device tensors)."""
@@ -444,6 +466,7 @@ def sp_soft_topk(n_vis, *, score, kbar, tau, group_size=0, stream=None, alpha=No
     return {"alpha": alpha, "k": k}
 
 
+@_on_its_stream
 def sp_vp_gate(*, X, noise, alpha, out=None, stream=None):
     """Eq. 9 on bf16 rows: out = sqrt(alpha) X + sqrt(1 - alpha) noise."""
     torch = _torch()
@@ -457,6 +480,7 @@ def sp_vp_gate(*, X, noise, alpha, out=None, stream=None):
 
 # ----------------------------------------------------------------------------- compaction
 
+@_on_its_stream
 def sp_compact(n_vis, n_txt, *, X, text, idx, count, k_cap, projector_mode=False, index_mode=False, stream=None,
                out: Optional[Dict] = None) -> Dict:
     """Compaction into new zero-filled outputs, or into `out` (a dict a
@@ -548,6 +572,7 @@ class Model:
             pass
 
 
+@_on_its_stream
 def sp_project(model: Model, *, vis_row_map, vis_cu, packed, rows_cap, B, vis_packed=None, X=None, vis_src=None,
                stream=None, ws=None):
     """The projector on the kept rows: from vis_packed (projector-mode
@@ -570,6 +595,7 @@ def kv_cache(model: Model, B: int, S_cap: int, device=None):
                        device=device or model.device)
 
 
+@_on_its_stream
 def sp_prefill(model: Model, *, x, cu_seqlens, pos, B, T_cap, max_seqlen_cap, residual=None, stream=None,
                ws=None, hidden=None, kv=None, pos3=None):
     torch = _torch()
@@ -585,6 +611,7 @@ def sp_prefill(model: Model, *, x, cu_seqlens, pos, B, T_cap, max_seqlen_cap, re
     return {"hidden": hidden, "err": err, "_ws": ws}
 
 
+@_on_its_stream
 def sp_decode(model: Model, *, x, lens, kv, max_len_cap, stream=None, ws=None, hidden=None, rope_pos=None) -> Dict:
     """One generation step: x [B, d] bf16 new tokens, lens [B] int32 cached lengths
     (incremented on the device), kv the cache of kv_cache() / sp_prefill;
@@ -603,6 +630,7 @@ def sp_decode(model: Model, *, x, lens, kv, max_len_cap, stream=None, ws=None, h
     return {"hidden": hidden, "err": err, "_ws": ws}
 
 
+@_on_its_stream
 def sp_mrope_positions(n_vis, n_txt, grid_w, *, idx, count, k_cap, T_cap, stream=None, pos3=None, err=None):
     """(t, h, w) rotary positions [T_cap, 4] int32 of the packed, pruned batch."""
     torch = _torch()
@@ -718,6 +746,7 @@ def paged_pool(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, n_l
     return torch.zeros((n_layers, 2, n_pages, page_size, n_kv_heads * head_dim), dtype=torch.bfloat16, device=device)
 
 
+@_on_its_stream
 def sp_paged_append(*, qkv, kv, table, n_heads, n_kv_heads, head_dim, lens=None, cu_rows=None, rope=None, pos=None,
                     pos3=None, mrope_section=None, q_out=None, keys_only=False, err=None, stream=None) -> Dict:
     """Rows q | k | v [T, (n_heads + 2 n_kv_heads) head_dim] into the pages of kv (one layer's pool): row j of
@@ -768,6 +797,7 @@ def prefix_attention_workspace(*, T_cap, B, n_heads, n_kv_heads, head_dim, n_gro
     return workspace(n, device)
 
 
+@_on_its_stream
 def sp_prefix_attention(*, q, kv, table, lens, n_heads, n_kv_heads, head_dim, prefix_table=None, prefix_lens=None,
                         group_cu=None, cu_rows=None, scale=0.0, out=None, lse=None, ws=None, err=None,
                         stream=None) -> Dict:
@@ -812,6 +842,7 @@ def sp_prefix_attention(*, q, kv, table, lens, n_heads, n_kv_heads, head_dim, pr
     return {"out": out, "lse": lse, "err": err, "_ws": ws}
 
 
+@_on_its_stream
 def sp_prefill_paged(model: Model, *, x, cu_seqlens, pos, B, T_cap, max_seqlen_cap, kv, table, residual=None,
                      stream=None, ws=None, hidden=None, pos3=None, err=None) -> Dict:
     """sp_prefill with the keys and values put into pages: kv [n_layers, 2, n_pages, page_size, width] (paged_pool),
@@ -840,6 +871,7 @@ def sp_prefill_paged(model: Model, *, x, cu_seqlens, pos, B, T_cap, max_seqlen_c
     return {"hidden": hidden, "err": err, "_ws": ws}
 
 
+@_on_its_stream
 def sp_decode_paged(model: Model, *, x, lens, rope_pos, kv, table, prefix_table=None, prefix_lens=None, group_cu=None,
                     hidden=None, ws=None, err=None, stream=None) -> Dict:
     """One generation step over pages: x [B, d] bf16 new tokens, lens / rope_pos [B] int32 own cached positions and
@@ -889,6 +921,7 @@ def beam_select_workspace(*, B, W, V, n_out, device="cuda"):
     return workspace(n, device)
 
 
+@_on_its_stream
 def sp_beam_select(*, logits, cum, n_out, done=None, eos=0, score=None, parent=None, token=None, ws=None,
                    stream=None) -> Dict:
     """The n_out best continuations of every element's beams: logits [B, W, V] fp32 or bf16 (rows may lie apart),
@@ -942,6 +975,7 @@ def sp_beam_select(*, logits, cum, n_out, done=None, eos=0, score=None, parent=N
     return {"score": score, "parent": parent, "token": token, "_ws": ws}
 
 
+@_on_its_stream
 def sp_beam_reorder(*, kv, table, own_table, lens, parent, err=None, stream=None):
     """Puts the cache into the beams' new order: table rows and the rows of the partly filled pages of all layers
     (kv [n_layers, 2, n_pages, page_size, width]) follow parent [B, W or more] (its first W columns); table is
@@ -1008,6 +1042,7 @@ class Pipeline:
         _check(lib().sp_pipeline(self.sel.handle, self.model.handle, C.byref(io), ptr(self.ws), self.ws.numel(),
                                  _stream(stream)), "sp_pipeline")
 
+    @_on_its_stream
     def host(self, X_host, E_host, bias_host, out_idx, out_count, out_cu, out_hidden, stream=None):
         """sp_pipeline_host on (pinned) host tensors; outputs written to host tensors."""
         torch = _torch()
