@@ -694,9 +694,10 @@ SP_API sp_status sp_decode_paged(const sp_model* m, const sp_decode_paged_io* io
  *   cum[w] + log softmax(logits[w])[v],
  * best first.  Scores are compared in 64 bits; equal ones go to the lower beam,
  * then the lower token (within a beam the order is that of the logits).  A
- * row's sum is taken in fp32, in an order that depends on its first logit's
- * place within 16 bytes: rows of equal logits have equal scores when they lie
- * alike (ld and logits multiples of 16 bytes), else to that sum's rounding.
+ * row's sum is taken in fp32, good to about 2^-20 of it: scores of two beams that
+ * are nearer than that can change places.  Beams of an element with equal logits
+ * have equal sums, to the bit.  (Row strides that are no multiple of 16 bytes take
+ * up to a quarter longer.)
  *   - A beam with cum -infinity (or NaN) is not alive: it proposes nothing.
  *   - A finished beam (done != 0) proposes only itself: token eos, score cum;
  *     its logits are not read.

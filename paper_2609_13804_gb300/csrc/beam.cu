@@ -5,9 +5,9 @@
 // Within a beam the order is that of the logits, so one pass over a row finds its m, its sum and its n_out
 // largest logits together; which beams they came from matters only for the n_out best of each row, whose
 // scores are formed and compared in 64 bits (two beams' scores can be nearer than fp32 tells apart).  Equal
-// ones: the lower beam, then the lower token.  (The sum's order follows the 16-byte pieces of the row, so equal rows
-// that start at different places within 16 bytes can differ in its last bits.  Pieces by token instead would have every
-// thread put each from two loads.)
+// ones: the lower beam, then the lower token.  Equal rows have equal scores, to the bit: their logits are added in the same
+// order, by pieces of 16 bytes.  Where the rows of a call begin at different places within 16 bytes these are pieces of
+// the row, each put together from two aligned loads, else the aligned pieces.
 #include <algorithm>
 
 #include "common.cuh"
@@ -86,6 +86,15 @@ struct Chunk<false> {
   }
 };
 
+// 16 bytes that begin WORD words and `bits` bits into a, and go on in b
+template <bool F32, int WORD>
+SP_DEVINL uint4 piece_at(const uint4& a, const uint4& b, uint32_t bits) {
+  const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  if (F32) return make_uint4(w[WORD], w[WORD + 1], w[WORD + 2], w[WORD + 3]);
+  return make_uint4(__funnelshift_r(w[WORD], w[WORD + 1], bits), __funnelshift_r(w[WORD + 1], w[WORD + 2], bits),
+                    __funnelshift_r(w[WORD + 2], w[WORD + 3], bits), __funnelshift_r(w[WORD + 3], w[WORD + 4], bits));
+}
+
 // Two fp32 numbers as one operand of Blackwell's packed arithmetic
 SP_DEVINL unsigned long long pack2(float lo, float hi) {
   unsigned long long r;
@@ -141,15 +150,20 @@ __device__ __noinline__ int cut_list(unsigned long long* list, int n, int n_out)
 // in order, and (m, sum) go to part.
 // Bound by issue (some 6 instructions a logit with the exponential's) and by what a slice costs besides, about 3 us:
 // 256 rows of 152,064 bf16 logits, a fifth of them finished, 62 MB, 18 us (3.4 TB/s); 4 rows of 32,000 fp32 3.5 us.
-template <bool F32>
-__global__ void __launch_bounds__(BS_NT, 3)
+// SHIFT: the rows begin at different places within 16 bytes.  The aligned pieces go through the ring as they lie; a
+// lane puts each of its pieces from its own and the next lane's (the warp's last from a piece loaded beside).  Both
+// kernels, 64 x 4 rows of 152,063 bf16 logits 29.4 us (23.1 by aligned pieces, which tie by where a row lies), 16 x 4 of
+// 50,257 fp32 14.0 (12.2): some 45 instructions more for 32 or 16 logits of a thread.
+template <bool F32, bool SHIFT>
+__global__ void __launch_bounds__(BS_NT, SHIFT ? 2 : 3)
 beam_scan_kernel(const void* __restrict__ logits, long long ld, int V, const float* __restrict__ cum,
                  const unsigned char* __restrict__ done, int n_out, int slice, float2* __restrict__ part_ms,
                  unsigned long long* __restrict__ part_key) {
   using K = Chunk<F32>;
   __shared__ unsigned long long list_s[BS_WARPS][BS_CAP];
   __shared__ unsigned long long list_all[BS_WARPS * 32];
-  extern __shared__ uint4 ring[];  // [BS_RING][BS_LOADS][BS_NT]: a thread's own loads, read by itself only
+  extern __shared__ uint4 ring[];  // [BS_RING][BS_LOADS][BS_NT]: a thread's own loads (SHIFT: read by the lane before too)
+  uint4* beside = ring + BS_RING * BS_LOADS * BS_NT;  // SHIFT: [BS_RING][BS_WARPS][BS_LOADS] behind each warp's loads
   __shared__ float2 ms_s[BS_WARPS];
   __shared__ float tile_max[BS_BLOCK][BS_NT];
   __shared__ uint32_t bound_s[2][BS_WARPS];
@@ -164,7 +178,8 @@ beam_scan_kernel(const void* __restrict__ logits, long long ld, int V, const flo
   const char* base = static_cast<const char*>(logits) + row * ld * esz;
   const int v0 = min(blockIdx.x * slice, V), v1 = min(v0 + slice, V);
   // whole 16-byte chunks of the slice; what is before and behind them goes one by one
-  const int head = min((int)((16 - (reinterpret_cast<uintptr_t>(base + (size_t)v0 * esz) & 15)) & 15) / esz, v1 - v0);
+  const uint32_t off = reinterpret_cast<uintptr_t>(base + (size_t)v0 * esz) & 15;  // (the same for all slices of a row)
+  const int head = SHIFT ? 0 : min((int)((16 - off) & 15) / esz, v1 - v0);
   const int c0 = v0 + head, chunks = (v1 - c0) / K::N, c1 = c0 + chunks * K::N;
   unsigned long long* list = list_s[warp];
   int n = 0;
@@ -182,17 +197,34 @@ beam_scan_kernel(const void* __restrict__ logits, long long ld, int V, const flo
     }
     n = __popc(all);
   }
-  const uint4* src = reinterpret_cast<const uint4*>(base + (size_t)c0 * esz);
+  const uint4* src = reinterpret_cast<const uint4*>(base + (size_t)c0 * esz - (SHIFT ? off : 0));
   unsigned long long T = 0;  // keys above T are candidates
   const int tile_chunks = BS_NT * BS_LOADS;
+  // SHIFT: aligned piece c, as far as it holds the slice's chunks (0 .. chunks - 1 begin in it, the last ends in the next)
+  auto part = [&](uint4* to, int c) {
+    const uint32_t n = c < chunks ? 16 : c == chunks && c > 0 ? off : 0;
+    if (n) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(src + c), "r"(n) : "memory");
+  };
   auto load = [&](int t) {  // (what lies past the slice is not loaded, and read as -infinity)
     uint4* to = ring + (t % BS_RING) * (BS_LOADS * BS_NT) + tid;
 #pragma unroll
     for (int q = 0; q < BS_LOADS; ++q) {
       const int c = t * tile_chunks + q * BS_NT + tid;
-      if (c < chunks)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to + q * BS_NT)), "l"(src + c) : "memory");
+      if (!SHIFT) {
+        if (c < chunks)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to + q * BS_NT)), "l"(src + c) : "memory");
+      } else if (c == 0 && chunks > 0 && off != 0 && row == 0 && v0 == 0) {
+        // (what lies before the first row may be no one's: its first piece is put there by elements)
+        for (int k = off / esz; k < K::N; ++k) {
+          if (F32) reinterpret_cast<float*>(to)[k] = reinterpret_cast<const float*>(base)[k - off / esz];
+          else reinterpret_cast<__nv_bfloat16*>(to)[k] = reinterpret_cast<const __nv_bfloat16*>(base)[k - off / esz];
+        }
+      } else {
+        part(to + q * BS_NT, c);
+      }
     }
+    if (SHIFT && off != 0 && lane < BS_LOADS)
+      part(beside + ((t % BS_RING) * BS_WARPS + warp) * BS_LOADS + lane, t * tile_chunks + lane * BS_NT + (warp + 1) * 32);
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
   const int tiles = (chunks + tile_chunks - 1) / tile_chunks;
@@ -247,12 +279,29 @@ beam_scan_kernel(const void* __restrict__ logits, long long ld, int V, const flo
     const int te = min(tb + BS_BLOCK, tiles);
     bm = -INFINITY;
     for (int t = tb; t < te; ++t) {
+      if (SHIFT) __syncwarp();  // the tile that is overwritten has been read by the lanes before
       load(t + BS_RING - 1);
       asm volatile("cp.async.wait_group %0;" ::"n"(BS_RING - 1) : "memory");
       const uint4* from = ring + (t % BS_RING) * (BS_LOADS * BS_NT) + tid;
       uint4 u[BS_LOADS];
 #pragma unroll
       for (int q = 0; q < BS_LOADS; ++q) u[q] = from[q * BS_NT];
+      if (SHIFT && off != 0) {
+        __syncwarp();  // the next lane's loads have landed
+        const uint4* next = lane < 31 ? from + 1 : beside + ((t % BS_RING) * BS_WARPS + warp) * BS_LOADS;
+        const int step = lane < 31 ? BS_NT : 1;
+        const uint32_t bits = (off & 2) * 8;
+        uint4 b[BS_LOADS];
+#pragma unroll
+        for (int q = 0; q < BS_LOADS; ++q) b[q] = next[q * step];
+#pragma unroll
+        for (int q = 0; q < BS_LOADS; ++q) {
+          if (off < 4) u[q] = piece_at<F32, 0>(u[q], b[q], bits);  // (off is the CTA's)
+          else if (off < 8) u[q] = piece_at<F32, 1>(u[q], b[q], bits);
+          else if (off < 12) u[q] = piece_at<F32, 2>(u[q], b[q], bits);
+          else u[q] = piece_at<F32, 3>(u[q], b[q], bits);
+        }
+      }
       if (t == tiles - 1) {
 #pragma unroll
         for (int q = 0; q < BS_LOADS; ++q)
@@ -599,10 +648,13 @@ cudaError_t beam_select_launch(const void* logits, bool f32, long long ld, int B
   auto* ms = static_cast<float2*>(ws);
   auto* key = reinterpret_cast<unsigned long long*>(static_cast<char*>(ws) + (((size_t)rows * S * 8 + 255) & ~size_t(255)));
   prof_begin_launch(st);
-  auto* scan = f32 ? beam_scan_kernel<true> : beam_scan_kernel<false>;
-  constexpr int ring = BS_RING * BS_LOADS * BS_NT * 16;
-  static std::atomic<unsigned long long> allowed[2];
-  cudaError_t r = allow_smem(scan, ring, allowed[f32]);
+  // (beams of one element whose rows begin at different places within 16 bytes)
+  const bool shift = W > 1 && ld * (f32 ? 4 : 2) % 16 != 0;
+  auto* scan = f32 ? (shift ? beam_scan_kernel<true, true> : beam_scan_kernel<true, false>)
+                   : (shift ? beam_scan_kernel<false, true> : beam_scan_kernel<false, false>);
+  const int ring = (BS_RING * BS_LOADS * BS_NT + (shift ? BS_RING * BS_WARPS * BS_LOADS : 0)) * 16;
+  static std::atomic<unsigned long long> allowed[2][2];
+  cudaError_t r = allow_smem(scan, ring, allowed[f32][shift]);
   if (r == cudaSuccess)
     r = launch_pdl(scan, dim3(S, rows), dim3(BS_NT), (size_t)ring, st, logits, ld, V, cum, done, n_out, slice, ms, key);
   prof_end_launch(st, SP_K_MISC, 0.0, (double)rows * V * (f32 ? 4 : 2));

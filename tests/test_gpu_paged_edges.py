@@ -125,3 +125,30 @@ def test_one_long_sequence_among_255_short_ones(sp):
             o, size = (torch.einsum("hk,khd->hd", w, x[:see]).reshape(-1) for x in (V, V.abs()))
             assert ((r["out"][row].double() - o).abs() <= U * o.abs() + (U + 2.0 ** -11) * size).all(), (b, j)
             assert ((lse[row].double() - torch.logsumexp(z, dim=-1)).abs() <= 2.0 ** -12).all()
+
+
+# ----------------------------------------------------------------------------- equal beams
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [5, 700, 1001, 2049, 32003, 152063])
+def test_equal_beams_tie_wherever_their_rows_begin(sp, V, dtype):
+    """Rows of equal logits have equal sums, and a tie goes to the lower beam, although rows of V elements begin at
+    different places within 16 bytes."""
+    g = gen(V)
+    x = (3 * torch.randn((2, 1, V), device=DEV, generator=g)).to(dtype).expand(2, 4, V).contiguous()
+    P.select_case(sp, x, torch.zeros((2, 4), device=DEV), 8)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("skip", [1, 2, 3, 5, 7])
+def test_equal_beams_of_rows_apart_and_a_first_row_off_16_bytes(sp, skip, dtype):
+    g = gen(skip)
+    for V, ld in ((9000, 9001 + skip), (4095, 4103), (40, 47)):
+        full = torch.full((1 + 3 * 5 * ld + ld,), torch.nan, device=DEV, dtype=dtype)
+        x = full[skip:skip + 15 * ld].view(3, 5, ld)[..., :V]
+        x.copy_((3 * torch.randn((3, 1, V), device=DEV, generator=g)).to(dtype))
+        x[1, :, ::3] = torch.nan
+        x[1, :, 1::7] = -torch.inf
+        x[2, :, V // 2] = torch.inf
+        cum = torch.full((3, 5), -1.5, device=DEV)
+        P.select_case(sp, x, cum, 10)
