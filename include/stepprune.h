@@ -700,7 +700,7 @@ SP_API sp_status sp_decode_paged(const sp_model* m, const sp_decode_paged_io* io
  * up to a quarter longer.)
  *   - A beam with cum -infinity (or NaN) is not alive: it proposes nothing.
  *   - A finished beam (done != 0) proposes only itself: token eos, score cum;
- *     its logits are not read.
+ *     its logits have no effect, whatever they hold (some of them are read).
  *   - NaN and -infinity logits have no weight and are never chosen; a row with
  *     +infinity spreads its weight over them (the softmax's limit).
  * Places for which no continuation is left get score -infinity, parent and

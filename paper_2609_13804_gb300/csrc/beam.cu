@@ -271,7 +271,9 @@ beam_scan_kernel(const void* __restrict__ logits, long long ld, int V, const flo
   };
 #pragma unroll
   for (int t = 0; t < BS_RING - 1; ++t) load(t);
-  if (over || !(cw > -INFINITY)) {  // (the join reads nothing of such a beam's row)
+  // (The join reads nothing of such a beam's row.  Told before the first loads, it would cost the others the wait for
+  // done and cum: four rows of 32,000 fp32 logits 7.9 us instead of 7.7.)
+  if (over || !(cw > -INFINITY)) {
     asm volatile("cp.async.wait_all;" ::: "memory");
     return;
   }
