@@ -177,6 +177,7 @@ prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tslot;
+  // in this order: the kernel behind this one may read its inputs without a wait of its own (prefix_warp_kernel, late)
   pdl_wait();
   pdl_trigger();
   build_plan<TC_NT>(a, p, plan, blockIdx.x == 0);

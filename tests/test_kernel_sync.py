@@ -47,3 +47,47 @@ def test_warp_waits_order_the_other_lanes():
             found.append(m.group(1))
             assert re.search(r"__syncwarp\(\);\s*return __shfl_sync\([^;]*;\s*\}$", m.group(0)), m.group(1)
     assert "mbar_wait_warp" in found and "mbar_poll_cluster_warp" in found
+
+
+def _kernel(text, kernel):
+    """The text of a kernel's body."""
+    text = text[re.search(r"\b%s\([^;]*?\)\s*\{" % kernel, text).end():]
+    depth = 1
+    for i, ch in enumerate(text):
+        depth += (ch == "{") - (ch == "}")
+        if depth == 0:
+            return text[:i]
+    raise AssertionError("no end of " + kernel)
+
+
+def _waits_first(body):
+    """Whether every thread waits for the kernel before this one, outside any condition, before the first trigger."""
+    wait = re.search(r"(?:^|[;{}])\s*pdl_wait\(\);", body)
+    trigger = re.search(r"\bpdl_trigger\(\);", body)
+    if wait is None or (trigger is not None and trigger.start() < wait.end() - 1):
+        return False
+    return body[:wait.end()].count("{") == body[:wait.end()].count("}")
+
+
+def test_what_runs_beside_the_tensor_kernel_finds_its_inputs_complete():
+    """prefix_warp_kernel behind prefix_tc_kernel (`late`) reads queries, lengths, tables and pages before any wait of its
+    own.  What wrote them is complete because the tensor kernel waits before it lets the next kernel start; the warp
+    kernel's own end waits for the tensor kernel, so that the merge finds both complete."""
+    tc, warp = _kernel(_source("prefix_attn_tc.cu"), "prefix_tc_kernel"), _kernel(_source("prefix_attn.cu"), "prefix_warp_kernel")
+    assert _waits_first(tc), "the tensor kernel lets the warp kernel start before what came before is complete"
+    assert not _waits_first(re.sub(r"pdl_wait\(\);\s*pdl_trigger\(\);", "pdl_trigger(); pdl_wait();", tc))
+    assert not _waits_first(tc.replace("pdl_wait();", "if (warp == 0) pdl_wait();"))
+    first = re.search(r"pdl_\w+\(\);", warp)
+    assert warp[:first.end()].rstrip().endswith("if (!late) pdl_wait();")
+    assert re.search(r"if \(late\) pdl_wait\(\);\s*$", warp), "the merge would not wait for the tensor kernel"
+    calls = _source("prefix_attn.cu")
+    calls = calls[calls.index("prefix_attention_launch("):]
+    assert calls.index("prefix_tc_launch(") < calls.index("prefix_warp_kernel<128>") and "L.tc.workers ? 1 : 0)" in calls
+    assert _waits_first(_kernel(_source("prefix_attn.cu"), "prefix_merge_kernel"))
+
+
+@pytest.mark.parametrize("name,kernel", [("prefix_attn.cu", "prefix_row_kernel"), ("paged.cu", "paged_append_kernel"),
+                                         ("beam.cu", "beam_scan_kernel"), ("beam.cu", "beam_join_kernel"),
+                                         ("beam.cu", "beam_reorder_kernel")])
+def test_paged_kernels_wait_before_they_let_the_next_start(name, kernel):
+    assert _waits_first(_kernel(_source(name), kernel))
