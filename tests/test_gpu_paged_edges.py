@@ -152,3 +152,49 @@ def test_equal_beams_of_rows_apart_and_a_first_row_off_16_bytes(sp, skip, dtype)
         x[2, :, V // 2] = torch.inf
         cum = torch.full((3, 5), -1.5, device=DEV)
         P.select_case(sp, x, cum, 10)
+
+
+# ----------------------------------------------------------------------------- rising scores, long items
+
+def rising_call(sp, seed, heads, rows, own, prefix, *, top, page=64):
+    """One call whose scores rise from 0 to about `top` along the prefix (each key of it a little above those before),
+    compared with the plain form.  Scores stay within the 64 that the bound is derived for."""
+    Hq, Hkv, dh = heads
+    g = gen(seed)
+    both, pages = tables(g, own + [prefix], page)
+    kv = normal(g, 2, pages, page, Hkv * dh, std=0.3)
+    u = torch.where(torch.rand(dh, device=DEV, generator=g) < 0.5, -1.0, 1.0)
+    T = sum(rows)
+    q = (2 * u.repeat(Hq) + 0.3 * torch.randn((T, Hq * dh), device=DEV, generator=g)).to(torch.bfloat16)
+    k = torch.arange(prefix, device=DEV)
+    at = both[-1, k // page].long(), k % page
+    # 2 dh b / sqrt(dh) = top k / prefix
+    rise = (top * k / prefix / (2 * dh ** 0.5))[:, None] * u.repeat(Hkv)
+    kv[0][at] = (kv[0][at].float() + rise).to(torch.bfloat16)
+    table, ptable = widen(both[:-1].contiguous(), page), widen(both[-1:].contiguous(), page)
+    lse = torch.zeros((T, Hq), device=DEV)
+    r = sp.sp_prefix_attention(q=q, kv=kv, table=table, lens=ints(own), cu_rows=starts(rows) if max(rows) > 1 else None,
+                               n_heads=Hq, n_kv_heads=Hkv, head_dim=dh, prefix_table=ptable, prefix_lens=ints([prefix]),
+                               group_cu=ints([0, len(rows)]), lse=lse)
+    assert int(r["err"].item()) == 0
+    ref, rl, size = P.plain_attention(q, kv, page, heads, rows, table, own, [0, len(rows)], ptable, [prefix], dh ** -0.5)
+    assert rl.max() < 64
+    bad = (r["out"].double() - ref).abs() - (U * ref.abs() + (U + 2.0 ** -12) * size)
+    assert bad.max().item() <= 0, f"off by {bad.max().item()} over the bound"
+    assert ((lse.double() - rl).abs() <= 2.0 ** -13).all()  # (what the bound grants a score)
+
+
+@pytest.mark.parametrize("heads", [(8, 2, 64), (8, 2, 128), (32, 8, 128)])
+@pytest.mark.parametrize("rows", [[1] * 40, [16] * 32])
+def test_scores_that_rise_from_tile_to_tile(sp, heads, rows):
+    """Key tiles of 128 whose largest scores are more than 8 (in powers of two) apart: the tensor kernel rescales what
+    it has summed tile by tile, in segments of four tiles and of ten."""
+    rising_call(sp, 51, heads, rows, [max(n, 20) for n in rows], 1024, top=50)
+
+
+@pytest.mark.parametrize("heads", [(4, 2, 64), (4, 2, 128), (2, 2, 128)])
+@pytest.mark.parametrize("rows,prefix", [([1], 15000), ([1] * 4, 4500), ([3, 1], 9001)])
+@pytest.mark.parametrize("top", [0, 50])
+def test_items_of_many_segments(sp, heads, rows, prefix, top):
+    """Few rows over thousands of keys by plan and merge: far more than 32 segments of one item, whose maxima rise."""
+    rising_call(sp, 52, heads, rows, [30 + n for n in rows], prefix, top=top)
