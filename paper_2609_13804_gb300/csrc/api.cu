@@ -1409,8 +1409,8 @@ static sp_status decode_paged_impl(const sp_model* m, const sp_decode_paged_io* 
   if (s0 != SP_OK) return s0;
   if (!io->x || !io->lens || !io->rope_pos || !io->hidden)
     return fail(SP_ERR_INVALID_ARG, "%s: x, lens, rope_pos, hidden required", who);
-  if (io->n_groups < 0 || io->n_groups > SP_MAX_BATCH || (io->n_groups > 0 && io->prefix_max_pages < 1) ||
-      (long long)io->prefix_max_pages * pg.page_size > (1ll << 30))
+  if (io->n_groups < 0 || io->n_groups > SP_MAX_BATCH ||
+      (io->n_groups > 0 && (io->prefix_max_pages < 1 || (long long)io->prefix_max_pages * pg.page_size > (1ll << 30))))
     return fail(SP_ERR_SHAPE, "%s: n_groups must be in 0..SP_MAX_BATCH, prefix_max_pages at least 1 with groups", who);
   if (io->n_groups > 0 && (!io->group_cu || !io->prefix_table || !io->prefix_lens))
     return fail(SP_ERR_INVALID_ARG, "%s: groups need group_cu, prefix_table and prefix_lens", who);

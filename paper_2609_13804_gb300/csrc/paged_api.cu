@@ -112,8 +112,9 @@ sp_status sp_prefix_attention(const sp_prefix_attention_io* io, void* workspace,
   const int dq = io->n_heads * io->head_dim;
   if (io->B < 1 || io->B > SP_MAX_BATCH || io->T_cap < 0 || (!io->cu_rows && io->T_cap != io->B))
     return report(SP_ERR_SHAPE, "%s: B must be in 1..SP_MAX_BATCH and T_cap >= 0 (= B without cu_rows)", who);
-  if (io->n_groups < 0 || io->n_groups > SP_MAX_BATCH || (io->n_groups > 0 && io->prefix_max_pages < 1) ||
-      (long long)io->prefix_max_pages * io->cache.page_size > (1ll << 30))
+  if (io->n_groups < 0 || io->n_groups > SP_MAX_BATCH ||
+      (io->n_groups > 0 && (io->prefix_max_pages < 1 ||
+                            (long long)io->prefix_max_pages * io->cache.page_size > (1ll << 30))))
     return report(SP_ERR_SHAPE, "%s: n_groups must be in 0..SP_MAX_BATCH, prefix_max_pages at least 1 with groups", who);
   if ((long long)io->T_cap * io->n_heads > (1ll << 28))
     return report(SP_ERR_SHAPE, "%s: T_cap * n_heads must be at most 2^28", who);

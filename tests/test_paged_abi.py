@@ -143,3 +143,11 @@ def test_null_and_workspace_queries(L):
     assert L.sp_prefix_attention_workspace(0, 1, 0, 4, 2, 64) > 0
     assert L.sp_beam_select_workspace(1, 17, 10, 1) == 0
     assert L.sp_beam_select_workspace(1, 1, 10, 1) > 0
+
+
+def test_group_arguments_count_with_groups_only(L):
+    """Without groups their arguments are ignored, whatever they hold: the call goes on to its workspace."""
+    for pages in (-1, 0, 1 << 30, (1 << 31) - 1):
+        assert L.sp_prefix_attention(C.byref(attend(prefix_max_pages=pages)), OK, 64, None) == WORKSPACE
+    assert L.sp_prefix_attention(C.byref(attend(n_groups=1, prefix_max_pages=1 << 27, group_cu=OK, prefix_table=OK,
+                                                prefix_lens=OK)), OK, 64, None) == SHAPE
