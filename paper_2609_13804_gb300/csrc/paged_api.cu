@@ -95,9 +95,13 @@ sp_status sp_paged_append(const sp_paged_append_io* io, sp_stream stream) {
 }
 
 size_t sp_prefix_attention_workspace(int T_cap, int B, int n_groups, int n_heads, int n_kv_heads, int head_dim) {
+  const char* who = "sp_prefix_attention_workspace";
+  if (check_heads(who, n_heads, n_kv_heads, head_dim) != SP_OK) return 0;
   if (T_cap < 0 || B < 1 || B > SP_MAX_BATCH || n_groups < 0 || n_groups > SP_MAX_BATCH ||
-      check_heads("sp_prefix_attention_workspace", n_heads, n_kv_heads, head_dim) != SP_OK)
+      (long long)T_cap * n_heads > (1ll << 28)) {
+    report(SP_ERR_SHAPE, "%s: B must be in 1..SP_MAX_BATCH, n_groups in 0..SP_MAX_BATCH, T_cap >= 0, T_cap * n_heads at most 2^28", who);
     return 0;
+  }
   return prefix_attention_bytes(T_cap, B, n_groups, n_heads, n_kv_heads, head_dim) + 256;
 }
 

@@ -151,3 +151,11 @@ def test_group_arguments_count_with_groups_only(L):
         assert L.sp_prefix_attention(C.byref(attend(prefix_max_pages=pages)), OK, 64, None) == WORKSPACE
     assert L.sp_prefix_attention(C.byref(attend(n_groups=1, prefix_max_pages=1 << 27, group_cu=OK, prefix_table=OK,
                                                 prefix_lens=OK)), OK, 64, None) == SHAPE
+
+
+@pytest.mark.parametrize("sizes", [(-1, 4, 1, 4, 2, 64), (4, 257, 0, 4, 2, 64), (4, 4, 257, 4, 2, 64), (1 << 20, 4, 0, 512, 4, 64)])
+def test_workspace_query_of_refused_sizes(L, sizes):
+    """Sizes that the call refuses have no workspace, and the message says which."""
+    L.sp_paged_append(None, None)  # (another message before)
+    assert L.sp_prefix_attention_workspace(*sizes) == 0
+    assert b"sp_prefix_attention_workspace" in L.sp_last_error() and b"n_groups" in L.sp_last_error()
