@@ -287,6 +287,15 @@ def _stream(stream) -> Optional[int]:
     return stream.cuda_stream
 
 
+def _as_stream(stream, device):
+    """A torch stream of a call's `stream`, which may be a handle."""
+    torch = _torch()
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    handle = stream if isinstance(stream, int) else stream.cuda_stream
+    return torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)
+
+
 def _on_its_stream(call):
     """Makes the stream that a call is given torch's current one while the call runs: what it allocates and clears then
     belongs to that stream, in order with its kernels."""
@@ -294,13 +303,10 @@ def _on_its_stream(call):
     def on_stream(*args, stream=None, **kw):
         if stream is None:
             return call(*args, **kw)
-        torch = _torch()
-        if not isinstance(stream, torch.cuda.Stream):
-            handle = stream if isinstance(stream, int) else stream.cuda_stream
-            dev = next((d for d in (getattr(a, "device", None) for a in (*args, *kw.values()))
-                        if getattr(d, "type", None) == "cuda"), None)
-            stream = torch.cuda.ExternalStream(handle, device=dev) if handle else torch.cuda.default_stream(dev)
-        with torch.cuda.stream(stream):
+        device = next((d for d in (getattr(a, "device", None) for a in (*args, *kw.values()))
+                       if getattr(d, "type", None) == "cuda"), None)
+        stream = _as_stream(stream, device)
+        with _torch().cuda.stream(stream):
             return call(*args, stream=stream, **kw)
     return on_stream
 
@@ -680,15 +686,22 @@ _pack_reorder = _packer(sp_beam_reorder_io)
 _pack_decode = _packer(sp_decode_paged_io)
 
 
-def _enter(who: str, t):
-    """(device index, guard): makes the tensor's device current where it is not; leave() with the guard."""
+def _enter(who: str, t, stream):
+    """(device index, guard): makes the tensor's device current where it is not, and the call's stream if it names one
+    (as _on_its_stream does, without its cost for the calls that name none); leave() with the guard."""
     torch = _torch()
     dev = t.get_device()
     if dev < 0:
         raise ValueError(f"{who}: tensors must be on a CUDA device")
-    if torch.cuda.current_device() == dev:
+    if stream is not None:
+        stream = _as_stream(stream, dev)
+        if stream.device_index != dev:
+            raise ValueError(f"{who}: the stream is device {stream.device_index}'s, the tensors are on device {dev}")
+        guard = torch.cuda.stream(stream)
+    elif torch.cuda.current_device() == dev:
         return dev, None
-    guard = torch.cuda.device(dev)
+    else:
+        guard = torch.cuda.device(dev)
     guard.__enter__()
     return dev, guard
 
@@ -746,7 +759,6 @@ def paged_pool(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, n_l
     return torch.zeros((n_layers, 2, n_pages, page_size, n_kv_heads * head_dim), dtype=torch.bfloat16, device=device)
 
 
-@_on_its_stream
 def sp_paged_append(*, qkv, kv, table, n_heads, n_kv_heads, head_dim, lens=None, cu_rows=None, rope=None, pos=None,
                     pos3=None, mrope_section=None, q_out=None, keys_only=False, err=None, stream=None) -> Dict:
     """Rows q | k | v [T, (n_heads + 2 n_kv_heads) head_dim] into the pages of kv (one layer's pool): row j of
@@ -755,7 +767,7 @@ def sp_paged_append(*, qkv, kv, table, n_heads, n_kv_heads, head_dim, lens=None,
     leaves them as they are.  The queries go to q_out (new when None; a view of qkv's first columns rotates in
     place; keys_only: nowhere).  Returns q and err."""
     torch, who = _torch(), "sp_paged_append"
-    dev, guard = _enter(who, qkv)
+    dev, guard = _enter(who, qkv, stream)
     try:
         i32, bf16 = torch.int32, torch.bfloat16
         T, B, mp = qkv.shape[0], table.shape[0], table.shape[-1]
@@ -797,7 +809,6 @@ def prefix_attention_workspace(*, T_cap, B, n_heads, n_kv_heads, head_dim, n_gro
     return workspace(n, device)
 
 
-@_on_its_stream
 def sp_prefix_attention(*, q, kv, table, lens, n_heads, n_kv_heads, head_dim, prefix_table=None, prefix_lens=None,
                         group_cu=None, cu_rows=None, scale=0.0, out=None, lse=None, ws=None, err=None,
                         stream=None) -> Dict:
@@ -806,7 +817,7 @@ def sp_prefix_attention(*, q, kv, table, lens, n_heads, n_kv_heads, head_dim, pr
     pages (table, lens: positions with these rows' own).  Returns out [T, n_heads head_dim] bf16, lse (the given
     [T, n_heads] fp32 tensor or None) and err."""
     torch, who = _torch(), "sp_prefix_attention"
-    dev, guard = _enter(who, q)
+    dev, guard = _enter(who, q, stream)
     try:
         i32, bf16 = torch.int32, torch.bfloat16
         T, B, mp = q.shape[0], table.shape[0], table.shape[-1]
@@ -842,13 +853,12 @@ def sp_prefix_attention(*, q, kv, table, lens, n_heads, n_kv_heads, head_dim, pr
     return {"out": out, "lse": lse, "err": err, "_ws": ws}
 
 
-@_on_its_stream
 def sp_prefill_paged(model: Model, *, x, cu_seqlens, pos, B, T_cap, max_seqlen_cap, kv, table, residual=None,
                      stream=None, ws=None, hidden=None, pos3=None, err=None) -> Dict:
     """sp_prefill with the keys and values put into pages: kv [n_layers, 2, n_pages, page_size, width] (paged_pool),
     table [B, pages] int32."""
     torch, who, m = _torch(), "sp_prefill_paged", model.shape
-    dev, guard = _enter(who, x)
+    dev, guard = _enter(who, x, stream)
     try:
         if kv.dim() != 5:
             raise ValueError("sp_prefill_paged: kv must be the pools of all layers")
@@ -871,14 +881,13 @@ def sp_prefill_paged(model: Model, *, x, cu_seqlens, pos, B, T_cap, max_seqlen_c
     return {"hidden": hidden, "err": err, "_ws": ws}
 
 
-@_on_its_stream
 def sp_decode_paged(model: Model, *, x, lens, rope_pos, kv, table, prefix_table=None, prefix_lens=None, group_cu=None,
                     hidden=None, ws=None, err=None, stream=None) -> Dict:
     """One generation step over pages: x [B, d] bf16 new tokens, lens / rope_pos [B] int32 own cached positions and
     rotary positions (both incremented on the device), kv [n_layers, 2, n_pages, page_size, width], table [B, pages]
     the sequences' own pages; sequences group_cu[g] .. group_cu[g+1] - 1 share prefix_table[g], prefix_lens[g]."""
     torch, who, m = _torch(), "sp_decode_paged", model.shape
-    dev, guard = _enter(who, x)
+    dev, guard = _enter(who, x, stream)
     try:
         i32 = torch.int32
         B, mp = x.shape[0], table.shape[-1]
@@ -921,14 +930,13 @@ def beam_select_workspace(*, B, W, V, n_out, device="cuda"):
     return workspace(n, device)
 
 
-@_on_its_stream
 def sp_beam_select(*, logits, cum, n_out, done=None, eos=0, score=None, parent=None, token=None, ws=None,
                    stream=None) -> Dict:
     """The n_out best continuations of every element's beams: logits [B, W, V] fp32 or bf16 (rows may lie apart),
     cum [B, W] fp32, done [B, W] bool or None (a finished beam proposes itself with token eos).  Returns score,
     parent (beam) and token [B, n_out], best first; places without a continuation hold -infinity, -1, -1."""
     torch, who = _torch(), "sp_beam_select"
-    dev, guard = _enter(who, logits)
+    dev, guard = _enter(who, logits, stream)
     try:
         f32, i32 = torch.float32, torch.int32
         is_f32 = logits.dtype is f32
@@ -975,13 +983,12 @@ def sp_beam_select(*, logits, cum, n_out, done=None, eos=0, score=None, parent=N
     return {"score": score, "parent": parent, "token": token, "_ws": ws}
 
 
-@_on_its_stream
 def sp_beam_reorder(*, kv, table, own_table, lens, parent, err=None, stream=None):
     """Puts the cache into the beams' new order: table rows and the rows of the partly filled pages of all layers
     (kv [n_layers, 2, n_pages, page_size, width]) follow parent [B, W or more] (its first W columns); table is
     updated in place.  Returns err."""
     torch, who = _torch(), "sp_beam_reorder"
-    dev, guard = _enter(who, kv)
+    dev, guard = _enter(who, kv, stream)
     try:
         i32 = torch.int32
         if kv.dim() != 5 or parent.dim() != 2 or table.dim() != 2:
