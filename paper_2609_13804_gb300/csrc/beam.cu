@@ -199,7 +199,7 @@ beam_scan_kernel(const void* __restrict__ logits, long long ld, int V, const flo
   }
   const uint4* src = reinterpret_cast<const uint4*>(base + (size_t)c0 * esz - (SHIFT ? off : 0));
   unsigned long long T = 0;  // keys above T are candidates
-  const int tile_chunks = BS_NT * BS_LOADS;
+  const int tile_chunks = BS_NT * BS_LOADS, tiles = (chunks + tile_chunks - 1) / tile_chunks;
   // SHIFT: aligned piece c, as far as it holds the slice's chunks (0 .. chunks - 1 begin in it, the last ends in the next)
   auto part = [&](uint4* to, int c) {
     const uint32_t n = c < chunks ? 16 : c == chunks && c > 0 ? off : 0;
@@ -210,9 +210,10 @@ beam_scan_kernel(const void* __restrict__ logits, long long ld, int V, const flo
 #pragma unroll
     for (int q = 0; q < BS_LOADS; ++q) {
       const int c = t * tile_chunks + q * BS_NT + tid;
-      if (!SHIFT) {
+      if (!SHIFT) {  // (behind the last tile: nothing)
         if (c < chunks)
           asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to + q * BS_NT)), "l"(src + c) : "memory");
+      } else if (t >= tiles) {
       } else if (c == 0 && chunks > 0 && off != 0 && row == 0 && v0 == 0) {
         // (what lies before the first row may be no one's: its first piece is put there by elements)
         for (int k = off / esz; k < K::N; ++k) {
@@ -227,7 +228,6 @@ beam_scan_kernel(const void* __restrict__ logits, long long ld, int V, const flo
       part(beside + ((t % BS_RING) * BS_WARPS + warp) * BS_LOADS + lane, t * tile_chunks + lane * BS_NT + (warp + 1) * 32);
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  const int tiles = (chunks + tile_chunks - 1) / tile_chunks;
   float bm = -INFINITY;  // the thread's maximum of the block
   auto take = [&](const uint4 (&u)[BS_LOADS], int place) {
     float lm = -INFINITY;

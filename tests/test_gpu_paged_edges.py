@@ -198,3 +198,11 @@ def test_scores_that_rise_from_tile_to_tile(sp, heads, rows):
 def test_items_of_many_segments(sp, heads, rows, prefix, top):
     """Few rows over thousands of keys by plan and merge: far more than 32 segments of one item, whose maxima rise."""
     rising_call(sp, 52, heads, rows, [30 + n for n in rows], prefix, top=top)
+
+
+@pytest.mark.parametrize("dtype,V", [(torch.float32, 4099), (torch.float32, 8191), (torch.bfloat16, 8195), (torch.bfloat16, 16391)])
+def test_equal_beams_of_whole_tiles(sp, dtype, V):
+    """One slice to a row of so many rows: its chunks fill whole tiles, and some are left behind the last."""
+    g = gen(V)
+    x = (3 * torch.randn((80, 1, V), device=DEV, generator=g)).to(dtype).expand(80, 4, V).contiguous()
+    P.select_case(sp, x, torch.zeros((80, 4), device=DEV), 8)
