@@ -536,14 +536,15 @@ SP_API sp_status sp_decode(const sp_model* m, const sp_decode_io* io, void* work
                            sp_stream stream);
 
 /* ------------------------------------------------------------------------ */
-/* Several sequences over one pruned prefix: a paged cache and beams.         */
+/* Several sequences over one prefix: a paged cache and beams.                */
 /* ------------------------------------------------------------------------ */
 
 /*
- * Questions about one image, samples and beams continue the same prefix.  In a
- * paged cache they share its keys and values: a pool of pages of page_size
- * positions, and per sequence a table of its pages.  Position p of a sequence
- * is row p % page_size of page table[p / page_size].  One layer's pool is
+ * Samples and beams of a question continue the same pruned prefix (another
+ * question keeps other tokens; questions share an unpruned one).  In a paged cache
+ * they share its keys and values: a pool of pages of page_size positions, and per
+ * sequence a table of its pages.  Position p of a sequence is row p % page_size of
+ * page table[p / page_size].  One layer's pool is
  *   kv  DEVICE [2][n_pages][page_size][n_kv_heads * head_dim] bf16 (K, then V).
  * Table entries behind a sequence's pages are not read (-1, say).  A page
  * outside 0..n_pages-1 where one is needed sets SP_DEVERR_INDEX; nothing is
@@ -697,7 +698,7 @@ SP_API sp_status sp_decode_paged(const sp_model* m, const sp_decode_paged_io* io
  * row's sum is taken in fp32, good to about 2^-20 of it: scores of two beams that
  * are nearer than that can change places.  Beams of an element with equal logits
  * have equal sums, to the bit.  (Row strides that are no multiple of 16 bytes take
- * up to a quarter longer.)
+ * up to a fifth longer.)
  *   - A beam with cum -infinity (or NaN) is not alive: it proposes nothing.
  *   - A finished beam (done != 0) proposes only itself: token eos, score cum;
  *     its logits have no effect, whatever they hold (some of them are read).

@@ -152,8 +152,8 @@ __device__ __noinline__ int cut_list(unsigned long long* list, int n, int n_out)
 // 256 rows of 152,064 bf16 logits, a fifth of them finished, 62 MB, 18 us (3.4 TB/s); 4 rows of 32,000 fp32 3.5 us.
 // SHIFT: the rows begin at different places within 16 bytes.  The aligned pieces go through the ring as they lie; a
 // lane puts each of its pieces from its own and the next lane's (the warp's last from a piece loaded beside).  Both
-// kernels, 64 x 4 rows of 152,063 bf16 logits 29.4 us (23.1 by aligned pieces, which tie by where a row lies), 16 x 4 of
-// 50,257 fp32 14.0 (12.2): some 45 instructions more for 32 or 16 logits of a thread.
+// kernels, 64 x 4 rows of 152,063 bf16 logits 27.5 us (23.1 by aligned pieces, which tie by where a row lies), 16 x 4 of
+// 50,257 fp32 13.7 (12.2): some 30 instructions more for the 32 or 16 logits of a thread and tile.
 template <bool F32, bool SHIFT>
 __global__ void __launch_bounds__(BS_NT, SHIFT ? 2 : 3)
 beam_scan_kernel(const void* __restrict__ logits, long long ld, int V, const float* __restrict__ cum,
@@ -200,32 +200,44 @@ beam_scan_kernel(const void* __restrict__ logits, long long ld, int V, const flo
   const uint4* src = reinterpret_cast<const uint4*>(base + (size_t)c0 * esz - (SHIFT ? off : 0));
   unsigned long long T = 0;  // keys above T are candidates
   const int tile_chunks = BS_NT * BS_LOADS, tiles = (chunks + tile_chunks - 1) / tile_chunks;
-  // SHIFT: aligned piece c, as far as it holds the slice's chunks (0 .. chunks - 1 begin in it, the last ends in the next)
+  auto copy16 = [&](uint4* to, int c) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(src + c) : "memory");
+  };
+  // SHIFT: aligned piece c, as far as it holds the slice's chunks (0 .. chunks - 1 begin in it, the last ends in the next).
+  // What lies before the first row may be no one's: its first piece is put there by elements.
+  const bool first = SHIFT && row == 0 && v0 == 0 && off != 0;
   auto part = [&](uint4* to, int c) {
-    const uint32_t n = c < chunks ? 16 : c == chunks && c > 0 ? off : 0;
-    if (n) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(src + c), "r"(n) : "memory");
+    if (first && c == 0 && chunks > 0) {
+      for (int k = off / esz; k < K::N; ++k) {
+        if (F32) reinterpret_cast<float*>(to)[k] = reinterpret_cast<const float*>(base)[k - off / esz];
+        else reinterpret_cast<__nv_bfloat16*>(to)[k] = reinterpret_cast<const __nv_bfloat16*>(base)[k - off / esz];
+      }
+    } else if (c < chunks) {
+      copy16(to, c);
+    } else if (c == chunks && c > 0 && off != 0) {
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(src + c), "r"(off) : "memory");
+    }
   };
   auto load = [&](int t) {  // (what lies past the slice is not loaded, and read as -infinity)
     uint4* to = ring + (t % BS_RING) * (BS_LOADS * BS_NT) + tid;
+    const int c = t * tile_chunks + tid;
+    if (!SHIFT) {
 #pragma unroll
-    for (int q = 0; q < BS_LOADS; ++q) {
-      const int c = t * tile_chunks + q * BS_NT + tid;
-      if (!SHIFT) {  // (behind the last tile: nothing)
-        if (c < chunks)
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to + q * BS_NT)), "l"(src + c) : "memory");
-      } else if (t >= tiles) {
-      } else if (c == 0 && chunks > 0 && off != 0 && row == 0 && v0 == 0) {
-        // (what lies before the first row may be no one's: its first piece is put there by elements)
-        for (int k = off / esz; k < K::N; ++k) {
-          if (F32) reinterpret_cast<float*>(to)[k] = reinterpret_cast<const float*>(base)[k - off / esz];
-          else reinterpret_cast<__nv_bfloat16*>(to)[k] = reinterpret_cast<const __nv_bfloat16*>(base)[k - off / esz];
-        }
+      for (int q = 0; q < BS_LOADS; ++q)
+        if (c + q * BS_NT < chunks) copy16(to + q * BS_NT, c + q * BS_NT);
+    } else if (t < tiles) {
+      uint4* last = beside + ((t % BS_RING) * BS_WARPS + warp) * BS_LOADS + lane;
+      const int c_last = t * tile_chunks + lane * BS_NT + (warp + 1) * 32;
+      if ((t + 1) * tile_chunks < chunks && !(first && t == 0)) {  // (whole pieces, the one behind the tile too)
+#pragma unroll
+        for (int q = 0; q < BS_LOADS; ++q) copy16(to + q * BS_NT, c + q * BS_NT);
+        if (off != 0 && lane < BS_LOADS) copy16(last, c_last);
       } else {
-        part(to + q * BS_NT, c);
+#pragma unroll 1
+        for (int q = 0; q < BS_LOADS; ++q) part(to + q * BS_NT, c + q * BS_NT);
+        if (off != 0 && lane < BS_LOADS) part(last, c_last);
       }
     }
-    if (SHIFT && off != 0 && lane < BS_LOADS)
-      part(beside + ((t % BS_RING) * BS_WARPS + warp) * BS_LOADS + lane, t * tile_chunks + lane * BS_NT + (warp + 1) * 32);
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
   float bm = -INFINITY;  // the thread's maximum of the block
