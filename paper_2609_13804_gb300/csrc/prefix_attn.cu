@@ -747,8 +747,9 @@ constexpr int kTcVectors = 32;
 // vectors per warp of the GPU, taking every sequence and prefix as long as the tables can hold and the rows as evenly
 // spread, and none has more than kFewKeys keys (whose many segments cost the merge more).  Us of a call with that
 // kernel and with prefix_tc_kernel, 40 heads of 128 and one kv head: 16 rows and a prefix of 250 keys (0.5 tiles per
-// warp) 11.6 and 15.8, of 2,000 (4) 18.8 and 18.1, 64 rows and 250 keys (2) 14.9 and 17.3; 64 heads, 4 kv heads, 64 rows
-// in 16 prefixes of 250 keys (3.4) 17.3 and 19.8; of 1,000 (13; 28 heads) 30 and 22.
+// warp) 11.5 and 15.4, of 2,000 (4) 18.8 and 17.9, 64 rows and 250 keys (2) 15.1 and 16.7; 64 heads, 4 kv heads, 64 rows
+// in 16 prefixes of 250 keys (3.4) 17.4 and 19.3 (the second each with a prefix table for 2,064 positions); of 1,000 (13;
+// 28 heads, once with the limit raised) 30 and 22.
 constexpr int kFewTiles = 7, kFewKeys = 2048;
 
 // A plan's arrays in its part of the workspace (base NULL: sizes only); returns its bytes.
@@ -812,12 +813,13 @@ static PrefixLayout prefix_layout(int T_cap, int B, int n_groups, int Hq, int Hk
 // Rows and warps of a CTA of prefix_row_kernel where a call goes to it (rows 0: it does not): up to RK_VECS heads per kv
 // head, as long as a warp's share of the CTA's tiles, with tables as full as they can be and rows evenly spread, is short
 // (kRowTiles), or no prefix is read by two CTAs of a kv head and half the SMs have one (kRowTilesAlone).  Us with it and
-// without, single tokens: four rows of 32 heads of 128 and one prefix of 240 keys (1.2 tiles a warp) 5.8 and 11.1, of
-// 2,000 keys (9) 13.9 and 16.1; 16 rows of 28 heads, 4 kv heads, 2,000 keys (9) 13.9 and 17.5; 4 rows, 4,000 keys (18) 22.3
-// and 19.3; 64 rows, one prefix of 2,944 keys (27) 33.0 and 23.3; without sharing, 64 rows of 32 heads and 500 keys (33,
-// CTAs of one warp) 95.7 and 99.  Questions: 3 rows of 28 heads and 250 keys 7.6 and 10.7, four of 16 rows and 1,000 keys
-// (11) 16.1 and 21.2, 16 of 48 rows without a prefix (6, CTAs of one warp) 23.5 and 28.1.  Not CTAs of one warp for few
-// rows of a sequence that lie in several: 128 of 4 rows 22.1 and 16.3.
+// without (the same call with tables for 16,400 positions), single tokens: four rows of 32 heads of 128, one prefix of 240
+// and 20 own keys (1.2 tiles a warp) 5.7 and 11.0, of 2,000 keys (9) 14.9 and 18.4; 16 rows of 28 heads, 4 kv heads, 2,000
+// keys (9) 14.7 and 18.2; without sharing, 64 rows of 32 heads and 500 keys (33, CTAs of one warp) 93 and 94.  Questions:
+// 3 rows of 28 heads and 250 keys 7.5 and 10.6, four of 16 rows and 1,000 keys (11) 15.8 and 19.2, 16 of 48 rows without a
+// prefix (6, CTAs of one warp) 21.7 and 30.6, of 32 heads on as many kv heads 24.0 and 46.0.  Beyond the limits (each once
+// with the limit raised): 4 rows, 4,000 keys (18) 22.3 and 19.3; 64 rows, one prefix of 2,944 keys (27) 33.0 and 23.3; not
+// CTAs of one warp for few rows of a sequence that lie in several: 128 of 4 rows 22.1 and 16.3.
 struct RowLayout {
   int rows, warps;
 };

@@ -22,10 +22,10 @@
 // segment's slot, in whole 64-byte pieces.  The scores run up to two tiles ahead; those of tile j + 3 reuse tile
 // j's buffer once its O += P V is done.
 // Tensor memory: S / P buffer b at columns 128 b, O at 384.
-// Bound by the chain scores -> softmax -> product through the three buffers tensor memory holds: a tile's takes some
-// 5,300 cycles, three are in flight, so 1,760 cycles (0.93 us) a tile, 58% of the tensor pipe's rate while they run.
-// 128 rows of 28 query heads over 16,384 keys: 32 us with start and end (980 TFLOP/s).  (Two pipelines of a row tile
-// each with single 128-key buffers took 71 us when this took 51: only tiles in flight hide the chain.)
+// Bound by the chain scores -> softmax -> product through the three buffers tensor memory holds: three tiles are in
+// flight, and a tile takes 0.89 us of a CTA (by the difference of prefixes of 16,384 and 32,768 keys; 1,024 cycles of the
+// tensor pipe).  128 rows of 28 query heads over 16,384 keys, the merge included: 41.7 us (720 TFLOP/s).  (Two pipelines
+// of a row tile each with single 128-key buffers took 71 us when this took 51: only tiles in flight hide the chain.)
 #include <algorithm>
 
 #include "internal.h"

@@ -7,7 +7,7 @@
 // vectors are cut into row tiles, the keys into key tiles; an item is (entry, row tile, kv head).  An item
 // counts `over` units for what it costs whatever its length (its query vectors in, its result out) and one
 // for each of its key tiles, and the items' units, one after the other, are one list of N.  P workers (warps,
-// or the two pipelines of a CTA) take equal consecutive parts of it, whatever the entries' lengths: worker w
+// or CTAs of the tensor kernel) take equal consecutive parts of it, whatever the entries' lengths: worker w
 // the units [w N / P, (w + 1) N / P).  The key tiles of an item that one worker takes are a segment; it writes
 // its running max, sum and weighted values in 32 bits to slot (item index + worker index), which is its own:
 // going along the list, each next segment has the next item or the next worker.  prefix_merge_kernel joins
