@@ -603,7 +603,8 @@ SP_API sp_status sp_paged_append(const sp_paged_append_io* io, sp_stream stream)
  * cache.lens[b] positions (these rows' own keys, appended before, among them),
  * those up to lens[b] - n_b + j.  Sequences outside every group have no prefix.
  *   out = softmax(scale <q, k>) v over the visible keys, lse = log sum exp of
- *   the scaled scores; a row that sees no key gets zeros and lse -infinity.
+ *   the scaled scores; a row that sees no key, or only keys with a score of
+ *   -infinity, gets zeros and lse -infinity.
  * A prefix is read once for all rows that share it (in small calls by several
  * CTAs, from the L2 cache).  Scores, statistics and sums are fp32; the weights are rounded to bf16 for the product with V.
  * Lengths are read on the device (they may change between replays of a graph);

@@ -206,3 +206,27 @@ def test_equal_beams_of_whole_tiles(sp, dtype, V):
     g = gen(V)
     x = (3 * torch.randn((80, 1, V), device=DEV, generator=g)).to(dtype).expand(80, 4, V).contiguous()
     P.select_case(sp, x, torch.zeros((80, 4), device=DEV), 8)
+
+
+# ----------------------------------------------------------------------------- infinite scores
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("rows,own", MIXES)
+@pytest.mark.parametrize("wide", [False, True])
+def test_keys_with_a_score_of_minus_infinity_have_no_weight(sp, dh, rows, own, wide):
+    """A prefix of such keys: rows with own keys see those alone (so its values do not matter), rows without see nothing."""
+    a = shared_call(gen(dh + len(rows)), dh, rows, own, wide)
+    a["q"].abs_()
+    for k in range(300):
+        a["kv"][0, int(a["prefix_table"][0, k // 16]), k % 16] = -torch.inf
+    ref, rl = sp.sp_prefix_attention(**a)["out"].clone(), a["lse"].clone()
+    alone = torch.zeros_like(rl)
+    b = sp.sp_prefix_attention(**{**a, "lse": alone, "prefix_table": None})["out"]
+    if own[0] == 0:
+        assert (ref == 0).all() and torch.isinf(rl).all() and (rl < 0).all() and (b == 0).all()
+        return
+    # (cut into other segments: both within the bound, where the weights' sum of |v| is at most the largest |v|)
+    most = a["kv"][1].abs().max().double()
+    x, y = ref.double(), b.double()
+    assert ((x - y).abs() <= 2 * (U * torch.maximum(x.abs(), y.abs()) + (U + 2.0 ** -12) * most)).all()
+    assert ((rl - alone).abs() <= 2 * (1e-5 + 1e-6 * rl.abs())).all()
