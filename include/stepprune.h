@@ -20,7 +20,7 @@
  *   sp_pipeline  all four, back to back on one stream.
  * and the generation after it: sp_decode over a cache per sequence, and over
  * pages that sequences share (sp_prefill_paged, sp_decode_paged and the
- * operators they and beam search are made of).
+ * operators they, beam search and speculative sampling are made of).
  *
  * Conventions (all entry points):
  *   - Pointers marked DEVICE are device memory owned by the caller; HOST marks
@@ -69,6 +69,8 @@ extern "C" {
 #define SP_MAX_KMAX 1024          /* per-episode cap on retained tokens */
 #define SP_MAX_NVIS 16384         /* visual tokens of one image */
 #define SP_MAX_BEAMS 16           /* beams of one element */
+#define SP_MAX_DRAFT_ROWS 1024    /* rows of one sequence that sp_draft_verify looks at */
+#define SP_MAX_TABLE_ROWS 4096    /* rows of a table that sp_pages_* work on */
 
 typedef enum {
   SP_OK = 0,
@@ -85,6 +87,7 @@ typedef enum {
 /* Bits of the DEVICE error word. */
 #define SP_DEVERR_TIMEOUT 0x1   /* a bounded wait (mbarrier / flag) ran out */
 #define SP_DEVERR_INDEX 0x2     /* an index outside its range was skipped */
+#define SP_DEVERR_PAGES 0x4     /* a cache had too few free pages */
 
 typedef struct CUstream_st* sp_stream; /* a cudaStream_t; NULL is the legacy default stream */
 
@@ -757,6 +760,120 @@ typedef struct {
 } sp_beam_reorder_io;
 
 SP_API sp_status sp_beam_reorder(const sp_beam_reorder_io* io, sp_stream stream);
+
+/*
+ * Verification of drafted tokens (speculative sampling), and without drafts the
+ * sampling of a token for every sequence.  Sequence b has the rows
+ * cu_rows[b] .. cu_rows[b + 1] - 1 of logits, n of them: row j holds the target's
+ * logits behind its j-th drafted token draft[row j], the last row those behind
+ * all of them (its draft is not read).  With t = temperature[b],
+ * p_j = softmax(logits[row j] / t) and q_j = softmax(draft_logits[row j] / t):
+ *   - draft j stays iff u[row j] q_j(d_j) < p_j(d_j) and those before it do;
+ *   - the token after the a that stay is argmax r(v) / noise[b, v] over the tokens
+ *     with r(v) > 0, of equal ones the lowest, with r = max(p_a - q_a, 0) where a
+ *     draft was rejected (p_a if that leaves nothing) and r = p_a behind the last.
+ *     With u uniform in [0, 1) and noise exponentially distributed with mean 1
+ *     tokens are distributed as the target's.
+ *   - Drafts without draft_logits are taken as certain (q_j is 1 at d_j): of a
+ *     rejected one's row the others are left.
+ * A sequence is greedy where temperature[b] is not above 0, and every one is
+ * without noise: drafts stay while they are the target's largest logit (of equal
+ * ones the lowest token), which is the next token too; u, noise and draft_logits
+ * have no effect on it, and log-probabilities are those at temperature 1.
+ *   n_accept[b] = a, token[b] = the drafts that stay, the next token and -1 behind
+ *   it, logp[b] = log p of each (0 behind them).  A sequence without rows gets
+ *   n_accept -1, one with more than max_rows, or rows outside 0 .. T_cap - 1, sets
+ *   SP_DEVERR_INDEX besides.  A draft outside the vocabulary is rejected and sets
+ *   SP_DEVERR_INDEX.
+ * NaN and -infinity logits have no weight; a row with +infinity spreads its weight
+ * over them.  A token whose noise is NaN or below 0 is not drawn.  Where no token can
+ * be drawn (a row without weight) the next token is -1, its logp -infinity.  A draft
+ * with u NaN is rejected.
+ * Sums are fp32, good to about 2^-20: the answers move only where u q and p, or the
+ * two best scores of a race, are nearer than that.  The workspace keeps nothing;
+ * calls whose GPU work overlaps need one each.
+ */
+typedef struct {
+  int B, V;                 /* 1..SP_MAX_BATCH, 1..2^24 */
+  int T_cap;                /* rows of logits, 0..2^24; B without cu_rows */
+  int max_rows;             /* of a sequence, 1..SP_MAX_DRAFT_ROWS: drafts + 1 */
+  const int* cu_rows;       /* DEVICE [B + 1] ascending, or NULL: one row per sequence */
+  const void* logits;       /* DEVICE [T_cap, ld] fp32 or bf16, aligned to its type */
+  int logits_f32;           /* 1: fp32, 0: bf16 (draft_logits too) */
+  long long ld;             /* elements between rows, at least V */
+  const int* draft;         /* DEVICE [T_cap]; may be NULL with max_rows 1 */
+  const void* draft_logits; /* DEVICE [T_cap, ld_draft], or NULL (a sequence's last row is not read) */
+  long long ld_draft;
+  const float* u;           /* DEVICE [T_cap]; may be NULL with max_rows 1 or without noise */
+  const float* noise;       /* DEVICE [B, ld_noise], or NULL: every sequence is greedy */
+  long long ld_noise;
+  const float* temperature; /* DEVICE [B], or NULL: 1 */
+  int* n_accept;            /* DEVICE [B] */
+  int* token;               /* DEVICE [B, max_rows] */
+  float* logp;              /* DEVICE [B, max_rows] or NULL */
+  int* err;                 /* DEVICE error word or NULL */
+} sp_draft_verify_io;
+
+SP_API size_t sp_draft_verify_workspace(int T_cap, int B, int V);
+SP_API sp_status sp_draft_verify(const sp_draft_verify_io* io, void* workspace, size_t workspace_bytes,
+                                 sp_stream stream);
+
+/*
+ * The pages of a cache that sequences share.  Row s of table names the pages of
+ * sequence s (negative: none), lens[s] its cached positions, and refs[p] is the
+ * number of table entries that name page p: 0 where it is free.  Prefixes that
+ * sequences share (sp_prefix_attention's) are rows as well.  A program begins with
+ * an empty table (-1) and zeros in lens and refs; these calls keep the books, and
+ * it adds to lens what it appends.  They all work on the state of the tables
+ * before the call: order of the rows matters only where pages run out.
+ *   sp_pages_trim     entries behind the page of a row's last position are
+ *                     released: what a rejected draft had, or (with lens 0) all of
+ *                     an ended sequence's.
+ *   sp_pages_fork     row s becomes a continuation of row parent[s] (-1 or s: it
+ *                     stays): it takes the pages of the parent's lens positions,
+ *                     and its length; its own are released.  Nothing is copied.
+ *   sp_pages_reserve  row s gets room for add[s] positions behind its lens: a page
+ *                     where its table has none, and one of its own in place of one
+ *                     that other entries name, into which the positions it has there
+ *                     are copied (all layers).  lens does not change.  (A page that
+ *                     several rows of a call write to is copied for each of them.)
+ *   sp_pages_compact  row s keeps positions keep[s][0 .. count[s] - 1], in that
+ *                     order (count -1: it stays): leading pages whose positions stay
+ *                     in place are kept, the others go to pages of its own and the
+ *                     old ones are released; lens[s] becomes count[s].  Other rows
+ *                     that share the old pages keep them as they are.
+ * Fresh pages are the free ones of the lowest numbers before the call, in order of
+ * rows and their places.  If they do not suffice, rows are served from the first on
+ * until one does not fit: it and those behind it stay as they were, and
+ * SP_DEVERR_PAGES is set.
+ * A length outside the table, a parent outside -1 .. S - 1, or a count outside
+ * -1 .. keep_cap sets SP_DEVERR_INDEX and the row stays as it was.  An entry of
+ * n_pages or more sets SP_DEVERR_INDEX and counts as none; a position of keep outside
+ * the row sets it and what it would have moved is undefined.
+ * The workspace (reserve, compact) keeps nothing; calls whose GPU work overlaps need
+ * one each.
+ */
+typedef struct {
+  void* kv;                 /* DEVICE [n_layers][2][n_pages][page_size][row_elems] bf16 (reserve, compact) */
+  int n_layers;             /* 1..SP_MAX_LM_LAYERS */
+  int n_pages, page_size;   /* as in sp_paged_kv */
+  int row_elems;            /* n_kv_heads * head_dim, a multiple of 8 */
+  int S;                    /* rows of table, 1..SP_MAX_TABLE_ROWS */
+  int* table;               /* DEVICE [S, max_pages] */
+  int max_pages;            /* S * max_pages at most 2^30 */
+  int* lens;                /* DEVICE [S] */
+  int* refs;                /* DEVICE [n_pages], 16-byte aligned */
+  int* err;                 /* DEVICE error word or NULL */
+} sp_pages;
+
+SP_API sp_status sp_pages_trim(const sp_pages* p, sp_stream stream);
+SP_API sp_status sp_pages_fork(const sp_pages* p, const int* parent, sp_stream stream);
+SP_API size_t sp_pages_workspace(int S, int max_pages);
+SP_API sp_status sp_pages_reserve(const sp_pages* p, const int* add, void* workspace, size_t workspace_bytes,
+                                  sp_stream stream);
+/* keep: DEVICE [S, ld_keep], its first keep_cap columns; S * keep_cap at most 2^30.  count: DEVICE [S]. */
+SP_API sp_status sp_pages_compact(const sp_pages* p, const int* keep, long long ld_keep, int keep_cap,
+                                  const int* count, void* workspace, size_t workspace_bytes, sp_stream stream);
 
 /* ------------------------------------------------------------------------ */
 /* The whole path: select -> compact -> project -> prefill.                  */

@@ -25,6 +25,9 @@ SP_MAX_LM_LAYERS = 96
 SP_MAX_KMAX = 1024
 SP_MAX_NVIS = 16384
 SP_MAX_BEAMS = 16
+SP_MAX_DRAFT_ROWS = 1024
+SP_MAX_TABLE_ROWS = 4096
+SP_DEVERR_TIMEOUT, SP_DEVERR_INDEX, SP_DEVERR_PAGES = 1, 2, 4
 
 STATUS = {0: "SP_OK", 1: "SP_ERR_INVALID_ARG", 2: "SP_ERR_SHAPE", 3: "SP_ERR_ALIGN", 4: "SP_ERR_WORKSPACE",
           5: "SP_ERR_CUDA", 6: "SP_ERR_TIMEOUT", 7: "SP_ERR_UNSUPPORTED", 8: "SP_ERR_DEVICE"}
@@ -41,6 +44,8 @@ EXPORTS = [
     "sp_mrope_positions", "sp_wait_probe",
     "sp_paged_append", "sp_prefix_attention_workspace", "sp_prefix_attention", "sp_beam_select_workspace",
     "sp_beam_select", "sp_beam_reorder", "sp_prefill_paged", "sp_decode_paged_workspace", "sp_decode_paged",
+    "sp_draft_verify_workspace", "sp_draft_verify", "sp_pages_trim", "sp_pages_fork", "sp_pages_workspace",
+    "sp_pages_reserve", "sp_pages_compact",
 ]
 SP_SELECT_NOALLOC_SCRATCH_BYTES = 64 << 20
 
@@ -162,6 +167,18 @@ class sp_beam_reorder_io(C.Structure):
                 ("max_pages", C.c_int), ("lens", P), ("parent", P), ("ld_parent", C.c_int), ("err", P)]
 
 
+class sp_draft_verify_io(C.Structure):
+    _fields_ = [("B", C.c_int), ("V", C.c_int), ("T_cap", C.c_int), ("max_rows", C.c_int), ("cu_rows", P),
+                ("logits", P), ("logits_f32", C.c_int), ("ld", C.c_longlong), ("draft", P), ("draft_logits", P),
+                ("ld_draft", C.c_longlong), ("u", P), ("noise", P), ("ld_noise", C.c_longlong), ("temperature", P),
+                ("n_accept", P), ("token", P), ("logp", P), ("err", P)]
+
+
+class sp_pages(C.Structure):
+    _fields_ = [("kv", P), ("n_layers", C.c_int), ("n_pages", C.c_int), ("page_size", C.c_int), ("row_elems", C.c_int),
+                ("S", C.c_int), ("table", P), ("max_pages", C.c_int), ("lens", P), ("refs", P), ("err", P)]
+
+
 class sp_pipeline_io(C.Structure):
     _fields_ = [("sel", sp_select_in), ("k_cap", C.c_int), ("idx", P), ("count", P), ("cu_seqlens", P),
                 ("hidden", P), ("err", P)]
@@ -218,6 +235,13 @@ def lib():
         "sp_beam_select_workspace": (C.c_size_t, [C.c_int] * 4),
         "sp_beam_select": (C.c_int, [P, P, C.c_size_t, P]),
         "sp_beam_reorder": (C.c_int, [P, P]),
+        "sp_draft_verify_workspace": (C.c_size_t, [C.c_int] * 3),
+        "sp_draft_verify": (C.c_int, [P, P, C.c_size_t, P]),
+        "sp_pages_trim": (C.c_int, [P, P]),
+        "sp_pages_fork": (C.c_int, [P, P, P]),
+        "sp_pages_workspace": (C.c_size_t, [C.c_int] * 2),
+        "sp_pages_reserve": (C.c_int, [P, P, P, C.c_size_t, P]),
+        "sp_pages_compact": (C.c_int, [P, P, C.c_longlong, C.c_int, P, P, C.c_size_t, P]),
         "sp_prefill_paged": (C.c_int, [P, C.POINTER(sp_prefill_io), C.POINTER(sp_paged_kv), P, C.c_size_t, P]),
         "sp_decode_paged_workspace": (C.c_size_t, [P, C.c_int, C.c_int]),
         "sp_decode_paged": (C.c_int, [P, P, P, C.c_size_t, P]),
@@ -652,7 +676,7 @@ def sp_mrope_positions(n_vis, n_txt, grid_w, *, idx, count, k_cap, T_cap, stream
     return {"pos3": pos3, "err": err}
 
 
-# ----------------------------------------------------------------------------- paged cache, shared prefixes, beams
+# ----------------------------------------------------------------------------- paged cache: prefixes, beams, drafts, pages
 #
 # A generation step makes these calls for every layer, and most take the GPU a few microseconds: the arguments are
 # checked with few Python operations and packed by `struct` (an argument struct filled by ctypes costs as much as
@@ -684,6 +708,8 @@ _pack_attention = _packer(sp_prefix_attention_io)
 _pack_select = _packer(sp_beam_select_io)
 _pack_reorder = _packer(sp_beam_reorder_io)
 _pack_decode = _packer(sp_decode_paged_io)
+_pack_verify = _packer(sp_draft_verify_io)
+_pack_pages = _packer(sp_pages)
 
 
 def _enter(who: str, t, stream):
@@ -1006,6 +1032,172 @@ def sp_beam_reorder(*, kv, table, own_table, lens, parent, err=None, stream=None
                            _arg(who, "lens", lens, i32, dev, (R,)), parent.data_ptr(),
                            parent.stride(0) if B > 1 else parent.shape[1], _arg(who, "err", err, i32, dev, (1,)))
         st = lib().sp_beam_reorder(io, _raw_stream(stream, dev))
+        if st:
+            _check(st, who)
+    finally:
+        _leave(guard)
+    return err
+
+
+def draft_verify_workspace(*, T_cap, B, V, device="cuda"):
+    """A workspace for sp_draft_verify calls of these sizes."""
+    with _torch().cuda.device(device):
+        n = lib().sp_draft_verify_workspace(int(T_cap), int(B), int(V))
+    if n == 0:
+        raise SPError("sp_draft_verify_workspace: " + lib().sp_last_error().decode(errors="replace"))
+    return workspace(n, device)
+
+
+def _logits(who, name, t, dtype, dev, shape):
+    """(address, row stride) of rows of numbers, which may lie apart."""
+    if t is None or t.dtype is not dtype or t.shape != shape or t.get_device() != dev or (shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{who}: {name} must be {dtype} {tuple(shape)} on device {dev}, a row's elements side by side")
+    return t.data_ptr(), t.stride(0) if shape[0] > 1 else shape[1]
+
+
+def sp_draft_verify(*, logits, noise=None, cu_rows=None, draft=None, draft_logits=None, u=None, temperature=None,
+                    max_rows=1, n_accept=None, token=None, logp=None, err=None, ws=None, stream=None) -> Dict:
+    """Which drafted tokens of every sequence stay, and the token after them.  logits [T, V] fp32 or bf16 (rows may
+    lie apart): rows cu_rows[b] .. cu_rows[b + 1] - 1 are sequence b's, max_rows of them at most (cu_rows None: one
+    row per sequence, a token is sampled).  draft [T] int32: the token behind row j; draft_logits [T, V] the logits
+    it was drawn from (None: it is taken as certain), u [T] uniform and noise [B, V] exponentially distributed
+    fp32 numbers (noise None: greedy), temperature [B] fp32 (None: 1; not above 0: greedy).  Returns n_accept [B],
+    token and logp [B, max_rows], err."""
+    torch, who = _torch(), "sp_draft_verify"
+    dev, guard = _enter(who, logits, stream)
+    try:
+        f32, i32, where = torch.float32, torch.int32, logits.device
+        is_f32 = logits.dtype is f32
+        if logits.dim() != 2 or not (is_f32 or logits.dtype is torch.bfloat16):
+            raise ValueError("sp_draft_verify: logits must be [T, V] fp32 or bf16")
+        T, V = logits.shape
+        B = T if cu_rows is None else cu_rows.shape[0] - 1
+        x, ld = _logits(who, "logits", logits, logits.dtype, dev, (T, V))
+        y = ld_y = e = ld_e = 0
+        if draft_logits is not None:
+            y, ld_y = _logits(who, "draft_logits", draft_logits, logits.dtype, dev, (T, V))
+        if noise is not None:
+            e, ld_e = _logits(who, "noise", noise, f32, dev, (B, V))
+        shape = (B, max_rows)
+        if n_accept is None:
+            n_accept = torch.empty(B, dtype=i32, device=where)
+        if token is None:
+            token = torch.empty(shape, dtype=i32, device=where)
+        if logp is None:
+            logp = torch.empty(shape, dtype=f32, device=where)
+        if err is None:
+            err = torch.zeros(1, dtype=i32, device=where)
+        if ws is None:
+            ws = draft_verify_workspace(T_cap=T, B=B, V=V, device=where)
+        n = ws.numel()
+        io = _pack_verify(B, V, T, max_rows, _opt(who, "cu_rows", cu_rows, i32, dev, (B + 1,)), x, is_f32, ld,
+                          _opt(who, "draft", draft, i32, dev, (T,)), y, ld_y, _opt(who, "u", u, f32, dev, (T,)), e, ld_e,
+                          _opt(who, "temperature", temperature, f32, dev, (B,)),
+                          _arg(who, "n_accept", n_accept, i32, dev, (B,)), _arg(who, "token", token, i32, dev, shape),
+                          _arg(who, "logp", logp, f32, dev, shape), _arg(who, "err", err, i32, dev, (1,)))
+        st = lib().sp_draft_verify(io, _arg(who, "ws", ws, torch.uint8, dev, (n,)), n, _raw_stream(stream, dev))
+        if st:
+            _check(st, who)
+    finally:
+        _leave(guard)
+    return {"n_accept": n_accept, "token": token, "logp": logp, "err": err, "_ws": ws}
+
+
+def pages_workspace(*, S, max_pages, device="cuda"):
+    """A workspace for sp_pages_reserve and sp_pages_compact calls on tables of this size."""
+    with _torch().cuda.device(device):
+        n = lib().sp_pages_workspace(int(S), int(max_pages))
+    if n == 0:
+        raise SPError("sp_pages_workspace: " + lib().sp_last_error().decode(errors="replace"))
+    return workspace(n, device)
+
+
+def _pages(who, kv, table, lens, refs, page_size, err, dev):
+    """The packed sp_pages of a call, and its error word."""
+    torch = _torch()
+    i32 = torch.int32
+    k = layers = width = 0
+    pages, page = refs.shape[0], page_size
+    if kv is not None:
+        if kv.dim() != 5:
+            raise ValueError(f"{who}: kv must be the pools of all layers [n_layers, 2, n_pages, page_size, width]")
+        layers, _, _, page, width = kv.shape
+        k = _arg(who, "kv", kv, torch.bfloat16, dev, (layers, 2, pages, page, width))
+    if table.dim() != 2:
+        raise ValueError(f"{who}: table must be [rows, pages]")
+    S, mp = table.shape
+    if err is None:
+        err = torch.zeros(1, dtype=i32, device=table.device)
+    return _pack_pages(k, layers, pages, page, width, S, _arg(who, "table", table, i32, dev, (S, mp)), mp,
+                       _arg(who, "lens", lens, i32, dev, (S,)), _arg(who, "refs", refs, i32, dev, (pages,)),
+                       _arg(who, "err", err, i32, dev, (1,))), err
+
+
+def sp_pages_trim(*, table, lens, refs, page_size, err=None, stream=None):
+    """Releases the pages behind every row's last position: table [S, pages], lens [S], refs [n_pages] int32 (entries
+    that name each page).  Returns err."""
+    who = "sp_pages_trim"
+    dev, guard = _enter(who, table, stream)
+    try:
+        io, err = _pages(who, None, table, lens, refs, page_size, err, dev)
+        st = lib().sp_pages_trim(io, _raw_stream(stream, dev))
+        if st:
+            _check(st, who)
+    finally:
+        _leave(guard)
+    return err
+
+
+def sp_pages_fork(*, table, lens, refs, page_size, parent, err=None, stream=None):
+    """Row s continues row parent[s] (-1: it stays as it is): it shares the parent's pages and takes its length.
+    Returns err."""
+    who = "sp_pages_fork"
+    dev, guard = _enter(who, table, stream)
+    try:
+        io, err = _pages(who, None, table, lens, refs, page_size, err, dev)
+        st = lib().sp_pages_fork(io, _arg(who, "parent", parent, _torch().int32, dev, (table.shape[0],)),
+                                 _raw_stream(stream, dev))
+        if st:
+            _check(st, who)
+    finally:
+        _leave(guard)
+    return err
+
+
+def sp_pages_reserve(*, kv, table, lens, refs, add, ws=None, err=None, stream=None):
+    """Room for add[s] positions behind every row's lens[s]: pages of its own, shared ones copied first (kv
+    [n_layers, 2, n_pages, page_size, width], all layers).  Returns err."""
+    torch, who = _torch(), "sp_pages_reserve"
+    dev, guard = _enter(who, table, stream)
+    try:
+        io, err = _pages(who, kv, table, lens, refs, 0, err, dev)
+        S, mp = table.shape
+        if ws is None:
+            ws = pages_workspace(S=S, max_pages=mp, device=table.device)
+        n = ws.numel()
+        st = lib().sp_pages_reserve(io, _arg(who, "add", add, torch.int32, dev, (S,)),
+                                    _arg(who, "ws", ws, torch.uint8, dev, (n,)), n, _raw_stream(stream, dev))
+        if st:
+            _check(st, who)
+    finally:
+        _leave(guard)
+    return err
+
+
+def sp_pages_compact(*, kv, table, lens, refs, keep, count, ws=None, err=None, stream=None):
+    """Row s keeps the positions keep[s, :count[s]] (keep [S, n] int32, rows may lie apart; count -1: the row stays as it
+    is) and becomes that long.  Returns err."""
+    torch, who = _torch(), "sp_pages_compact"
+    dev, guard = _enter(who, table, stream)
+    try:
+        io, err = _pages(who, kv, table, lens, refs, 0, err, dev)
+        S, mp = table.shape
+        k, ld = _logits(who, "keep", keep, torch.int32, dev, (S, keep.shape[-1]))
+        if ws is None:
+            ws = pages_workspace(S=S, max_pages=mp, device=table.device)
+        n = ws.numel()
+        st = lib().sp_pages_compact(io, k, ld, keep.shape[1], _arg(who, "count", count, torch.int32, dev, (S,)),
+                                    _arg(who, "ws", ws, torch.uint8, dev, (n,)), n, _raw_stream(stream, dev))
         if st:
             _check(st, who)
     finally:

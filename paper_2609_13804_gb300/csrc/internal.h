@@ -373,6 +373,45 @@ cudaError_t beam_reorder_launch(void* kv, int n_layers, int n_pages, int page_sh
                                 const int* own, int max_pages, const int* lens, const int* parent, int ld_parent,
                                 int B, int W, int* err, cudaStream_t st);
 
+// ------------------------------------------------------------- drafted tokens (verify.cu), pages (pages.cu)
+// sp_draft_verify_io's fields, checked
+struct VerifyArgs {
+  int B, V, T_cap, max_rows;
+  const int* cu_rows;  // NULL: row b is sequence b's
+  const void* logits;
+  bool logits_f32;
+  long long ld;
+  const int* draft;
+  const void* draft_logits;  // NULL: the drafts have no distribution
+  long long ld_draft;
+  const float* u;
+  const float* noise;        // NULL: every sequence is greedy
+  long long ld_noise;
+  const float* temperature;  // NULL: 1
+  int* n_accept;
+  int* token;
+  float* logp;               // may be NULL
+  int* err;
+};
+size_t verify_bytes(int T_cap, int V);
+cudaError_t verify_launch(const VerifyArgs& a, void* ws, cudaStream_t st);
+struct PagesArgs {
+  uint4* kv;  // [planes][n_pages][page][row16]
+  int planes, n_pages, page_shift, row16;
+  int S;
+  int* table;  // [S, max_pages]
+  int max_pages;
+  int* lens;
+  int* refs;
+  int* err;
+};
+cudaError_t pages_trim_launch(const PagesArgs& a, cudaStream_t st);
+cudaError_t pages_fork_launch(const PagesArgs& a, const int* parent, cudaStream_t st);
+// keep NULL: reserves add (of every row); else compacts to keep's first add entries (-1: the row stays as it is)
+size_t pages_bytes(int S, int max_pages);
+cudaError_t pages_move_launch(const PagesArgs& a, const int* add, const int* keep, long long ld_keep, int keep_cap, void* ws,
+                              cudaStream_t st);
+
 // ------------------------------------------------------------- entry-point helpers (api.cu)
 // Records a thread-local error message (sp_last_error) and returns `s`.
 sp_status report(sp_status s, const char* fmt, ...);

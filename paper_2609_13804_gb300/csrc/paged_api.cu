@@ -1,4 +1,4 @@
-// Entry points of generation over a paged cache: argument checks on the host and the launches.
+// Entry points of generation over a paged cache (attention, beams, drafted tokens, pages): argument checks on the host and the launches.
 #include <climits>
 #include <cmath>
 
@@ -227,6 +227,155 @@ sp_status sp_beam_reorder(const sp_beam_reorder_io* io, sp_stream stream) {
                                  (cudaStream_t)stream),
              who);
   return SP_OK;
+}
+
+static sp_status check_drafts(const char* who, int T_cap, int B, int V) {
+  if (B < 1 || B > SP_MAX_BATCH || V < 1 || V > (1 << 24))
+    return report(SP_ERR_SHAPE, "%s: B must be in 1..SP_MAX_BATCH and V in 1..2^24", who);
+  if (T_cap < 0 || T_cap > (1 << 24)) return report(SP_ERR_SHAPE, "%s: T_cap must be in 0..2^24", who);
+  return SP_OK;
+}
+
+size_t sp_draft_verify_workspace(int T_cap, int B, int V) {
+  if (check_drafts("sp_draft_verify_workspace", T_cap, B, V) != SP_OK) return 0;
+  return verify_bytes(T_cap, V) + 256;
+}
+
+sp_status sp_draft_verify(const sp_draft_verify_io* io, void* workspace, size_t workspace_bytes, sp_stream stream) {
+  const char* who = "sp_draft_verify";
+  if (!io) return report(SP_ERR_INVALID_ARG, "%s: NULL io", who);
+  const sp_status s = check_drafts(who, io->T_cap, io->B, io->V);
+  if (s != SP_OK) return s;
+  if (io->max_rows < 1 || io->max_rows > SP_MAX_DRAFT_ROWS || (!io->cu_rows && io->T_cap != io->B))
+    return report(SP_ERR_SHAPE, "%s: max_rows must be in 1..SP_MAX_DRAFT_ROWS, T_cap = B without cu_rows", who);
+  if (!io->n_accept || !io->token || (io->T_cap > 0 && !io->logits))
+    return report(SP_ERR_INVALID_ARG, "%s: logits, n_accept, token required", who);
+  const bool drafts = io->max_rows > 1 && io->T_cap > 0;
+  if (drafts && (!io->draft || (io->noise && !io->u)))
+    return report(SP_ERR_INVALID_ARG, "%s: rows behind drafts need draft, and u with noise", who);
+  const bool with_q = drafts && io->noise && io->draft_logits;
+  if (io->ld < io->V || (with_q && io->ld_draft < io->V) || (io->noise && io->ld_noise < io->V))
+    return report(SP_ERR_SHAPE, "%s: row strides must be at least V", who);
+  const size_t esz = io->logits_f32 ? 4 : 2;
+  if (!al(io->logits, esz) || (with_q && !al(io->draft_logits, esz)) || !al(io->noise, 4))
+    return report(SP_ERR_ALIGN, "%s: logits, draft_logits, noise must be aligned to their types", who);
+  const size_t need = verify_bytes(io->T_cap, io->V) + 256;
+  if (!workspace || workspace_bytes < need)
+    return report(SP_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", who, workspace_bytes, need);
+  VerifyArgs a;
+  a.B = io->B;
+  a.V = io->V;
+  a.T_cap = io->T_cap;
+  a.max_rows = io->max_rows;
+  a.cu_rows = io->cu_rows;
+  a.logits = io->logits;
+  a.logits_f32 = io->logits_f32 != 0;
+  a.ld = io->ld;
+  a.draft = io->draft;
+  a.draft_logits = with_q ? io->draft_logits : nullptr;
+  a.ld_draft = io->ld_draft;
+  a.u = io->u;
+  a.noise = io->noise;
+  a.ld_noise = io->ld_noise;
+  a.temperature = io->temperature;
+  a.n_accept = io->n_accept;
+  a.token = io->token;
+  a.logp = io->logp;
+  a.err = io->err;
+  void* base = reinterpret_cast<void*>((reinterpret_cast<uintptr_t>(workspace) + 255) & ~uintptr_t(255));
+  SP_PG_CUDA(verify_launch(a, base, (cudaStream_t)stream), who);
+  return SP_OK;
+}
+
+static sp_status check_rows(const char* who, int S, int max_pages) {
+  if (S < 1 || S > SP_MAX_TABLE_ROWS || max_pages < 1 || (long long)S * max_pages > (1ll << 30))
+    return report(SP_ERR_SHAPE, "%s: S must be in 1..SP_MAX_TABLE_ROWS, S * max_pages in 1..2^30", who);
+  return SP_OK;
+}
+
+// moves: the call moves positions, so it needs the pool
+static sp_status page_args(const char* who, const sp_pages* p, bool moves, PagesArgs* a) {
+  if (!p) return report(SP_ERR_INVALID_ARG, "%s: NULL pages", who);
+  const sp_status s = check_rows(who, p->S, p->max_pages);
+  if (s != SP_OK) return s;
+  const int shift = page_shift_of(p->page_size);
+  if (shift < 0) return report(SP_ERR_SHAPE, "%s: page_size must be a power of two in 16..1024", who);
+  if (p->n_pages < 1 || (long long)p->n_pages * p->page_size > (1ll << 30) ||
+      (long long)p->max_pages * p->page_size > (1ll << 30))
+    return report(SP_ERR_SHAPE, "%s: n_pages must be at least 1, n_pages and max_pages at most 2^30 positions", who);
+  if (!p->table || !p->lens || !p->refs || (moves && !p->kv))
+    return report(SP_ERR_INVALID_ARG, "%s: %stable, lens, refs required", who, moves ? "kv, " : "");
+  if (moves && (p->n_layers < 1 || p->n_layers > SP_MAX_LM_LAYERS))
+    return report(SP_ERR_SHAPE, "%s: n_layers must be in 1..SP_MAX_LM_LAYERS", who);
+  if (moves && (p->row_elems < 8 || p->row_elems % 8 != 0 || p->row_elems > (1 << 20)))
+    return report(SP_ERR_SHAPE, "%s: row_elems must be a multiple of 8 in 8..2^20", who);
+  if ((moves && !al(p->kv, 16)) || !al(p->refs, 16))
+    return report(SP_ERR_ALIGN, "%s: %srefs must be 16-byte aligned", who, moves ? "kv and " : "");
+  a->kv = static_cast<uint4*>(p->kv);
+  a->planes = 2 * p->n_layers;
+  a->n_pages = p->n_pages;
+  a->page_shift = shift;
+  a->row16 = p->row_elems / 8;
+  a->S = p->S;
+  a->table = p->table;
+  a->max_pages = p->max_pages;
+  a->lens = p->lens;
+  a->refs = p->refs;
+  a->err = p->err;
+  return SP_OK;
+}
+
+sp_status sp_pages_trim(const sp_pages* p, sp_stream stream) {
+  PagesArgs a;
+  const sp_status s = page_args("sp_pages_trim", p, false, &a);
+  if (s != SP_OK) return s;
+  SP_PG_CUDA(pages_trim_launch(a, (cudaStream_t)stream), "sp_pages_trim");
+  return SP_OK;
+}
+
+sp_status sp_pages_fork(const sp_pages* p, const int* parent, sp_stream stream) {
+  PagesArgs a;
+  const sp_status s = page_args("sp_pages_fork", p, false, &a);
+  if (s != SP_OK) return s;
+  if (!parent) return report(SP_ERR_INVALID_ARG, "sp_pages_fork: parent required");
+  SP_PG_CUDA(pages_fork_launch(a, parent, (cudaStream_t)stream), "sp_pages_fork");
+  return SP_OK;
+}
+
+size_t sp_pages_workspace(int S, int max_pages) {
+  if (check_rows("sp_pages_workspace", S, max_pages) != SP_OK) return 0;
+  return pages_bytes(S, max_pages) + 256;
+}
+
+static sp_status move_pages(const char* who, const PagesArgs& a, const int* add, const int* keep, long long ld_keep,
+                            int keep_cap, void* workspace, size_t workspace_bytes, cudaStream_t stream) {
+  const size_t need = pages_bytes(a.S, a.max_pages) + 256;
+  if (!workspace || workspace_bytes < need)
+    return report(SP_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", who, workspace_bytes, need);
+  void* base = reinterpret_cast<void*>((reinterpret_cast<uintptr_t>(workspace) + 255) & ~uintptr_t(255));
+  SP_PG_CUDA(pages_move_launch(a, add, keep, ld_keep, keep_cap, base, stream), who);
+  return SP_OK;
+}
+
+sp_status sp_pages_reserve(const sp_pages* p, const int* add, void* workspace, size_t workspace_bytes, sp_stream stream) {
+  const char* who = "sp_pages_reserve";
+  PagesArgs a;
+  const sp_status s = page_args(who, p, true, &a);
+  if (s != SP_OK) return s;
+  if (!add) return report(SP_ERR_INVALID_ARG, "%s: add required", who);
+  return move_pages(who, a, add, nullptr, 0, 0, workspace, workspace_bytes, (cudaStream_t)stream);
+}
+
+sp_status sp_pages_compact(const sp_pages* p, const int* keep, long long ld_keep, int keep_cap, const int* count,
+                           void* workspace, size_t workspace_bytes, sp_stream stream) {
+  const char* who = "sp_pages_compact";
+  PagesArgs a;
+  const sp_status s = page_args(who, p, true, &a);
+  if (s != SP_OK) return s;
+  if (!keep || !count) return report(SP_ERR_INVALID_ARG, "%s: keep and count required", who);
+  if (keep_cap < 1 || ld_keep < keep_cap || (long long)a.S * keep_cap > (1ll << 30))
+    return report(SP_ERR_SHAPE, "%s: keep_cap must be at least 1 and at most ld_keep, S * keep_cap at most 2^30", who);
+  return move_pages(who, a, count, keep, ld_keep, keep_cap, workspace, workspace_bytes, (cudaStream_t)stream);
 }
 
 }  // extern "C"
