@@ -783,8 +783,8 @@ SP_API sp_status sp_beam_reorder(const sp_beam_reorder_io* io, sp_stream stream)
  *   n_accept[b] = a, token[b] = the drafts that stay, the next token and -1 behind
  *   it, logp[b] = log p of each (0 behind them).  A sequence without rows gets
  *   n_accept -1, one with more than max_rows, or rows outside 0 .. T_cap - 1, sets
- *   SP_DEVERR_INDEX besides.  A draft outside the vocabulary is rejected and sets
- *   SP_DEVERR_INDEX.
+ *   SP_DEVERR_INDEX besides.  A draft outside the vocabulary is rejected; where that
+ *   ends its sequence SP_DEVERR_INDEX is set.
  * NaN and -infinity logits have no weight; a row with +infinity spreads its weight
  * over them.  A token whose noise is NaN or below 0 is not drawn.  Where no token can
  * be drawn (a row without weight) the next token is -1, its logp -infinity.  A draft
@@ -812,6 +812,7 @@ typedef struct {
   int* token;               /* DEVICE [B, max_rows] */
   float* logp;              /* DEVICE [B, max_rows] or NULL */
   int* err;                 /* DEVICE error word or NULL */
+  int clear_err;            /* 1: the call sets *err to 0 first (a word of its own) */
 } sp_draft_verify_io;
 
 SP_API size_t sp_draft_verify_workspace(int T_cap, int B, int V);

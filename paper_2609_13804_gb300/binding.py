@@ -171,7 +171,7 @@ class sp_draft_verify_io(C.Structure):
     _fields_ = [("B", C.c_int), ("V", C.c_int), ("T_cap", C.c_int), ("max_rows", C.c_int), ("cu_rows", P),
                 ("logits", P), ("logits_f32", C.c_int), ("ld", C.c_longlong), ("draft", P), ("draft_logits", P),
                 ("ld_draft", C.c_longlong), ("u", P), ("noise", P), ("ld_noise", C.c_longlong), ("temperature", P),
-                ("n_accept", P), ("token", P), ("logp", P), ("err", P)]
+                ("n_accept", P), ("token", P), ("logp", P), ("err", P), ("clear_err", C.c_int)]
 
 
 class sp_pages(C.Structure):
@@ -1080,21 +1080,30 @@ def sp_draft_verify(*, logits, noise=None, cu_rows=None, draft=None, draft_logit
             e, ld_e = _logits(who, "noise", noise, f32, dev, (B, V))
         shape = (B, max_rows)
         if n_accept is None:
-            n_accept = torch.empty(B, dtype=i32, device=where)
+            n_accept = torch.empty((B,), dtype=i32, device=where)
+            na = n_accept.data_ptr()
+        else:
+            na = _arg(who, "n_accept", n_accept, i32, dev, (B,))
         if token is None:
             token = torch.empty(shape, dtype=i32, device=where)
+            tk = token.data_ptr()
+        else:
+            tk = _arg(who, "token", token, i32, dev, shape)
         if logp is None:
             logp = torch.empty(shape, dtype=f32, device=where)
-        if err is None:
-            err = torch.zeros(1, dtype=i32, device=where)
+            lp = logp.data_ptr()
+        else:
+            lp = _arg(who, "logp", logp, f32, dev, shape)
+        clear = err is None
+        if clear:
+            err = torch.empty((1,), dtype=i32, device=where)
         if ws is None:
             ws = draft_verify_workspace(T_cap=T, B=B, V=V, device=where)
         n = ws.numel()
         io = _pack_verify(B, V, T, max_rows, _opt(who, "cu_rows", cu_rows, i32, dev, (B + 1,)), x, is_f32, ld,
                           _opt(who, "draft", draft, i32, dev, (T,)), y, ld_y, _opt(who, "u", u, f32, dev, (T,)), e, ld_e,
-                          _opt(who, "temperature", temperature, f32, dev, (B,)),
-                          _arg(who, "n_accept", n_accept, i32, dev, (B,)), _arg(who, "token", token, i32, dev, shape),
-                          _arg(who, "logp", logp, f32, dev, shape), _arg(who, "err", err, i32, dev, (1,)))
+                          _opt(who, "temperature", temperature, f32, dev, (B,)), na, tk, lp,
+                          _arg(who, "err", err, i32, dev, (1,)), clear)
         st = lib().sp_draft_verify(io, _arg(who, "ws", ws, torch.uint8, dev, (n,)), n, _raw_stream(stream, dev))
         if st:
             _check(st, who)

@@ -392,8 +392,9 @@ struct VerifyArgs {
   int* token;
   float* logp;               // may be NULL
   int* err;
+  bool clear_err;            // *err is set to 0 before it is used
 };
-size_t verify_bytes(int T_cap, int V);
+size_t verify_bytes(int T_cap, int B, int V);
 cudaError_t verify_launch(const VerifyArgs& a, void* ws, cudaStream_t st);
 struct PagesArgs {
   uint4* kv;  // [planes][n_pages][page][row16]

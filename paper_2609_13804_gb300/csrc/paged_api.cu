@@ -238,7 +238,7 @@ static sp_status check_drafts(const char* who, int T_cap, int B, int V) {
 
 size_t sp_draft_verify_workspace(int T_cap, int B, int V) {
   if (check_drafts("sp_draft_verify_workspace", T_cap, B, V) != SP_OK) return 0;
-  return verify_bytes(T_cap, V) + 256;
+  return verify_bytes(T_cap, B, V) + 256;
 }
 
 sp_status sp_draft_verify(const sp_draft_verify_io* io, void* workspace, size_t workspace_bytes, sp_stream stream) {
@@ -259,7 +259,7 @@ sp_status sp_draft_verify(const sp_draft_verify_io* io, void* workspace, size_t 
   const size_t esz = io->logits_f32 ? 4 : 2;
   if (!al(io->logits, esz) || (with_q && !al(io->draft_logits, esz)) || !al(io->noise, 4))
     return report(SP_ERR_ALIGN, "%s: logits, draft_logits, noise must be aligned to their types", who);
-  const size_t need = verify_bytes(io->T_cap, io->V) + 256;
+  const size_t need = verify_bytes(io->T_cap, io->B, io->V) + 256;
   if (!workspace || workspace_bytes < need)
     return report(SP_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", who, workspace_bytes, need);
   VerifyArgs a;
@@ -282,6 +282,7 @@ sp_status sp_draft_verify(const sp_draft_verify_io* io, void* workspace, size_t 
   a.token = io->token;
   a.logp = io->logp;
   a.err = io->err;
+  a.clear_err = io->clear_err != 0;
   void* base = reinterpret_cast<void*>((reinterpret_cast<uintptr_t>(workspace) + 255) & ~uintptr_t(255));
   SP_PG_CUDA(verify_launch(a, base, (cudaStream_t)stream), who);
   return SP_OK;

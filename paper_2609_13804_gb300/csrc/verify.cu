@@ -26,7 +26,8 @@ constexpr int VF_CLUSTER = 8;  // CTAs of a sequence's race, at most
 // A slice's maximum, its sum of exp((x - m) / t) and the first token that holds the maximum (greedy sequences).
 struct __align__(16) RowPart {
   float m, s;
-  int at, unused;
+  int at;
+  float xd;  // slice 0: the row's logit of the draft, -infinity where there is none
 };
 
 struct Seq {
@@ -52,51 +53,120 @@ SP_DEVINL Seq sequence(const VerifyArgs& a, int b) {
 // them), 0 for NaN and -infinity.
 SP_DEVINL float weight(float x, float m, float c) { return x == m ? 1.f : x < m ? ex2((x - m) * c) : 0.f; }
 
-// Sums of every row, a slice to a CTA: blockIdx.x = which * slices + slice (which: 0 the target's, 1 the draft's).
+// A thread's share of a slice: its maximum, its sum and the first batch of loads that holds the maximum; with noise the
+// best of its race too, the logit and noise of which are kept: scores of threads with different maxima are formed again.
+struct Share {
+  float m, s;
+  int first;
+  float x, e;  // the race's best so far
+  int at;      // -1: none
+};
+
+// Tokens v0 .. v1 - 1 of a row, 16 bytes at a time where they lie whole in the slice.
 template <bool F32>
-__global__ void __launch_bounds__(VF_NT, 4) verify_sums_kernel(const VerifyArgs a, int slices, int slice, RowPart* part) {
+struct Slice {
   using K = Chunk<F32>;
-  __shared__ float2 ms_s[VF_WARPS];
-  __shared__ int at_s[VF_WARPS];
-  pdl_wait();
-  const int which = blockIdx.x / slices, sl = blockIdx.x % slices, j = blockIdx.z;
-  const Seq q = sequence(a, blockIdx.y);
-  if (j >= q.n || (which == 1 && (q.greedy || j == q.n - 1))) return;
-  const int row = q.row0 + j, tid = threadIdx.x;
-  constexpr int esz = F32 ? 4 : 2;
-  const char* base = static_cast<const char*>(which ? a.draft_logits : a.logits) + row * (which ? a.ld_draft : a.ld) * esz;
-  const int v0 = min(sl * slice, a.V), v1 = min(v0 + slice, a.V);
-  // whole 16-byte pieces of the slice; what is before and behind them goes one by one
-  const int off = reinterpret_cast<uintptr_t>(base + (size_t)v0 * esz) & 15;
-  const int c0 = v0 + min(((16 - off) & 15) / esz, v1 - v0), chunks = (v1 - c0) / K::N, c1 = c0 + chunks * K::N;
-  const uint4* src = reinterpret_cast<const uint4*>(base + (size_t)c0 * esz);
-  float m = -INFINITY, s = 0.f;
-  int first = -1;  // the first batch of loads that holds m
-  const int beside = tid < c0 - v0 ? v0 + tid : c1 + tid - (c0 - v0);
-  const float mine = beside < (tid < c0 - v0 ? c0 : v1) ? K::one(base, beside) : -INFINITY;
-  for (int c = tid; c < chunks; c += VF_NT * VF_LOADS) {
+  static constexpr int esz = F32 ? 4 : 2;
+  const char* base;
+  int v0, v1, c0, c1, chunks;
+  SP_DEVINL Slice(const void* row, int from, int to) : base(static_cast<const char*>(row)), v0(from), v1(to) {
+    const int off = reinterpret_cast<uintptr_t>(base + (size_t)v0 * esz) & 15;
+    c0 = v0 + min(((16 - off) & 15) / esz, v1 - v0);
+    chunks = (v1 - c0) / K::N;
+    c1 = c0 + chunks * K::N;
+  }
+  SP_DEVINL const uint4* src() const { return reinterpret_cast<const uint4*>(base + (size_t)c0 * esz); }
+  // the token beside the whole pieces that this thread takes (fewer than 16), -1: none
+  SP_DEVINL int beside() const {
+    const int i = threadIdx.x, head = c0 - v0;
+    return i < head ? v0 + i : c1 + i - head < v1 ? c1 + i - head : -1;
+  }
+  // the first token of this thread that holds the maximum `top`
+  SP_DEVINL int first_of(float top, int first) const {
+    int at = 0x7fffffff;
+    if (beside() >= 0 && K::one(base, beside()) == top) at = beside();
+    if (first >= 0) {
+#pragma unroll 1
+      for (int i = 0; i < VF_LOADS * K::N; ++i) {
+        const int c = first + i / K::N * VF_NT, v = c0 + c * K::N + i % K::N;
+        if (c < chunks && K::one(base, v) == top) return min(at, v);
+      }
+    }
+    return at;
+  }
+};
+
+template <bool F32, bool RACE>
+SP_DEVINL Share scan(const Slice<F32>& sl, float cc, const float* noise) {
+  using K = Chunk<F32>;
+  constexpr int E4 = K::N / 4;
+  Share r{-INFINITY, 0.f, -1, 0.f, 1.f, -1};
+  float best = 0.f;  // (relative to r.m)
+  auto race = [&](float x, float w, float e, int v) {
+    const float score = __fdividef(w, e);  // (e = 0: infinity, or NaN for w = 0, which is no candidate)
+    if (score > best) {
+      best = score;
+      r.x = x;
+      r.e = e;
+      r.at = v;
+    }
+  };
+  const int beside = sl.beside();
+  const float mine = beside >= 0 ? K::one(sl.base, beside) : -INFINITY;
+  const uint4* src = sl.src();
+  const float* e = RACE ? noise + sl.c0 : nullptr;
+  const bool e16 = (reinterpret_cast<uintptr_t>(e) & 15) == 0;
+  for (int c = threadIdx.x; c < sl.chunks; c += VF_NT * VF_LOADS) {
     uint4 u[VF_LOADS];
 #pragma unroll
     for (int k = 0; k < VF_LOADS; ++k)
-      u[k] = c + k * VF_NT < chunks ? __ldcs(src + c + k * VF_NT) : make_uint4(K::kNone, K::kNone, K::kNone, K::kNone);
+      u[k] = c + k * VF_NT < sl.chunks ? __ldcs(src + c + k * VF_NT) : make_uint4(K::kNone, K::kNone, K::kNone, K::kNone);
+    float4 n[RACE ? VF_LOADS * E4 : 1];
+    if (RACE) {
+#pragma unroll
+      for (int k = 0; k < VF_LOADS * E4; ++k) {
+        const int at = ((c + k / E4 * VF_NT) * E4 + k % E4) * 4;
+        n[k] = make_float4(1.f, 1.f, 1.f, 1.f);
+        if (c + k / E4 * VF_NT < sl.chunks) {
+          if (e16) n[k] = __ldcs(reinterpret_cast<const float4*>(e + at));
+          else n[k] = make_float4(__ldg(e + at), __ldg(e + at + 1), __ldg(e + at + 2), __ldg(e + at + 3));
+        }
+      }
+    }
     float lm = -INFINITY;
 #pragma unroll
     for (int k = 0; k < VF_LOADS; ++k) lm = fmaxf(lm, K::top(u[k]));
     if (lm == -INFINITY) continue;
-    if (lm > m) {
-      s = m == -INFINITY ? 0.f : s * ex2((m - lm) * q.c);
-      m = lm;
-      first = c;
+    if (lm > r.m) {
+      const float f = r.m == -INFINITY ? 0.f : ex2((r.m - lm) * cc);
+      r.s *= f;
+      best *= f;
+      r.m = lm;
+      r.first = c;
+    }
+    if (RACE) {
+      float sum = 0.f;
+#pragma unroll
+      for (int k = 0; k < VF_LOADS; ++k)
+#pragma unroll
+        for (int i = 0; i < K::N; ++i) {
+          const float x = K::at(u[k], i), w = weight(x, r.m, cc);
+          const float4& f = n[k * E4 + i / 4];
+          sum += w;
+          race(x, w, i % 4 == 0 ? f.x : i % 4 == 1 ? f.y : i % 4 == 2 ? f.z : f.w, sl.c0 + (c + k * VF_NT) * K::N + i);
+        }
+      r.s += sum;
+      continue;
     }
     // (x - m first, exactly where it matters: m log2 e rounded would shift the whole sum)
-    const unsigned long long nm = pack2(-m, -m), cc = pack2(q.c, q.c);
+    const unsigned long long nm = pack2(-r.m, -r.m), c2 = pack2(cc, cc);
     unsigned long long sum[2] = {0ull, 0ull};
 #pragma unroll
     for (int k = 0; k < VF_LOADS; ++k)
 #pragma unroll
       for (int i = 0; i < K::N; i += 2) {
         float x, y;
-        unpack2(mul2(add2(pack2(K::at(u[k], i), K::at(u[k], i + 1)), nm), cc), x, y);
+        unpack2(mul2(add2(pack2(K::at(u[k], i), K::at(u[k], i + 1)), nm), c2), x, y);
         sum[(i >> 1) & 1] = add2(sum[(i >> 1) & 1], pack2(ex2(x), ex2(y)));
       }
     float sa, sb;
@@ -107,76 +177,163 @@ __global__ void __launch_bounds__(VF_NT, 4) verify_sums_kernel(const VerifyArgs 
 #pragma unroll
       for (int k = 0; k < VF_LOADS; ++k)
 #pragma unroll
-        for (int i = 0; i < K::N; ++i) ts += weight(K::at(u[k], i), m, q.c);
+        for (int i = 0; i < K::N; ++i) ts += weight(K::at(u[k], i), r.m, cc);
     }
-    s += ts;
+    r.s += ts;
   }
   if (mine > -INFINITY) {
-    const float mn = fmaxf(m, mine);
-    s = (m > -INFINITY ? s * weight(m, mn, q.c) : 0.f) + weight(mine, mn, q.c);
-    if (mine > m) first = -1;
-    m = mn;
-  }
-  pdl_trigger();
-  const int warp = tid >> 5, lane = tid & 31;
-  const float mw = warp_max(m);
-  const float sw = warp_sum(m > -INFINITY ? (m == mw ? s : s * ex2((m - mw) * q.c)) : 0.f);
-  if (lane == 0) ms_s[warp] = make_float2(mw, sw);
-  __syncthreads();
-  float top = -INFINITY;
-#pragma unroll
-  for (int w = 0; w < VF_WARPS; ++w) top = fmaxf(top, ms_s[w].x);
-  int at = 0x7fffffff;
-  if (q.greedy && m == top && m > -INFINITY) {  // the first of this thread's tokens with the maximum
-    if (mine == top) at = beside;
-    if (first >= 0) {
-#pragma unroll 1
-      for (int i = 0; i < VF_LOADS * K::N; ++i) {
-        const int c = first + i / K::N * VF_NT, v = c0 + c * K::N + i % K::N;
-        if (c < chunks && K::one(base, v) == top) {
-          at = min(at, v);
-          break;
-        }
+    const float mn = fmaxf(r.m, mine), f = r.m > -INFINITY ? weight(r.m, mn, cc) : 0.f;
+    if (mine > r.m) r.first = -1;
+    r.s = r.s * f + weight(mine, mn, cc);
+    best *= f;
+    r.m = mn;
+    if (RACE) {
+      const float score = __fdividef(weight(mine, mn, cc), __ldg(noise + beside));
+      if (score > best || (score == best && beside < r.at)) {
+        r.x = mine;
+        r.e = __ldg(noise + beside);
+        r.at = beside;
       }
     }
   }
-  if (q.greedy) {
+  return r;
+}
+
+// Joins the CTA's shares: the slice's maximum in every thread, its sum (and a greedy sequence's first token with the
+// maximum, of `first` of every thread) in thread 0.
+template <typename First>
+SP_DEVINL RowPart join_cta(float m, float s, float c, bool greedy, First first) {
+  __shared__ float2 ms_s[VF_WARPS];
+  __shared__ int at_s[VF_WARPS];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const float mw = warp_max(m);
+  const float sw = warp_sum(m > -INFINITY ? (m == mw ? s : s * ex2((m - mw) * c)) : 0.f);
+  if (lane == 0) ms_s[warp] = make_float2(mw, sw);
+  __syncthreads();
+  float top = -INFINITY, sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < VF_WARPS; ++w) top = fmaxf(top, ms_s[w].x);
+  int at = 0x7fffffff;
+  if (greedy) {
+    if (m == top && m > -INFINITY) at = first(top);
     at = __reduce_min_sync(0xffffffffu, at);
     if (lane == 0) at_s[warp] = at;
     __syncthreads();
   }
-  if (tid == 0) {
-    float sum = 0.f;
+  if (threadIdx.x == 0)
     for (int w = 0; w < VF_WARPS; ++w) {
-      if (ms_s[w].x > -INFINITY) sum += ms_s[w].x == top ? ms_s[w].y : ms_s[w].y * ex2((ms_s[w].x - top) * q.c);
-      if (q.greedy) at = min(at, at_s[w]);
+      if (ms_s[w].x > -INFINITY) sum += ms_s[w].x == top ? ms_s[w].y : ms_s[w].y * ex2((ms_s[w].x - top) * c);
+      if (greedy) at = min(at, at_s[w]);
     }
-    part[((size_t)row * 2 + which) * slices + sl] = RowPart{top, sum, at, 0};
-  }
+  return RowPart{top, sum, at, 0.f};
 }
 
-// A row's maximum, sum and (greedy) first token with the maximum, joined by a warp from its slices; every lane has them.
-SP_DEVINL RowPart join_row(const RowPart* part, int slices, float c) {
-  const int lane = threadIdx.x & 31;
-  RowPart r{-INFINITY, 0.f, 0x7fffffff, 0};
+// A row as its decision and its race need it.
+struct __align__(16) Row {
+  float mp, sp, mq, sq;  // maxima and sums of the target's and the draft's logits
+  float xd;              // the target's logit of the draft
+  int at;                // greedy: the first token with the maximum
+  int stays;             // the draft does
+  int unused;
+};
+
+// What a call leaves in its workspace between kernels.
+struct VerifyWork {
+  RowPart* part;  // [T_cap][2][slices]
+  Row* rows;      // [T_cap], ordered calls only
+  int* count;     // [T_cap] slices of a row that are done, from kUnset on (ordered calls)
+  int* end;       // [B] the first row of a sequence known to reject its draft, kUnset: none (ordered calls)
+};
+constexpr int kUnset = 0x7f7f7f7f;
+
+// A row's slices, joined by a warp; whether its draft stays.  Every lane has the result.
+SP_DEVINL Row decide(const VerifyArgs& a, const Seq& q, int j, const RowPart* part, int slices) {
+  const int lane = threadIdx.x & 31, row = q.row0 + j;
+  const bool last = j == q.n - 1, with_q = a.draft_logits && !q.greedy && !last;
+  const RowPart none{-INFINITY, 0.f, 0x7fffffff, -INFINITY};
+  RowPart p = none, r = none;
   if (lane < slices) {
-    const int4 v = __ldcg(reinterpret_cast<const int4*>(part) + lane);
-    r = RowPart{__int_as_float(v.x), __int_as_float(v.y), v.z, 0};
+    const int4* from = reinterpret_cast<const int4*>(part + (size_t)row * 2 * slices) + lane;
+    const int4 v = __ldcg(from);
+    p = RowPart{__int_as_float(v.x), __int_as_float(v.y), v.z, __int_as_float(v.w)};
+    if (with_q) {
+      const int4 w = __ldcg(from + slices);
+      r = RowPart{__int_as_float(w.x), __int_as_float(w.y), w.z, __int_as_float(w.w)};
+    }
   }
-  const float m = warp_max(r.m);
-  const float s = warp_sum(r.m > -INFINITY ? (r.m == m ? r.s : r.s * ex2((r.m - m) * c)) : 0.f);
-  const int at = __reduce_min_sync(0xffffffffu, r.m == m ? r.at : 0x7fffffff);
-  return RowPart{m, s, at, 0};
+  const int d = last ? -1 : __ldg(a.draft + row);
+  const float u = last || q.greedy ? 0.f : __ldg(a.u + row);
+  Row o;
+  o.mp = warp_max(p.m);
+  o.mq = warp_max(r.m);
+  o.sp = warp_sum(p.m > -INFINITY ? (p.m == o.mp ? p.s : p.s * ex2((p.m - o.mp) * q.c)) : 0.f);
+  o.sq = warp_sum(r.m > -INFINITY ? (r.m == o.mq ? r.s : r.s * ex2((r.m - o.mq) * q.c)) : 0.f);
+  o.at = __reduce_min_sync(0xffffffffu, p.m == o.mp ? p.at : 0x7fffffff);
+  o.xd = __shfl_sync(0xffffffffu, p.xd, 0);
+  const float yd = __shfl_sync(0xffffffffu, r.xd, 0);
+  o.unused = 0;
+  if (last) o.stays = 0;
+  else if (q.greedy) o.stays = d == o.at;
+  else {  // u q(d) < p(d), the sums multiplied out; without weight anywhere p is 0
+    const float pd = o.sp > 0.f ? weight(o.xd, o.mp, q.c) : 0.f;
+    const float qd = !with_q ? 1.f : o.sq > 0.f ? weight(yd, o.mq, q.c) : 0.f;
+    o.stays = u * qd * o.sp < pd * (with_q && o.sq > 0.f ? o.sq : 1.f);
+  }
+  return o;
 }
 
-// p(x) and log p(x) of a logit in a row, from its maximum and sum, in 64 bits.
-SP_DEVINL double prob(float x, const RowPart& r, float t) {
-  if (!(x > -INFINITY) || !(x <= r.m)) return 0.0;
-  return (x == r.m ? 1.0 : exp(((double)x - (double)r.m) / (double)t)) / (double)r.s;
+// Sums of every row, a slice to a CTA: blockIdx.x = which * slices + slice (which: 0 the target's, 1 the draft's),
+// blockIdx.z the row of the sequence.  ORDERED: the CTA that ends a row decides about its draft, and rows behind one that
+// rejects are passed over.  CTAs start in the order of their numbers, so in a call of many waves most of those rows
+// are never read; nothing waits, and what is read needlessly has no effect.
+template <bool F32, bool ORDERED>
+__global__ void __launch_bounds__(VF_NT, 4) verify_sums_kernel(const VerifyArgs a, int slices, int slice, VerifyWork work) {
+  using K = Chunk<F32>;
+  __shared__ int last_s;
+  pdl_wait();
+  const int which = blockIdx.x / slices, sl = blockIdx.x % slices, b = blockIdx.y, j = blockIdx.z;
+  if (a.clear_err && a.err && blockIdx.x + b + j == 0 && threadIdx.x == 0) *a.err = 0;
+  const Seq q = sequence(a, b);
+  const bool last = j == q.n - 1;
+  if (j >= q.n || (which == 1 && (q.greedy || last))) return;
+  if (ORDERED && __ldcg(work.end + b) < j) return;
+  const int row = q.row0 + j;
+  const char* base = static_cast<const char*>(which ? a.draft_logits : a.logits) +
+                     row * (which ? a.ld_draft : a.ld) * (F32 ? 4 : 2);
+  float xd = -INFINITY;
+  if (sl == 0 && threadIdx.x == 0 && !last) {
+    const int d = __ldg(a.draft + row);
+    if (d >= 0 && d < a.V) xd = K::one(base, d);
+  }
+  const int v0 = min(sl * slice, a.V), v1 = min(v0 + slice, a.V);
+  const Slice<F32> s(base, v0, v1);
+  const Share t = scan<F32, false>(s, q.c, nullptr);
+  pdl_trigger();
+  RowPart r = join_cta(t.m, t.s, q.c, q.greedy, [&](float top) { return s.first_of(top, t.first); });
+  r.xd = xd;
+  if (threadIdx.x == 0) work.part[((size_t)row * 2 + which) * slices + sl] = r;
+  if (ORDERED) {
+    if (threadIdx.x == 0) {
+      __threadfence();
+      const int all = slices * (a.draft_logits && !q.greedy && !last ? 2 : 1);
+      last_s = atomicAdd(work.count + row, 1) == kUnset + all - 1;
+    }
+    __syncthreads();
+    if (last_s && threadIdx.x < 32) {
+      __threadfence();
+      const Row o = decide(a, q, j, work.part, slices);
+      if (threadIdx.x == 0) {
+        work.rows[row] = o;
+        __threadfence();
+        if (!o.stays) atomicMin(work.end + b, j);
+      }
+    }
+  }
 }
-SP_DEVINL float log_prob(float x, const RowPart& r, float t) {
-  if (!(x > -INFINITY) || !(x <= r.m)) return -INFINITY;
-  return (float)((x == r.m ? 0.0 : ((double)x - (double)r.m) / (double)t) - log((double)r.s));
+
+SP_DEVINL float log_prob(float x, float m, float s, float t) {
+  if (!(x > -INFINITY) || !(x <= m)) return -INFINITY;
+  return (x == m ? 0.f : __fdividef(x - m, t)) - logf(s);  // (both at most 0: nothing cancels)
 }
 
 // A race's score and token as one key that sorts by (score, lower token first); scores are above 0, 0: none.
@@ -205,42 +362,40 @@ struct Race {
   // The best of tokens v0 .. v1 - 1 for this thread of the CTA.
   SP_DEVINL unsigned long long run(int v0, int v1) const {
     using K = Chunk<F32>;
-    constexpr int esz = F32 ? 4 : 2;
+    constexpr int esz = F32 ? 4 : 2, E4 = K::N / 4;
     float best = 0.f;
     int at = 0;
-    const char* pb = static_cast<const char*>(p) + (size_t)v0 * esz;
-    const char* qb = static_cast<const char*>(q) + (size_t)v0 * esz;
-    const int off = reinterpret_cast<uintptr_t>(pb) & 15, head = min(((16 - off) & 15) / esz, v1 - v0);
-    const int c0 = v0 + head;
-    const bool together = (!q || (reinterpret_cast<uintptr_t>(qb) & 15) == off) &&
-                          (reinterpret_cast<uintptr_t>(e + c0) & 15) == 0;
-    if (!together) {
+    const Slice<F32> s(p, v0, v1);
+    const char* qb = static_cast<const char*>(q);
+    if (q && ((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(q)) & 15) != 0) {  // no pieces in common
 #pragma unroll 4
-      for (int v = v0 + threadIdx.x; v < v1; v += VF_NT)
-        take(K::one(p, v), q ? K::one(q, v) : 0.f, __ldg(e + v), v, best, at);
+      for (int v = v0 + threadIdx.x; v < v1; v += VF_NT) take(K::one(p, v), K::one(q, v), __ldg(e + v), v, best, at);
       return best > 0.f ? race_key(best, at) : 0ull;
     }
-    const int chunks = (v1 - c0) / K::N, c1 = c0 + chunks * K::N;
     unsigned long long key = 0;
-    if (threadIdx.x < head + v1 - c1) {
-      const int v = threadIdx.x < head ? v0 + threadIdx.x : c1 + threadIdx.x - head;
+    if (s.beside() >= 0) {
+      const int v = s.beside();
       take(K::one(p, v), q ? K::one(q, v) : 0.f, __ldg(e + v), v, best, at);
       if (best > 0.f) key = race_key(best, at);
       best = 0.f;
     }
-    const uint4* ps = reinterpret_cast<const uint4*>(static_cast<const char*>(p) + (size_t)c0 * esz);
-    const uint4* qs = reinterpret_cast<const uint4*>(static_cast<const char*>(q) + (size_t)c0 * esz);
-    const float4* es = reinterpret_cast<const float4*>(e + c0);
+    const uint4* ps = s.src();
+    const uint4* qs = reinterpret_cast<const uint4*>(qb + (size_t)s.c0 * esz);
+    const float* es = e + s.c0;
+    const bool e16 = (reinterpret_cast<uintptr_t>(es) & 15) == 0;
 #pragma unroll 2
-    for (int c = threadIdx.x; c < chunks; c += VF_NT) {
+    for (int c = threadIdx.x; c < s.chunks; c += VF_NT) {
       const uint4 x = __ldg(ps + c), y = q ? __ldg(qs + c) : make_uint4(0, 0, 0, 0);
-      float4 n[K::N / 4];
+      float4 n[E4];
 #pragma unroll
-      for (int k = 0; k < K::N / 4; ++k) n[k] = __ldcs(es + c * (K::N / 4) + k);
+      for (int k = 0; k < E4; ++k) {
+        const float* f = es + (c * E4 + k) * 4;
+        n[k] = e16 ? __ldcs(reinterpret_cast<const float4*>(f)) : make_float4(__ldg(f), __ldg(f + 1), __ldg(f + 2), __ldg(f + 3));
+      }
 #pragma unroll
       for (int i = 0; i < K::N; ++i) {
         const float4& f = n[i / 4];
-        take(K::at(x, i), K::at(y, i), i % 4 == 0 ? f.x : i % 4 == 1 ? f.y : i % 4 == 2 ? f.z : f.w, c0 + c * K::N + i,
+        take(K::at(x, i), K::at(y, i), i % 4 == 0 ? f.x : i % 4 == 1 ? f.y : i % 4 == 2 ? f.z : f.w, s.c0 + c * K::N + i,
              best, at);
       }
     }
@@ -261,96 +416,105 @@ SP_DEVINL unsigned long long cta_max(unsigned long long k, unsigned long long* s
   return k;
 }
 
-// A cluster per sequence: every CTA finds the row where it ends, each races over its slice of it.
-template <bool F32>
-__global__ void __launch_bounds__(VF_NT) verify_end_kernel(const VerifyArgs a, int slices, const RowPart* part) {
+// What a sequence is left with: a row that is not there.
+SP_DEVINL void no_rows(const VerifyArgs& a, int b, bool wrong) {
+  for (int j = threadIdx.x; j < a.max_rows; j += VF_NT) {
+    a.token[(size_t)b * a.max_rows + j] = -1;
+    if (a.logp) a.logp[(size_t)b * a.max_rows + j] = 0.f;
+  }
+  if (threadIdx.x == 0) {
+    if (wrong) set_error(a.err, SP_DEVERR_INDEX);
+    a.n_accept[b] = -1;
+  }
+}
+
+// A cluster per sequence: every CTA finds the row where it ends (ORDERED: is told), each races over its slice of it.
+template <bool F32, bool ORDERED>
+__global__ void __launch_bounds__(VF_NT) verify_end_kernel(const VerifyArgs a, int slices, VerifyWork work) {
   using K = Chunk<F32>;
-  __shared__ RowPart p_s[VF_WARPS], q_s[VF_WARPS];
-  __shared__ int accept_s[VF_WARPS];
+  __shared__ Row row_s[VF_WARPS];
   __shared__ unsigned long long key_s[VF_WARPS], cluster_s[VF_CLUSTER];
-  pdl_wait();
-  pdl_trigger();
+  // Before the wait: what no kernel of this call writes.  (The sums wait for whatever ran before them ahead of their
+  // trigger, so it is over.)
   const int C = gridDim.x, rank = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const Seq q = sequence(a, b);
-  int* token = a.token + (size_t)b * a.max_rows;
-  float* logp = a.logp ? a.logp + (size_t)b * a.max_rows : nullptr;
-  if (rank == 0)
-    for (int j = max(q.n, 0) + tid; j < a.max_rows; j += VF_NT) {
-      token[j] = -1;
-      if (logp) logp[j] = 0.f;
-    }
-  if (q.n <= 0) {  // (no row, or rows that are not there)
-    if (rank == 0 && tid == 0) {
-      if (q.n < 0) set_error(a.err, SP_DEVERR_INDEX);
-      a.n_accept[b] = -1;
-    }
+  pdl_wait();
+  pdl_trigger();
+  if (q.n <= 0) {
+    if (rank == 0) no_rows(a, b, q.n < 0);
     return;
   }
-  constexpr int esz = F32 ? 4 : 2;
-  auto logits = [&](int j) { return static_cast<const char*>(a.logits) + (q.row0 + j) * a.ld * esz; };
-  auto draft_logits = [&](int j) { return static_cast<const char*>(a.draft_logits) + (q.row0 + j) * a.ld_draft * esz; };
+  int* token = a.token + (size_t)b * a.max_rows;
+  float* logp = a.logp ? a.logp + (size_t)b * a.max_rows : nullptr;
+  auto logits = [&](int j) { return static_cast<const char*>(a.logits) + (q.row0 + j) * a.ld * (F32 ? 4 : 2); };
+  auto stays = [&](int j, const Row& r) {  // a draft that stays, written by a warp's first lane
+    const int d = __ldg(a.draft + q.row0 + j);
+    if (d < 0 || d >= a.V) set_error(a.err, SP_DEVERR_INDEX);
+    token[j] = d;
+    if (logp) logp[j] = log_prob(r.xd, r.mp, r.sp, q.t);
+  };
   int end = -1;
-  for (int j0 = 0; end < 0; j0 += VF_WARPS) {  // a warp to a row
-    const int j = j0 + warp;
-    bool stays = true;
-    if (j < q.n) {
-      const int row = q.row0 + j;
-      const int d = j < q.n - 1 ? __ldg(a.draft + row) : -1;
-      const bool there = d >= 0 && d < a.V;
-      const RowPart p = join_row(part + ((size_t)row * 2) * slices, slices, q.c);
-      const bool with_q = a.draft_logits && !q.greedy && j < q.n - 1;
-      RowPart r{0.f, 0.f, 0, 0};
-      if (with_q) r = join_row(part + ((size_t)row * 2 + 1) * slices, slices, q.c);
-      if (lane == 0) {
-        stays = false;
-        if (j < q.n - 1) {
-          if (!there) {
-            if (rank == 0) set_error(a.err, SP_DEVERR_INDEX);
-          } else if (q.greedy) {
-            stays = d == p.at;
-          } else {
-            const double pd = prob(K::one(logits(j), d), p, q.t);
-            const double qd = with_q ? prob(K::one(draft_logits(j), d), r, q.t) : 1.0;
-            stays = (double)__ldg(a.u + row) * qd < pd;
-          }
-        }
-        p_s[warp] = p;
-        q_s[warp] = r;
+  Row r;
+  if (ORDERED) {
+    end = __ldcg(work.end + b);
+    if (end >= q.n) {  // (sequences whose offsets overlap)
+      if (rank == 0) no_rows(a, b, true);
+      return;
+    }
+    auto load = [&](int j) {
+      const int4* from = reinterpret_cast<const int4*>(work.rows + q.row0 + j);
+      const int4 x = __ldcg(from), y = __ldcg(from + 1);
+      return Row{__int_as_float(x.x), __int_as_float(x.y), __int_as_float(x.z), __int_as_float(x.w), __int_as_float(y.x),
+                 y.y, y.z, 0};
+    };
+    r = load(end);
+    if (rank == C - 1)
+      for (int j = tid; j < end; j += VF_NT) stays(j, load(j));
+  } else {
+    for (int j0 = 0; end < 0; j0 += VF_WARPS) {  // a warp to a row
+      const int j = j0 + warp;
+      Row mine;
+      mine.stays = 1;
+      if (j < q.n) mine = decide(a, q, j, work.part, slices);
+      if (lane == 0) row_s[warp] = mine;
+      __syncthreads();
+      const unsigned int out = __ballot_sync(0xffffffffu, lane < VF_WARPS && !row_s[lane % VF_WARPS].stays);
+      const int w = out ? __ffs(out) - 1 : VF_WARPS;
+      if (out) {
+        end = j0 + w;
+        r = row_s[w];
       }
+      if (rank == C - 1 && lane == 0 && j < q.n && warp < w) stays(j, mine);
+      if (end < 0) __syncthreads();
     }
-    if (lane == 0) accept_s[warp] = stays;
-    __syncthreads();
-    int w = 0;
-    while (w < VF_WARPS && accept_s[w]) ++w;
-    if (w < VF_WARPS) end = j0 + w;
-    if (rank == 0 && lane == 0 && j < q.n && warp < w) {
-      const int d = __ldg(a.draft + q.row0 + j);
-      token[j] = d;
-      if (logp) logp[j] = log_prob(K::one(logits(j), d), p_s[warp], q.t);
-    }
-    if (end < 0) __syncthreads();
   }
-  const RowPart p = p_s[end % VF_WARPS], r = q_s[end % VF_WARPS];
   const bool drafted = end < q.n - 1;
-  if (rank == 0)
-    for (int j = end + 1 + tid; j < q.n; j += VF_NT) {
+  int d = -1;
+  if (drafted) {
+    d = __ldg(a.draft + q.row0 + end);
+    if (rank == 0 && tid == 0 && (d < 0 || d >= a.V)) set_error(a.err, SP_DEVERR_INDEX);
+  }
+  if (rank == C - 1)
+    for (int j = end + 1 + tid; j < a.max_rows; j += VF_NT) {
       token[j] = -1;
       if (logp) logp[j] = 0.f;
     }
   // (sequences whose offsets overlap can find another's sums: never a token that is not there)
-  int next = p.m > -INFINITY && p.at >= 0 && p.at < a.V ? p.at : -1;
+  int next = r.mp > -INFINITY && r.at >= 0 && r.at < a.V ? r.at : -1;
   if (!q.greedy) {
     if (C > 1) cluster_sync_all();  // every CTA of the cluster runs
     Race<F32> race;
     race.p = logits(end);
-    race.q = drafted && a.draft_logits ? draft_logits(end) : nullptr;
+    race.q = drafted && a.draft_logits
+                 ? static_cast<const char*>(a.draft_logits) + (q.row0 + end) * a.ld_draft * (F32 ? 4 : 2)
+                 : nullptr;
     race.e = a.noise + (size_t)b * a.ld_noise;
-    race.mp = p.m;
-    race.ip = p.s > 0.f ? 1.f / p.s : 0.f;
-    race.mq = r.m;
-    race.iq = r.s > 0.f ? 1.f / r.s : 0.f;
+    race.mp = r.mp;
+    race.ip = r.sp > 0.f ? 1.f / r.sp : 0.f;
+    race.mq = r.mq;
+    race.iq = r.sq > 0.f ? 1.f / r.sq : 0.f;
     race.c = q.c;
-    race.out = drafted && !a.draft_logits ? __ldg(a.draft + q.row0 + end) : -1;
+    race.out = a.draft_logits ? -1 : d;
     const int per = (((a.V + C - 1) / C) + 7) & ~7;
     const int v0 = min(rank * per, a.V), v1 = min(v0 + per, a.V);
     unsigned long long key = cta_max(race.run(v0, v1), key_s);
@@ -373,7 +537,74 @@ __global__ void __launch_bounds__(VF_NT) verify_end_kernel(const VerifyArgs a, i
   if (rank == 0 && tid == 0) {
     a.n_accept[b] = end;
     token[end] = next;
-    if (logp) logp[end] = next >= 0 ? log_prob(K::one(logits(end), next), p, q.t) : -INFINITY;
+    if (logp) logp[end] = next >= 0 ? log_prob(K::one(logits(end), next), r.mp, r.sp, q.t) : -INFINITY;
+  }
+}
+
+// Without drafts: a cluster per sequence, the sums and the race in one pass over its row.
+template <bool F32>
+__global__ void __launch_bounds__(VF_NT) verify_sample_kernel(const VerifyArgs a) {
+  struct __align__(16) Best {
+    float m, s, x, e;
+    int at, greedy_at, unused[2];
+  };
+  __shared__ Best best_s[VF_CLUSTER], mine_s;
+  __shared__ unsigned long long key_s[VF_WARPS];
+  pdl_wait();
+  pdl_trigger();
+  const int C = gridDim.x, rank = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+  const Seq q = sequence(a, b);
+  if (a.clear_err && a.err && rank + b == 0 && tid == 0 && !a.cu_rows) *a.err = 0;
+  if (q.n <= 0) {
+    if (rank == 0) no_rows(a, b, q.n < 0);
+    return;
+  }
+  const char* base = static_cast<const char*>(a.logits) + q.row0 * a.ld * (F32 ? 4 : 2);
+  const float* noise = q.greedy ? nullptr : a.noise + (size_t)b * a.ld_noise;
+  const int per = (((a.V + C - 1) / C) + 7) & ~7;
+  const Slice<F32> s(base, min(rank * per, a.V), min((rank + 1) * per, a.V));
+  const Share t = q.greedy ? scan<F32, false>(s, q.c, nullptr) : scan<F32, true>(s, q.c, noise);
+  const RowPart r = join_cta(t.m, t.s, q.c, q.greedy, [&](float top) { return s.first_of(top, t.first); });
+  const float score = t.at >= 0 ? __fdividef(weight(t.x, r.m, q.c), t.e) : 0.f;
+  const unsigned long long own = score > 0.f ? race_key(score, t.at) : 0ull, key = cta_max(own, key_s);
+  if (tid == 0) mine_s = Best{r.m, r.s, 0.f, 1.f, -1, r.at, {0, 0}};
+  __syncthreads();
+  if (own != 0 && own == key) {
+    mine_s.x = t.x;
+    mine_s.e = t.e;
+    mine_s.at = t.at;
+  }
+  if (C > 1) cluster_sync_all();  // every CTA of the cluster runs, and its best is there
+  else __syncthreads();
+  if (C > 1) {
+    if (tid < 8) {
+      const uint32_t to = mapa_shared(smem_u32(reinterpret_cast<uint32_t*>(&best_s[rank]) + tid), 0);
+      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(to), "r"(reinterpret_cast<uint32_t*>(&mine_s)[tid]) : "memory");
+    }
+    cluster_sync_all();
+    if (rank != 0) return;
+  } else if (tid == 0) {
+    best_s[0] = mine_s;
+  }
+  if (tid == 0) {
+    float m = -INFINITY, sum = 0.f, x = -INFINITY;
+    for (int i = 0; i < C; ++i) m = fmaxf(m, best_s[i].m);
+    unsigned long long k = 0;
+    int next = -1;
+    for (int i = 0; i < C; ++i) {
+      const Best& o = best_s[i];
+      if (o.m == -INFINITY) continue;
+      sum += o.m == m ? o.s : o.s * ex2((o.m - m) * q.c);
+      if (q.greedy) {
+        if (next < 0 && o.m == m) next = o.greedy_at, x = m;
+      } else if (o.at >= 0) {
+        const float sc = __fdividef(weight(o.x, m, q.c), o.e);
+        if (sc > 0.f && race_key(sc, o.at) > k) k = race_key(sc, o.at), next = o.at, x = o.x;
+      }
+    }
+    a.n_accept[b] = 0;
+    a.token[b] = next;
+    if (a.logp) a.logp[b] = next >= 0 ? log_prob(x, m, sum, q.t) : -INFINITY;
   }
 }
 
@@ -385,22 +616,17 @@ static int verify_slices(int rows, int V) {
   return std::max(1, std::min(std::min(std::max(want, (V + 32767) / 32768), VF_SLICES), (V + 4095) / 4096));
 }
 
-size_t verify_bytes(int T_cap, int V) { return (size_t)T_cap * 2 * verify_slices(T_cap, V) * sizeof(RowPart); }
+static size_t align256(size_t n) { return (n + 255) & ~size_t(255); }
 
-cudaError_t verify_launch(const VerifyArgs& a, void* ws, cudaStream_t st) {
-  auto* part = static_cast<RowPart*>(ws);
-  const int slices = verify_slices(a.T_cap, a.V), slice = (((a.V + slices - 1) / slices) + 7) & ~7;
-  cudaError_t r = cudaSuccess;
-  if (a.T_cap > 0) {
-    prof_begin_launch(st);
-    r = launch_pdl(a.logits_f32 ? verify_sums_kernel<true> : verify_sums_kernel<false>,
-                   dim3(slices * (a.draft_logits ? 2 : 1), a.B, a.max_rows), dim3(VF_NT), 0, st, a, slices, slice, part);
-    prof_end_launch(st, SP_K_MISC, 0.0, (double)a.T_cap * a.V * (a.logits_f32 ? 4 : 2) * (a.draft_logits ? 2 : 1));
-    if (r != cudaSuccess) return r;
-  }
-  const int C = a.noise ? std::max(1, std::min(VF_CLUSTER, (a.V + 2047) / 2048)) : 1;
+size_t verify_bytes(int T_cap, int B, int V) {
+  const size_t T = (size_t)T_cap;
+  return align256(T * 2 * verify_slices(T_cap, V) * sizeof(RowPart)) + align256(T * sizeof(Row)) + align256((T + B) * 4);
+}
+
+template <typename Kernel, typename... Args>
+static cudaError_t launch_clusters(Kernel* k, int C, int B, cudaStream_t st, Args... args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(C, a.B);
+  cfg.gridDim = dim3(C, B);
   cfg.blockDim = dim3(VF_NT);
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
@@ -411,9 +637,50 @@ cudaError_t verify_launch(const VerifyArgs& a, void* ws, cudaStream_t st) {
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = pdl_enabled() ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, k, args...);
+}
+
+cudaError_t verify_launch(const VerifyArgs& a, void* ws, cudaStream_t st) {
+  const int sms = device_sm_count();
+  const double bytes = (double)a.T_cap * a.V * (a.logits_f32 ? 4 : 2);
+  // CTAs of a sequence: four per SM where there are few, one wave of them where there are many
+  const int C = std::max(1, std::min(std::min(VF_CLUSTER, (a.V + 2047) / 2048), sms * 4 / a.B));
+  cudaError_t r;
+  if (a.max_rows == 1) {
+    if (a.cu_rows && a.clear_err && a.err) {
+      r = cudaMemsetAsync(a.err, 0, 4, st);
+      if (r != cudaSuccess) return r;
+    }
+    prof_begin_launch(st);
+    r = launch_clusters(a.logits_f32 ? verify_sample_kernel<true> : verify_sample_kernel<false>, C, a.B, st, a);
+    prof_end_launch(st, SP_K_MISC, 0.0, bytes + (a.noise ? 4.0 * a.B * a.V : 0.0));
+    return r;
+  }
+  const int slices = verify_slices(a.T_cap, a.V), slice = (((a.V + slices - 1) / slices) + 7) & ~7;
+  const int sets = a.draft_logits ? 2 : 1;
+  char* base = static_cast<char*>(ws);
+  VerifyWork w;
+  w.part = reinterpret_cast<RowPart*>(base);
+  base += align256((size_t)a.T_cap * 2 * slices * sizeof(RowPart));
+  w.rows = reinterpret_cast<Row*>(base);
+  base += align256((size_t)a.T_cap * sizeof(Row));
+  w.count = reinterpret_cast<int*>(base);
+  w.end = w.count + a.T_cap;
+  const bool ordered = (long long)a.T_cap * sets * slices > 4 * sms;
+  if (ordered) {
+    r = cudaMemsetAsync(w.count, 0x7f, ((size_t)a.T_cap + a.B) * 4, st);
+    if (r != cudaSuccess) return r;
+  }
   prof_begin_launch(st);
-  r = cudaLaunchKernelEx(&cfg, a.logits_f32 ? verify_end_kernel<true> : verify_end_kernel<false>, a, slices,
-                         (const RowPart*)part);
+  auto* sums = ordered ? (a.logits_f32 ? verify_sums_kernel<true, true> : verify_sums_kernel<false, true>)
+                       : (a.logits_f32 ? verify_sums_kernel<true, false> : verify_sums_kernel<false, false>);
+  r = launch_pdl(sums, dim3(slices * sets, a.B, a.max_rows), dim3(VF_NT), 0, st, a, slices, slice, w);
+  prof_end_launch(st, SP_K_MISC, 0.0, bytes * sets);
+  if (r != cudaSuccess) return r;
+  prof_begin_launch(st);
+  auto* end = ordered ? (a.logits_f32 ? verify_end_kernel<true, true> : verify_end_kernel<false, true>)
+                      : (a.logits_f32 ? verify_end_kernel<true, false> : verify_end_kernel<false, false>);
+  r = launch_clusters(end, a.noise ? C : 1, a.B, st, a, slices, w);
   prof_end_launch(st, SP_K_MISC, 0.0, 0.0);
   return r;
 }

@@ -31,7 +31,7 @@ def pages(**k):
 
 
 def test_layouts():
-    assert C.sizeof(b.sp_draft_verify_io) == 4 * 4 + 8 * 2 + 4 + 4 + 8 * 12
+    assert C.sizeof(b.sp_draft_verify_io) == 4 * 4 + 8 * 2 + 4 + 4 + 8 * 12 + 8
     assert C.sizeof(b.sp_pages) == 8 + 4 * 5 + 4 + 8 + 4 + 4 + 8 * 3
 
 
@@ -101,4 +101,4 @@ def test_pages_refusals_of_the_other_arguments(L):
 
 def test_packed_arguments_are_the_structs(L):
     assert b._pack_pages(OK, 2, 9, 16, 64, 3, OK, 4, OK, OK, OK) == bytes(pages())
-    assert b._pack_verify(2, 100, 6, 4, OK, OK, 1, 100, OK, OK, 100, OK, OK, 100, OK, OK, OK, OK, OK) == bytes(verify())
+    assert b._pack_verify(2, 100, 6, 4, OK, OK, 1, 100, OK, OK, 100, OK, OK, 100, OK, OK, OK, OK, OK, 1) == bytes(verify(clear_err=1))
