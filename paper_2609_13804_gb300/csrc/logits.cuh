@@ -12,6 +12,12 @@ SP_DEVINL float ex2(float x) {
   return y;
 }
 
+SP_DEVINL float rcp(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // Running max and sum of exponentials; +infinity counts its occurrences (the limit of the softmax).
 struct MaxSum {
   float m, s;
@@ -35,6 +41,10 @@ struct Chunk<true> {
   SP_DEVINL static float top(const uint4& u) {  // (fmaxf passes over NaN)
     return fmaxf(fmaxf(__uint_as_float(u.x), __uint_as_float(u.y)), fmaxf(__uint_as_float(u.z), __uint_as_float(u.w)));
   }
+  SP_DEVINL static uint4 without_nan(const uint4& u) {  // NaN becomes -infinity
+    auto f = [](uint32_t x) { return __float_as_uint(fmaxf(__uint_as_float(x), -INFINITY)); };
+    return make_uint4(f(u.x), f(u.y), f(u.z), f(u.w));
+  }
   SP_DEVINL static float one(const void* row, int v) { return __ldg(static_cast<const float*>(row) + v); }
 };
 template <>
@@ -49,6 +59,15 @@ struct Chunk<false> {
     const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&u);
     const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));  // (NaN passed over)
     return fmaxf(__low2float(m), __high2float(m));
+  }
+  SP_DEVINL static uint4 without_nan(const uint4& u) {
+    const __nv_bfloat162 low = __float2bfloat162_rn(-INFINITY);
+    uint4 r;
+    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&u);
+    __nv_bfloat162* o = reinterpret_cast<__nv_bfloat162*>(&r);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) o[k] = __hmax2(h[k], low);
+    return r;
   }
   SP_DEVINL static float one(const void* row, int v) {
     return __bfloat162float(static_cast<const __nv_bfloat16*>(row)[v]);
@@ -65,6 +84,11 @@ SP_DEVINL void unpack2(unsigned long long v, float& lo, float& hi) { asm("mov.b6
 SP_DEVINL unsigned long long add2(unsigned long long a, unsigned long long b) {
   unsigned long long r;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+SP_DEVINL unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
   return r;
 }
 SP_DEVINL unsigned long long mul2(unsigned long long a, unsigned long long b) {

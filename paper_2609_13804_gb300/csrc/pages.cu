@@ -36,43 +36,44 @@ __global__ void __launch_bounds__(PT_NT) pages_trim_kernel(const PagesArgs a) {
 // ------------------------------------------------------------------------- fork
 
 constexpr int PF_NT = 512, PF_CTAS = 8;
-constexpr int PF_COLS = 8;  // table columns at once
+constexpr int PF_ENTRIES = 1 << 15;  // table entries in shared memory, at most
 
 // A row's new entries are its parent's of the same columns, so a CTA needs the old entries of all rows in its columns and
 // no others.  One cluster: the lengths change when all of its CTAs have read them.
-__global__ void __launch_bounds__(PF_NT) pages_fork_kernel(const PagesArgs a, const int* __restrict__ parent) {
-  extern __shared__ int fork_s[];  // [S] old lengths, [S][PF_COLS] old entries
-  int* len_s = fork_s;
-  int* old_s = fork_s + a.S;
+__global__ void __launch_bounds__(PF_NT) pages_fork_kernel(const PagesArgs a, const int* __restrict__ parent, int cols_shift) {
+  extern __shared__ int fork_s[];  // [S] old lengths, [S] the rows that they continue, [S][columns] old entries
+  int *len_s = fork_s, *from_s = fork_s + a.S, *old_s = fork_s + 2 * a.S;
   pdl_wait();
   pdl_trigger();
-  const int tid = threadIdx.x, n = a.S * PF_COLS;
-  for (int s = tid; s < a.S; s += PF_NT) len_s[s] = a.lens[s];
+  const int tid = threadIdx.x, cols = 1 << cols_shift, n = a.S << cols_shift;
+  for (int s = tid; s < a.S; s += PF_NT) {
+    len_s[s] = a.lens[s];
+    from_s[s] = __ldg(parent + s);
+  }
+  int c0 = blockIdx.x << cols_shift;
+  auto load = [&]() {
+    for (int i = tid; i < n; i += PF_NT) {
+      const int c = c0 + (i & (cols - 1));
+      old_s[i] = c < a.max_pages ? a.table[(size_t)(i >> cols_shift) * a.max_pages + c] : -1;
+    }
+  };
+  load();
   __syncthreads();
   const long long most = (long long)a.max_pages << a.page_shift;
-  // the row that row s continues, itself where it stays
-  auto from = [&](int s) {
-    const int p = __ldg(parent + s);
-    if (p == -1) return s;
+  for (int s = tid; s < a.S; s += PF_NT) {  // a row that stays continues itself
+    const int p = from_s[s];
     if (p < 0 || p >= a.S || len_s[p] < 0 || len_s[p] > most) {
-      set_error(a.err, SP_DEVERR_INDEX);
-      return s;
+      if (p != -1) set_error(a.err, SP_DEVERR_INDEX);
+      from_s[s] = s;
     }
-    return p;
-  };
-  for (int c0 = blockIdx.x * PF_COLS; c0 < a.max_pages; c0 += gridDim.x * PF_COLS) {
+  }
+  __syncthreads();
+  for (;;) {
     for (int i = tid; i < n; i += PF_NT) {
-      const int c = c0 + i % PF_COLS;
-      old_s[i] = c < a.max_pages ? a.table[(size_t)(i / PF_COLS) * a.max_pages + c] : -1;
-    }
-    __syncthreads();
-    for (int i = tid; i < n; i += PF_NT) {
-      const int s = i / PF_COLS, c = c0 + i % PF_COLS;
-      if (c >= a.max_pages) continue;
-      const int p = from(s);
-      if (p == s) continue;
+      const int s = i >> cols_shift, k = i & (cols - 1), c = c0 + k, p = from_s[s];
+      if (c >= a.max_pages || p == s) continue;
       const int old = old_s[i];
-      int now = c < (len_s[p] + (1 << a.page_shift) - 1) >> a.page_shift ? old_s[p * PF_COLS + i % PF_COLS] : -1;
+      int now = c < (len_s[p] + (1 << a.page_shift) - 1) >> a.page_shift ? old_s[(p << cols_shift) + k] : -1;
       if (now >= a.n_pages || old >= a.n_pages) set_error(a.err, SP_DEVERR_INDEX);
       if (now >= a.n_pages || now < 0) now = -1;
       if (now == old) continue;
@@ -80,27 +81,31 @@ __global__ void __launch_bounds__(PF_NT) pages_fork_kernel(const PagesArgs a, co
       if (old >= 0 && old < a.n_pages) atomicSub(a.refs + old, 1);
       a.table[(size_t)s * a.max_pages + c] = now;
     }
+    c0 += gridDim.x << cols_shift;
+    if (c0 >= a.max_pages) break;
+    __syncthreads();
+    load();
     __syncthreads();
   }
   cluster_sync_all();
   if (blockIdx.x == 0)
-    for (int s = tid; s < a.S; s += PF_NT) {
-      const int p = from(s);
-      if (p != s) a.lens[s] = len_s[p];
-    }
+    for (int s = tid; s < a.S; s += PF_NT)
+      if (from_s[s] != s) a.lens[s] = len_s[from_s[s]];
 }
 
 // ------------------------------------------------------------------------- reserve, compact
 
-constexpr int PP_NT = 1024, PP_WARPS = PP_NT / 32;
+constexpr int PP_NT = 1024, PP_WARPS = PP_NT / 32, PP_CTAS = 8;
 
-// What the plan leaves for the copies: the positions that move, row by row, and where they were.
+// What the kernels of a call leave each other.
 struct PageMoves {
-  int* start;    // [S + 1] moved positions before each row's
-  int* old_len;  // [S]
-  int* old;      // [S, max_pages] the entries that rows had: compact all of them; reserve those that are replaced (-1: none
-                 // was there, -2: the entry stays)
-  int* free;     // [S, max_pages] the free pages that the call takes, in order
+  int* need;     // [S] pages that a row needs
+  int* move;     // [S] positions of it that move
+  int* start;    // [S + 1] positions that move before each row's
+  int* was;      // [S] compact: the row's length before; reserve: whether shared pages of it are replaced
+  int* old;      // [S, max_pages] the entries that rows had (reserve: those of the places that are replaced)
+  int* place;    // [S, max_pages] reserve: the places of a row that get pages
+  int* count;    // [PP_CTAS] free pages that each CTA of the plan has found
 };
 
 // Exclusive prefix sums of v over the CTA's threads; total in every thread.
@@ -126,175 +131,206 @@ SP_DEVINL int cta_prefix(int v, int* warp_s, int& total) {
   return x - v + (warp > 0 ? before : 0);
 }
 
-// Which free pages the rows take, in order of rows and places, and the tables and counts after it.  One CTA.
+// Which free pages the rows take, in order of rows and places, and the tables and counts after it.  One cluster: a warp
+// finds what a row needs, while its CTA looks through its share of the counts for free pages; then every CTA knows all
+// rows' needs and gives its free pages to the places they fall to.
 template <bool COMPACT>
 __global__ void __launch_bounds__(PP_NT)
 pages_plan_kernel(const PagesArgs a, const int* __restrict__ add, const int* __restrict__ keep, long long ld_keep, int keep_cap,
                   PageMoves mv) {
-  extern __shared__ int plan_s[];  // [S] pages that a row needs, [S] pages before it, [S] positions that move
-  __shared__ int warp_s[PP_WARPS];
-  int *need_s = plan_s, *before_s = plan_s + a.S, *move_s = plan_s + 2 * a.S;
+  extern __shared__ int before_s[];  // [S + 1] pages that rows before each one need
+  __shared__ int warp_s[PP_WARPS], free_s[PP_CTAS];
   pdl_wait();
   pdl_trigger();
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, S = a.S, shift = a.page_shift, page = 1 << shift;
+  const int tid = threadIdx.x, rank = blockIdx.x, lane = tid & 31, S = a.S, shift = a.page_shift, page = 1 << shift;
+  const int warp = rank * PP_WARPS + (tid >> 5), warps = PP_CTAS * PP_WARPS;
   const long long most = (long long)a.max_pages << shift;
-  // The places [lo, hi) of a row that may get pages, and the positions that it will have in them before any is added.
-  auto places = [&](int s, int& lo, int& hi) {
-    const int len = a.lens[s], n = __ldg(add + s);
-    lo = hi = 0;
-    if (COMPACT) {
-      if (n == -1) return false;
-      if (n < 0 || n > keep_cap || n > most || len < 0 || len > most) return false;
+  // this CTA's share of the counts: p0 .. p1 - 1, a piece of four to a thread and turn
+  const int share = (((a.n_pages + PP_CTAS - 1) / PP_CTAS) + 3) & ~3;
+  const int p0 = min(rank * share, a.n_pages), p1 = min(p0 + share, a.n_pages);
+  auto free_at = [&](int p) {  // bits of the free ones of four pages
+    unsigned int free = 0;
+    if (p + 3 < p1) {
+      const int4 r = __ldcg(reinterpret_cast<const int4*>(a.refs + p));
+      free = (r.x == 0) | (r.y == 0) << 1 | (r.z == 0) << 2 | (r.w == 0) << 3;
     } else {
-      if (len < 0 || n < 0 || (long long)len + n > most) return false;
-      if (n > 0) {
-        lo = len >> shift;
-        hi = (int)(((long long)len + n + page - 1) >> shift);
-      }
+      for (int k = 0; p + k < p1; ++k) free |= (unsigned)(__ldcg(a.refs + p + k) == 0) << k;
     }
-    return true;
+    return free;
   };
-  for (int s = warp; s < S; s += PP_WARPS) {
-    int lo, hi, need = 0, move = 0;
-    const bool ok = places(s, lo, hi);
+  const unsigned int free0 = p0 + tid * 4 < p1 ? free_at(p0 + tid * 4) : 0u;
+  int mine = __popc(free0);
+  for (int p = p0 + (tid + PP_NT) * 4; p < p1; p += PP_NT * 4) mine += __popc(free_at(p));
+  for (int s = warp; s < S; s += warps) {
+    const int len = a.lens[s], n = __ldg(add + s);
     const int* row = a.table + (size_t)s * a.max_pages;
-    if (!ok) {
-      if (lane == 0 && !(COMPACT && __ldg(add + s) == -1)) set_error(a.err, SP_DEVERR_INDEX);
-    } else if (COMPACT) {
-      const int n = __ldg(add + s);
-      int first = n;  // the first position that moves
-      for (int i0 = 0; i0 < n; i0 += 32) {
-        const unsigned int other = __ballot_sync(0xffffffffu, i0 + lane < n && __ldg(keep + s * ld_keep + i0 + lane) != i0 + lane);
-        if (other) {
-          first = i0 + __ffs(other) - 1;
-          break;
+    int* old = mv.old + (size_t)s * a.max_pages;
+    int need = 0, move = 0, released = 0;
+    if (COMPACT) {
+      if (n < 0 || n > keep_cap || n > most || len < 0 || len > most) {
+        if (n != -1 && lane == 0) set_error(a.err, SP_DEVERR_INDEX);
+        need = -1;  // the row stays as it is
+      } else {
+        int first = n;  // the first position that moves
+        for (int i0 = 0; i0 < n; i0 += 32) {
+          const unsigned int other = __ballot_sync(0xffffffffu, i0 + lane < n && __ldg(keep + s * ld_keep + i0 + lane) != i0 + lane);
+          if (other) {
+            first = i0 + __ffs(other) - 1;
+            break;
+          }
         }
+        const int pages = (n + page - 1) >> shift, stay = first == n ? pages : first >> shift;
+        need = pages - stay;
+        move = first == n ? 0 : n - (stay << shift);
+        for (int c = lane; c < a.max_pages; c += 32) old[c] = row[c];
+        released = len;
       }
-      const int pages = (n + page - 1) >> shift, stay = first == n ? pages : first >> shift;
-      need = pages - stay;
-      move = first == n ? 0 : n - (stay << shift);
-    } else {
-      for (int c = lo + lane; c < hi; c += 32) {
-        const int e = row[c];
+    } else if (len < 0 || n < 0 || (long long)len + n > most) {
+      if (lane == 0) set_error(a.err, SP_DEVERR_INDEX);
+    } else if (n > 0) {
+      const int lo = len >> shift, hi = (int)(((long long)len + n + page - 1) >> shift);
+      int shares = 0;
+      for (int c0 = lo; c0 < hi; c0 += 32) {
+        const int c = c0 + lane, e = c < hi ? row[c] : -1;
         const bool there = e >= 0 && e < a.n_pages;
         if (e >= a.n_pages) set_error(a.err, SP_DEVERR_INDEX);
-        const bool shared = there && a.refs[e] > 1;
-        need += !there || shared;
-        mv.old[(size_t)s * a.max_pages + c] = shared ? e : there ? -2 : -1;
-        if (c == lo && shared) move = a.lens[s] & (page - 1);
+        const bool shared = there && __ldcg(a.refs + e) > 1;
+        const unsigned int all = __ballot_sync(0xffffffffu, c < hi && (!there || shared));
+        if (c < hi && (!there || shared)) {
+          mv.place[(size_t)s * a.max_pages + need + __popc(all & ((1u << lane) - 1u))] = c;
+          old[c] = shared ? e : -1;
+        }
+        need += __popc(all);
+        shares += shared;
+        if (c0 == lo && __shfl_sync(0xffffffffu, (int)shared, 0)) move = len & (page - 1);
       }
-      need = __reduce_add_sync(0xffffffffu, need);
-      move = __reduce_add_sync(0xffffffffu, move);
+      released = __any_sync(0xffffffffu, shares > 0);
     }
     if (lane == 0) {
-      need_s[s] = need;
-      move_s[s] = move;
+      mv.need[s] = need;
+      mv.move[s] = move;
+      mv.was[s] = released;
     }
   }
-  __syncthreads();
+  int sum;
+  const int at0 = cta_prefix(mine, warp_s, sum);  // (of its first piece, where it has no more)
+  if (tid == 0) mv.count[rank] = sum;
+  cluster_sync_all();
+  if (tid < PP_CTAS) free_s[tid] = __ldcg(mv.count + tid);
   int total = 0;
   for (int s0 = 0; s0 < S; s0 += PP_NT) {
     const int s = s0 + tid;
-    int sum;
-    const int before = total + cta_prefix(s < S ? need_s[s] : 0, warp_s, sum);
+    const int before = total + cta_prefix(s < S ? max(__ldcg(mv.need + s), 0) : 0, warp_s, sum);
     if (s < S) before_s[s] = before;
     total += sum;
   }
-  // the first `total` free pages, in order
-  int found = 0;
-  const int n4 = (a.n_pages + 3) >> 2;
-  for (int i0 = 0; i0 < n4 && found < total; i0 += PP_NT) {
-    const int p = (i0 + tid) * 4;
-    unsigned int free = 0;
-    if (p + 3 < a.n_pages) {
-      const int4 r = __ldcg(reinterpret_cast<const int4*>(a.refs) + i0 + tid);
-      free = (r.x == 0) | (r.y == 0) << 1 | (r.z == 0) << 2 | (r.w == 0) << 3;
-    } else {
-      for (int k = 0; k < 4; ++k)
-        if (p + k < a.n_pages) free |= (unsigned)(a.refs[p + k] == 0) << k;
-    }
-    int sum;
-    int at = found + cta_prefix(__popc(free), warp_s, sum);
-    for (; free && at < total; free &= free - 1) mv.free[at++] = p + __ffs(free) - 1;
-    found += sum;
+  if (tid == 0) before_s[S] = total;
+  __syncthreads();
+  int base = 0, found = 0;  // free pages before this CTA's, and all
+  for (int i = 0; i < PP_CTAS; ++i) {
+    if (i < rank) base += free_s[i];
+    found += free_s[i];
   }
-  __syncthreads();  // (the list is written)
-  // the tables and the counts
-  for (int s = warp; s < S; s += PP_WARPS) {
-    int lo, hi;
-    const bool ok = places(s, lo, hi);
-    // rows are served in order until one does not fit
-    if (!ok || before_s[s] + need_s[s] > found) {
-      if (lane == 0) {
-        if (ok) set_error(a.err, SP_DEVERR_PAGES);
-        move_s[s] = 0;
-      }
-      continue;
+  // Rows are served in order until one does not fit.
+  // The k-th free page: to the row that needs it, and the place.
+  auto give = [&](int k, int page_id) {
+    int x = 0, y = S - 1;  // the last row with at most k pages before it (rows that need none lie before it, or behind)
+    while (x < y) {
+      const int mid = (x + y + 1) >> 1;
+      if (before_s[mid] <= k) x = mid; else y = mid - 1;
     }
-    int* row = a.table + (size_t)s * a.max_pages;
-    int at = before_s[s];
+    if (before_s[x + 1] > found) return;
+    const int at = k - before_s[x];
+    int c;
+    if (COMPACT) {
+      const int n = __ldg(add + x), pages = (n + page - 1) >> shift;
+      c = pages - (before_s[x + 1] - before_s[x]) + at;
+    } else {
+      c = __ldcg(mv.place + (size_t)x * a.max_pages + at);
+    }
+    a.refs[page_id] = 1;
+    a.table[(size_t)x * a.max_pages + c] = page_id;
+  };
+  auto give_all = [&](unsigned int free, int at, int p) {
+    for (; free && at < total; free &= free - 1) give(at++, p + __ffs(free) - 1);
+  };
+  const bool again = share > PP_NT * 4;  // counts are looked at a second time
+  if (!again) {
+    give_all(free0, base + at0, p0 + tid * 4);
+  } else {
+    for (int q0 = p0; q0 < p1 && base < total; q0 += PP_NT * 4) {
+      const unsigned int free = q0 + tid * 4 < p1 ? free_at(q0 + tid * 4) : 0u;
+      const int at = base + cta_prefix(__popc(free), warp_s, sum);
+      give_all(free, at, q0 + tid * 4);
+      base += sum;
+    }
+  }
+  // Only now are pages released: counts must not fall to 0 under the eyes of those who look for free pages.
+  if (again) cluster_sync_all();
+  for (int s = warp; s < S; s += warps) {
+    if (__ldcg(mv.need + s) < (COMPACT ? 0 : 1) || before_s[s + 1] > found) continue;
+    const int* old = mv.old + (size_t)s * a.max_pages;
+    const int taken = before_s[s + 1] - before_s[s];
     if (COMPACT) {
       const int n = __ldg(add + s), pages = (n + page - 1) >> shift;
-      const int stay = move_s[s] ? (n - move_s[s]) >> shift : pages;
-      if (lane == 0) mv.old_len[s] = a.lens[s];
-      for (int c = lane; c < a.max_pages; c += 32) {
-        const int e = row[c];
-        mv.old[(size_t)s * a.max_pages + c] = e;
-        if (c < stay) continue;
-        const int now = c < pages ? mv.free[at + c - stay] : -1;
+      for (int c = pages - taken + lane; c < a.max_pages; c += 32) {
+        const int e = __ldcg(old + c);
         if (e >= 0 && e < a.n_pages) atomicSub(a.refs + e, 1);
         else if (e >= a.n_pages) set_error(a.err, SP_DEVERR_INDEX);
-        if (now >= 0) a.refs[now] = 1;
-        row[c] = now;
+        if (c >= pages) a.table[(size_t)s * a.max_pages + c] = -1;
       }
-      __syncwarp();
       if (lane == 0) a.lens[s] = n;
-    } else {
-      for (int c0 = lo; c0 < hi; c0 += 32) {
-        const int c = c0 + lane, e = c < hi ? mv.old[(size_t)s * a.max_pages + c] : -2;  // (this lane wrote it)
-        const unsigned int all = __ballot_sync(0xffffffffu, e != -2);
-        if (e != -2) {
-          const int now = mv.free[at + __popc(all & ((1u << lane) - 1u))];
-          if (e >= 0) atomicSub(a.refs + e, 1);
-          a.refs[now] = 1;
-          row[c] = now;
-        }
-        at += __popc(all);
+    } else if (__ldcg(mv.was + s)) {
+      for (int i = lane; i < taken; i += 32) {
+        const int e = __ldcg(old + __ldcg(mv.place + (size_t)s * a.max_pages + i));
+        if (e >= 0) atomicSub(a.refs + e, 1);
       }
     }
   }
-  __syncthreads();
-  int moved = 0;
-  for (int s0 = 0; s0 < S; s0 += PP_NT) {
-    const int s = s0 + tid;
-    int sum;
-    const int before = cta_prefix(s < S ? move_s[s] : 0, warp_s, sum) + moved;
-    if (s < S) mv.start[s] = before;
-    moved += sum;
+  if (rank == 0) {
+    int moved = 0;
+    for (int s0 = 0; s0 < S; s0 += PP_NT) {
+      const int s = s0 + tid;
+      const bool on = s < S && before_s[s + 1] <= found;
+      const int before = moved + cta_prefix(on ? __ldcg(mv.move + s) : 0, warp_s, sum);
+      if (s < S) mv.start[s] = before;
+      moved += sum;
+    }
+    if (tid == 0) {
+      mv.start[S] = moved;
+      if (total > found) set_error(a.err, SP_DEVERR_PAGES);
+    }
   }
-  if (tid == 0) mv.start[S] = moved;
 }
 
-constexpr int PM_NT = 256, PM_POS = 8;  // positions of a warp's share
+constexpr int PM_NT = 256, PM_WARPS = PM_NT / 32;
+constexpr int PM_LOADS = 8;    // 16-byte loads of a lane at once
+constexpr int PM_PIECES = 512;  // of a warp's share of a plane, about
 
-// The rows of the positions that move, all planes (a layer's keys or values).  A warp takes PM_POS positions of one plane.
+// The rows of the positions that move, all planes (a layer's keys or values).  A warp takes a few positions of a few planes
+// (positions: about PM_PIECES pieces of 16 bytes; planes: several where enough warps have work): it looks up where they
+// were and go once, then copies.
 template <bool COMPACT>
-__global__ void __launch_bounds__(PM_NT)
-pages_copy_kernel(const PagesArgs a, const int* __restrict__ keep, long long ld_keep, PageMoves mv) {
+__global__ void __launch_bounds__(PM_NT, 3)
+pages_copy_kernel(const PagesArgs a, const int* __restrict__ keep, long long ld_keep, PageMoves mv, int lanes_shift, int pos_shift) {
   extern __shared__ int start_s[];  // [S + 1]
   pdl_wait();
   pdl_trigger();
   const int S = a.S, lane = threadIdx.x & 31, shift = a.page_shift, mask = (1 << shift) - 1;
-  if (__ldcg(mv.start + S) == 0) return;
+  const int total = __ldcg(mv.start + S);
+  if (total == 0) return;
   for (int i = threadIdx.x; i <= S; i += PM_NT) start_s[i] = __ldcg(mv.start + i);
   __syncthreads();
-  const int total = start_s[S];
-  const int shares = (total + PM_POS - 1) / PM_POS;
-  const long long units = (long long)shares * a.planes;
-  for (long long u = blockIdx.x * (long long)(PM_NT / 32) + (threadIdx.x >> 5); u < units; u += (long long)gridDim.x * (PM_NT / 32)) {
-    const int plane = (int)(u / shares), pos = (int)(u % shares) * PM_POS + lane;
-    long long src = -1, dst = 0;  // rows of the plane
-    if (lane < PM_POS && pos < total) {
+  const int shares = (total + (1 << pos_shift) - 1) >> pos_shift;
+  const int warps = gridDim.x * PM_WARPS;
+  const int planes = (long long)shares * a.planes > 8ll * warps ? 4 : 1;  // at a time
+  const long long units = (long long)shares * ((a.planes + planes - 1) / planes);
+  const int L = 1 << lanes_shift;  // lanes of a row
+  const int steps = (a.row16 + L - 1) >> lanes_shift, groups = ((1 << pos_shift) + (32 >> lanes_shift) - 1) >> (5 - lanes_shift);
+  for (long long u = blockIdx.x * (long long)PM_WARPS + (threadIdx.x >> 5); u < units; u += warps) {
+    const int plane0 = (int)(u / shares) * planes, pos = ((int)(u % shares) << pos_shift) + lane;
+    int src = -1, dst = 0;  // rows of a plane
+    if (lane < 1 << pos_shift && pos < total) {
       int x = 0, y = S - 1;  // the row it belongs to: the last that begins at or before it
       while (x < y) {
         const int mid = (x + y + 1) >> 1;
@@ -306,30 +342,41 @@ pages_copy_kernel(const PagesArgs a, const int* __restrict__ keep, long long ld_
       if (COMPACT) {
         const int to = len - (start_s[x + 1] - start_s[x]) + at, from = __ldg(keep + x * ld_keep + to);
         int e = -1;
-        if (from >= 0 && from < __ldcg(mv.old_len + x)) e = __ldcg(old + (from >> shift));
-        if (e >= 0 && e < a.n_pages) src = ((long long)e << shift) + (from & mask);
-        else if (plane == 0) set_error(a.err, SP_DEVERR_INDEX);
-        dst = ((long long)__ldcg(table + (to >> shift)) << shift) + (to & mask);
+        if (from >= 0 && from < __ldcg(mv.was + x)) e = __ldcg(old + (from >> shift));
+        if (e >= 0 && e < a.n_pages) src = (e << shift) + (from & mask);
+        else if (plane0 == 0) set_error(a.err, SP_DEVERR_INDEX);
+        dst = (__ldcg(table + (to >> shift)) << shift) + (to & mask);
       } else {
-        src = ((long long)__ldcg(old + (len >> shift)) << shift) + at;
-        dst = ((long long)__ldcg(table + (len >> shift)) << shift) + at;
+        src = (__ldcg(old + (len >> shift)) << shift) + at;
+        dst = (__ldcg(table + (len >> shift)) << shift) + at;
       }
     }
-    uint4* pl = a.kv + ((size_t)plane * a.n_pages << shift) * a.row16;
-    for (int i = lane; i - lane < PM_POS * a.row16; i += 32 * 8) {
-      uint4 v[8];
-      uint4* to[8];
+    for (int plane = plane0; plane < min(plane0 + planes, a.planes); ++plane) {
+      uint4* pl = a.kv + ((size_t)plane * a.n_pages << shift) * a.row16;
+      for (int g0 = 0, s0 = 0; g0 < groups;) {
+        uint4 v[PM_LOADS];
+        int group = g0, step = s0;
+        unsigned int have = 0;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int w = i + 32 * k, r = min(w / a.row16, PM_POS - 1), at = w - r * a.row16;
-        const long long from = __shfl_sync(0xffffffffu, src, r);
-        to[k] = pl + __shfl_sync(0xffffffffu, dst, r) * a.row16 + at;
-        if (at >= a.row16 || from < 0) to[k] = nullptr;
-        else v[k] = __ldcs(pl + from * a.row16 + at);
+        for (int k = 0; k < PM_LOADS; ++k) {
+          const int r = (group << (5 - lanes_shift)) + (lane >> lanes_shift), at = (step << lanes_shift) + (lane & (L - 1));
+          const int from = __shfl_sync(0xffffffffu, src, r & 31);
+          if (group < groups && at < a.row16 && from >= 0) {
+            v[k] = __ldcs(pl + (size_t)from * a.row16 + at);
+            have |= 1u << k;
+          }
+          if (++step == steps) step = 0, ++group;
+        }
+        group = g0, step = s0;
+#pragma unroll
+        for (int k = 0; k < PM_LOADS; ++k) {
+          const int r = (group << (5 - lanes_shift)) + (lane >> lanes_shift), at = (step << lanes_shift) + (lane & (L - 1));
+          const int to = __shfl_sync(0xffffffffu, dst, r & 31);
+          if (have >> k & 1) pl[(size_t)to * a.row16 + at] = v[k];
+          if (++step == steps) step = 0, ++group;
+        }
+        g0 = group, s0 = step;
       }
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (to[k]) *to[k] = v[k];
     }
   }
 }
@@ -343,26 +390,35 @@ cudaError_t pages_trim_launch(const PagesArgs& a, cudaStream_t st) {
   return r;
 }
 
-cudaError_t pages_fork_launch(const PagesArgs& a, const int* parent, cudaStream_t st) {
-  const int smem = a.S * (1 + PF_COLS) * 4;
-  static std::atomic<unsigned long long> allowed;
-  cudaError_t r = allow_smem(pages_fork_kernel, SP_MAX_TABLE_ROWS * (1 + PF_COLS) * 4, allowed);
-  if (r != cudaSuccess) return r;
+// One cluster of `ctas`.
+template <typename Kernel, typename... Args>
+static cudaError_t launch_cluster(Kernel* k, int ctas, int threads, size_t smem, cudaStream_t st, Args... args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(std::min((a.max_pages + PF_COLS - 1) / PF_COLS, PF_CTAS));
-  cfg.blockDim = dim3(PF_NT);
+  cfg.gridDim = dim3(ctas);
+  cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = cfg.gridDim.x;
+  attr[0].val.clusterDim.x = ctas;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = pdl_enabled() ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, k, args...);
+}
+
+cudaError_t pages_fork_launch(const PagesArgs& a, const int* parent, cudaStream_t st) {
+  static std::atomic<unsigned long long> allowed;
+  cudaError_t r = allow_smem(pages_fork_kernel, (2 * SP_MAX_TABLE_ROWS + PF_ENTRIES) * 4, allowed);
+  if (r != cudaSuccess) return r;
+  // columns at once: as many as give every CTA of the cluster one turn, where they fit
+  int shift = 3;
+  while (((long long)PF_CTAS << shift) < a.max_pages && ((long long)a.S << (shift + 1)) <= PF_ENTRIES) ++shift;
+  const int ctas = (int)std::min<long long>((a.max_pages + (1ll << shift) - 1) >> shift, PF_CTAS);
   prof_begin_launch(st);
-  r = cudaLaunchKernelEx(&cfg, pages_fork_kernel, a, parent);
+  r = launch_cluster(pages_fork_kernel, ctas, PF_NT, (size_t)a.S * (2 + (1 << shift)) * 4, st, a, parent, shift);
   prof_end_launch(st, SP_K_MISC, 0.0, 0.0);
   return r;
 }
@@ -370,7 +426,7 @@ cudaError_t pages_fork_launch(const PagesArgs& a, const int* parent, cudaStream_
 static size_t align256(size_t n) { return (n + 255) & ~size_t(255); }
 
 size_t pages_bytes(int S, int max_pages) {
-  return 2 * align256(((size_t)S + 1) * 4) + 2 * align256((size_t)S * max_pages * 4);
+  return 4 * align256(((size_t)S + 1) * 4) + 2 * align256((size_t)S * max_pages * 4) + 256;
 }
 
 cudaError_t pages_move_launch(const PagesArgs& a, const int* add, const int* keep, long long ld_keep, int keep_cap, void* ws,
@@ -378,21 +434,25 @@ cudaError_t pages_move_launch(const PagesArgs& a, const int* add, const int* kee
   const size_t rows = align256(((size_t)a.S + 1) * 4), entries = align256((size_t)a.S * a.max_pages * 4);
   char* base = static_cast<char*>(ws);
   PageMoves mv;
-  mv.start = reinterpret_cast<int*>(base);
-  mv.old_len = reinterpret_cast<int*>(base + rows);
-  mv.old = reinterpret_cast<int*>(base + 2 * rows);
-  mv.free = reinterpret_cast<int*>(base + 2 * rows + entries);
-  static std::atomic<unsigned long long> allowed[2];
-  auto* plan = keep ? pages_plan_kernel<true> : pages_plan_kernel<false>;
-  cudaError_t r = allow_smem(plan, SP_MAX_TABLE_ROWS * 12, allowed[keep != nullptr]);
-  if (r != cudaSuccess) return r;
+  mv.count = reinterpret_cast<int*>(base);
+  base += 256;
+  mv.need = reinterpret_cast<int*>(base);
+  mv.move = reinterpret_cast<int*>(base + rows);
+  mv.start = reinterpret_cast<int*>(base + 2 * rows);
+  mv.was = reinterpret_cast<int*>(base + 3 * rows);
+  mv.old = reinterpret_cast<int*>(base + 4 * rows);
+  mv.place = reinterpret_cast<int*>(base + 4 * rows + entries);
   prof_begin_launch(st);
-  r = launch_pdl(plan, dim3(1), dim3(PP_NT), (size_t)a.S * 12, st, a, add, keep, ld_keep, keep_cap, mv);
+  cudaError_t r = launch_cluster(keep ? pages_plan_kernel<true> : pages_plan_kernel<false>, PP_CTAS, PP_NT,
+                                 ((size_t)a.S + 1) * 4, st, a, add, keep, ld_keep, keep_cap, mv);
   prof_end_launch(st, SP_K_MISC, 0.0, 0.0);
   if (r != cudaSuccess) return r;
+  int lanes = 0, pos = 0;
+  while (lanes < 5 && 1 << lanes < a.row16) ++lanes;
+  while (pos < 5 && a.row16 << (pos + 1) <= PM_PIECES) ++pos;
   prof_begin_launch(st);
-  r = launch_pdl(keep ? pages_copy_kernel<true> : pages_copy_kernel<false>, dim3(device_sm_count() * 8), dim3(PM_NT),
-                 ((size_t)a.S + 1) * 4, st, a, keep, ld_keep, mv);
+  r = launch_pdl(keep ? pages_copy_kernel<true> : pages_copy_kernel<false>, dim3(device_sm_count() * 3), dim3(PM_NT),
+                 ((size_t)a.S + 1) * 4, st, a, keep, ld_keep, mv, lanes, pos);
   prof_end_launch(st, SP_K_MISC, 0.0, 0.0);
   return r;
 }

@@ -103,7 +103,7 @@ SP_DEVINL Share scan(const Slice<F32>& sl, float cc, const float* noise) {
   Share r{-INFINITY, 0.f, -1, 0.f, 1.f, -1};
   float best = 0.f;  // (relative to r.m)
   auto race = [&](float x, float w, float e, int v) {
-    const float score = __fdividef(w, e);  // (e = 0: infinity, or NaN for w = 0, which is no candidate)
+    const float score = w * rcp(e);  // (e = 0: infinity, or NaN for w = 0, which is no candidate)
     if (score > best) {
       best = score;
       r.x = x;
@@ -344,61 +344,102 @@ SP_DEVINL unsigned long long race_key(float score, int v) {
 // The row where a sequence ends, as its race needs it.
 template <bool F32>
 struct Race {
+  using K = Chunk<F32>;
+  static constexpr int E4 = K::N / 4;
   const void *p, *q;  // q NULL: nothing is taken off
   const float* e;
-  float mp, ip, mq, iq, c;  // maxima and inverse sums
+  float mp, sp, mq, sq, c;  // maxima and sums
   int out;                  // a token whose probability is taken off whole (a draft without a distribution), -1: none
 
-  SP_DEVINL void take(float x, float y, float noise, int v, float& best, int& at) const {
-    float r = weight(x, mp, c) * ip;
-    if (q) r = fmaxf(r - weight(y, mq, c) * iq, 0.f);
-    if (v == out) r = 0.f;
-    const float score = __fdividef(r, noise);  // (noise 0: infinity, or NaN for r = 0, which is no candidate)
-    if (score > best) {
-      best = score;
-      at = v;
+  // The best of tokens v0 .. v1 - 1, one at a time, for this thread of the CTA.
+  SP_DEVINL unsigned long long slowly(int v0, int v1, int step) const {
+    const float ip = sp > 0.f ? 1.f / sp : 0.f, iq = sq > 0.f ? 1.f / sq : 0.f;
+    float best = 0.f;
+    int at = 0;
+#pragma unroll 4
+    for (int v = v0; v < v1; v += step) {
+      float r = v == out ? 0.f : weight(K::one(p, v), mp, c) * ip;
+      if (q) r = fmaxf(r - weight(K::one(q, v), mq, c) * iq, 0.f);
+      const float score = r * rcp(__ldg(e + v));  // (noise 0: infinity, or NaN for r = 0, which is no candidate)
+      if (score > best) {
+        best = score;
+        at = v;
+      }
+    }
+    return best > 0.f ? race_key(best, at) : 0ull;
+  }
+  struct Piece {
+    uint4 x, y;
+    float4 n[E4];
+  };
+  template <bool DRAFTED>
+  SP_DEVINL void pieces(const Slice<F32>& s, float& best, int& at) const {
+    const uint4* ps = s.src();
+    const uint4* qs = reinterpret_cast<const uint4*>(static_cast<const char*>(q) + (size_t)s.c0 * Slice<F32>::esz);
+    const float* es = e + s.c0;
+    const bool e16 = (reinterpret_cast<uintptr_t>(es) & 15) == 0;
+    // p(v) = exp2((x - m) log2 e / t - log2 sum), two at a time
+    const unsigned long long c2 = pack2(c, c), mp2 = pack2(-mp, -mp), lp2 = pack2(-log2f(sp), -log2f(sp));
+    const unsigned long long mq2 = pack2(-mq, -mq), lq2 = pack2(-log2f(sq), -log2f(sq));
+    auto load = [&](Piece& g, int c) {
+      g.x = __ldg(ps + c);
+      if (DRAFTED) g.y = __ldg(qs + c);
+#pragma unroll
+      for (int k = 0; k < E4; ++k) {
+        const float* f = es + (c * E4 + k) * 4;
+        g.n[k] = e16 ? __ldcs(reinterpret_cast<const float4*>(f)) : make_float4(__ldg(f), __ldg(f + 1), __ldg(f + 2), __ldg(f + 3));
+      }
+    };
+    auto take = [&](const Piece& g, int c) {
+      float score[K::N], top = 0.f;
+      const uint4 y = DRAFTED ? K::without_nan(g.y) : g.x;  // (a NaN of the target's makes no score)
+#pragma unroll
+      for (int i = 0; i < K::N; i += 2) {
+        float a, b;
+        unpack2(fma2(add2(pack2(K::at(g.x, i), K::at(g.x, i + 1)), mp2), c2, lp2), a, b);
+        a = ex2(a), b = ex2(b);
+        if (DRAFTED) {
+          float u, v;
+          unpack2(fma2(add2(pack2(K::at(y, i), K::at(y, i + 1)), mq2), c2, lq2), u, v);
+          a = fmaxf(a - ex2(u), 0.f), b = fmaxf(b - ex2(v), 0.f);
+        }
+        const float4& f = g.n[i / 4];
+        score[i] = a * rcp(i % 4 == 0 ? f.x : f.z);
+        score[i + 1] = b * rcp(i % 4 == 0 ? f.y : f.w);
+        top = fmaxf(top, fmaxf(score[i], score[i + 1]));  // (passes over NaN)
+      }
+      if (top > best) {
+        const int v = s.c0 + c * K::N;
+#pragma unroll
+        for (int i = 0; i < K::N; ++i)
+          if (score[i] > best && v + i != out) {
+            best = score[i];
+            at = v + i;
+          }
+      }
+    };
+    for (int c = threadIdx.x; c < s.chunks; c += 2 * VF_NT) {
+      Piece g, h;
+      load(g, c);
+      const bool two = c + VF_NT < s.chunks;
+      if (two) load(h, c + VF_NT);
+      take(g, c);
+      if (two) take(h, c + VF_NT);
     }
   }
   // The best of tokens v0 .. v1 - 1 for this thread of the CTA.
   SP_DEVINL unsigned long long run(int v0, int v1) const {
-    using K = Chunk<F32>;
-    constexpr int esz = F32 ? 4 : 2, E4 = K::N / 4;
+    const Slice<F32> s(p, v0, v1);
+    // rows that have no 16-byte pieces in common, a maximum at infinity, no weight: token by token
+    const bool with_q = q && sq > 0.f;
+    if ((with_q && ((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(q)) & 15) != 0) || !(sp > 0.f) ||
+        mp == INFINITY || (with_q && mq == INFINITY))
+      return slowly(v0 + threadIdx.x, v1, VF_NT);
+    unsigned long long key = s.beside() >= 0 ? slowly(s.beside(), s.beside() + 1, 1) : 0ull;
     float best = 0.f;
     int at = 0;
-    const Slice<F32> s(p, v0, v1);
-    const char* qb = static_cast<const char*>(q);
-    if (q && ((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(q)) & 15) != 0) {  // no pieces in common
-#pragma unroll 4
-      for (int v = v0 + threadIdx.x; v < v1; v += VF_NT) take(K::one(p, v), K::one(q, v), __ldg(e + v), v, best, at);
-      return best > 0.f ? race_key(best, at) : 0ull;
-    }
-    unsigned long long key = 0;
-    if (s.beside() >= 0) {
-      const int v = s.beside();
-      take(K::one(p, v), q ? K::one(q, v) : 0.f, __ldg(e + v), v, best, at);
-      if (best > 0.f) key = race_key(best, at);
-      best = 0.f;
-    }
-    const uint4* ps = s.src();
-    const uint4* qs = reinterpret_cast<const uint4*>(qb + (size_t)s.c0 * esz);
-    const float* es = e + s.c0;
-    const bool e16 = (reinterpret_cast<uintptr_t>(es) & 15) == 0;
-#pragma unroll 2
-    for (int c = threadIdx.x; c < s.chunks; c += VF_NT) {
-      const uint4 x = __ldg(ps + c), y = q ? __ldg(qs + c) : make_uint4(0, 0, 0, 0);
-      float4 n[E4];
-#pragma unroll
-      for (int k = 0; k < E4; ++k) {
-        const float* f = es + (c * E4 + k) * 4;
-        n[k] = e16 ? __ldcs(reinterpret_cast<const float4*>(f)) : make_float4(__ldg(f), __ldg(f + 1), __ldg(f + 2), __ldg(f + 3));
-      }
-#pragma unroll
-      for (int i = 0; i < K::N; ++i) {
-        const float4& f = n[i / 4];
-        take(K::at(x, i), K::at(y, i), i % 4 == 0 ? f.x : i % 4 == 1 ? f.y : i % 4 == 2 ? f.z : f.w, s.c0 + c * K::N + i,
-             best, at);
-      }
-    }
+    if (with_q) pieces<true>(s, best, at);
+    else pieces<false>(s, best, at);
     return best > 0.f ? max(key, race_key(best, at)) : key;
   }
 };
@@ -510,9 +551,9 @@ __global__ void __launch_bounds__(VF_NT) verify_end_kernel(const VerifyArgs a, i
                  : nullptr;
     race.e = a.noise + (size_t)b * a.ld_noise;
     race.mp = r.mp;
-    race.ip = r.sp > 0.f ? 1.f / r.sp : 0.f;
+    race.sp = r.sp;
     race.mq = r.mq;
-    race.iq = r.sq > 0.f ? 1.f / r.sq : 0.f;
+    race.sq = r.sq;
     race.c = q.c;
     race.out = a.draft_logits ? -1 : d;
     const int per = (((a.V + C - 1) / C) + 7) & ~7;
