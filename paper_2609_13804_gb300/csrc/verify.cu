@@ -20,6 +20,8 @@ namespace {
 
 constexpr int VF_NT = 256, VF_WARPS = VF_NT / 32;
 constexpr int VF_LOADS = 4;    // 16-byte loads of a thread at once
+constexpr int VF_RING = 3;     // batches of loads in shared memory
+constexpr int VF_RING_BYTES = VF_RING * VF_LOADS * VF_NT * 16;
 constexpr int VF_SLICES = 32;  // of a row, at most: a lane joins each
 constexpr int VF_CLUSTER = 8;  // CTAs of a sequence's race, at most
 
@@ -34,7 +36,7 @@ struct Seq {
   int row0, n;    // its rows (0: none)
   bool greedy;
   float t;        // temperature, 1 where greedy
-  float c;        // log2 e / t, kept within the finite numbers so that 0 c is 0
+  float c;        // log2 e / t, kept so that 0 c is 0 and -infinity c is -infinity
 };
 
 SP_DEVINL Seq sequence(const VerifyArgs& a, int b) {
@@ -45,7 +47,7 @@ SP_DEVINL Seq sequence(const VerifyArgs& a, int b) {
   const float t = a.temperature ? __ldg(a.temperature + b) : 1.f;
   q.greedy = !a.noise || !(t > 0.f);
   q.t = q.greedy ? 1.f : t;
-  q.c = fmaxf(fminf(kLog2e / q.t, FLT_MAX), FLT_MIN);
+  q.c = fmaxf(fminf(kLog2e / q.t, 0x1p64f), FLT_MIN);
   return q;
 }
 
@@ -53,10 +55,15 @@ SP_DEVINL Seq sequence(const VerifyArgs& a, int b) {
 // them), 0 for NaN and -infinity.
 SP_DEVINL float weight(float x, float m, float c) { return x == m ? 1.f : x < m ? ex2((x - m) * c) : 0.f; }
 
+// Where a row's exponents m c are of ordinary size, weights are exp2(x c - z) with the whole number z next to m c: one fused
+// multiply-add, rounded once (m c itself, rounded, would shift all of them), and powers of two between threads whose
+// maxima differ.  Else (maxima at infinity or at a type's lowest value, temperatures near 0) they are weight()'s.
+SP_DEVINL bool ordinary(float mc) { return fabsf(mc) < 4194304.f; }
+
 // A thread's share of a slice: its maximum, its sum and the first batch of loads that holds the maximum; with noise the
 // best of its race too, the logit and noise of which are kept: scores of threads with different maxima are formed again.
 struct Share {
-  float m, s;
+  float m, z, s;  // (s in units of exp2(z) where that is ordinary, else of exp(m / t))
   int first;
   float x, e;  // the race's best so far
   int at;      // -1: none
@@ -96,11 +103,129 @@ struct Slice {
   }
 };
 
-template <bool F32, bool RACE>
-SP_DEVINL Share scan(const Slice<F32>& sl, float cc, const float* noise) {
+// Raises a share's maximum to m; what it had counts `the result` as much.
+SP_DEVINL float raise_to(float m, float c, Share& r) {
+  const float mc = m * c, z = rintf(mc);
+  float f;
+  if (r.m == -INFINITY) {
+    f = 0.f;
+  } else if (ordinary(mc) && ordinary(r.m * c)) {
+    f = ex2(r.z - z);
+  } else {
+    f = ex2((r.m - m) * c);
+    if (ordinary(r.m * c)) f *= ex2(__fmaf_rn(-r.m, c, r.z));
+    if (ordinary(mc)) f *= ex2(__fmaf_rn(m, c, -z));
+  }
+  r.s *= f;
+  r.m = m;
+  r.z = z;
+  return f;
+}
+
+// A logit's weight in a share's units.
+SP_DEVINL float share_weight(float x, float c, const Share& r) {
+  if (!ordinary(r.m * c)) return weight(x, r.m, c);
+  return x > -INFINITY ? ex2(__fmaf_rn(x, c, -r.z)) : 0.f;
+}
+
+// A share's sum in units of exp(m / t).
+SP_DEVINL float share_sum(float c, const Share& r) { return ordinary(r.m * c) ? r.s * ex2(__fmaf_rn(-r.m, c, r.z)) : r.s; }
+
+// The largest logit of a batch.
+template <bool F32>
+SP_DEVINL float batch_top(const uint4 (&u)[VF_LOADS]) {
+  float lm = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < VF_LOADS; ++k) lm = fmaxf(lm, Chunk<F32>::top(u[k]));
+  return lm;
+}
+
+// A batch of loads (its first at c); again(k) is its k-th once more.
+template <bool F32, typename Again>
+SP_DEVINL void add_batch(const uint4 (&u)[VF_LOADS], int c, float cc, Share& r, Again again) {
+  using K = Chunk<F32>;
+  const float lm = batch_top<F32>(u);
+  if (lm > r.m) {
+    raise_to(lm, cc, r);
+    r.first = c;
+  }
+  float sum[2] = {0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < VF_LOADS; ++k)
+#pragma unroll
+    for (int i = 0; i < K::N; ++i) sum[i & 1] += ex2(__fmaf_rn(K::at(u[k], i), cc, -r.z));
+  float ts = sum[0] + sum[1];
+  if (!(ts < INFINITY) || !ordinary(r.m * cc)) {  // a NaN among them, or no ordinary maximum
+    ts = 0.f;
+#pragma unroll 1
+    for (int k = 0; k < VF_LOADS && lm > -INFINITY; ++k) {
+      const uint4 v = again(k);
+#pragma unroll
+      for (int i = 0; i < K::N; ++i) ts += share_weight(K::at(v, i), cc, r);
+    }
+  }
+  r.s += ts;
+}
+
+// One logit that lies beside the batches; what the share had counts `the result` as much, -1: it has no weight.
+SP_DEVINL float add_one(float x, float c, Share& r) {
+  if (!(x > -INFINITY)) return -1.f;
+  float f = 1.f;
+  if (x > r.m) {
+    f = raise_to(x, c, r);
+    r.first = -1;
+  }
+  r.s += share_weight(x, c, r);
+  return f;
+}
+
+// A thread's share of a slice.  Its loads go through shared memory of its own (VF_RING batches of VF_LOADS), so no thread
+// waits for another; `meanwhile` runs while the first are on their way.
+template <bool F32, typename Meanwhile>
+SP_DEVINL Share sum_slice(const Slice<F32>& sl, float cc, uint4* ring, Meanwhile meanwhile) {
+  using K = Chunk<F32>;
+  constexpr int STEP = VF_NT * VF_LOADS;
+  Share r{-INFINITY, 0.f, 0.f, -1, 0.f, 1.f, -1};
+  const uint4* src = sl.src();
+  uint4* own = ring + threadIdx.x;
+  auto load = [&](int c0, int place) {
+    const int c = c0 + threadIdx.x;
+#pragma unroll
+    for (int k = 0; k < VF_LOADS; ++k)
+      if (c + k * VF_NT < sl.chunks)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(own + place * STEP + k * VF_NT)),
+                     "l"(src + c + k * VF_NT) : "memory");
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll
+  for (int i = 0; i < VF_RING - 1; ++i) load(i * STEP, i);
+  const int beside = sl.beside();
+  const float mine = beside >= 0 ? K::one(sl.base, beside) : -INFINITY;
+  meanwhile();
+  for (int c0 = 0, place = 0; c0 < sl.chunks; c0 += STEP) {
+    load(c0 + (VF_RING - 1) * STEP, place == 0 ? VF_RING - 1 : place - 1);
+    asm volatile("cp.async.wait_group %0;" ::"n"(VF_RING - 1) : "memory");
+    const int c = c0 + threadIdx.x;
+    auto piece = [&](int k) {
+      return c + k * VF_NT < sl.chunks ? own[place * STEP + k * VF_NT] : make_uint4(K::kNone, K::kNone, K::kNone, K::kNone);
+    };
+    uint4 u[VF_LOADS];
+#pragma unroll
+    for (int k = 0; k < VF_LOADS; ++k) u[k] = piece(k);
+    add_batch<F32>(u, c, cc, r, piece);
+    if (++place == VF_RING) place = 0;
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  add_one(mine, cc, r);
+  return r;
+}
+
+// The same with the race.
+template <bool F32>
+SP_DEVINL Share scan_race(const Slice<F32>& sl, float cc, const float* noise) {
   using K = Chunk<F32>;
   constexpr int E4 = K::N / 4;
-  Share r{-INFINITY, 0.f, -1, 0.f, 1.f, -1};
+  Share r{-INFINITY, 0.f, 0.f, -1, 0.f, 1.f, -1};
   float best = 0.f;  // (relative to r.m)
   auto race = [&](float x, float w, float e, int v) {
     const float score = w * rcp(e);  // (e = 0: infinity, or NaN for w = 0, which is no candidate)
@@ -114,15 +239,15 @@ SP_DEVINL Share scan(const Slice<F32>& sl, float cc, const float* noise) {
   const int beside = sl.beside();
   const float mine = beside >= 0 ? K::one(sl.base, beside) : -INFINITY;
   const uint4* src = sl.src();
-  const float* e = RACE ? noise + sl.c0 : nullptr;
+  const float* e = noise + sl.c0;
   const bool e16 = (reinterpret_cast<uintptr_t>(e) & 15) == 0;
   for (int c = threadIdx.x; c < sl.chunks; c += VF_NT * VF_LOADS) {
     uint4 u[VF_LOADS];
 #pragma unroll
     for (int k = 0; k < VF_LOADS; ++k)
       u[k] = c + k * VF_NT < sl.chunks ? __ldcs(src + c + k * VF_NT) : make_uint4(K::kNone, K::kNone, K::kNone, K::kNone);
-    float4 n[RACE ? VF_LOADS * E4 : 1];
-    if (RACE) {
+    float4 n[VF_LOADS * E4];
+    {
 #pragma unroll
       for (int k = 0; k < VF_LOADS * E4; ++k) {
         const int at = ((c + k / E4 * VF_NT) * E4 + k % E4) * 4;
@@ -133,67 +258,32 @@ SP_DEVINL Share scan(const Slice<F32>& sl, float cc, const float* noise) {
         }
       }
     }
-    float lm = -INFINITY;
-#pragma unroll
-    for (int k = 0; k < VF_LOADS; ++k) lm = fmaxf(lm, K::top(u[k]));
+    const float lm = batch_top<F32>(u);
     if (lm == -INFINITY) continue;
-    if (lm > r.m) {
-      const float f = r.m == -INFINITY ? 0.f : ex2((r.m - lm) * cc);
-      r.s *= f;
-      best *= f;
-      r.m = lm;
-      r.first = c;
-    }
-    if (RACE) {
-      float sum = 0.f;
-#pragma unroll
-      for (int k = 0; k < VF_LOADS; ++k)
-#pragma unroll
-        for (int i = 0; i < K::N; ++i) {
-          const float x = K::at(u[k], i), w = weight(x, r.m, cc);
-          const float4& f = n[k * E4 + i / 4];
-          sum += w;
-          race(x, w, i % 4 == 0 ? f.x : i % 4 == 1 ? f.y : i % 4 == 2 ? f.z : f.w, sl.c0 + (c + k * VF_NT) * K::N + i);
-        }
-      r.s += sum;
-      continue;
-    }
-    // (x - m first, exactly where it matters: m log2 e rounded would shift the whole sum)
-    const unsigned long long nm = pack2(-r.m, -r.m), c2 = pack2(cc, cc);
-    unsigned long long sum[2] = {0ull, 0ull};
+    if (lm > r.m) best *= raise_to(lm, cc, r);
+    const bool usual = ordinary(r.m * cc);
+    float sum = 0.f;
 #pragma unroll
     for (int k = 0; k < VF_LOADS; ++k)
 #pragma unroll
-      for (int i = 0; i < K::N; i += 2) {
-        float x, y;
-        unpack2(mul2(add2(pack2(K::at(u[k], i), K::at(u[k], i + 1)), nm), c2), x, y);
-        sum[(i >> 1) & 1] = add2(sum[(i >> 1) & 1], pack2(ex2(x), ex2(y)));
+      for (int i = 0; i < K::N; ++i) {
+        const float x = K::at(u[k], i);
+        float w = ex2(__fmaf_rn(x, cc, -r.z));
+        if (!usual || !(w < INFINITY)) w = share_weight(x, cc, r);
+        const float4& f = n[k * E4 + i / 4];
+        sum += w;
+        race(x, w, i % 4 == 0 ? f.x : i % 4 == 1 ? f.y : i % 4 == 2 ? f.z : f.w, sl.c0 + (c + k * VF_NT) * K::N + i);
       }
-    float sa, sb;
-    unpack2(add2(sum[0], sum[1]), sa, sb);
-    float ts = sa + sb;
-    if (ts != ts) {  // a NaN, or infinity less infinity, among them
-      ts = 0.f;
-#pragma unroll
-      for (int k = 0; k < VF_LOADS; ++k)
-#pragma unroll
-        for (int i = 0; i < K::N; ++i) ts += weight(K::at(u[k], i), r.m, cc);
-    }
-    r.s += ts;
+    r.s += sum;
   }
-  if (mine > -INFINITY) {
-    const float mn = fmaxf(r.m, mine), f = r.m > -INFINITY ? weight(r.m, mn, cc) : 0.f;
-    if (mine > r.m) r.first = -1;
-    r.s = r.s * f + weight(mine, mn, cc);
+  const float f = add_one(mine, cc, r);
+  if (f >= 0.f) {
     best *= f;
-    r.m = mn;
-    if (RACE) {
-      const float score = __fdividef(weight(mine, mn, cc), __ldg(noise + beside));
-      if (score > best || (score == best && beside < r.at)) {
-        r.x = mine;
-        r.e = __ldg(noise + beside);
-        r.at = beside;
-      }
+    const float n = __ldg(noise + beside), score = share_weight(mine, cc, r) * rcp(n);
+    if (score > best || (score == best && beside < r.at)) {
+      r.x = mine;
+      r.e = n;
+      r.at = beside;
     }
   }
   return r;
@@ -288,28 +378,29 @@ SP_DEVINL Row decide(const VerifyArgs& a, const Seq& q, int j, const RowPart* pa
 // are never read; nothing waits, and what is read needlessly has no effect.
 template <bool F32, bool ORDERED>
 __global__ void __launch_bounds__(VF_NT, 4) verify_sums_kernel(const VerifyArgs a, int slices, int slice, VerifyWork work) {
-  using K = Chunk<F32>;
+  extern __shared__ uint4 ring[];
   __shared__ int last_s;
   pdl_wait();
   const int which = blockIdx.x / slices, sl = blockIdx.x % slices, b = blockIdx.y, j = blockIdx.z;
   if (a.clear_err && a.err && blockIdx.x + b + j == 0 && threadIdx.x == 0) *a.err = 0;
+  const int ended = ORDERED ? __ldcg(work.end + b) : kUnset;
   const Seq q = sequence(a, b);
   const bool last = j == q.n - 1;
-  if (j >= q.n || (which == 1 && (q.greedy || last))) return;
-  if (ORDERED && __ldcg(work.end + b) < j) return;
+  if (j >= q.n || (which == 1 && (q.greedy || last)) || ended < j) return;
   const int row = q.row0 + j;
   const char* base = static_cast<const char*>(which ? a.draft_logits : a.logits) +
                      row * (which ? a.ld_draft : a.ld) * (F32 ? 4 : 2);
   float xd = -INFINITY;
-  if (sl == 0 && threadIdx.x == 0 && !last) {
-    const int d = __ldg(a.draft + row);
-    if (d >= 0 && d < a.V) xd = K::one(base, d);
-  }
   const int v0 = min(sl * slice, a.V), v1 = min(v0 + slice, a.V);
   const Slice<F32> s(base, v0, v1);
-  const Share t = scan<F32, false>(s, q.c, nullptr);
+  const Share t = sum_slice<F32>(s, q.c, ring, [&]() {
+    if (sl == 0 && threadIdx.x == 0 && !last) {
+      const int d = __ldg(a.draft + row);
+      if (d >= 0 && d < a.V) xd = Chunk<F32>::one(base, d);
+    }
+  });
   pdl_trigger();
-  RowPart r = join_cta(t.m, t.s, q.c, q.greedy, [&](float top) { return s.first_of(top, t.first); });
+  RowPart r = join_cta(t.m, share_sum(q.c, t), q.c, q.greedy, [&](float top) { return s.first_of(top, t.first); });
   r.xd = xd;
   if (threadIdx.x == 0) work.part[((size_t)row * 2 + which) * slices + sl] = r;
   if (ORDERED) {
@@ -351,17 +442,31 @@ struct Race {
   float mp, sp, mq, sq, c;  // maxima and sums
   int out;                  // a token whose probability is taken off whole (a draft without a distribution), -1: none
 
+  // Scores are in units of the target's (a race does not ask for them): of exp2(z), z next to m c, or of exp(m / t).  q is
+  // brought to the same by k.
+  bool usual;
+  float zp, zq, k;
+  SP_DEVINL void prepare() {
+    if (q && !(sq > 0.f)) q = nullptr;  // a draft without weight takes nothing off
+    usual = ordinary(mp * c) && (!q || ordinary(mq * c));
+    zp = rintf(mp * c);
+    zq = rintf(mq * c);
+    k = !q ? 0.f : usual ? -(sp * ex2(__fmaf_rn(mp, c, -zp))) / (sq * ex2(__fmaf_rn(mq, c, -zq))) : -sp / sq;
+  }
   // The best of tokens v0 .. v1 - 1, one at a time, for this thread of the CTA.
   SP_DEVINL unsigned long long slowly(int v0, int v1, int step) const {
-    const float ip = sp > 0.f ? 1.f / sp : 0.f, iq = sq > 0.f ? 1.f / sq : 0.f;
     float best = 0.f;
     int at = 0;
 #pragma unroll 4
     for (int v = v0; v < v1; v += step) {
-      float r = v == out ? 0.f : weight(K::one(p, v), mp, c) * ip;
-      if (q) r = fmaxf(r - weight(K::one(q, v), mq, c) * iq, 0.f);
+      const float x = K::one(p, v);
+      float r = usual ? ex2(__fmaf_rn(x, c, -zp)) : weight(x, mp, c);
+      if (q) {
+        const float y = K::one(q, v);
+        r = fmaxf(__fmaf_rn(k, usual ? ex2(__fmaf_rn(fmaxf(y, -INFINITY), c, -zq)) : weight(y, mq, c), r), 0.f);
+      }
       const float score = r * rcp(__ldg(e + v));  // (noise 0: infinity, or NaN for r = 0, which is no candidate)
-      if (score > best) {
+      if (score > best && v != out) {
         best = score;
         at = v;
       }
@@ -378,9 +483,7 @@ struct Race {
     const uint4* qs = reinterpret_cast<const uint4*>(static_cast<const char*>(q) + (size_t)s.c0 * Slice<F32>::esz);
     const float* es = e + s.c0;
     const bool e16 = (reinterpret_cast<uintptr_t>(es) & 15) == 0;
-    // p(v) = exp2((x - m) log2 e / t - log2 sum), two at a time
-    const unsigned long long c2 = pack2(c, c), mp2 = pack2(-mp, -mp), lp2 = pack2(-log2f(sp), -log2f(sp));
-    const unsigned long long mq2 = pack2(-mq, -mq), lq2 = pack2(-log2f(sq), -log2f(sq));
+    const float c_ = c;
     auto load = [&](Piece& g, int c) {
       g.x = __ldg(ps + c);
       if (DRAFTED) g.y = __ldg(qs + c);
@@ -394,19 +497,12 @@ struct Race {
       float score[K::N], top = 0.f;
       const uint4 y = DRAFTED ? K::without_nan(g.y) : g.x;  // (a NaN of the target's makes no score)
 #pragma unroll
-      for (int i = 0; i < K::N; i += 2) {
-        float a, b;
-        unpack2(fma2(add2(pack2(K::at(g.x, i), K::at(g.x, i + 1)), mp2), c2, lp2), a, b);
-        a = ex2(a), b = ex2(b);
-        if (DRAFTED) {
-          float u, v;
-          unpack2(fma2(add2(pack2(K::at(y, i), K::at(y, i + 1)), mq2), c2, lq2), u, v);
-          a = fmaxf(a - ex2(u), 0.f), b = fmaxf(b - ex2(v), 0.f);
-        }
+      for (int i = 0; i < K::N; ++i) {
+        float r = ex2(__fmaf_rn(K::at(g.x, i), c_, -zp));
+        if (DRAFTED) r = fmaxf(__fmaf_rn(k, ex2(__fmaf_rn(K::at(y, i), c_, -zq)), r), 0.f);
         const float4& f = g.n[i / 4];
-        score[i] = a * rcp(i % 4 == 0 ? f.x : f.z);
-        score[i + 1] = b * rcp(i % 4 == 0 ? f.y : f.w);
-        top = fmaxf(top, fmaxf(score[i], score[i + 1]));  // (passes over NaN)
+        score[i] = r * rcp(i % 4 == 0 ? f.x : i % 4 == 1 ? f.y : i % 4 == 2 ? f.z : f.w);
+        top = fmaxf(top, score[i]);  // (passes over NaN)
       }
       if (top > best) {
         const int v = s.c0 + c * K::N;
@@ -430,15 +526,14 @@ struct Race {
   // The best of tokens v0 .. v1 - 1 for this thread of the CTA.
   SP_DEVINL unsigned long long run(int v0, int v1) const {
     const Slice<F32> s(p, v0, v1);
-    // rows that have no 16-byte pieces in common, a maximum at infinity, no weight: token by token
-    const bool with_q = q && sq > 0.f;
-    if ((with_q && ((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(q)) & 15) != 0) || !(sp > 0.f) ||
-        mp == INFINITY || (with_q && mq == INFINITY))
+    if (!(sp > 0.f)) return 0ull;
+    // rows that have no 16-byte pieces in common, maxima that are not ordinary: token by token
+    if (!usual || (q && ((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(q)) & 15) != 0))
       return slowly(v0 + threadIdx.x, v1, VF_NT);
     unsigned long long key = s.beside() >= 0 ? slowly(s.beside(), s.beside() + 1, 1) : 0ull;
     float best = 0.f;
     int at = 0;
-    if (with_q) pieces<true>(s, best, at);
+    if (q) pieces<true>(s, best, at);
     else pieces<false>(s, best, at);
     return best > 0.f ? max(key, race_key(best, at)) : key;
   }
@@ -456,6 +551,10 @@ SP_DEVINL unsigned long long cta_max(unsigned long long k, unsigned long long* s
   for (int w = 0; w < VF_WARPS; ++w) k = max(k, s[w]);
   return k;
 }
+
+// A cluster barrier in two halves: that every CTA runs is known long before anything is written to another's memory.
+SP_DEVINL void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+SP_DEVINL void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 // What a sequence is left with: a row that is not there.
 SP_DEVINL void no_rows(const VerifyArgs& a, int b, bool wrong) {
@@ -477,12 +576,19 @@ __global__ void __launch_bounds__(VF_NT) verify_end_kernel(const VerifyArgs a, i
   __shared__ unsigned long long key_s[VF_WARPS], cluster_s[VF_CLUSTER];
   // Before the wait: what no kernel of this call writes.  (The sums wait for whatever ran before them ahead of their
   // trigger, so it is over.)
-  const int C = gridDim.x, rank = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int C = gridDim.x, rank = blockIdx.x, b = gridDim.y - 1 - blockIdx.y,  // (the rows read last lie in L2)
+            tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const Seq q = sequence(a, b);
+  const int per = (((a.V + C - 1) / C) + 7) & ~7, v0 = min(rank * per, a.V), v1 = min(v0 + per, a.V);
+  if (q.n > 0 && !q.greedy)
+    for (int v = v0 + tid * 32; v < v1; v += VF_NT * 32)
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(a.noise + (size_t)b * a.ld_noise + v));
+  if (C > 1) cluster_arrive();
   pdl_wait();
   pdl_trigger();
   if (q.n <= 0) {
     if (rank == 0) no_rows(a, b, q.n < 0);
+    if (C > 1) cluster_wait();
     return;
   }
   int* token = a.token + (size_t)b * a.max_rows;
@@ -500,6 +606,7 @@ __global__ void __launch_bounds__(VF_NT) verify_end_kernel(const VerifyArgs a, i
     end = __ldcg(work.end + b);
     if (end >= q.n) {  // (sequences whose offsets overlap)
       if (rank == 0) no_rows(a, b, true);
+      if (C > 1) cluster_wait();
       return;
     }
     auto load = [&](int j) {
@@ -542,8 +649,8 @@ __global__ void __launch_bounds__(VF_NT) verify_end_kernel(const VerifyArgs a, i
     }
   // (sequences whose offsets overlap can find another's sums: never a token that is not there)
   int next = r.mp > -INFINITY && r.at >= 0 && r.at < a.V ? r.at : -1;
+  if (C > 1) cluster_wait();  // every CTA of the cluster runs
   if (!q.greedy) {
-    if (C > 1) cluster_sync_all();  // every CTA of the cluster runs
     Race<F32> race;
     race.p = logits(end);
     race.q = drafted && a.draft_logits
@@ -556,21 +663,22 @@ __global__ void __launch_bounds__(VF_NT) verify_end_kernel(const VerifyArgs a, i
     race.sq = r.sq;
     race.c = q.c;
     race.out = a.draft_logits ? -1 : d;
-    const int per = (((a.V + C - 1) / C) + 7) & ~7;
-    const int v0 = min(rank * per, a.V), v1 = min(v0 + per, a.V);
+    race.prepare();
     unsigned long long key = cta_max(race.run(v0, v1), key_s);
     if (C > 1) {
       if (tid == 0) {
         const uint32_t to = mapa_shared(smem_u32(&cluster_s[rank]), 0);
         asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(to), "l"(key) : "memory");
       }
-      cluster_sync_all();
+      cluster_arrive();
+      cluster_wait();
       if (rank != 0) return;
       for (int i = 0; i < C; ++i) key = max(key, cluster_s[i]);
     }
     if (key == 0 && drafted) {  // p and q are the same (or p is all at the draft): from p
       race.q = nullptr;
       race.out = -1;
+      race.prepare();
       key = cta_max(race.run(0, a.V), key_s);
     }
     next = key != 0 ? (int)~(uint32_t)key : -1;
@@ -589,24 +697,27 @@ __global__ void __launch_bounds__(VF_NT) verify_sample_kernel(const VerifyArgs a
     float m, s, x, e;
     int at, greedy_at, unused[2];
   };
+  extern __shared__ uint4 ring[];
   __shared__ Best best_s[VF_CLUSTER], mine_s;
   __shared__ unsigned long long key_s[VF_WARPS];
+  const int C = gridDim.x, rank = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+  if (C > 1) cluster_arrive();
   pdl_wait();
   pdl_trigger();
-  const int C = gridDim.x, rank = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
   const Seq q = sequence(a, b);
   if (a.clear_err && a.err && rank + b == 0 && tid == 0 && !a.cu_rows) *a.err = 0;
   if (q.n <= 0) {
     if (rank == 0) no_rows(a, b, q.n < 0);
+    if (C > 1) cluster_wait();
     return;
   }
   const char* base = static_cast<const char*>(a.logits) + q.row0 * a.ld * (F32 ? 4 : 2);
   const float* noise = q.greedy ? nullptr : a.noise + (size_t)b * a.ld_noise;
   const int per = (((a.V + C - 1) / C) + 7) & ~7;
   const Slice<F32> s(base, min(rank * per, a.V), min((rank + 1) * per, a.V));
-  const Share t = q.greedy ? scan<F32, false>(s, q.c, nullptr) : scan<F32, true>(s, q.c, noise);
-  const RowPart r = join_cta(t.m, t.s, q.c, q.greedy, [&](float top) { return s.first_of(top, t.first); });
-  const float score = t.at >= 0 ? __fdividef(weight(t.x, r.m, q.c), t.e) : 0.f;
+  const Share t = q.greedy ? sum_slice<F32>(s, q.c, ring, []() {}) : scan_race<F32>(s, q.c, noise);
+  const RowPart r = join_cta(t.m, share_sum(q.c, t), q.c, q.greedy, [&](float top) { return s.first_of(top, t.first); });
+  const float score = t.at >= 0 ? weight(t.x, r.m, q.c) * rcp(t.e) : 0.f;
   const unsigned long long own = score > 0.f ? race_key(score, t.at) : 0ull, key = cta_max(own, key_s);
   if (tid == 0) mine_s = Best{r.m, r.s, 0.f, 1.f, -1, r.at, {0, 0}};
   __syncthreads();
@@ -615,60 +726,77 @@ __global__ void __launch_bounds__(VF_NT) verify_sample_kernel(const VerifyArgs a
     mine_s.e = t.e;
     mine_s.at = t.at;
   }
-  if (C > 1) cluster_sync_all();  // every CTA of the cluster runs, and its best is there
-  else __syncthreads();
+  __syncthreads();
   if (C > 1) {
+    cluster_wait();  // every CTA of the cluster runs
     if (tid < 8) {
       const uint32_t to = mapa_shared(smem_u32(reinterpret_cast<uint32_t*>(&best_s[rank]) + tid), 0);
       asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(to), "r"(reinterpret_cast<uint32_t*>(&mine_s)[tid]) : "memory");
     }
-    cluster_sync_all();
+    cluster_arrive();
+    cluster_wait();
     if (rank != 0) return;
-  } else if (tid == 0) {
-    best_s[0] = mine_s;
+  } else {
+    if (tid == 0) best_s[0] = mine_s;
+    __syncwarp();
   }
-  if (tid == 0) {
-    float m = -INFINITY, sum = 0.f, x = -INFINITY;
-    for (int i = 0; i < C; ++i) m = fmaxf(m, best_s[i].m);
+  if (tid < 32) {  // a lane to a CTA's best
+    const bool in = tid < C;
+    const Best o = best_s[in ? tid : 0];
+    const float m = warp_max(in ? o.m : -INFINITY);
+    const bool some = in && o.m > -INFINITY;
+    const float sum = warp_sum(!some ? 0.f : o.m == m ? o.s : o.s * ex2((o.m - m) * q.c));
     unsigned long long k = 0;
-    int next = -1;
-    for (int i = 0; i < C; ++i) {
-      const Best& o = best_s[i];
-      if (o.m == -INFINITY) continue;
-      sum += o.m == m ? o.s : o.s * ex2((o.m - m) * q.c);
-      if (q.greedy) {
-        if (next < 0 && o.m == m) next = o.greedy_at, x = m;
-      } else if (o.at >= 0) {
-        const float sc = __fdividef(weight(o.x, m, q.c), o.e);
-        if (sc > 0.f && race_key(sc, o.at) > k) k = race_key(sc, o.at), next = o.at, x = o.x;
-      }
+    if (q.greedy) {
+      if (some && o.m == m) k = race_key(1.f, o.greedy_at);
+    } else if (some && o.at >= 0) {
+      const float sc = weight(o.x, m, q.c) * rcp(o.e);
+      if (sc > 0.f) k = race_key(sc, o.at);
     }
-    a.n_accept[b] = 0;
-    a.token[b] = next;
-    if (a.logp) a.logp[b] = next >= 0 ? log_prob(x, m, sum, q.t) : -INFINITY;
+    const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(k >> 32));
+    const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(k >> 32) == hi ? (uint32_t)k : 0u);
+    const bool won = k != 0 && k == (((unsigned long long)hi << 32) | lo);
+    if (won || (hi == 0 && tid == 0)) {
+      a.n_accept[b] = 0;
+      a.token[b] = won ? (int)~lo : -1;
+      if (a.logp) a.logp[b] = won ? log_prob(q.greedy ? m : o.x, m, sum, q.t) : -INFINITY;
+    }
   }
 }
 
 }  // namespace
 
-static int verify_slices(int rows, int V) {
-  rows = std::max(rows, 1);
-  const int want = (device_sm_count() * 4 + rows / 2) / rows;
-  return std::max(1, std::min(std::min(std::max(want, (V + 32767) / 32768), VF_SLICES), (V + 4095) / 4096));
+// How a call's rows are cut.  CTAs of the sums that run at once: four per SM.  Rows that fit one wave of them are cut into as
+// many slices as do (of at least 2,048 logits), more into slices of about 51,200.  In order, with decisions on the way, where
+// several rows of a sequence can be passed over and they are more than is soon read (64 sequences of 8 drafts, 152,064 bf16
+// logits: 72 us in order, 77 not; of 5 drafts, 96 of 50,001 fp32: 56, 52; 200 of 3, 5,000 fp32: 26, 21).
+struct Cut {
+  int slices;
+  bool ordered;
+};
+static Cut verify_cut(int T_cap, int B, int V, int max_rows, bool drafted, bool f32) {
+  const int rows = std::max(drafted ? 2 * T_cap - std::min(B, T_cap) : T_cap, 1), slots = device_sm_count() * 4;
+  Cut c;
+  c.ordered = rows > slots && max_rows > 3 && (double)rows * V * (f32 ? 4 : 2) > 0x1p28;
+  c.slices = rows > slots ? (V + 51199) / 51200 : (slots + rows / 2) / rows;
+  c.slices = std::max(1, std::min(std::min(c.slices, VF_SLICES), (V + 2047) / 2048));
+  return c;
 }
 
 static size_t align256(size_t n) { return (n + 255) & ~size_t(255); }
 
 size_t verify_bytes(int T_cap, int B, int V) {
   const size_t T = (size_t)T_cap;
-  return align256(T * 2 * verify_slices(T_cap, V) * sizeof(RowPart)) + align256(T * sizeof(Row)) + align256((T + B) * 4);
+  const int slices = std::max(verify_cut(T_cap, B, V, 1, false, false).slices, verify_cut(T_cap, B, V, 1, true, false).slices);
+  return align256(T * 2 * slices * sizeof(RowPart)) + align256(T * sizeof(Row)) + align256((T + B) * 4);
 }
 
 template <typename Kernel, typename... Args>
-static cudaError_t launch_clusters(Kernel* k, int C, int B, cudaStream_t st, Args... args) {
+static cudaError_t launch_clusters(Kernel* k, int C, int B, size_t smem, cudaStream_t st, Args... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(C, B);
   cfg.blockDim = dim3(VF_NT);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -693,12 +821,17 @@ cudaError_t verify_launch(const VerifyArgs& a, void* ws, cudaStream_t st) {
       if (r != cudaSuccess) return r;
     }
     prof_begin_launch(st);
-    r = launch_clusters(a.logits_f32 ? verify_sample_kernel<true> : verify_sample_kernel<false>, C, a.B, st, a);
+    static std::atomic<unsigned long long> allowed[2];
+    auto* k = a.logits_f32 ? verify_sample_kernel<true> : verify_sample_kernel<false>;
+    r = allow_smem(k, VF_RING_BYTES, allowed[a.logits_f32]);
+    if (r == cudaSuccess) r = launch_clusters(k, C, a.B, VF_RING_BYTES, st, a);
     prof_end_launch(st, SP_K_MISC, 0.0, bytes + (a.noise ? 4.0 * a.B * a.V : 0.0));
     return r;
   }
-  const int slices = verify_slices(a.T_cap, a.V), slice = (((a.V + slices - 1) / slices) + 7) & ~7;
   const int sets = a.draft_logits ? 2 : 1;
+  const Cut cut = verify_cut(a.T_cap, a.B, a.V, a.max_rows, sets == 2, a.logits_f32);
+  const int slices = cut.slices, slice = (((a.V + slices - 1) / slices) + 7) & ~7;
+  const bool ordered = cut.ordered;
   char* base = static_cast<char*>(ws);
   VerifyWork w;
   w.part = reinterpret_cast<RowPart*>(base);
@@ -707,7 +840,6 @@ cudaError_t verify_launch(const VerifyArgs& a, void* ws, cudaStream_t st) {
   base += align256((size_t)a.T_cap * sizeof(Row));
   w.count = reinterpret_cast<int*>(base);
   w.end = w.count + a.T_cap;
-  const bool ordered = (long long)a.T_cap * sets * slices > 4 * sms;
   if (ordered) {
     r = cudaMemsetAsync(w.count, 0x7f, ((size_t)a.T_cap + a.B) * 4, st);
     if (r != cudaSuccess) return r;
@@ -715,13 +847,16 @@ cudaError_t verify_launch(const VerifyArgs& a, void* ws, cudaStream_t st) {
   prof_begin_launch(st);
   auto* sums = ordered ? (a.logits_f32 ? verify_sums_kernel<true, true> : verify_sums_kernel<false, true>)
                        : (a.logits_f32 ? verify_sums_kernel<true, false> : verify_sums_kernel<false, false>);
-  r = launch_pdl(sums, dim3(slices * sets, a.B, a.max_rows), dim3(VF_NT), 0, st, a, slices, slice, w);
+  static std::atomic<unsigned long long> allowed[2][2];
+  r = allow_smem(sums, VF_RING_BYTES, allowed[ordered][a.logits_f32]);
+  if (r != cudaSuccess) return r;
+  r = launch_pdl(sums, dim3(slices * sets, a.B, a.max_rows), dim3(VF_NT), VF_RING_BYTES, st, a, slices, slice, w);
   prof_end_launch(st, SP_K_MISC, 0.0, bytes * sets);
   if (r != cudaSuccess) return r;
   prof_begin_launch(st);
   auto* end = ordered ? (a.logits_f32 ? verify_end_kernel<true, true> : verify_end_kernel<false, true>)
                       : (a.logits_f32 ? verify_end_kernel<true, false> : verify_end_kernel<false, false>);
-  r = launch_clusters(end, a.noise ? C : 1, a.B, st, a, slices, w);
+  r = launch_clusters(end, a.noise ? C : 1, a.B, 0, st, a, slices, w);
   prof_end_launch(st, SP_K_MISC, 0.0, 0.0);
   return r;
 }
