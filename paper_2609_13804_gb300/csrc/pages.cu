@@ -96,6 +96,7 @@ __global__ void __launch_bounds__(PF_NT) pages_fork_kernel(const PagesArgs a, co
 // ------------------------------------------------------------------------- reserve, compact
 
 constexpr int PP_NT = 1024, PP_WARPS = PP_NT / 32, PP_CTAS = 8;
+constexpr int PP_LOADS = 4;  // of a lane at once
 
 // What the kernels of a call leave each other.
 struct PageMoves {
@@ -135,7 +136,7 @@ SP_DEVINL int cta_prefix(int v, int* warp_s, int& total) {
 // finds what a row needs, while its CTA looks through its share of the counts for free pages; then every CTA knows all
 // rows' needs and gives its free pages to the places they fall to.
 template <bool COMPACT>
-__global__ void __launch_bounds__(PP_NT)
+__global__ void __launch_bounds__(PP_NT, 1)
 pages_plan_kernel(const PagesArgs a, const int* __restrict__ add, const int* __restrict__ keep, long long ld_keep, int keep_cap,
                   PageMoves mv) {
   extern __shared__ int before_s[];  // [S + 1] pages that rows before each one need
@@ -148,19 +149,19 @@ pages_plan_kernel(const PagesArgs a, const int* __restrict__ add, const int* __r
   // this CTA's share of the counts: p0 .. p1 - 1, a piece of four to a thread and turn
   const int share = (((a.n_pages + PP_CTAS - 1) / PP_CTAS) + 3) & ~3;
   const int p0 = min(rank * share, a.n_pages), p1 = min(p0 + share, a.n_pages);
-  auto free_at = [&](int p) {  // bits of the free ones of four pages
+  auto bits = [](const int4& r) -> unsigned int {  // of the free ones of four pages
+    return (r.x == 0) | (r.y == 0) << 1 | (r.z == 0) << 2 | (r.w == 0) << 3;
+  };
+  auto free_at = [&](int p) {
+    if (p + 3 < p1) return bits(__ldcg(reinterpret_cast<const int4*>(a.refs + p)));
     unsigned int free = 0;
-    if (p + 3 < p1) {
-      const int4 r = __ldcg(reinterpret_cast<const int4*>(a.refs + p));
-      free = (r.x == 0) | (r.y == 0) << 1 | (r.z == 0) << 2 | (r.w == 0) << 3;
-    } else {
-      for (int k = 0; p + k < p1; ++k) free |= (unsigned)(__ldcg(a.refs + p + k) == 0) << k;
-    }
+    for (int k = 0; p + k < p1; ++k) free |= (unsigned)(__ldcg(a.refs + p + k) == 0) << k;
     return free;
   };
-  const unsigned int free0 = p0 + tid * 4 < p1 ? free_at(p0 + tid * 4) : 0u;
-  int mine = __popc(free0);
-  for (int p = p0 + (tid + PP_NT) * 4; p < p1; p += PP_NT * 4) mine += __popc(free_at(p));
+  int4 refs0 = make_int4(1, 1, 1, 1);  // (its first piece, looked at behind the rows)
+  const bool whole0 = p0 + tid * 4 + 3 < p1;
+  if (whole0) refs0 = __ldcg(reinterpret_cast<const int4*>(a.refs + p0 + tid * 4));
+  int need0 = 0, released0 = 0;  // of this warp's first row
   for (int s = warp; s < S; s += warps) {
     const int len = a.lens[s], n = __ldg(add + s);
     const int* row = a.table + (size_t)s * a.max_pages;
@@ -182,6 +183,7 @@ pages_plan_kernel(const PagesArgs a, const int* __restrict__ add, const int* __r
         const int pages = (n + page - 1) >> shift, stay = first == n ? pages : first >> shift;
         need = pages - stay;
         move = first == n ? 0 : n - (stay << shift);
+#pragma unroll 4
         for (int c = lane; c < a.max_pages; c += 32) old[c] = row[c];
         released = len;
       }
@@ -190,19 +192,34 @@ pages_plan_kernel(const PagesArgs a, const int* __restrict__ add, const int* __r
     } else if (n > 0) {
       const int lo = len >> shift, hi = (int)(((long long)len + n + page - 1) >> shift);
       int shares = 0;
-      for (int c0 = lo; c0 < hi; c0 += 32) {
-        const int c = c0 + lane, e = c < hi ? row[c] : -1;
-        const bool there = e >= 0 && e < a.n_pages;
-        if (e >= a.n_pages) set_error(a.err, SP_DEVERR_INDEX);
-        const bool shared = there && __ldcg(a.refs + e) > 1;
-        const unsigned int all = __ballot_sync(0xffffffffu, c < hi && (!there || shared));
-        if (c < hi && (!there || shared)) {
-          mv.place[(size_t)s * a.max_pages + need + __popc(all & ((1u << lane) - 1u))] = c;
-          old[c] = shared ? e : -1;
+      for (int c0 = lo; c0 < hi; c0 += 32 * PP_LOADS) {
+        int e[PP_LOADS], named[PP_LOADS];
+#pragma unroll
+        for (int k = 0; k < PP_LOADS; ++k) {
+          const int c = c0 + 32 * k + lane;
+          e[k] = c < hi ? row[c] : -1;
         }
-        need += __popc(all);
-        shares += shared;
-        if (c0 == lo && __shfl_sync(0xffffffffu, (int)shared, 0)) move = len & (page - 1);
+#pragma unroll
+        for (int k = 0; k < PP_LOADS; ++k) {
+          if (e[k] >= a.n_pages) {
+            set_error(a.err, SP_DEVERR_INDEX);
+            e[k] = -1;
+          }
+          named[k] = e[k] >= 0 ? __ldcg(a.refs + e[k]) : 0;
+        }
+#pragma unroll
+        for (int k = 0; k < PP_LOADS; ++k) {
+          const int c = c0 + 32 * k + lane;
+          const bool shared = named[k] > 1, gets = c < hi && (e[k] < 0 || shared);
+          const unsigned int all = __ballot_sync(0xffffffffu, gets);
+          if (gets) {
+            mv.place[(size_t)s * a.max_pages + need + __popc(all & ((1u << lane) - 1u))] = c;
+            old[c] = shared ? e[k] : -1;
+          }
+          need += __popc(all);
+          shares += shared;
+          if (c0 == lo && k == 0 && __shfl_sync(0xffffffffu, (int)shared, 0)) move = len & (page - 1);
+        }
       }
       released = __any_sync(0xffffffffu, shares > 0);
     }
@@ -211,15 +228,20 @@ pages_plan_kernel(const PagesArgs a, const int* __restrict__ add, const int* __r
       mv.move[s] = move;
       mv.was[s] = released;
     }
+    if (s == warp) need0 = need, released0 = released;
   }
+  const unsigned int free0 = whole0 ? bits(refs0) : p0 + tid * 4 < p1 ? free_at(p0 + tid * 4) : 0u;
+  int mine = __popc(free0);
+  for (int p = p0 + (tid + PP_NT) * 4; p < p1; p += PP_NT * 4) mine += __popc(free_at(p));
   int sum;
   const int at0 = cta_prefix(mine, warp_s, sum);  // (of its first piece, where it has no more)
   if (tid == 0) mv.count[rank] = sum;
   cluster_sync_all();
   if (tid < PP_CTAS) free_s[tid] = __ldcg(mv.count + tid);
-  int total = 0;
+  int total = 0, move0 = 0;
   for (int s0 = 0; s0 < S; s0 += PP_NT) {
     const int s = s0 + tid;
+    if (s0 == 0 && rank == 0 && s < S) move0 = __ldcg(mv.move + s);
     const int before = total + cta_prefix(s < S ? max(__ldcg(mv.need + s), 0) : 0, warp_s, sum);
     if (s < S) before_s[s] = before;
     total += sum;
@@ -231,28 +253,31 @@ pages_plan_kernel(const PagesArgs a, const int* __restrict__ add, const int* __r
     if (i < rank) base += free_s[i];
     found += free_s[i];
   }
-  // Rows are served in order until one does not fit.
-  // The k-th free page: to the row that needs it, and the place.
-  auto give = [&](int k, int page_id) {
-    int x = 0, y = S - 1;  // the last row with at most k pages before it (rows that need none lie before it, or behind)
-    while (x < y) {
-      const int mid = (x + y + 1) >> 1;
-      if (before_s[mid] <= k) x = mid; else y = mid - 1;
-    }
-    if (before_s[x + 1] > found) return;
-    const int at = k - before_s[x];
-    int c;
-    if (COMPACT) {
-      const int n = __ldg(add + x), pages = (n + page - 1) >> shift;
-      c = pages - (before_s[x + 1] - before_s[x]) + at;
-    } else {
-      c = __ldcg(mv.place + (size_t)x * a.max_pages + at);
-    }
-    a.refs[page_id] = 1;
-    a.table[(size_t)x * a.max_pages + c] = page_id;
-  };
+  // (rows are served in order until one does not fit)
+  // Free pages from the at-th on, of four pages from p: each to the row that needs it, and the place.
   auto give_all = [&](unsigned int free, int at, int p) {
-    for (; free && at < total; free &= free - 1) give(at++, p + __ffs(free) - 1);
+    int x = -1;
+    for (; free && at < total; free &= free - 1, ++at) {
+      if (x < 0 || before_s[x + 1] <= at) {  // the last row with at most `at` pages before it
+        int y = S - 1;
+        x = max(x, 0);
+        while (x < y) {
+          const int mid = (x + y + 1) >> 1;
+          if (before_s[mid] <= at) x = mid; else y = mid - 1;
+        }
+      }
+      if (before_s[x + 1] > found) return;
+      const int k = at - before_s[x], id = p + __ffs(free) - 1;
+      int c;
+      if (COMPACT) {
+        const int n = __ldg(add + x), pages = (n + page - 1) >> shift;
+        c = pages - (before_s[x + 1] - before_s[x]) + k;
+      } else {
+        c = __ldcg(mv.place + (size_t)x * a.max_pages + k);
+      }
+      a.refs[id] = 1;
+      a.table[(size_t)x * a.max_pages + c] = id;
+    }
   };
   const bool again = share > PP_NT * 4;  // counts are looked at a second time
   if (!again) {
@@ -268,11 +293,12 @@ pages_plan_kernel(const PagesArgs a, const int* __restrict__ add, const int* __r
   // Only now are pages released: counts must not fall to 0 under the eyes of those who look for free pages.
   if (again) cluster_sync_all();
   for (int s = warp; s < S; s += warps) {
-    if (__ldcg(mv.need + s) < (COMPACT ? 0 : 1) || before_s[s + 1] > found) continue;
+    if ((s == warp ? need0 : __ldcg(mv.need + s)) < (COMPACT ? 0 : 1) || before_s[s + 1] > found) continue;
     const int* old = mv.old + (size_t)s * a.max_pages;
     const int taken = before_s[s + 1] - before_s[s];
     if (COMPACT) {
       const int n = __ldg(add + s), pages = (n + page - 1) >> shift;
+#pragma unroll 4
       for (int c = pages - taken + lane; c < a.max_pages; c += 32) {
         const int e = __ldcg(old + c);
         if (e >= 0 && e < a.n_pages) atomicSub(a.refs + e, 1);
@@ -280,7 +306,7 @@ pages_plan_kernel(const PagesArgs a, const int* __restrict__ add, const int* __r
         if (c >= pages) a.table[(size_t)s * a.max_pages + c] = -1;
       }
       if (lane == 0) a.lens[s] = n;
-    } else if (__ldcg(mv.was + s)) {
+    } else if (s == warp ? released0 : __ldcg(mv.was + s)) {
       for (int i = lane; i < taken; i += 32) {
         const int e = __ldcg(old + __ldcg(mv.place + (size_t)s * a.max_pages + i));
         if (e >= 0) atomicSub(a.refs + e, 1);
@@ -292,7 +318,7 @@ pages_plan_kernel(const PagesArgs a, const int* __restrict__ add, const int* __r
     for (int s0 = 0; s0 < S; s0 += PP_NT) {
       const int s = s0 + tid;
       const bool on = s < S && before_s[s + 1] <= found;
-      const int before = moved + cta_prefix(on ? __ldcg(mv.move + s) : 0, warp_s, sum);
+      const int before = moved + cta_prefix(!on ? 0 : s0 == 0 ? move0 : __ldcg(mv.move + s), warp_s, sum);
       if (s < S) mv.start[s] = before;
       moved += sum;
     }
@@ -317,13 +343,14 @@ pages_copy_kernel(const PagesArgs a, const int* __restrict__ keep, long long ld_
   pdl_wait();
   pdl_trigger();
   const int S = a.S, lane = threadIdx.x & 31, shift = a.page_shift, mask = (1 << shift) - 1;
-  const int total = __ldcg(mv.start + S);
-  if (total == 0) return;
   for (int i = threadIdx.x; i <= S; i += PM_NT) start_s[i] = __ldcg(mv.start + i);
   __syncthreads();
+  const int total = start_s[S];
+  if (total == 0) return;
   const int shares = (total + (1 << pos_shift) - 1) >> pos_shift;
   const int warps = gridDim.x * PM_WARPS;
-  const int planes = (long long)shares * a.planes > 8ll * warps ? 4 : 1;  // at a time
+  // planes at a time: as many as give every warp one turn, where few do
+  const int turns = (int)min(((long long)shares * a.planes + warps - 1) / warps, 8ll), planes = turns <= 4 ? turns : 4;
   const long long units = (long long)shares * ((a.planes + planes - 1) / planes);
   const int L = 1 << lanes_shift;  // lanes of a row
   const int steps = (a.row16 + L - 1) >> lanes_shift, groups = ((1 << pos_shift) + (32 >> lanes_shift) - 1) >> (5 - lanes_shift);
