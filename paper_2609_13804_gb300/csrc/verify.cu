@@ -367,7 +367,7 @@ SP_DEVINL Row decide(const VerifyArgs& a, const Seq& q, int j, const RowPart* pa
   else {  // u q(d) < p(d), the sums multiplied out; without weight anywhere p is 0
     const float pd = o.sp > 0.f ? weight(o.xd, o.mp, q.c) : 0.f;
     const float qd = !with_q ? 1.f : o.sq > 0.f ? weight(yd, o.mq, q.c) : 0.f;
-    o.stays = u * qd * o.sp < pd * (with_q && o.sq > 0.f ? o.sq : 1.f);
+    o.stays = pd > 0.f && u * qd * o.sp < pd * (with_q && o.sq > 0.f ? o.sq : 1.f);
   }
   return o;
 }
@@ -844,12 +844,12 @@ cudaError_t verify_launch(const VerifyArgs& a, void* ws, cudaStream_t st) {
     r = cudaMemsetAsync(w.count, 0x7f, ((size_t)a.T_cap + a.B) * 4, st);
     if (r != cudaSuccess) return r;
   }
-  prof_begin_launch(st);
   auto* sums = ordered ? (a.logits_f32 ? verify_sums_kernel<true, true> : verify_sums_kernel<false, true>)
                        : (a.logits_f32 ? verify_sums_kernel<true, false> : verify_sums_kernel<false, false>);
   static std::atomic<unsigned long long> allowed[2][2];
   r = allow_smem(sums, VF_RING_BYTES, allowed[ordered][a.logits_f32]);
   if (r != cudaSuccess) return r;
+  prof_begin_launch(st);
   r = launch_pdl(sums, dim3(slices * sets, a.B, a.max_rows), dim3(VF_NT), VF_RING_BYTES, st, a, slices, slice, w);
   prof_end_launch(st, SP_K_MISC, 0.0, bytes * sets);
   if (r != cudaSuccess) return r;

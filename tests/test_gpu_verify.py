@@ -185,6 +185,52 @@ def test_a_large_batch(sp):
     compare(sp.sp_draft_verify(**s), expect(s), 6)
 
 
+def test_rows_in_order(sp):
+    """Enough reading (more than 2^28 bytes of more rows than CTAs run at once) for rows behind a rejected draft to be passed
+    over: 1,396 rows of 50,001 fp32 logits, some of NaN where nothing may look."""
+    counts = [6] * 126 + [2, 4]
+    s = problem(6, 50001, counts, near=0.4)
+    want = expect(s)
+    got = sp.sp_draft_verify(**s)
+    assert int(got["err"].item()) == 0
+    compare(got, want, 6)
+    first = [6 * b for b in range(126)]
+    late = [first[b] + n + 1 for b, (n, _, _, _) in enumerate(want[:126]) if n < 5]  # the row behind a sequence's end
+    s["logits"][late] = torch.nan
+    s["draft_logits"][late] = torch.nan
+    again = sp.sp_draft_verify(**s)
+    assert all(torch.equal(got[k], again[k]) for k in ("n_accept", "token", "logp"))
+    s["cu_rows"][5], s["cu_rows"][9] = 20, 60  # rows that belong to two, or to none: nothing outside is touched
+    r = sp.sp_draft_verify(**s)
+    assert int(r["err"].item()) == 2
+    assert ((r["token"] >= -1) & (r["token"] < 50001)).all()
+
+
+@pytest.mark.parametrize("max_rows", [1, 3])
+def test_a_padded_batch(sp, max_rows):
+    """Sequences without rows and rows without a sequence, which are not read."""
+    counts = [max_rows, 0, 1, 0]
+    s = problem(8, 1001, counts)
+    T = sum(counts)
+    for k in ("logits", "draft_logits"):
+        s[k] = torch.cat((s[k], torch.full((3, 1001), torch.nan, device=DEV)))
+    s["draft"] = torch.cat((s["draft"], ints([1 << 30] * 3)))
+    s["u"] = torch.cat((s["u"], torch.full((3,), torch.nan, device=DEV)))
+    s["max_rows"] = max_rows
+    got = sp.sp_draft_verify(**s)
+    assert int(got["err"].item()) == 0
+    compare(got, expect(s), max_rows)
+    # as a program's graph has it: wide strides, an error word that is kept
+    err = ints([8])
+    wide = torch.zeros((4, 1203), device=DEV)
+    wide[:, :1001] = s["noise"]
+    again = sp.sp_draft_verify(**dict(s, noise=wide[:, :1001], err=err))
+    assert int(err.item()) == 8 and all(torch.equal(got[k], again[k]) for k in ("n_accept", "token", "logp"))
+    none = sp.sp_draft_verify(**dict(s, logits=s["logits"][:0], draft_logits=s["draft_logits"][:0], draft=s["draft"][:0], u=s["u"][:0],
+                                     cu_rows=ints([0] * 5)))
+    assert int(none["err"].item()) == 0 and (none["n_accept"] == -1).all() and (none["token"] == -1).all()
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_masks_infinities_and_nan(sp, dtype):
     V = 777
