@@ -63,10 +63,11 @@ SP_DEVINL bool ordinary(float mc) { return fabsf(mc) < 4194304.f; }
 // A thread's share of a slice: its maximum, its sum and the first batch of loads that holds the maximum; with noise the
 // best of its race too, the logit and noise of which are kept: scores of threads with different maxima are formed again.
 struct Share {
-  float m, z, s;  // (s in units of exp2(z) where that is ordinary, else of exp(m / t))
+  float m, z, s;  // (s in units of exp2(z) where m c is ordinary, else of exp(m / t))
   int first;
   float x, e;  // the race's best so far
   int at;      // -1: none
+  bool usual;  // m c is ordinary
 };
 
 // Tokens v0 .. v1 - 1 of a row, 16 bytes at a time where they lie whole in the slice.
@@ -106,30 +107,32 @@ struct Slice {
 // Raises a share's maximum to m; what it had counts `the result` as much.
 SP_DEVINL float raise_to(float m, float c, Share& r) {
   const float mc = m * c, z = rintf(mc);
+  const bool usual = ordinary(mc);
   float f;
-  if (r.m == -INFINITY) {
-    f = 0.f;
-  } else if (ordinary(mc) && ordinary(r.m * c)) {
-    f = ex2(r.z - z);
+  if (usual && r.usual) {
+    f = ex2(r.z - z);  // (0 at first, when both are -infinity)
   } else {
-    f = ex2((r.m - m) * c);
-    if (ordinary(r.m * c)) f *= ex2(__fmaf_rn(-r.m, c, r.z));
-    if (ordinary(mc)) f *= ex2(__fmaf_rn(m, c, -z));
+    f = r.m == -INFINITY ? 0.f : ex2((r.m - m) * c);
+    if (r.usual && r.m > -INFINITY) f *= ex2(__fmaf_rn(-r.m, c, r.z));
+    if (usual) f *= ex2(__fmaf_rn(m, c, -z));
   }
   r.s *= f;
   r.m = m;
   r.z = z;
+  r.usual = usual;
   return f;
 }
 
 // A logit's weight in a share's units.
 SP_DEVINL float share_weight(float x, float c, const Share& r) {
-  if (!ordinary(r.m * c)) return weight(x, r.m, c);
+  if (!r.usual) return weight(x, r.m, c);
   return x > -INFINITY ? ex2(__fmaf_rn(x, c, -r.z)) : 0.f;
 }
 
 // A share's sum in units of exp(m / t).
-SP_DEVINL float share_sum(float c, const Share& r) { return ordinary(r.m * c) ? r.s * ex2(__fmaf_rn(-r.m, c, r.z)) : r.s; }
+SP_DEVINL float share_sum(float c, const Share& r) {
+  return r.usual && r.m > -INFINITY ? r.s * ex2(__fmaf_rn(-r.m, c, r.z)) : r.s;
+}
 
 // The largest logit of a batch.
 template <bool F32>
@@ -155,7 +158,7 @@ SP_DEVINL void add_batch(const uint4 (&u)[VF_LOADS], int c, float cc, Share& r, 
 #pragma unroll
     for (int i = 0; i < K::N; ++i) sum[i & 1] += ex2(__fmaf_rn(K::at(u[k], i), cc, -r.z));
   float ts = sum[0] + sum[1];
-  if (!(ts < INFINITY) || !ordinary(r.m * cc)) {  // a NaN among them, or no ordinary maximum
+  if (!(ts < INFINITY) || !r.usual) {  // a NaN among them, or no ordinary maximum
     ts = 0.f;
 #pragma unroll 1
     for (int k = 0; k < VF_LOADS && lm > -INFINITY; ++k) {
@@ -180,21 +183,30 @@ SP_DEVINL float add_one(float x, float c, Share& r) {
 }
 
 // A thread's share of a slice.  Its loads go through shared memory of its own (VF_RING batches of VF_LOADS), so no thread
-// waits for another; `meanwhile` runs while the first are on their way.
+// waits for another; `meanwhile` runs while the first are on their way.  Batches that lie whole in the slice are loaded and
+// read without a check of every piece.
 template <bool F32, typename Meanwhile>
 SP_DEVINL Share sum_slice(const Slice<F32>& sl, float cc, uint4* ring, Meanwhile meanwhile) {
   using K = Chunk<F32>;
   constexpr int STEP = VF_NT * VF_LOADS;
-  Share r{-INFINITY, 0.f, 0.f, -1, 0.f, 1.f, -1};
-  const uint4* src = sl.src();
+  Share r{-INFINITY, -INFINITY, 0.f, -1, 0.f, 1.f, -1, true};
+  const uint4* src = sl.src() + threadIdx.x;
   uint4* own = ring + threadIdx.x;
-  auto load = [&](int c0, int place) {
-    const int c = c0 + threadIdx.x;
+  const int left = sl.chunks - threadIdx.x;  // pieces from this thread's first on
+  auto copy = [&](uint4* to, const uint4* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
+  };
+  auto load = [&](int c0, int place) {  // (c0: the batch's first piece, the same for all threads)
+    const uint4* from = src + c0;
+    uint4* to = own + place * STEP;
+    if (c0 + STEP <= sl.chunks) {
 #pragma unroll
-    for (int k = 0; k < VF_LOADS; ++k)
-      if (c + k * VF_NT < sl.chunks)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(own + place * STEP + k * VF_NT)),
-                     "l"(src + c + k * VF_NT) : "memory");
+      for (int k = 0; k < VF_LOADS; ++k) copy(to + k * VF_NT, from + k * VF_NT);
+    } else {
+#pragma unroll
+      for (int k = 0; k < VF_LOADS; ++k)
+        if (c0 + k * VF_NT < left) copy(to + k * VF_NT, from + k * VF_NT);
+    }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
 #pragma unroll
@@ -205,14 +217,20 @@ SP_DEVINL Share sum_slice(const Slice<F32>& sl, float cc, uint4* ring, Meanwhile
   for (int c0 = 0, place = 0; c0 < sl.chunks; c0 += STEP) {
     load(c0 + (VF_RING - 1) * STEP, place == 0 ? VF_RING - 1 : place - 1);
     asm volatile("cp.async.wait_group %0;" ::"n"(VF_RING - 1) : "memory");
-    const int c = c0 + threadIdx.x;
+    const uint4* at = own + place * STEP;
+    const bool whole = c0 + STEP <= sl.chunks;
     auto piece = [&](int k) {
-      return c + k * VF_NT < sl.chunks ? own[place * STEP + k * VF_NT] : make_uint4(K::kNone, K::kNone, K::kNone, K::kNone);
+      return whole || c0 + k * VF_NT < left ? at[k * VF_NT] : make_uint4(K::kNone, K::kNone, K::kNone, K::kNone);
     };
     uint4 u[VF_LOADS];
+    if (whole) {
 #pragma unroll
-    for (int k = 0; k < VF_LOADS; ++k) u[k] = piece(k);
-    add_batch<F32>(u, c, cc, r, piece);
+      for (int k = 0; k < VF_LOADS; ++k) u[k] = at[k * VF_NT];
+    } else {
+#pragma unroll
+      for (int k = 0; k < VF_LOADS; ++k) u[k] = piece(k);
+    }
+    add_batch<F32>(u, c0 + threadIdx.x, cc, r, piece);
     if (++place == VF_RING) place = 0;
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
@@ -225,7 +243,7 @@ template <bool F32>
 SP_DEVINL Share scan_race(const Slice<F32>& sl, float cc, const float* noise) {
   using K = Chunk<F32>;
   constexpr int E4 = K::N / 4;
-  Share r{-INFINITY, 0.f, 0.f, -1, 0.f, 1.f, -1};
+  Share r{-INFINITY, -INFINITY, 0.f, -1, 0.f, 1.f, -1, true};
   float best = 0.f;  // (relative to r.m)
   auto race = [&](float x, float w, float e, int v) {
     const float score = w * rcp(e);  // (e = 0: infinity, or NaN for w = 0, which is no candidate)
@@ -261,7 +279,6 @@ SP_DEVINL Share scan_race(const Slice<F32>& sl, float cc, const float* noise) {
     const float lm = batch_top<F32>(u);
     if (lm == -INFINITY) continue;
     if (lm > r.m) best *= raise_to(lm, cc, r);
-    const bool usual = ordinary(r.m * cc);
     float sum = 0.f;
 #pragma unroll
     for (int k = 0; k < VF_LOADS; ++k)
@@ -269,7 +286,7 @@ SP_DEVINL Share scan_race(const Slice<F32>& sl, float cc, const float* noise) {
       for (int i = 0; i < K::N; ++i) {
         const float x = K::at(u[k], i);
         float w = ex2(__fmaf_rn(x, cc, -r.z));
-        if (!usual || !(w < INFINITY)) w = share_weight(x, cc, r);
+        if (!r.usual || !(w < INFINITY)) w = share_weight(x, cc, r);
         const float4& f = n[k * E4 + i / 4];
         sum += w;
         race(x, w, i % 4 == 0 ? f.x : i % 4 == 1 ? f.y : i % 4 == 2 ? f.z : f.w, sl.c0 + (c + k * VF_NT) * K::N + i);
@@ -783,6 +800,13 @@ static Cut verify_cut(int T_cap, int B, int V, int max_rows, bool drafted, bool 
   return c;
 }
 
+// Logits of a slice: whole batches, where it has some (slices that each end in a part of a batch, of three 7 instead of
+// 6.2, cost their sums a tenth).
+static int slice_of(int V, int slices, bool f32) {
+  const int batch = VF_NT * VF_LOADS * (f32 ? 4 : 8), least = (V + slices - 1) / slices;
+  return least > batch / 2 ? (least + batch - 1) / batch * batch : (least + 7) & ~7;
+}
+
 static size_t align256(size_t n) { return (n + 255) & ~size_t(255); }
 
 size_t verify_bytes(int T_cap, int B, int V) {
@@ -830,7 +854,7 @@ cudaError_t verify_launch(const VerifyArgs& a, void* ws, cudaStream_t st) {
   }
   const int sets = a.draft_logits ? 2 : 1;
   const Cut cut = verify_cut(a.T_cap, a.B, a.V, a.max_rows, sets == 2, a.logits_f32);
-  const int slices = cut.slices, slice = (((a.V + slices - 1) / slices) + 7) & ~7;
+  const int slices = cut.slices, slice = slice_of(a.V, slices, a.logits_f32);
   const bool ordered = cut.ordered;
   char* base = static_cast<char*>(ws);
   VerifyWork w;
