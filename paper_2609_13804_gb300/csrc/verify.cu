@@ -6,7 +6,10 @@
 // a maximum is taken over the race, so it needs no sum of r, and its answer moves only if two of V scores are nearer
 // than fp32 tells apart.
 //
-// Two kernels: the sums of every row, then per sequence the decision and the race over the one row where it ends.
+// Two kernels: the sums of every row (a maximum and a sum of exponentials, one pass), then per sequence the decision and the
+// race over the one row where it ends.  Bound by reading: every row that is looked at once, the last one twice and the noise.
+// Without drafts one kernel does both in one pass.  Sums and scores are fp32; decisions multiply sums out, so nothing is
+// rounded to fewer bits anywhere.
 #include <algorithm>
 #include <cfloat>
 
@@ -393,6 +396,10 @@ SP_DEVINL Row decide(const VerifyArgs& a, const Seq& q, int j, const RowPart* pa
 // blockIdx.z the row of the sequence.  ORDERED: the CTA that ends a row decides about its draft, and rows behind one that
 // rejects are passed over.  CTAs start in the order of their numbers, so in a call of many waves most of those rows
 // are never read; nothing waits, and what is read needlessly has no effect.
+// 256 sequences of 5 drafts (2.1 stay), 152,064 bf16 logits: 470 of 856 MB read in 92 us, 5.1 TB/s; all of them, where every
+// draft stays, in 141, 6.1 TB/s.  A CTA of a row that is passed over costs the call 1.7 ns, a slice's beginning and end some 5 us
+// that three other CTAs of the SM fill; issue 57%, about 9 instructions a logit.  (CTAs that stay, fetch slices from a
+// counter and keep bulk copies in flight: 137 to 200.)
 template <bool F32, bool ORDERED>
 __global__ void __launch_bounds__(VF_NT, 4) verify_sums_kernel(const VerifyArgs a, int slices, int slice, VerifyWork work) {
   extern __shared__ uint4 ring[];
@@ -586,6 +593,9 @@ SP_DEVINL void no_rows(const VerifyArgs& a, int b, bool wrong) {
 }
 
 // A cluster per sequence: every CTA finds the row where it ends (ORDERED: is told), each races over its slice of it.
+// Bound by reading p, q and the noise, and by the chain sums -> decision -> race -> two exchanges (3 to 4 us of a small call's
+// 6): 256 sequences of 152,064 bf16 logits, 295 MB, about 60 us behind the sums.  (Reading only the noise, and logits where a
+// segment's maximum and the least noise of 8 tokens let one win: 88, a dependent load for every fourth warp.)
 template <bool F32, bool ORDERED>
 __global__ void __launch_bounds__(VF_NT) verify_end_kernel(const VerifyArgs a, int slices, VerifyWork work) {
   using K = Chunk<F32>;
@@ -707,7 +717,8 @@ __global__ void __launch_bounds__(VF_NT) verify_end_kernel(const VerifyArgs a, i
   }
 }
 
-// Without drafts: a cluster per sequence, the sums and the race in one pass over its row.
+// Without drafts: a cluster per sequence, the sums and the race in one pass over its row.  64 rows of 32,000 fp32 logits, 16 MB:
+// 8.5 us, a chain of temperature -> loads -> join -> exchange; 256 of 152,064 bf16, 233 MB: 62 us (3.8 TB/s).
 template <bool F32>
 __global__ void __launch_bounds__(VF_NT) verify_sample_kernel(const VerifyArgs a) {
   struct __align__(16) Best {
