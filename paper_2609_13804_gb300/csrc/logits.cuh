@@ -41,10 +41,6 @@ struct Chunk<true> {
   SP_DEVINL static float top(const uint4& u) {  // (fmaxf passes over NaN)
     return fmaxf(fmaxf(__uint_as_float(u.x), __uint_as_float(u.y)), fmaxf(__uint_as_float(u.z), __uint_as_float(u.w)));
   }
-  SP_DEVINL static uint4 without_nan(const uint4& u) {  // NaN becomes -infinity
-    auto f = [](uint32_t x) { return __float_as_uint(fmaxf(__uint_as_float(x), -INFINITY)); };
-    return make_uint4(f(u.x), f(u.y), f(u.z), f(u.w));
-  }
   SP_DEVINL static float one(const void* row, int v) { return __ldg(static_cast<const float*>(row) + v); }
 };
 template <>
@@ -60,17 +56,46 @@ struct Chunk<false> {
     const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));  // (NaN passed over)
     return fmaxf(__low2float(m), __high2float(m));
   }
-  SP_DEVINL static uint4 without_nan(const uint4& u) {
-    const __nv_bfloat162 low = __float2bfloat162_rn(-INFINITY);
-    uint4 r;
-    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&u);
-    __nv_bfloat162* o = reinterpret_cast<__nv_bfloat162*>(&r);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) o[k] = __hmax2(h[k], low);
-    return r;
-  }
   SP_DEVINL static float one(const void* row, int v) {
     return __bfloat162float(static_cast<const __nv_bfloat16*>(row)[v]);
+  }
+};
+
+// 16 bytes of logits with -infinity for NaN.
+template <bool F32>
+SP_DEVINL uint4 without_nan(const uint4& u) {
+  auto f = [](uint32_t x) -> uint32_t {
+    if (F32) return __float_as_uint(fmaxf(__uint_as_float(x), -INFINITY));
+    const __nv_bfloat162 m = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&x), __float2bfloat162_rn(-INFINITY));
+    return *reinterpret_cast<const uint32_t*>(&m);
+  };
+  return make_uint4(f(u.x), f(u.y), f(u.z), f(u.w));
+}
+
+// Four logits, which go with 16 bytes of fp32 numbers of the same tokens: a warp's loads of both are contiguous.
+template <bool F32>
+struct Four;
+template <>
+struct Four<true> {
+  using T = uint4;
+  static constexpr int kBytes = 16;
+  SP_DEVINL static T none() { return make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }
+  SP_DEVINL static float at(const T& u, int k) { return Chunk<true>::at(u, k); }
+  SP_DEVINL static float top(const T& u) { return Chunk<true>::top(u); }
+};
+template <>
+struct Four<false> {
+  using T = uint2;
+  static constexpr int kBytes = 8;
+  SP_DEVINL static T none() { return make_uint2(0xff80ff80u, 0xff80ff80u); }
+  SP_DEVINL static float at(const T& u, int k) {
+    const uint32_t w = k < 2 ? u.x : u.y;
+    return __uint_as_float((k & 1) ? (w & 0xffff0000u) : (w << 16));
+  }
+  SP_DEVINL static __nv_bfloat162 pair(uint32_t w) { return *reinterpret_cast<__nv_bfloat162*>(&w); }
+  SP_DEVINL static float top(const T& u) {
+    const __nv_bfloat162 m = __hmax2(pair(u.x), pair(u.y));
+    return fmaxf(__low2float(m), __high2float(m));
   }
 };
 

@@ -241,70 +241,110 @@ SP_DEVINL Share sum_slice(const Slice<F32>& sl, float cc, uint4* ring, Meanwhile
   return r;
 }
 
-// The same with the race.
+// The same with the race, four tokens and their noise at a time: batches of vr_loads() fours, vr_ring() of them (48 KB).
 template <bool F32>
-SP_DEVINL Share scan_race(const Slice<F32>& sl, float cc, const float* noise) {
+constexpr int vr_loads() { return F32 ? 2 : 4; }
+template <bool F32>
+constexpr int vr_ring() { return F32 ? 3 : 2; }
+template <bool F32>
+constexpr int vr_bytes() { return vr_ring<F32>() * vr_loads<F32>() * VF_NT * (16 + Four<F32>::kBytes); }
+
+template <bool F32>
+SP_DEVINL Share scan_race(const Slice<F32>& sl, float cc, uint4* ring, const float* noise) {
   using K = Chunk<F32>;
-  constexpr int E4 = K::N / 4;
+  using Q = Four<F32>;
+  using T = typename Q::T;
+  constexpr int LOADS = vr_loads<F32>(), RING = vr_ring<F32>(), STEP = VF_NT * LOADS;
   Share r{-INFINITY, -INFINITY, 0.f, -1, 0.f, 1.f, -1, true};
-  float best = 0.f;  // (relative to r.m)
-  auto race = [&](float x, float w, float e, int v) {
-    const float score = w * rcp(e);  // (e = 0: infinity, or NaN for w = 0, which is no candidate)
-    if (score > best) {
-      best = score;
-      r.x = x;
-      r.e = e;
-      r.at = v;
+  float best = 0.f;  // (in r's units)
+  const int tid = threadIdx.x, left = sl.chunks * (K::N / 4) - tid;  // fours from this thread's first on
+  const T* src = reinterpret_cast<const T*>(sl.src()) + tid;
+  const float* e = noise + sl.c0 + tid * 4;
+  const bool e16 = (reinterpret_cast<uintptr_t>(e) & 15) == 0;
+  uint4* own_n = ring + tid;
+  T* own_x = reinterpret_cast<T*>(ring + RING * STEP) + tid;
+  auto load = [&](int c0, int place) {
+#pragma unroll
+    for (int k = 0; k < LOADS; ++k) {
+      const int c = c0 + k * VF_NT, to = place * STEP + k * VF_NT;
+      if (c >= left) continue;
+      asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem_u32(own_x + to)), "l"(src + c), "n"(Q::kBytes) : "memory");
+      const float* from = e + (size_t)c * 4;
+      const uint32_t at = smem_u32(own_n + to);
+      if (e16) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(from) : "memory");
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(at + 4 * i), "l"(from + i) : "memory");
+      }
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
   };
+#pragma unroll
+  for (int i = 0; i < RING - 1; ++i) load(i * STEP, i);
   const int beside = sl.beside();
   const float mine = beside >= 0 ? K::one(sl.base, beside) : -INFINITY;
-  const uint4* src = sl.src();
-  const float* e = noise + sl.c0;
-  const bool e16 = (reinterpret_cast<uintptr_t>(e) & 15) == 0;
-  for (int c = threadIdx.x; c < sl.chunks; c += VF_NT * VF_LOADS) {
-    uint4 u[VF_LOADS];
+  for (int c0 = 0, place = 0; c0 < sl.chunks * (K::N / 4); c0 += STEP) {
+    load(c0 + (RING - 1) * STEP, place == 0 ? RING - 1 : place - 1);
+    asm volatile("cp.async.wait_group %0;" ::"n"(RING - 1) : "memory");
+    T x[LOADS];
+    uint4 n[LOADS];
+    float lm = -INFINITY;
 #pragma unroll
-    for (int k = 0; k < VF_LOADS; ++k)
-      u[k] = c + k * VF_NT < sl.chunks ? __ldcs(src + c + k * VF_NT) : make_uint4(K::kNone, K::kNone, K::kNone, K::kNone);
-    float4 n[VF_LOADS * E4];
-    {
-#pragma unroll
-      for (int k = 0; k < VF_LOADS * E4; ++k) {
-        const int at = ((c + k / E4 * VF_NT) * E4 + k % E4) * 4;
-        n[k] = make_float4(1.f, 1.f, 1.f, 1.f);
-        if (c + k / E4 * VF_NT < sl.chunks) {
-          if (e16) n[k] = __ldcs(reinterpret_cast<const float4*>(e + at));
-          else n[k] = make_float4(__ldg(e + at), __ldg(e + at + 1), __ldg(e + at + 2), __ldg(e + at + 3));
-        }
-      }
+    for (int k = 0; k < LOADS; ++k) {
+      x[k] = c0 + k * VF_NT < left ? own_x[place * STEP + k * VF_NT] : Q::none();
+      n[k] = own_n[place * STEP + k * VF_NT];  // (of fours that are not there too: they have no weight)
+      lm = fmaxf(lm, Q::top(x[k]));
     }
-    const float lm = batch_top<F32>(u);
-    if (lm == -INFINITY) continue;
     if (lm > r.m) best *= raise_to(lm, cc, r);
     float sum = 0.f;
+    auto weigh = [&](auto weight_of) {
 #pragma unroll
-    for (int k = 0; k < VF_LOADS; ++k)
+      for (int k = 0; k < LOADS; ++k) {
+        float score[4], top = 0.f;
 #pragma unroll
-      for (int i = 0; i < K::N; ++i) {
-        const float x = K::at(u[k], i);
-        float w = ex2(__fmaf_rn(x, cc, -r.z));
-        if (!r.usual || !(w < INFINITY)) w = share_weight(x, cc, r);
-        const float4& f = n[k * E4 + i / 4];
-        sum += w;
-        race(x, w, i % 4 == 0 ? f.x : i % 4 == 1 ? f.y : i % 4 == 2 ? f.z : f.w, sl.c0 + (c + k * VF_NT) * K::N + i);
+        for (int i = 0; i < 4; ++i) {
+          const float w = weight_of(Q::at(x[k], i));
+          sum += w;
+          // (noise 0: infinity, or NaN for w = 0, which is no candidate)
+          score[i] = w * rcp(__uint_as_float(i == 0 ? n[k].x : i == 1 ? n[k].y : i == 2 ? n[k].z : n[k].w));
+          top = fmaxf(top, score[i]);  // (passes over NaN)
+        }
+        if (top > best) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (score[i] > best) {
+              best = score[i];
+              r.at = sl.c0 + (c0 + k * VF_NT + tid) * 4 + i;
+            }
+        }
       }
+    };
+    if (r.usual) weigh([&](float v) { return ex2(__fmaf_rn(v, cc, -r.z)); });
+    if (!r.usual) weigh([&](float v) { return share_weight(v, cc, r); });
+    if (!(sum < INFINITY)) {  // a NaN among them, or no weight yet
+      sum = 0.f;
+#pragma unroll 1
+      for (int k = 0; k < LOADS && lm > -INFINITY; ++k) {
+        const T v = c0 + k * VF_NT < left ? own_x[place * STEP + k * VF_NT] : Q::none();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum += share_weight(Q::at(v, i), cc, r);
+      }
+    }
     r.s += sum;
+    if (++place == RING) place = 0;
   }
+  asm volatile("cp.async.wait_all;" ::: "memory");
   const float f = add_one(mine, cc, r);
   if (f >= 0.f) {
     best *= f;
-    const float n = __ldg(noise + beside), score = share_weight(mine, cc, r) * rcp(n);
-    if (score > best || (score == best && beside < r.at)) {
-      r.x = mine;
-      r.e = n;
-      r.at = beside;
-    }
+    const float score = share_weight(mine, cc, r) * rcp(__ldg(noise + beside));
+    if (score > best || (score == best && beside < r.at)) r.at = beside;
+  }
+  if (r.at >= 0) {
+    r.x = K::one(sl.base, r.at);
+    r.e = __ldg(noise + r.at);
   }
   return r;
 }
@@ -519,7 +559,7 @@ struct Race {
     };
     auto take = [&](const Piece& g, int c) {
       float score[K::N], top = 0.f;
-      const uint4 y = DRAFTED ? K::without_nan(g.y) : g.x;  // (a NaN of the target's makes no score)
+      const uint4 y = DRAFTED ? without_nan<F32>(g.y) : g.x;  // (a NaN of the target's makes no score)
 #pragma unroll
       for (int i = 0; i < K::N; ++i) {
         float r = ex2(__fmaf_rn(K::at(g.x, i), c_, -zp));
@@ -718,7 +758,8 @@ __global__ void __launch_bounds__(VF_NT) verify_end_kernel(const VerifyArgs a, i
 }
 
 // Without drafts: a cluster per sequence, the sums and the race in one pass over its row.  64 rows of 32,000 fp32 logits, 16 MB:
-// 8.5 us, a chain of temperature -> loads -> join -> exchange; 256 of 152,064 bf16, 233 MB: 62 us (3.8 TB/s).
+// 8 us, a chain of temperature -> loads -> join -> exchange; 256 of 152,064 bf16, 233 MB: 44 us (5.3 TB/s; 59 with 16 bytes of
+// logits and twice 16 of noise to a thread, which split every line of the noise between two loads).
 template <bool F32>
 __global__ void __launch_bounds__(VF_NT) verify_sample_kernel(const VerifyArgs a) {
   struct __align__(16) Best {
@@ -743,7 +784,7 @@ __global__ void __launch_bounds__(VF_NT) verify_sample_kernel(const VerifyArgs a
   const float* noise = q.greedy ? nullptr : a.noise + (size_t)b * a.ld_noise;
   const int per = (((a.V + C - 1) / C) + 7) & ~7;
   const Slice<F32> s(base, min(rank * per, a.V), min((rank + 1) * per, a.V));
-  const Share t = q.greedy ? sum_slice<F32>(s, q.c, ring, []() {}) : scan_race<F32>(s, q.c, noise);
+  const Share t = q.greedy ? sum_slice<F32>(s, q.c, ring, []() {}) : scan_race<F32>(s, q.c, ring, noise);
   const RowPart r = join_cta(t.m, share_sum(q.c, t), q.c, q.greedy, [&](float top) { return s.first_of(top, t.first); });
   const float score = t.at >= 0 ? weight(t.x, r.m, q.c) * rcp(t.e) : 0.f;
   const unsigned long long own = score > 0.f ? race_key(score, t.at) : 0ull, key = cta_max(own, key_s);
@@ -847,8 +888,7 @@ static cudaError_t launch_clusters(Kernel* k, int C, int B, size_t smem, cudaStr
 cudaError_t verify_launch(const VerifyArgs& a, void* ws, cudaStream_t st) {
   const int sms = device_sm_count();
   const double bytes = (double)a.T_cap * a.V * (a.logits_f32 ? 4 : 2);
-  // CTAs of a sequence: four per SM where there are few sequences, one wave of them where there are many
-  const int C = std::max(1, std::min(std::min(VF_CLUSTER, (a.V + 2047) / 2048), sms * 4 / a.B));
+  const int most = std::min(VF_CLUSTER, (a.V + 4095) / 4096);  // CTAs of a sequence: 4,096 logits for each at least
   cudaError_t r;
   if (a.max_rows == 1) {
     if (a.cu_rows && a.clear_err && a.err) {
@@ -856,10 +896,13 @@ cudaError_t verify_launch(const VerifyArgs& a, void* ws, cudaStream_t st) {
       if (r != cudaSuccess) return r;
     }
     prof_begin_launch(st);
+    // two CTAs per SM (128 sequences of 152,064 bf16 logits by two CTAs 27 us, by four 29; 256 by one 44, by two 50)
+    const int C = std::max(1, std::min(most, sms * 2 / a.B));
     static std::atomic<unsigned long long> allowed[2];
     auto* k = a.logits_f32 ? verify_sample_kernel<true> : verify_sample_kernel<false>;
-    r = allow_smem(k, VF_RING_BYTES, allowed[a.logits_f32]);
-    if (r == cudaSuccess) r = launch_clusters(k, C, a.B, VF_RING_BYTES, st, a);
+    const int ring = std::max(VF_RING_BYTES, a.logits_f32 ? vr_bytes<true>() : vr_bytes<false>());
+    r = allow_smem(k, ring, allowed[a.logits_f32]);
+    if (r == cudaSuccess) r = launch_clusters(k, C, a.B, ring, st, a);
     prof_end_launch(st, SP_K_MISC, 0.0, bytes + (a.noise ? 4.0 * a.B * a.V : 0.0));
     return r;
   }
@@ -891,10 +934,10 @@ cudaError_t verify_launch(const VerifyArgs& a, void* ws, cudaStream_t st) {
   prof_begin_launch(st);
   auto* end = ordered ? (a.logits_f32 ? verify_end_kernel<true, true> : verify_end_kernel<false, true>)
                       : (a.logits_f32 ? verify_end_kernel<true, false> : verify_end_kernel<false, false>);
-  // (here of many sequences too no fewer than 25,000 logits want: 256 sequences of 152,064 in six 156 us, in two 162, in
-  // eight 162; of 20,000 in two 31, in six 38)
-  const int ends = std::max(C, std::min(VF_CLUSTER, a.V / 25000));
-  r = launch_clusters(end, a.noise ? ends : 1, a.B, 0, st, a, slices, w);
+  // four CTAs per SM, and no more than 25,000 logits for one (256 sequences of 152,064 by six 152 us, by two 157, by
+  // eight 158; of 20,000 fp32 by two 31, by six 38)
+  const int C = std::max(1, std::min(most, std::max(sms * 4 / a.B, a.V / 25000)));
+  r = launch_clusters(end, a.noise ? C : 1, a.B, 0, st, a, slices, w);
   prof_end_launch(st, SP_K_MISC, 0.0, 0.0);
   return r;
 }
