@@ -7,6 +7,8 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
 
+from test_gpu_paged import single_precision  # noqa: E402, F401
+
 
 @pytest.fixture(scope="module")
 def sp():

@@ -6,7 +6,7 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
 
-from test_gpu_paged import U  # noqa: E402
+from test_gpu_paged import U, single_precision  # noqa: E402, F401
 from test_gpu_verify import compare, gen, ints, reference  # noqa: E402
 
 HQ, HKV, DH, PAGE, V, K = 8, 2, 64, 16, 303, 4

@@ -7,6 +7,9 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
+
+from test_gpu_paged import single_precision  # noqa: E402, F401
+
 # Sums are fp32.  exp((x - m) / t) is ex2 of z = (x - m) c with three roundings of 2^-24 in z (relative), 2^-22 of the
 # approximation: a term is off by at most ln 2 * 3 * 2^-24 |z| + 2^-22 of itself.  Averaged with the terms as weights |z|
 # is below log2 V + 2 < 20 for V < 2^18: 2^-18.6 + 2^-22 of the sum; adding up (some 2^10 terms a thread in pieces of 32,
