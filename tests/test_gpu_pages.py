@@ -159,7 +159,8 @@ class Cache:
         return full
 
 
-@pytest.mark.parametrize("page,width,layers", [(16, 8, 1), (16, 24, 3), (32, 512, 2), (64, 64, 1), (128, 1024, 1)])
+@pytest.mark.parametrize("page,width,layers", [(16, 8, 1), (16, 24, 3), (32, 40, 1), (16, 264, 2), (32, 512, 2), (64, 64, 1), (128, 1024, 1),
+                                               (16, 4104, 1)])
 def test_a_prompt_its_samples_and_their_ends(sp, page, width, layers):
     c = Cache(sp, 5, 6, 24, page, layers, width)
     c.reserve([2 * page + 3, 0, 0, 0, 1])
@@ -235,6 +236,21 @@ def test_pages_run_out(sp):
     assert c.n == [33, 20, 16, 0]
     assert not c.compact([list(range(20)), list(range(5)), list(range(3)), None])  # what only gets shorter needs none
     assert not c.compact([[0, 2, 4], None, None, None])
+
+
+def test_a_pool_of_one_page(sp):
+    c = Cache(sp, 2, 1, 1, 1024, 1, 8)
+    assert not c.reserve([1024, 0])
+    c.append([1024, 0])
+    assert c.reserve([0, 1])
+    c.fork([-1, 0])
+    assert c.compact([None, [1023]])                # the only page is shared
+    c.fork([-1, -1])
+    c.n[0] = 0
+    c.upload()
+    c.trim()
+    assert c.count == [1]
+    c.reserve([0, 0])
 
 
 def test_a_page_shared_by_the_rows_that_write_it(sp):

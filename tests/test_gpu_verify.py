@@ -182,6 +182,37 @@ def test_many_drafts_and_wide_rows(sp):
         compare(sp.sp_draft_verify(**s), expect(s), s["max_rows"])
 
 
+def test_the_largest(sp):
+    """More than a thousand drafts of a sequence, and more than four million tokens."""
+    s = problem(5, 33, [700, 1, 1024, 0], near=0.02, temps=(1.0, 0.9))
+    s["u"][:] = 0.0
+    s["u"][1720] = 1e9  # the last sequence ends at its row 1,019
+    got = sp.sp_draft_verify(**s)
+    compare(got, expect(s), 1024)
+    assert got["n_accept"].tolist() == [699, 0, 1019, -1]
+    with pytest.raises(sp.SPError):
+        sp.sp_draft_verify(**dict(s, max_rows=1025))
+    for counts in ([2, 1], [1, 1]):
+        s = problem(7, (1 << 22) + 3, counts, torch.bfloat16, near=0.2, temps=(1.0, 0.0))
+        compare(sp.sp_draft_verify(**s), expect(s), max(counts))
+
+
+def test_a_graph_of_rows_in_order(sp):
+    """Replayed, with other numbers in the same place."""
+    s = problem(9, 50001, [6] * 128, near=0.4)
+    u = s["u"].clone()
+    ref = [sp.sp_draft_verify(**dict(s, u=v)) for v in (u, u * 0.0)]
+    out = dict(ws=sp.draft_verify_workspace(T_cap=768, B=128, V=50001), err=ints([0]))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = sp.sp_draft_verify(**s, **out)
+    for i in (1, 0, 1):
+        s["u"].copy_(u * (1 - i))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(got[k], ref[i][k]) for k in ("n_accept", "token", "logp"))
+
+
 def test_a_large_batch(sp):
     """More rows than CTAs that run at once."""
     s = problem(4, 9000, [1 + b % 6 for b in range(256)], torch.bfloat16)
@@ -307,6 +338,16 @@ def test_without_noise_everything_is_greedy(sp):
     zero = sp.sp_draft_verify(**dict(s, temperature=torch.zeros(3, device=DEV)))
     for k in ("n_accept", "token", "logp"):
         assert torch.equal(zero[k], got[k])
+
+
+def test_temperatures_that_are_greedy(sp):
+    s = problem(21, 700, [3, 2, 4, 1], near=0.1, temps=(-1.0, math.nan, -math.inf, 0.0))
+    got = sp.sp_draft_verify(**s)
+    compare(got, expect(s), 4)
+    none = sp.sp_draft_verify(**dict(s, noise=None))
+    assert all(torch.equal(got[k], none[k]) for k in ("n_accept", "token", "logp"))
+    one = sp.sp_draft_verify(**dict(s, temperature=None))  # as 1
+    compare(one, expect(dict(s, temperature=torch.ones(4, device=DEV))), 4)
 
 
 def test_offsets_and_drafts_that_are_wrong(sp):
