@@ -270,9 +270,15 @@ def _check(status: int, what: str):
 
 # ----------------------------------------------------------------------------- tensors
 
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 def ptr(t) -> Optional[int]:
@@ -724,7 +730,7 @@ def _enter(who: str, t, stream):
         if stream.device_index != dev:
             raise ValueError(f"{who}: the stream is device {stream.device_index}'s, the tensors are on device {dev}")
         guard = torch.cuda.stream(stream)
-    elif torch.cuda.current_device() == dev:
+    elif torch._C._cuda_getDevice() == dev:  # (what torch.cuda.current_device() asks, which the tensor has initialised)
         return dev, None
     else:
         guard = torch.cuda.device(dev)
@@ -739,7 +745,7 @@ def _leave(guard):
 
 def _raw_stream(stream, dev: int) -> int:
     if stream is None:
-        return _torch()._C._cuda_getCurrentRawStream(dev)
+        return _torch_module._C._cuda_getCurrentRawStream(dev)  # (loaded: the call has tensors)
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
