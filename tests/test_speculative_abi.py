@@ -2,6 +2,7 @@
 launch (no GPU is needed; the addresses below are never dereferenced)."""
 import ctypes as C
 import os
+import re
 
 import pytest
 
@@ -102,3 +103,30 @@ def test_pages_refusals_of_the_other_arguments(L):
 def test_packed_arguments_are_the_structs(L):
     assert b._pack_pages(OK, 2, 9, 16, 64, 3, OK, 4, OK, OK, OK) == bytes(pages())
     assert b._pack_verify(2, 100, 6, 4, OK, OK, 1, 100, OK, OK, 100, OK, OK, 100, OK, OK, OK, OK, OK, 1) == bytes(verify(clear_err=1))
+
+
+def _body(kernel):
+    from test_kernel_sync import _kernel, _source
+    return _kernel(_source("verify.cu"), kernel)
+
+
+def test_the_end_kernel_reads_nothing_of_the_sums_before_its_wait():
+    """It starts while the sums run: until its wait it may read what the caller gave, which no kernel of the call writes.  That
+    was written before the sums' own wait, and they let it start only behind that."""
+    sums, end = _body("verify_sums_kernel"), _body("verify_end_kernel")
+    assert sums.index("pdl_wait()") < sums.index("pdl_trigger()")
+    assert not re.search(r"\ba\.\w+\s*\[|__ldg|__ldcg|\bwork\.", sums[:sums.index("pdl_wait()")])
+    before = end[:end.index("pdl_wait()")]
+    assert "work" not in before and "pdl_trigger" not in before
+    assert not re.search(r"\ba\.(n_accept|token|logp|err)\b", before)
+
+
+@pytest.mark.parametrize("kernel", ["verify_end_kernel", "verify_sample_kernel"])
+def test_every_cta_of_a_cluster_waits_before_it_ends(kernel):
+    """A CTA that leaves early has taken part in the cluster's first barrier, and the others' memory is written behind it."""
+    text = _body(kernel)
+    assert text.index("cluster_arrive()") < text.index("cluster_wait()")
+    assert text.rindex("cluster_wait()", 0, text.index("mapa_shared")) > text.index("cluster_arrive()")
+    head = text[:text.index("mapa_shared")]
+    for m in re.finditer(r"return;", head):
+        assert "cluster_wait();" in head[max(0, m.start() - 60):m.start()], head[m.start() - 60:m.end()]
