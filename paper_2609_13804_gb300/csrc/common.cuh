@@ -148,6 +148,12 @@ SP_DEVINL int ld_acquire_gpu(const int* p) {
   return v;
 }
 
+SP_DEVINL int ld_relaxed_gpu(const int* p) {
+  int v;
+  asm volatile("ld.relaxed.gpu.global.b32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
+}
+
 SP_DEVINL void st_release_gpu(int* p, int v) {
   asm volatile("st.release.gpu.global.b32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
 }

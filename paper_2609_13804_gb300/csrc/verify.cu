@@ -447,10 +447,11 @@ __global__ void __launch_bounds__(VF_NT, 4) verify_sums_kernel(const VerifyArgs 
   pdl_wait();
   const int which = blockIdx.x / slices, sl = blockIdx.x % slices, b = blockIdx.y, j = blockIdx.z;
   if (a.clear_err && a.err && blockIdx.x + b + j == 0 && threadIdx.x == 0) *a.err = 0;
-  const int ended = ORDERED ? __ldcg(work.end + b) : kUnset;
+  const int ended = ORDERED ? ld_relaxed_gpu(work.end + b) : kUnset;
   const Seq q = sequence(a, b);
   const bool last = j == q.n - 1;
-  if (j >= q.n || (which == 1 && (q.greedy || last)) || ended < j) return;
+  if (j >= q.n || (which == 1 && (q.greedy || last))) return;
+  if (ORDERED && __syncthreads_or(ended < j)) return;  // (the end moves while threads look at it: the CTA goes on, or ends, as one)
   const int row = q.row0 + j;
   const char* base = static_cast<const char*>(which ? a.draft_logits : a.logits) +
                      row * (which ? a.ld_draft : a.ld) * (F32 ? 4 : 2);

@@ -1,0 +1,23 @@
+"""Synchronisation of the kernels for drafted tokens that no run shows reliably when it is missing, read from their sources."""
+import re
+
+from test_kernel_sync import _kernel, _source
+
+
+def _ends_uniformly(body):
+    """Whether what other CTAs change while the kernel runs ends a CTA only as a whole: what a thread has read of work.end is
+    used in a vote of the CTA and nowhere else."""
+    head = body[:body.index("sum_slice")]
+    if len(re.findall(r"\bwork\.end\b", head)) != 1:
+        return False
+    name = re.search(r"\bint (\w+) = [^;]*\bwork\.end\b[^;]*;", head)
+    uses = [m.start() for m in re.finditer(r"\b%s\b" % name.group(1), body) if m.start() > name.end()]
+    return bool(uses) and all(re.search(r"__syncthreads_or\([^()]*$", body[:at]) for at in uses)
+
+
+def test_rows_that_are_passed_over_end_whole_ctas():
+    """Rows in order: the sequence's end moves while a CTA looks at it.  Warps that saw different ends would part before the
+    barriers of the sums."""
+    body = _kernel(_source("verify.cu"), "verify_sums_kernel")
+    assert _ends_uniformly(body)
+    assert not _ends_uniformly(re.sub(r"__syncthreads_or", "", body))
