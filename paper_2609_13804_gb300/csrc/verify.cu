@@ -472,11 +472,12 @@ __global__ void __launch_bounds__(VF_NT, 4) verify_sums_kernel(const VerifyArgs 
     if (threadIdx.x == 0) {
       __threadfence();
       const int all = slices * (a.draft_logits && !q.greedy && !last ? 2 : 1);
-      last_s = atomicAdd(work.count + row, 1) == kUnset + all - 1;
+      const bool done = atomicAdd(work.count + row, 1) == kUnset + all - 1;
+      if (done) __threadfence();  // (by the thread that counted; the barrier hands the other slices' parts on to its warp)
+      last_s = done;
     }
     __syncthreads();
     if (last_s && threadIdx.x < 32) {
-      __threadfence();
       const Row o = decide(a, q, j, work.part, slices);
       if (threadIdx.x == 0) {
         work.rows[row] = o;

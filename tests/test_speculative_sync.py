@@ -21,3 +21,16 @@ def test_rows_that_are_passed_over_end_whole_ctas():
     body = _kernel(_source("verify.cu"), "verify_sums_kernel")
     assert _ends_uniformly(body)
     assert not _ends_uniformly(re.sub(r"__syncthreads_or", "", body))
+
+
+def _count_is_acquired(body):
+    """Whether the thread that counts a slice puts a fence on both sides of the count, ahead of the barrier that hands what
+    other CTAs wrote on to its warp."""
+    return re.search(r"__threadfence\(\);[^}]*\bconst bool (\w+) = atomicAdd\(work\.count\b[^;]*;\s*if \(\1\) __threadfence\(\);[^}]*\}"
+                     r"\s*__syncthreads\(\);", body) is not None
+
+
+def test_the_last_slice_of_a_row_sees_the_others():
+    body = _kernel(_source("verify.cu"), "verify_sums_kernel")
+    assert _count_is_acquired(body)
+    assert not _count_is_acquired(re.sub(r"if \(\w+\) __threadfence\(\);", "", body))
