@@ -70,8 +70,8 @@ __global__ void __launch_bounds__(PF_NT) pages_fork_kernel(const PagesArgs a, co
     }
   }
   __syncthreads();
-  // (relaxed: it orders other CTAs' reads of the lengths, which are over, before the writes behind the wait, and no writes)
-  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+  // (release: this CTA's reads of the lengths come before the writes behind the wait)
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   for (;;) {
     for (int i = tid; i < n; i += PF_NT) {
       const int s = i >> cols_shift, k = i & (cols - 1), c = c0 + k, p = from_s[s];
@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(PF_NT) pages_fork_kernel(const PagesArgs a, co
     __syncthreads();
   }
   __syncwarp();
-  asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   if (blockIdx.x == 0)
     for (int s = tid; s < a.S; s += PF_NT)
       if (from_s[s] != s) a.lens[s] = len_s[from_s[s]];

@@ -34,3 +34,19 @@ def test_the_last_slice_of_a_row_sees_the_others():
     body = _kernel(_source("verify.cu"), "verify_sums_kernel")
     assert _count_is_acquired(body)
     assert not _count_is_acquired(re.sub(r"if \(\w+\) __threadfence\(\);", "", body))
+
+
+def _lengths_are_read_before_they_change(body):
+    """Whether every CTA's reads of the lengths are released by its arrival at the cluster's barrier and the writes lie behind
+    a wait that acquires them."""
+    arrive, wait = body.find("barrier.cluster.arrive.release"), body.find("barrier.cluster.wait.acquire")
+    reads = [m.start() for m in re.finditer(r"= a\.lens\[", body)]
+    writes = [m.start() for m in re.finditer(r"\ba\.lens\[[^;]*\]\s*= ", body)]
+    return bool(reads and writes) and max(reads) < arrive < wait < min(writes) and "arrive.relaxed" not in body
+
+
+def test_forks_read_all_lengths_before_one_changes():
+    body = _kernel(_source("pages.cu"), "pages_fork_kernel")
+    assert _lengths_are_read_before_they_change(body)
+    assert not _lengths_are_read_before_they_change(body.replace("arrive.release", "arrive.relaxed"))
+    assert not _lengths_are_read_before_they_change(body.replace("wait.acquire", "wait"))
