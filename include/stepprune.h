@@ -785,10 +785,11 @@ SP_API sp_status sp_beam_reorder(const sp_beam_reorder_io* io, sp_stream stream)
  *   n_accept -1, one with more than max_rows, or rows outside 0 .. T_cap - 1, sets
  *   SP_DEVERR_INDEX besides.  A draft outside the vocabulary is rejected; where that
  *   ends its sequence SP_DEVERR_INDEX is set.
- * NaN and -infinity logits have no weight; a row with +infinity spreads its weight
- * over them.  A token whose noise is NaN or below 0 is not drawn.  Where no token can
- * be drawn (a row without weight) the next token is -1, its logp -infinity.  A draft
- * with u NaN is rejected.
+ * NaN and -infinity logits have no weight, nor have those whose weight is below 2^-126
+ * of the row's largest; a row with +infinity spreads its weight over them.  A token
+ * whose noise is NaN or below 0 is not drawn.  Where no token can be drawn (a row
+ * without weight) the next token is -1, its logp -infinity.  A draft with u NaN is
+ * rejected.
  * Sums are fp32, good to about 2^-20: the answers move only where u q and p, or the
  * two best scores of a race, are nearer than that.  The workspace keeps nothing;
  * calls whose GPU work overlaps need one each.

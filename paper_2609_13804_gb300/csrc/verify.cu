@@ -71,6 +71,7 @@ struct Share {
   float x, e;  // the race's best so far
   int at;      // -1: none
   bool usual;  // m c is ordinary
+  bool infinite;  // the race has had an infinite score (noise of 0): others were not kept, which count if its weight ends as 0
 };
 
 // Tokens v0 .. v1 - 1 of a row, 16 bytes at a time where they lie whole in the slice.
@@ -192,7 +193,7 @@ template <bool F32, typename Meanwhile>
 SP_DEVINL Share sum_slice(const Slice<F32>& sl, float cc, uint4* ring, Meanwhile meanwhile) {
   using K = Chunk<F32>;
   constexpr int STEP = VF_NT * VF_LOADS;
-  Share r{-INFINITY, -INFINITY, 0.f, -1, 0.f, 1.f, -1, true};
+  Share r{-INFINITY, -INFINITY, 0.f, -1, 0.f, 1.f, -1, true, false};
   const uint4* src = sl.src() + threadIdx.x;
   uint4* own = ring + threadIdx.x;
   const int left = sl.chunks - threadIdx.x;  // pieces from this thread's first on
@@ -255,7 +256,7 @@ SP_DEVINL Share scan_race(const Slice<F32>& sl, float cc, uint4* ring, const flo
   using Q = Four<F32>;
   using T = typename Q::T;
   constexpr int LOADS = vr_loads<F32>(), RING = vr_ring<F32>(), STEP = VF_NT * LOADS;
-  Share r{-INFINITY, -INFINITY, 0.f, -1, 0.f, 1.f, -1, true};
+  Share r{-INFINITY, -INFINITY, 0.f, -1, 0.f, 1.f, -1, true, false};
   float best = 0.f;  // (in r's units)
   const int tid = threadIdx.x, left = sl.chunks * (K::N / 4) - tid;  // fours from this thread's first on
   const T* src = reinterpret_cast<const T*>(sl.src()) + tid;
@@ -312,6 +313,7 @@ SP_DEVINL Share scan_race(const Slice<F32>& sl, float cc, uint4* ring, const flo
           top = fmaxf(top, score[i]);  // (passes over NaN)
         }
         if (top > best) {
+          r.infinite |= top == INFINITY;
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             if (score[i] > best) {
@@ -340,6 +342,7 @@ SP_DEVINL Share scan_race(const Slice<F32>& sl, float cc, uint4* ring, const flo
   if (f >= 0.f) {
     best *= f;
     const float score = share_weight(mine, cc, r) * rcp(__ldg(noise + beside));
+    r.infinite |= score == INFINITY;
     if (score > best || (score == best && beside < r.at)) r.at = beside;
   }
   if (r.at >= 0) {
@@ -759,19 +762,22 @@ __global__ void __launch_bounds__(VF_NT) verify_end_kernel(const VerifyArgs a, i
   }
 }
 
-// Without drafts: a cluster per sequence, the sums and the race in one pass over its row.  64 rows of 32,000 fp32 logits, 16 MB:
-// 8 us, a chain of temperature -> loads -> join -> exchange; 256 of 152,064 bf16, 233 MB: 44 us (5.3 TB/s; 59 with 16 bytes of
-// logits and twice 16 of noise to a thread, which split every line of the noise between two loads).
+// Without drafts: a cluster per sequence, the sums and the race in one pass over its row.  A thread keeps the best of its
+// scores next to its own maximum.  What has no weight next to the row's is dropped when shares are joined; where that may have
+// been an infinite score, or nothing is left, the first CTA races over the row again, next to its maximum.  64 rows of 32,000
+// fp32 logits, 16 MB: 8 us, a chain of temperature -> loads -> join -> exchange; 256 of 152,064 bf16, 233 MB: 44 us (5.3 TB/s; 59
+// with 16 bytes of logits and twice 16 of noise to a thread, which split every line of the noise between two loads).
 template <bool F32>
 __global__ void __launch_bounds__(VF_NT) verify_sample_kernel(const VerifyArgs a) {
+  using K = Chunk<F32>;
   struct __align__(16) Best {
     float m, s, x, e;
-    int at, greedy_at, unused[2];
+    int at, greedy_at, infinite, unused;
   };
   extern __shared__ uint4 ring[];
   __shared__ Best best_s[VF_CLUSTER], mine_s;
   __shared__ unsigned long long key_s[VF_WARPS];
-  const int C = gridDim.x, rank = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+  const int C = gridDim.x, rank = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 31;
   if (C > 1) cluster_arrive();
   pdl_wait();
   pdl_trigger();
@@ -790,13 +796,14 @@ __global__ void __launch_bounds__(VF_NT) verify_sample_kernel(const VerifyArgs a
   const RowPart r = join_cta(t.m, share_sum(q.c, t), q.c, q.greedy, [&](float top) { return s.first_of(top, t.first); });
   const float score = t.at >= 0 ? weight(t.x, r.m, q.c) * rcp(t.e) : 0.f;
   const unsigned long long own = score > 0.f ? race_key(score, t.at) : 0ull, key = cta_max(own, key_s);
-  if (tid == 0) mine_s = Best{r.m, r.s, 0.f, 1.f, -1, r.at, {0, 0}};
+  if (tid == 0) mine_s = Best{r.m, r.s, 0.f, 1.f, -1, r.at, 0, 0};
   __syncthreads();
   if (own != 0 && own == key) {
     mine_s.x = t.x;
     mine_s.e = t.e;
     mine_s.at = t.at;
   }
+  if (t.infinite) mine_s.infinite = 1;
   __syncthreads();
   if (C > 1) {
     cluster_wait();  // every CTA of the cluster runs
@@ -809,29 +816,45 @@ __global__ void __launch_bounds__(VF_NT) verify_sample_kernel(const VerifyArgs a
     if (rank != 0) return;
   } else {
     if (tid == 0) best_s[0] = mine_s;
-    __syncwarp();
+    __syncthreads();
   }
-  if (tid < 32) {  // a lane to a CTA's best
-    const bool in = tid < C;
-    const Best o = best_s[in ? tid : 0];
-    const float m = warp_max(in ? o.m : -INFINITY);
-    const bool some = in && o.m > -INFINITY;
-    const float sum = warp_sum(!some ? 0.f : o.m == m ? o.s : o.s * ex2((o.m - m) * q.c));
-    unsigned long long k = 0;
-    if (q.greedy) {
-      if (some && o.m == m) k = race_key(1.f, o.greedy_at);
-    } else if (some && o.at >= 0) {
-      const float sc = weight(o.x, m, q.c) * rcp(o.e);
-      if (sc > 0.f) k = race_key(sc, o.at);
-    }
-    const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(k >> 32));
-    const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(k >> 32) == hi ? (uint32_t)k : 0u);
-    const bool won = k != 0 && k == (((unsigned long long)hi << 32) | lo);
-    if (won || (hi == 0 && tid == 0)) {
-      a.n_accept[b] = 0;
-      a.token[b] = won ? (int)~lo : -1;
-      if (a.logp) a.logp[b] = won ? log_prob(q.greedy ? m : o.x, m, sum, q.t) : -INFINITY;
-    }
+  // a lane to a CTA's best, the same in every warp
+  const bool in = lane < C;
+  const Best o = best_s[in ? lane : 0];
+  const float m = warp_max(in ? o.m : -INFINITY);
+  const bool some = in && o.m > -INFINITY;
+  const float sum = warp_sum(!some ? 0.f : o.m == m ? o.s : o.s * ex2((o.m - m) * q.c));
+  unsigned long long k = 0;
+  if (q.greedy) {
+    if (some && o.m == m) k = race_key(1.f, o.greedy_at);
+  } else if (some && o.at >= 0) {
+    const float sc = weight(o.x, m, q.c) * rcp(o.e);
+    if (sc > 0.f) k = race_key(sc, o.at);
+  }
+  const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(k >> 32));
+  const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(k >> 32) == hi ? (uint32_t)k : 0u);
+  const unsigned int won = __ballot_sync(0xffffffffu, k != 0 && k == (((unsigned long long)hi << 32) | lo));
+  int next = won ? (int)~lo : -1;
+  float x = __shfl_sync(0xffffffffu, q.greedy ? m : o.x, won ? __ffs(won) - 1 : 0);
+  if (!q.greedy && m > -INFINITY && (!won || __any_sync(0xffffffffu, in && o.infinite))) {
+    Race<F32> race;
+    race.p = base;
+    race.q = nullptr;
+    race.e = noise;
+    race.mp = m;
+    race.sp = sum;
+    race.mq = race.sq = 0.f;
+    race.c = q.c;
+    race.out = -1;
+    race.prepare();
+    const unsigned long long best = cta_max(race.run(0, a.V), key_s);
+    next = best != 0 ? (int)~(uint32_t)best : -1;
+    if (next >= 0) x = K::one(base, next);
+  }
+  if (tid == 0) {
+    a.n_accept[b] = 0;
+    a.token[b] = next;
+    if (a.logp) a.logp[b] = next >= 0 ? log_prob(x, m, sum, q.t) : -INFINITY;
   }
 }
 

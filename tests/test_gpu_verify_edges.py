@@ -1,0 +1,93 @@
+"""Sampling and verification where a row's candidates have no weight next to its largest logit, drafts that are no token."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+from test_gpu_paged import single_precision  # noqa: E402, F401
+from test_gpu_verify import compare, expect, gen, ints, problem, rows  # noqa: E402
+
+
+@pytest.fixture(scope="module")
+def sp():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    from paper_2609_13804_gb300 import binding
+    return binding
+
+
+def as_rows_of_sequences(sp, s):
+    """The same tokens by the kernels for drafts: sequences of one row in a call of up to two."""
+    B = s["logits"].shape[0]
+    r = sp.sp_draft_verify(**dict(s, cu_rows=torch.arange(B + 1, dtype=torch.int32, device=DEV), max_rows=2, draft=ints([0] * B),
+                                  u=torch.zeros(B, device=DEV)))
+    assert (r["token"][:, 1] == -1).all()
+    return r["n_accept"], r["token"][:, 0], r["logp"][:, 0]
+
+
+# One CTA to a sequence (256 of them), and several: a thread's later tokens lie 1,024 apart (fp32: pairs of such fours).
+LATER = [1, 2, 3, 4, 1024, 2048, 4096, 8192]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,V,pad", [(256, 9000, 0), (256, 9001, 1), (256, 8997, 3), (3, 40000, 0), (3, 39999, 1)])
+def test_noise_of_zero_where_the_weight_is_zero(sp, dtype, B, V, pad):
+    """A token 900 temperatures below the largest logit has no weight in 64 bits either: its noise of 0 makes it no candidate,
+    and takes nothing from the tokens behind it, in its row or beside it."""
+    g = gen(51 + B + pad)
+    x = torch.full((B, V), -80.0, device=DEV)
+    noise = torch.empty((B, V), device=DEV).exponential_(generator=g)
+    early = torch.randint(0, 800, (B,), device=DEV, generator=g)
+    late = early + ints([LATER[b % len(LATER)] for b in range(B)]).long()
+    late[:2] = ints([V - 1, 0]).long()  # beside the whole pieces
+    at = torch.arange(B, device=DEV)
+    noise[at, early] = 0.0
+    early[1] = 5
+    noise[1, 5] = 0.0
+    x[at, late] = 10.0
+    s = dict(logits=rows(x, pad, dtype), noise=noise, temperature=torch.full((B,), 0.1, device=DEV))
+    got = sp.sp_draft_verify(**s)
+    assert got["token"][:, 0].tolist() == late.tolist()
+    assert (got["n_accept"] == 0).all() and (got["logp"] == 0.0).all()
+    n, token, logp = as_rows_of_sequences(sp, s)
+    assert torch.equal(token, got["token"][:, 0]) and torch.equal(logp, got["logp"][:, 0])
+    # with some weight it wins
+    x[at, early] = 9.0
+    x[at, late] = 10.0
+    s["logits"] = rows(x, pad, dtype)
+    won = sp.sp_draft_verify(**s)["token"][:, 0]
+    assert torch.equal(torch.where(early == late, late, early), won.long())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,V", [(256, 9000), (5, 33000)])
+def test_masked_tokens_with_noise_of_zero(sp, dtype, B, V):
+    """Masks of the type's lowest value, and noise that a program has set to 0 at masked tokens."""
+    s = problem(53 + B, V, [1] * B, dtype, False, temps=(1.0, 0.3, 0.05))
+    g = gen(54)
+    masked = torch.rand((B, V), device=DEV, generator=g) < 0.9
+    s["logits"][masked] = torch.finfo(dtype).min
+    s["noise"][masked & (torch.rand((B, V), device=DEV, generator=g) < 0.5)] = 0.0
+    got = sp.sp_draft_verify(**s)
+    compare(got, expect(s), 1)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("gap", [4, 1024, 2048, 4096, 8192])
+@pytest.mark.parametrize("low,mid", [(-80.0, 9.0), (-4.0, 3.0)])
+def test_what_a_token_without_weight_was_ahead_of(sp, dtype, gap, low, mid):
+    """Token 5 has noise 0 and no weight, the largest logit's token is not to be drawn: token 6 is what is left.  (Next to token
+    6 alone, 70 temperatures below it, token 5 would have some.)"""
+    B, V = 256, 9000
+    x = torch.full((B, V), -math.inf, device=DEV)
+    noise = torch.ones((B, V), device=DEV)
+    x[:, 5], x[:, 6], x[:, 5 + gap] = low, mid, 10.0
+    noise[:, 5], noise[:, 5 + gap] = 0.0, math.nan
+    s = dict(logits=x.to(dtype), noise=noise, temperature=torch.full((B,), 0.1, device=DEV))
+    got = sp.sp_draft_verify(**s)
+    assert (got["n_accept"] == 0).all() and (got["token"] == 6).all()
+    n, token, logp = as_rows_of_sequences(sp, s)
+    assert (token == 6).all() and torch.equal(logp, got["logp"][:, 0])
