@@ -426,7 +426,7 @@ SP_DEVINL Row decide(const VerifyArgs& a, const Seq& q, int j, const RowPart* pa
   const float yd = __shfl_sync(0xffffffffu, r.xd, 0);
   o.unused = 0;
   if (last) o.stays = 0;
-  else if (q.greedy) o.stays = d == o.at;
+  else if (q.greedy) o.stays = d == o.at && d >= 0 && d < a.V;  // (at: no token in a row without weight)
   else {  // u q(d) < p(d), the sums multiplied out; without weight anywhere p is 0
     const float pd = o.sp > 0.f ? weight(o.xd, o.mp, q.c) : 0.f;
     const float qd = !with_q ? 1.f : o.sq > 0.f ? weight(yd, o.mq, q.c) : 0.f;

@@ -91,3 +91,18 @@ def test_what_a_token_without_weight_was_ahead_of(sp, dtype, gap, low, mid):
     assert (got["n_accept"] == 0).all() and (got["token"] == 6).all()
     n, token, logp = as_rows_of_sequences(sp, s)
     assert (token == 6).all() and torch.equal(logp, got["logp"][:, 0])
+
+
+@pytest.mark.parametrize("draft", [2 ** 31 - 1, 700, -1, -2 ** 31])
+def test_a_draft_that_is_no_token_behind_a_row_without_weight(sp, draft):
+    """Greedy: such a row has no largest logit, and no draft is equal to that."""
+    s = problem(57, 700, [3, 3, 3], temps=(0.0, 1.0, 0.0))
+    s["logits"][[0, 3]] = math.nan
+    s["logits"][6] = -math.inf
+    s["draft"][[0, 3, 6]] = draft
+    for noise in (s["noise"], None):
+        got = sp.sp_draft_verify(**dict(s, noise=noise))
+        assert int(got["err"].item()) == 2
+        assert got["n_accept"].tolist() == [0, 0, 0]
+        assert got["token"].tolist() == [[-1] * 3] * 3
+        assert got["logp"].tolist() == [[-math.inf, 0.0, 0.0]] * 3
