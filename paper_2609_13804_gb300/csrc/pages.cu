@@ -180,9 +180,12 @@ pages_plan_kernel(const PagesArgs a, const int* __restrict__ add, const int* __r
         if (n != -1 && lane == 0) set_error(a.err, SP_DEVERR_INDEX);
         need = -1;  // the row stays as it is
       } else {
-        int first = n;  // the first position that moves
-        for (int i0 = 0; i0 < n; i0 += 32) {
-          const unsigned int other = __ballot_sync(0xffffffffu, i0 + lane < n && __ldg(keep + s * ld_keep + i0 + lane) != i0 + lane);
+        // the first position that moves (or that the row does not have, which the copy finds)
+        const int there = min(n, len);
+        int first = there;
+        for (int i0 = 0; i0 < there; i0 += 32) {
+          const unsigned int other =
+              __ballot_sync(0xffffffffu, i0 + lane < there && __ldg(keep + s * ld_keep + i0 + lane) != i0 + lane);
           if (other) {
             first = i0 + __ffs(other) - 1;
             break;
