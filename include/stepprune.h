@@ -792,7 +792,8 @@ SP_API sp_status sp_beam_reorder(const sp_beam_reorder_io* io, sp_stream stream)
  * rejected.
  * Sums are fp32, good to about 2^-20: the answers move only where u q and p, or the
  * two best scores of a race, are nearer than that.  The workspace keeps nothing;
- * calls whose GPU work overlaps need one each.
+ * calls whose GPU work overlaps need one each.  One for T_cap, B and V is enough for
+ * every call of no more of each.
  */
 typedef struct {
   int B, V;                 /* 1..SP_MAX_BATCH, 1..2^24 */

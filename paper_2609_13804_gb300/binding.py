@@ -1046,7 +1046,7 @@ def sp_beam_reorder(*, kv, table, own_table, lens, parent, err=None, stream=None
 
 
 def draft_verify_workspace(*, T_cap, B, V, device="cuda"):
-    """A workspace for sp_draft_verify calls of these sizes."""
+    """A workspace for sp_draft_verify calls of these sizes, and of smaller ones."""
     with _torch().cuda.device(device):
         n = lib().sp_draft_verify_workspace(int(T_cap), int(B), int(V))
     if n == 0:

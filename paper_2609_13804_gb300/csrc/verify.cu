@@ -16,6 +16,7 @@
 #include "common.cuh"
 #include "internal.h"
 #include "logits.cuh"
+#include "verify_cut.h"
 
 namespace sp {
 
@@ -25,7 +26,7 @@ constexpr int VF_NT = 256, VF_WARPS = VF_NT / 32;
 constexpr int VF_LOADS = 4;    // 16-byte loads of a thread at once
 constexpr int VF_RING = 3;     // batches of loads in shared memory
 constexpr int VF_RING_BYTES = VF_RING * VF_LOADS * VF_NT * 16;
-constexpr int VF_SLICES = 32;  // of a row, at most: a lane joins each
+static_assert(kRowSlices <= 32, "a lane joins each");
 constexpr int VF_CLUSTER = 8;  // CTAs of a sequence's race, at most
 
 // A slice's maximum, its sum of exp((x - m) / t) and the first token that holds the maximum (greedy sequences).
@@ -860,23 +861,6 @@ __global__ void __launch_bounds__(VF_NT) verify_sample_kernel(const VerifyArgs a
 
 }  // namespace
 
-// How a call's rows are cut.  CTAs of the sums that run at once: four per SM.  Rows that fit one wave of them are cut into as
-// many slices as do (of at least 2,048 logits), more into slices of about 51,200.  In order, with decisions on the way, where
-// several rows of a sequence can be passed over and they are more than is soon read (64 sequences of 8 drafts, 152,064 bf16
-// logits: 72 us in order, 77 not; of 5 drafts, 96 of 50,001 fp32: 56, 52; 200 of 3, 5,000 fp32: 26, 21).
-struct Cut {
-  int slices;
-  bool ordered;
-};
-static Cut verify_cut(int T_cap, int B, int V, int max_rows, bool drafted, bool f32) {
-  const int rows = std::max(drafted ? 2 * T_cap - std::min(B, T_cap) : T_cap, 1), slots = device_sm_count() * 4;
-  Cut c;
-  c.ordered = rows > slots && max_rows > 3 && (double)rows * V * (f32 ? 4 : 2) > 0x1p28;
-  c.slices = rows > slots ? (V + 51199) / 51200 : (slots + rows / 2) / rows;
-  c.slices = std::max(1, std::min(std::min(c.slices, VF_SLICES), (V + 2047) / 2048));
-  return c;
-}
-
 // Logits of a slice: whole batches, where it has some (slices that each end in a part of a batch, of three 7 instead of
 // 6.2, cost their sums a tenth).
 static int slice_of(int V, int slices, bool f32) {
@@ -886,10 +870,11 @@ static int slice_of(int V, int slices, bool f32) {
 
 static size_t align256(size_t n) { return (n + 255) & ~size_t(255); }
 
+static int verify_slots() { return device_sm_count() * 4; }
+
 size_t verify_bytes(int T_cap, int B, int V) {
   const size_t T = (size_t)T_cap;
-  const int slices = std::max(verify_cut(T_cap, B, V, 1, false, false).slices, verify_cut(T_cap, B, V, 1, true, false).slices);
-  return align256(T * 2 * slices * sizeof(RowPart)) + align256(T * sizeof(Row)) + align256((T + B) * 4);
+  return align256(2 * verify_parts(T_cap, V, verify_slots()) * sizeof(RowPart)) + align256(T * sizeof(Row)) + align256((T + B) * 4);
 }
 
 template <typename Kernel, typename... Args>
@@ -932,7 +917,7 @@ cudaError_t verify_launch(const VerifyArgs& a, void* ws, cudaStream_t st) {
     return r;
   }
   const int sets = a.draft_logits ? 2 : 1;
-  const Cut cut = verify_cut(a.T_cap, a.B, a.V, a.max_rows, sets == 2, a.logits_f32);
+  const Cut cut = verify_cut(a.T_cap, a.B, a.V, a.max_rows, sets == 2, a.logits_f32, verify_slots());
   const int slices = cut.slices, slice = slice_of(a.V, slices, a.logits_f32);
   const bool ordered = cut.ordered;
   char* base = static_cast<char*>(ws);

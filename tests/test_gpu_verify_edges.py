@@ -106,3 +106,16 @@ def test_a_draft_that_is_no_token_behind_a_row_without_weight(sp, draft):
         assert got["n_accept"].tolist() == [0, 0, 0]
         assert got["token"].tolist() == [[-1] * 3] * 3
         assert got["logp"].tolist() == [[-math.inf, 0.0, 0.0]] * 3
+
+
+def test_a_workspace_for_the_largest_step_serves_smaller_ones(sp):
+    for T, B, V in ((406, 64, 32000), (244, 64, 152064), (700, 256, 50001), (40, 8, 300000)):
+        most = sp.draft_verify_workspace(T_cap=T, B=B, V=V).numel()
+        for t in sorted(set(range(1, T + 1, 7)) | {T - 1, T // 2, 1}):
+            for b in {1, B // 2, B}:
+                for v in {1, 2049, V // 2, V - 1, V}:
+                    assert sp.draft_verify_workspace(T_cap=t, B=b, V=v).numel() <= most, (t, b, v)
+    s = problem(59, 32000, [7] * 15 + [6] * 50, torch.bfloat16, temps=(0.0,))  # 405 rows
+    ws = sp.draft_verify_workspace(T_cap=406, B=65, V=32000)
+    got = sp.sp_draft_verify(**dict(s, ws=ws))
+    assert all(torch.equal(got[k], v) for k, v in sp.sp_draft_verify(**s).items() if k in ("n_accept", "token", "logp"))
