@@ -119,3 +119,51 @@ def test_a_workspace_for_the_largest_step_serves_smaller_ones(sp):
     ws = sp.draft_verify_workspace(T_cap=406, B=65, V=32000)
     got = sp.sp_draft_verify(**dict(s, ws=ws))
     assert all(torch.equal(got[k], v) for k, v in sp.sp_draft_verify(**s).items() if k in ("n_accept", "token", "logp"))
+
+
+def test_sequences_beside_wrong_offsets(sp):
+    """Those that are right, and share no row with a wrong one, are what they are alone."""
+    s = problem(61, 400, [3, 3, 3, 3])
+    for cu, right in (([0, 4, 6, 9, 12], [1, 2, 3]), ([-1, 2, 5, 8, 13], [1, 2]), ([0, 3, 13, 9, 12], [0, 3]),
+                      ([0, 3, 3, 7, 9], [0, 3])):
+        got = sp.sp_draft_verify(**dict(s, cu_rows=ints(cu)))
+        assert int(got["err"].item()) == 2
+        for b in right:
+            i, j = cu[b], cu[b + 1]
+            one = {k: s[k][i:j] for k in ("logits", "draft_logits", "draft", "u")}
+            one.update(noise=s["noise"][b:b + 1], temperature=s["temperature"][b:b + 1], cu_rows=ints([0, j - i]))
+            want = expect(one)
+            assert want[0][3]  # (clear)
+            compare({k: got[k][b:b + 1] for k in ("n_accept", "token", "logp")}, want, 3)
+
+
+# A decision compares u q(d) sum(p) with p(d) sum(q), sums and weights next to the rows' maxima.  In steps of 2^-24: log2 e / t
+# is off by 1.5, x - m, its product and an exponential by 1, 1 and 4; so a weight of 2^-z is off by ln 2 * 3.5 z + 4 < 2.5 z + 4,
+# and with the two of a decision, their three products and two sums of 2^-17.5 = 91 the whole by less than 5 z + 8 + 3 + 2 * 91.
+def near(z):
+    return (200 + 5 * z) * 2.0 ** -24
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("model", [True, False])
+def test_decisions_about_unlikely_tokens(sp, dtype, model):
+    """Drafts down to 2^-110 of the likeliest token's probability, u a quarter more than the bound to either side of p / q."""
+    g, V, B = gen(63), 32000, 240
+    x = torch.randn((2 * B, V), device=DEV, generator=g) * 2
+    y = x + 0.7 * torch.randn((2 * B, V), device=DEV, generator=g)
+    t = torch.tensor([(1.0, 0.7, 1.5)[b % 3] for b in range(B)], device=DEV)
+    d = torch.randint(0, V, (2 * B,), device=DEV, generator=g)
+    first = torch.arange(0, 2 * B, 2, device=DEV)
+    down = torch.linspace(0, 110, B, device=DEV)
+    for v, z in ((x, down), (y, down[torch.randperm(B, device=DEV, generator=g)])):
+        v[first, d[first]] = v[first].amax(dim=1) - z * math.log(2.0) * t
+    x, y = x.to(dtype), y.to(dtype)
+    lp = torch.log_softmax(x[first].double() / t.double()[:, None], dim=1).gather(1, d[first, None])[:, 0]
+    lq = torch.log_softmax(y[first].double() / t.double()[:, None], dim=1).gather(1, d[first, None])[:, 0] if model else lp * 0
+    z = -torch.minimum(lp, lq) / math.log(2.0)  # (no less than below the likeliest)
+    side = torch.where(torch.arange(B, device=DEV) % 2 == 0, 1.0, -1.0).double()
+    u = torch.ones(2 * B, device=DEV)
+    u[first] = ((lp - lq).exp() * (1 + 1.25 * near(z) * side)).float()
+    got = sp.sp_draft_verify(logits=x, draft_logits=y if model else None, draft=d.int(), u=u, max_rows=2, temperature=t,
+                             noise=torch.ones((B, V), device=DEV), cu_rows=torch.arange(0, 2 * B + 1, 2, dtype=torch.int32, device=DEV))
+    assert got["n_accept"].tolist() == (side < 0).int().tolist()
