@@ -790,10 +790,13 @@ SP_API sp_status sp_beam_reorder(const sp_beam_reorder_io* io, sp_stream stream)
  * whose noise is NaN or below 0 is not drawn.  Where no token can be drawn (a row
  * without weight) the next token is -1, its logp -infinity.  A draft with u NaN is
  * rejected.
- * Sums are fp32, good to about 2^-20: the answers move only where u q and p, or the
- * two best scores of a race, are nearer than that.  The workspace keeps nothing;
- * calls whose GPU work overlaps need one each.  One for T_cap, B and V is enough for
- * every call of no more of each.
+ * Sums are fp32, good to 2^-17.5: the answers move only where u q and p, or the two
+ * best scores of a race, are nearer than (200 + 5 z) 2^-24 of p and q, for tokens
+ * 2^-z times as likely as the row's likeliest (2^-16 for z up to 11).
+ * The workspace keeps nothing; calls whose GPU work overlaps need one each.  One for
+ * T_cap, B and V is enough for every call of no more of each.  max_rows is to be near
+ * what sequences have: thread blocks are launched for B * max_rows rows (256 sequences
+ * of two rows: 24 us with max_rows 2 or 9, 47 with 64, 440 with 1,024).
  */
 typedef struct {
   int B, V;                 /* 1..SP_MAX_BATCH, 1..2^24 */
@@ -851,8 +854,9 @@ SP_API sp_status sp_draft_verify(const sp_draft_verify_io* io, void* workspace, 
  * SP_DEVERR_PAGES is set.
  * A length outside the table, a parent outside -1 .. S - 1, or a count outside
  * -1 .. keep_cap sets SP_DEVERR_INDEX and the row stays as it was.  An entry of
- * n_pages or more sets SP_DEVERR_INDEX and counts as none; a position of keep outside
- * the row sets it and what it would have moved is undefined.
+ * n_pages or more that a call takes, replaces or releases sets SP_DEVERR_INDEX and
+ * counts as none; a position of keep outside the row (keep[i] = i at or behind its
+ * length, too) sets it and what it would have moved is undefined.
  * The workspace (reserve, compact) keeps nothing; calls whose GPU work overlaps need
  * one each.
  */

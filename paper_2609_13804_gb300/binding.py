@@ -1067,8 +1067,8 @@ def sp_draft_verify(*, logits, noise=None, cu_rows=None, draft=None, draft_logit
     lie apart): rows cu_rows[b] .. cu_rows[b + 1] - 1 are sequence b's, max_rows of them at most (cu_rows None: one
     row per sequence, a token is sampled).  draft [T] int32: the token behind row j; draft_logits [T, V] the logits
     it was drawn from (None: it is taken as certain), u [T] uniform and noise [B, V] exponentially distributed
-    fp32 numbers (noise None: greedy), temperature [B] fp32 (None: 1; not above 0: greedy).  Returns n_accept [B],
-    token and logp [B, max_rows], err."""
+    fp32 numbers (noise None: greedy), temperature [B] fp32 (None: 1; not above 0: greedy).  max_rows costs time where
+    it is far above what sequences have.  Returns n_accept [B], token and logp [B, max_rows], err."""
     torch, who = _torch(), "sp_draft_verify"
     dev, guard = _enter(who, logits, stream)
     try:

@@ -40,8 +40,8 @@ constexpr int PF_NT = 512, PF_CTAS = 8;
 constexpr int PF_ENTRIES = 1 << 15;  // table entries in shared memory, at most
 
 // A row's new entries are its parent's of the same columns, so a CTA needs the old entries of all rows in its columns and
-// no others.  One cluster: the lengths change when all of its CTAs have read them.  Latency: 160 rows of 40 entries 4.1 us, 9 of
-// 275 3.4 (by strips of 8 columns 8.7).
+// no others.  One cluster: the lengths change when all of its CTAs have read them.  Latency: 160 rows of 40 entries 4.5 us, 9 of
+// 275 4.1 (by strips of 8 columns 8.7).
 __global__ void __launch_bounds__(PF_NT) pages_fork_kernel(const PagesArgs a, const int* __restrict__ parent, int cols_shift) {
   extern __shared__ int fork_s[];  // [S] old lengths, [S] the rows that they continue, [S][columns] old entries
   int *len_s = fork_s, *from_s = fork_s + a.S, *old_s = fork_s + 2 * a.S;

@@ -8,8 +8,9 @@
 //
 // Two kernels: the sums of every row (a maximum and a sum of exponentials, one pass), then per sequence the decision and the
 // race over the one row where it ends.  Bound by reading: every row that is looked at once, the last one twice and the noise.
-// Without drafts one kernel does both in one pass.  Sums and scores are fp32; decisions multiply sums out, so nothing is
-// rounded to fewer bits anywhere.
+// Without drafts one kernel does both in one pass.  Weights, sums and scores are fp32 and no operand is narrowed; exponentials,
+// the noise's reciprocals and a log-probability's quotient are the hardware's approximations, good to 2^-22.  Decisions
+// multiply sums out.
 #include <algorithm>
 #include <cfloat>
 
@@ -400,7 +401,10 @@ struct VerifyWork {
 };
 constexpr int kUnset = 0x7f7f7f7f;
 
-// A row's slices, joined by a warp; whether its draft stays.  Every lane has the result.
+// A row's slices, joined by a warp; whether its draft stays.  Every lane has the result.  In steps of 2^-24: the weight of a token
+// 2^-z times as likely as the likeliest is off by less than 2.5 z + 4 (c by 1.5, x - m and its product by 1 each, times z ln 2;
+// the exponential by 4), a sum by 2^-17.5 = 91 (its terms' mean z is below log2 V; adding up 2^-19), so what is compared by less
+// than 200 + 5 z.
 SP_DEVINL Row decide(const VerifyArgs& a, const Seq& q, int j, const RowPart* part, int slices) {
   const int lane = threadIdx.x & 31, row = q.row0 + j;
   const bool last = j == q.n - 1, with_q = a.draft_logits && !q.greedy && !last;
@@ -609,7 +613,7 @@ struct Race {
   }
 };
 
-// The largest of the CTA's keys, in every thread of warp 0.
+// The largest of the CTA's keys, in every thread (callers branch on it around barriers).
 SP_DEVINL unsigned long long cta_max(unsigned long long k, unsigned long long* s) {
   const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(k >> 32));
   const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(k >> 32) == hi ? (uint32_t)k : 0u);
